@@ -309,6 +309,184 @@ int tgrad_calibration_mfma(int kind, int64_t iterations, void* sink_dev, void* h
 /* Release the context (host memory only; device buffers stay the caller's). */
 int tgrad_destroy(tgrad_ctx* ctx);
 
+/*
+ * ---- Around tgrad_step: what a training step does before and behind it --------------------------------------------------
+ *
+ * The loss at its head (token log-probabilities, a clipped policy loss with a KL term, a preference loss; value and gradient
+ * with respect to the logits), the global norm of all gradients, clipping, and AdamW for the parameters that have no
+ * low-rank part.  The clip factor stays on the device: tgrad_group_adamw applies it to what it reads, so that clipping needs no
+ * pass over the gradients.
+ *
+ * Real element types, beside TGRAD_C64 and TGRAD_CBF16.
+ */
+enum { TGRAD_F32 = 2, TGRAD_BF16 = 3, TGRAD_F16 = 4 };
+
+typedef struct tgrad_group tgrad_group;   /* opaque; host memory owned by the library */
+
+/* One tensor of a group: dense, any shape.  Pointers need the alignment of their element type only. */
+typedef struct {
+  int64_t numel;        /* elements, >= 0 (a complex number counts once) */
+  void* grad;           /* gradient, grad_dtype; read by tgrad_group_grad_norm and tgrad_group_adamw */
+  void* out;            /* tgrad_group_scale / _clip: where the scaled gradient goes, grad_dtype; NULL = in place */
+  void* param;          /* tgrad_group_adamw: parameter, param_dtype, updated in place; NULL in a group that takes no steps */
+  void* exp_avg;        /* ... first moments: float32, (re, im) pairs of it for complex tensors */
+  void* exp_avg_sq;     /* ... second moments: float32, one per element (of |g|^2 for complex tensors, as in tgrad_step) */
+  int32_t grad_dtype;   /* any of the five types */
+  int32_t param_dtype;  /* real if grad_dtype is, complex if it is; ignored where param is NULL */
+  float lr_scale;       /* the tensor's learning rate is lr * lr_scale */
+  float weight_decay;   /* its decoupled (AdamW) decay */
+} tgrad_tensor;
+
+/* What tgrad_group_grad_norm leaves on the device. */
+typedef struct {
+  double sumsq;         /* sum of |g|^2 over all tensors, added up in float64, plus *add_sumsq */
+  float norm;           /* its root */
+  float coef;           /* min(1, max_norm / (norm + 1e-6)); 0 for an infinite norm, NaN for a NaN */
+} tgrad_norm;
+
+/*
+ * Bytes of device memory a group of n tensors needs.  Host-only, touches no GPU.  Errors: INVALID_ARG, UNSUPPORTED (more
+ * than 2^20 tensors, 2^40 elements in one, 2^43 in all).
+ */
+int tgrad_group_query_size(const tgrad_tensor* tensors, int64_t n, size_t* workspace_bytes);
+
+/*
+ * Create a group of n >= 1 tensors.
+ *  tensors        host pointer, n entries, copied.
+ *  workspace_dev  device pointer, >= workspace_bytes, 256-byte aligned; keeps the list of tensors until tgrad_group_destroy.
+ *  hip_stream     a hipStream_t (NULL = the default stream); every later call enqueues on it.  Does not wait.
+ * Tensors that are written (out, param, moments) must not overlap one another or, but for out == grad, anything that is read.
+ * Errors: INVALID_ARG (a null or misaligned pointer, a bad type, param without moments), UNSUPPORTED, HIP.
+ */
+int tgrad_group_init(tgrad_group** out, const tgrad_tensor* tensors, int64_t n, void* workspace_dev, void* hip_stream);
+
+/*
+ * New addresses, rates and decays for a group's tensors (gradients that are allocated anew in every step); numel, types and
+ * which pointers are NULL stay as at init.  Enqueued behind the calls before it.  Errors: INVALID_ARG, HIP.
+ */
+int tgrad_group_bind(tgrad_group* group, const tgrad_tensor* tensors);
+
+/*
+ * Global 2-norm of all gradients of the group and the factor that clips it.
+ *  max_norm       >= 0.
+ *  add_sumsq_dev  device pointer, 8-byte aligned, or NULL: sum of squares of gradients that lie elsewhere (another group's
+ *                 tgrad_norm.sumsq, other ranks'), added before the root.
+ *  norm_dev       device pointer, 8-byte aligned: receives the result.  May hold *add_sumsq_dev.
+ * The order of the sum depends on the sizes alone, never on timing.  Errors: INVALID_ARG, HIP.
+ */
+int tgrad_group_grad_norm(tgrad_group* group, float max_norm, const double* add_sumsq_dev, tgrad_norm* norm_dev);
+
+/*
+ * out = grad * norm_dev->coef for every tensor, in float32, rounded once to the type (nearest even).  In place, a factor of 1
+ * leaves everything as it is and reads nothing.  Errors: INVALID_ARG, HIP.
+ */
+int tgrad_group_scale(tgrad_group* group, const tgrad_norm* norm_dev);
+
+/* tgrad_group_grad_norm, then tgrad_group_scale with its result. */
+int tgrad_group_clip(tgrad_group* group, float max_norm, const double* add_sumsq_dev, tgrad_norm* norm_dev);
+
+typedef struct {
+  double lr, beta1, beta2, eps;   /* lr >= 0, 0 <= beta < 1, eps >= 0 */
+  int32_t skip_nonfinite;         /* 1: where norm_dev holds an infinite or NaN norm, nothing is written */
+} tgrad_adamw;
+
+/*
+ * One AdamW step of every tensor, tau = t + 1:  g' = coef g;  M <- beta1 M + (1 - beta1) g';
+ * V <- beta2 V + (1 - beta2) |g'|^2;  p <- p (1 - lr wd) - lr (M / (1 - beta1^tau)) / (sqrt(V / (1 - beta2^tau)) + eps).
+ * In float32; a bf16 or float16 parameter is widened exactly and rounded once to nearest even.
+ *  t         steps taken before this one, >= 0.
+ *  norm_dev  device pointer: the clip factor.  NULL = 1 (skip_nonfinite then has to be 0).
+ * Errors: INVALID_ARG (also for a group with a NULL param), HIP.
+ */
+int tgrad_group_adamw(tgrad_group* group, const tgrad_adamw* hyper, int64_t t, const tgrad_norm* norm_dev);
+
+/* Release the group (host memory only). */
+int tgrad_group_destroy(tgrad_group* group);
+
+/*
+ * Logits and the token of every row.  z = data / temperature.  A row whose target lies outside 0..vocab-1 (-100, say) is
+ * ignored: nothing of it is read, its log-probability is 0 and its gradient 0.
+ */
+typedef struct {
+  const void* data;         /* device pointer: TGRAD_F32, TGRAD_BF16 or TGRAD_F16, rows of `vocab` consecutive elements */
+  int64_t rows;             /* 0..2^31-1 */
+  int64_t vocab;            /* 1..2^31-1 */
+  int64_t row_stride;       /* elements from one row to the next, >= vocab */
+  const int64_t* targets;   /* device pointer, int64[rows] */
+  int32_t dtype;
+  float temperature;        /* > 0 */
+} tgrad_logits;
+
+/*
+ * logp[n] = z[n, y_n] - lse[n],  lse[n] = log sum_v exp z[n, v], in float32.  Entries of -inf have probability 0; a row of
+ * nothing else, or with a NaN or +inf in it, has a NaN.  Reads the logits once.
+ *  logp, lse   device pointers, float32[rows]; either may be NULL.
+ *  hip_stream  stream to enqueue on (NULL = the default stream).  Does not wait.  The same holds for the calls below.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_token_logprobs(const tgrad_logits* logits, float* logp, float* lse, void* hip_stream);
+
+/*
+ * dlogits[n, v] = dlogp[n] / temperature * ([v = y_n] - exp(z[n, v] - lse[n])), rounded once to the logits' type.
+ *  lse, dlogp      device pointers, float32[rows].  A row with dlogp = 0 is not read.
+ *  dlogits         device pointer, the logits' type, rows `dlogits_stride` >= vocab elements apart; what lies between them is
+ *                  left alone.  May be logits->data, with the same stride.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_token_logprobs_backward(const tgrad_logits* logits, const float* lse, const float* dlogp, void* dlogits,
+                                  int64_t dlogits_stride, void* hip_stream);
+
+typedef struct {
+  float clip_low, clip_high;   /* the ratio is clipped to 1 - clip_low .. 1 + clip_high; clip_low 0..1, clip_high >= 0 */
+  float kl_beta;               /* weight of the KL term; 0: it is only reported */
+} tgrad_policy;
+
+/* Bytes of scratch of tgrad_policy_loss and tgrad_preference_loss.  Host-only.  Errors: INVALID_ARG. */
+int tgrad_loss_query_size(int64_t rows, int64_t pairs, size_t* workspace_bytes);
+
+/*
+ * Clipped policy loss with a KL term towards a reference, and its gradient:
+ *   r = exp(logp - old);  pg = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A);  d = ref - logp;  kl = exp(d) - d - 1
+ *   loss = sum_n w_n (pg + kl_beta kl);  dlogits = dloss d loss / d logits.
+ * Where both arguments of the minimum are equal the gradient is that of the unclipped one.
+ *  weight, advantage, old_logp  device pointers, float32[rows].  weight carries the mask and the normalisation (1 / number of
+ *                tokens, say); a row of weight 0 is ignored like one without a target: none of its entries anywhere is read.
+ *  ref_logp      the same, or NULL: kl = 0.
+ *  dloss         device pointer to one float32 (a loss scale), or NULL: 1.
+ *  workspace_dev device pointer, >= tgrad_loss_query_size(rows, 0), 256-byte aligned.
+ *  stats         device pointer, float32[4]: sums over n of w (pg + kl_beta kl), w pg, w kl, w [clipped].
+ *  logp          device pointer, float32[rows], or NULL.
+ *  dlogits       as for tgrad_token_logprobs_backward, or NULL: no gradient.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_policy_loss(const tgrad_logits* logits, const tgrad_policy* policy, const float* weight, const float* advantage,
+                      const float* old_logp, const float* ref_logp, const float* dloss, void* workspace_dev, float* stats,
+                      float* logp, void* dlogits, int64_t dlogits_stride, void* hip_stream);
+
+typedef struct {
+  float beta;              /* > 0 */
+  float label_smoothing;   /* 0 .. 0.5: share of pairs that are labelled the wrong way round */
+} tgrad_preference;
+
+/*
+ * Preference loss on paired log ratios, and its gradient.  Sequence i is rows seq_start[i] .. seq_start[i + 1] - 1 of the logits; the first
+ * `pairs` sequences are the chosen answers, the next `pairs` the rejected ones, in the same order.
+ *   R_i = beta sum_n w_n (logp_n - ref_n);  h = R_chosen - R_rejected
+ *   loss = mean over pairs of -(1 - s) log sigma(h) - s log sigma(-h);  dlogits = dloss d loss / d logits.
+ * A sequence without rows, or whose weights are all 0, has R = 0.
+ *  seq_start  device pointer, int64[2 pairs + 1], ascending; bounds outside 0 .. rows are taken as the nearest inside.
+ *             Rows in no sequence have no gradient.  pairs >= 1.
+ *  weight, ref_logp  device pointers, float32[rows]; rows of weight 0 are ignored.
+ *  dloss, workspace_dev (tgrad_loss_query_size(rows, pairs)), logp, dlogits  as for tgrad_policy_loss.
+ *  loss       device pointer, one float32.
+ *  rewards    device pointer, float32[2 pairs]: R.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* preference, int64_t pairs,
+                          const int64_t* seq_start, const float* weight, const float* ref_logp, const float* dloss,
+                          void* workspace_dev, float* loss, float* rewards, float* logp, void* dlogits,
+                          int64_t dlogits_stride, void* hip_stream);
+
 /* Static description of a status code. */
 const char* tgrad_strerror(int status);
 

@@ -1,0 +1,56 @@
+"""What the bindings of the operators around the step share: tensor checks, type codes, streams."""
+from __future__ import annotations
+
+import functools
+
+import torch
+
+from . import tgrad as T
+
+REAL_TYPES = {torch.float32: T.TGRAD_F32, torch.bfloat16: T.TGRAD_BF16, torch.float16: T.TGRAD_F16}
+
+
+def refuse(what: str):
+    raise T.TgradError(T.TGRAD_ERR_INVALID_ARG, what)
+
+
+def on_stream(f):
+    """Adds `stream=`: the call runs with that stream current, so that what it allocates belongs to it (memory of another stream's
+    could still be in use there, and scratch could be handed out again before the kernels have run)."""
+    @functools.wraps(f)
+    def run(*args, stream=None, **kw):
+        if stream is None:
+            return f(*args, **kw)
+        with torch.cuda.stream(stream):
+            return f(*args, **kw)
+    return run
+
+
+def stream_of(device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def vector(t, n, dtype, device, what):
+    """Address of a dense vector of n elements (None stays None); anything else is refused."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        refuse("%s: %s[%d], dense, on the logits' device" % (what, dtype, n))
+    return t.data_ptr()
+
+
+def check(rc: int, where: str) -> None:
+    if rc != T.TGRAD_OK:
+        raise T.TgradError(rc, where)
+
+
+def call(device, fn, where, *args):
+    """One library call with `device` current."""
+    if torch.cuda.current_device() == device.index:
+        rc = fn(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args)
+    check(rc, where)
+
+

@@ -1,0 +1,390 @@
+// A group of tensors of any types and sizes: global gradient norm, clipping, AdamW.
+//
+// The list of tensors lies in device memory and is cut into pieces of kPiece elements; a table says for every piece which
+// tensor it belongs to, so that one launch serves any number of tensors and small ones cost no more than their bytes.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+#include "launch_util.h"
+#include "train_common.h"
+
+using namespace tgrad;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int64_t kPiece = 4096;          // elements
+constexpr int kMaxSums = 2048;            // workgroups that leave a partial sum
+constexpr int kPut = 32;                  // tensors per launch that writes the list
+
+struct Entry {                            // a tensor as the kernels see it
+  void* grad;
+  void* out;
+  void* param;
+  void* m;
+  void* v;
+  int64_t numel;
+  int32_t grad_dtype, param_dtype;
+  float lr_scale, weight_decay;
+};
+
+struct Piece {
+  int32_t entry, index;                   // elements index * kPiece ... of that tensor
+};
+
+struct PutArgs {
+  Entry e[kPut];
+  int32_t first_piece[kPut];
+};
+
+// Writes entries first .. first + gridDim.x - 1, and their part of the table where `pieces` is not null.
+__global__ void k_group_put(PutArgs a, int first, Entry* entries, Piece* pieces) {
+  const int b = blockIdx.x;
+  const Entry e = a.e[b];
+  if (threadIdx.x == 0) entries[first + b] = e;
+  if (!pieces) return;
+  const int64_t n = (e.numel + kPiece - 1) / kPiece;
+  for (int64_t i = threadIdx.x; i < n; i += blockDim.x) pieces[a.first_piece[b] + i] = Piece{first + b, (int32_t)i};
+}
+
+__global__ void k_group_zero(uint32_t* ticket) { *ticket = 0; }
+
+__device__ __forceinline__ float load_real(const void* p, int real, int64_t i) {
+  if (real == TGRAD_F32) return static_cast<const float*>(p)[i];
+  if (real == TGRAD_BF16) return Elem<TGRAD_BF16>::widen(static_cast<const uint16_t*>(p)[i]);
+  return Elem<TGRAD_F16>::widen(static_cast<const _Float16*>(p)[i]);
+}
+__device__ __forceinline__ void store_real(void* p, int real, int64_t i, float v) {
+  if (real == TGRAD_F32) static_cast<float*>(p)[i] = v;
+  else if (real == TGRAD_BF16) static_cast<uint16_t*>(p)[i] = Elem<TGRAD_BF16>::narrow(v);
+  else static_cast<_Float16*>(p)[i] = Elem<TGRAD_F16>::narrow(v);
+}
+
+// Real numbers of a piece: [first, first + count) of the tensor's.
+struct Span {
+  int64_t first;
+  int count;
+};
+__device__ __forceinline__ Span piece_span(const Entry& e, int index, bool cplx) {
+  const int64_t at = (int64_t)index * kPiece, left = e.numel - at;
+  const int n = (int)(left < kPiece ? left : kPiece);
+  return cplx ? Span{at * 2, n * 2} : Span{at, n};
+}
+
+// sum |g|^2.  Squares and sums in float64: the square of a float32 is exact there, and no finite gradient overflows.  Every
+// workgroup leaves one partial sum; the last one to come adds them up in the order of the workgroups, so that the result does
+// not depend on which one that is.
+__global__ __launch_bounds__(kThreads) void k_group_sumsq(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
+                                                          int64_t npieces, double* sums, uint32_t* ticket, float max_norm,
+                                                          const double* add, tgrad_norm* out) {
+  __shared__ double lds[kWaves];
+  __shared__ uint32_t last;
+  double acc = 0.;
+  for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
+    const Piece pc = pieces[p];
+    const Entry e = entries[pc.entry];
+    const int real = real_type(e.grad_dtype);
+    const Span s = piece_span(e, pc.index, complex_type(e.grad_dtype));
+    for (int i = threadIdx.x; i < s.count; i += kThreads) {
+      const double g = (double)load_real(e.grad, real, s.first + i);
+      acc += g * g;
+    }
+  }
+  acc = block_sum<kWaves>(acc, lds);
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(sums + blockIdx.x, acc, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  acc = 0.;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads)
+    acc += __hip_atomic_load(sums + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  acc = block_sum<kWaves>(acc, lds);
+  if (threadIdx.x == 0) {
+    if (add) acc += *add;
+    const float norm = (float)sqrt(acc);
+    const float c = max_norm / (norm + 1e-6f);
+    out->sumsq = acc;
+    out->norm = norm;
+    out->coef = c > 1.f ? 1.f : c;        // a NaN stays one
+    *ticket = 0;
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void k_group_scale(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
+                                                          int64_t npieces, const tgrad_norm* norm) {
+  const float coef = norm->coef;
+  for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
+    const Piece pc = pieces[p];
+    const Entry e = entries[pc.entry];
+    if (coef == 1.f && e.out == e.grad) continue;
+    const int real = real_type(e.grad_dtype);
+    const Span s = piece_span(e, pc.index, complex_type(e.grad_dtype));
+    for (int i = threadIdx.x; i < s.count; i += kThreads)
+      store_real(e.out, real, s.first + i, coef * load_real(e.grad, real, s.first + i));
+  }
+}
+
+struct AdamK {
+  double lr;
+  float beta1, beta2, one_beta1, one_beta2, inv_c1, inv_c2, eps;
+  bool skip_nonfinite;
+};
+
+__global__ __launch_bounds__(kThreads) void k_group_adamw(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
+                                                          int64_t npieces, AdamK h, const tgrad_norm* norm) {
+  const float coef = norm ? norm->coef : 1.f;
+  if (h.skip_nonfinite && !(fabsf(norm->norm) < INFINITY)) return;
+  for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
+    const Piece pc = pieces[p];
+    const Entry e = entries[pc.entry];
+    const bool cplx = complex_type(e.grad_dtype);
+    const int gr = real_type(e.grad_dtype), pr = real_type(e.param_dtype);
+    const double lr = h.lr * (double)e.lr_scale;
+    const float decay = (float)(1. - lr * (double)e.weight_decay), step = (float)(lr * (double)h.inv_c1);
+    const Span s = piece_span(e, pc.index, false);
+    float* M = static_cast<float*>(e.m);
+    float* V = static_cast<float*>(e.v);
+    for (int k = threadIdx.x; k < s.count; k += kThreads) {
+      const int64_t i = s.first + k;
+      if (!cplx) {
+        const float g = coef * load_real(e.grad, gr, i);
+        const float m = h.beta1 * M[i] + h.one_beta1 * g, v = h.beta2 * V[i] + h.one_beta2 * (g * g);
+        M[i] = m;
+        V[i] = v;
+        store_real(e.param, pr, i, decay * load_real(e.param, pr, i) - step * m / (sqrtf(v * h.inv_c2) + h.eps));
+      } else {
+        const float gx = coef * load_real(e.grad, gr, 2 * i), gy = coef * load_real(e.grad, gr, 2 * i + 1);
+        const float mx = h.beta1 * M[2 * i] + h.one_beta1 * gx, my = h.beta1 * M[2 * i + 1] + h.one_beta1 * gy;
+        const float v = h.beta2 * V[i] + h.one_beta2 * (gx * gx + gy * gy);
+        M[2 * i] = mx;
+        M[2 * i + 1] = my;
+        V[i] = v;
+        const float d = step / (sqrtf(v * h.inv_c2) + h.eps);
+        store_real(e.param, pr, 2 * i, decay * load_real(e.param, pr, 2 * i) - d * mx);
+        store_real(e.param, pr, 2 * i + 1, decay * load_real(e.param, pr, 2 * i + 1) - d * my);
+      }
+    }
+  }
+}
+
+constexpr size_t kAlign = 256;
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+struct Layout {
+  int64_t npieces = 0;
+  size_t entries = 0, pieces = 0, sums = 0, ticket = 0, bytes = 0;
+};
+
+bool known_type(int32_t dt) { return dt >= TGRAD_C64 && dt <= TGRAD_F16; }
+bool aligned(const void* p, int real) { return (uintptr_t)p % (uintptr_t)real_bytes(real) == 0; }
+
+int layout(const tgrad_tensor* t, int64_t n, Layout* l) {
+  if (!t || n < 1) return TGRAD_ERR_INVALID_ARG;
+  if (n > ((int64_t)1 << 20)) return TGRAD_ERR_UNSUPPORTED;
+  for (int64_t i = 0; i < n; ++i) {
+    if (t[i].numel < 0) return TGRAD_ERR_INVALID_ARG;
+    if (t[i].numel > ((int64_t)1 << 40)) return TGRAD_ERR_UNSUPPORTED;
+    l->npieces += (t[i].numel + kPiece - 1) / kPiece;
+    if (l->npieces > ((int64_t)1 << 31) - 1) return TGRAD_ERR_UNSUPPORTED;
+  }
+  size_t o = 0;
+  auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes); return at; };
+  l->entries = take((size_t)n * sizeof(Entry));
+  l->pieces = take((size_t)l->npieces * sizeof(Piece));
+  l->sums = take(kMaxSums * sizeof(double));
+  l->ticket = take(sizeof(uint32_t));
+  l->bytes = o;
+  return TGRAD_OK;
+}
+
+int check_tensor(const tgrad_tensor& t) {
+  if (!known_type(t.grad_dtype)) return TGRAD_ERR_INVALID_ARG;
+  if (!(std::isfinite(t.lr_scale) && std::isfinite(t.weight_decay) && t.lr_scale >= 0.f && t.weight_decay >= 0.f))
+    return TGRAD_ERR_INVALID_ARG;
+  const int gr = real_type(t.grad_dtype);
+  if (t.numel > 0 && !t.grad) return TGRAD_ERR_INVALID_ARG;
+  if (!aligned(t.grad, gr) || !aligned(t.out, gr)) return TGRAD_ERR_INVALID_ARG;
+  if (!t.param) return t.exp_avg || t.exp_avg_sq ? TGRAD_ERR_INVALID_ARG : TGRAD_OK;
+  if (!known_type(t.param_dtype) || complex_type(t.param_dtype) != complex_type(t.grad_dtype)) return TGRAD_ERR_INVALID_ARG;
+  if (t.numel > 0 && (!t.exp_avg || !t.exp_avg_sq)) return TGRAD_ERR_INVALID_ARG;
+  if (!aligned(t.param, real_type(t.param_dtype)) || !aligned(t.exp_avg, TGRAD_F32) || !aligned(t.exp_avg_sq, TGRAD_F32))
+    return TGRAD_ERR_INVALID_ARG;
+  if (t.numel > 0 && (t.param == t.grad || t.exp_avg == t.exp_avg_sq || t.param == t.exp_avg || t.param == t.exp_avg_sq))
+    return TGRAD_ERR_INVALID_ARG;
+  return TGRAD_OK;
+}
+
+// Host record of a tensor: what a later bind may not change.
+struct Kind {
+  int64_t numel;
+  int32_t grad_dtype, param_dtype;
+  bool out, param;
+};
+
+}  // namespace
+
+struct tgrad_group {
+  Layout lay;
+  char* ws;
+  hipStream_t stream;
+  std::vector<Kind> kinds;
+  bool steps;                              // every tensor has a parameter and moments
+
+  const Entry* entries() const { return reinterpret_cast<const Entry*>(ws + lay.entries); }
+  const Piece* pieces() const { return reinterpret_cast<const Piece*>(ws + lay.pieces); }
+};
+
+namespace {
+
+int launched() { return hipGetLastError() == hipSuccess ? TGRAD_OK : TGRAD_ERR_HIP; }
+bool pending() { return hipPeekAtLastError() != hipSuccess; }
+
+// The list goes to the device as kernel arguments: ordered on the stream, and the caller's array is free at once.
+void put(tgrad_group* g, const tgrad_tensor* t, bool table) {
+  const int64_t n = (int64_t)g->kinds.size();
+  int64_t piece = 0;
+  for (int64_t a = 0; a < n; a += kPut) {
+    PutArgs args;
+    const int cnt = (int)(n - a < kPut ? n - a : kPut);
+    for (int j = 0; j < cnt; ++j) {
+      const tgrad_tensor& x = t[a + j];
+      args.e[j] = Entry{x.grad, x.out ? x.out : x.grad, x.param, x.exp_avg, x.exp_avg_sq, x.numel,
+                        x.grad_dtype, x.param ? x.param_dtype : x.grad_dtype, x.lr_scale, x.weight_decay};
+      args.first_piece[j] = (int32_t)piece;
+      piece += (x.numel + kPiece - 1) / kPiece;
+    }
+    k_group_put<<<dim3(cnt), dim3(256), 0, g->stream>>>(args, (int)a, reinterpret_cast<Entry*>(g->ws + g->lay.entries),
+                                                        table ? reinterpret_cast<Piece*>(g->ws + g->lay.pieces) : nullptr);
+  }
+}
+
+int grid_for(const tgrad_group* g, int per_cu) {
+  const int64_t most = (int64_t)compute_units() * per_cu;
+  const int64_t n = g->lay.npieces < most ? g->lay.npieces : most;
+  return n < 1 ? 1 : (int)n;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tgrad_group_query_size(const tgrad_tensor* tensors, int64_t n, size_t* workspace_bytes) {
+  if (!workspace_bytes) return TGRAD_ERR_INVALID_ARG;
+  Layout l;
+  const int rc = layout(tensors, n, &l);
+  if (rc == TGRAD_OK) *workspace_bytes = l.bytes;
+  return rc;
+}
+
+int tgrad_group_init(tgrad_group** out, const tgrad_tensor* tensors, int64_t n, void* workspace_dev, void* hip_stream) {
+  if (!out) return TGRAD_ERR_INVALID_ARG;
+  *out = nullptr;
+  Layout l;
+  const int rc = layout(tensors, n, &l);
+  if (rc != TGRAD_OK) return rc;
+  if (!workspace_dev || (uintptr_t)workspace_dev % kAlign) return TGRAD_ERR_INVALID_ARG;
+  for (int64_t i = 0; i < n; ++i)
+    if (check_tensor(tensors[i]) != TGRAD_OK) return TGRAD_ERR_INVALID_ARG;
+  if (pending()) return TGRAD_ERR_HIP;
+  tgrad_group* g = new (std::nothrow) tgrad_group();
+  if (!g) return TGRAD_ERR_INVALID_ARG;
+  try {
+    g->kinds.resize((size_t)n);
+  } catch (...) {
+    delete g;
+    return TGRAD_ERR_INVALID_ARG;
+  }
+  g->lay = l;
+  g->ws = static_cast<char*>(workspace_dev);
+  g->stream = static_cast<hipStream_t>(hip_stream);
+  g->steps = true;
+  for (int64_t i = 0; i < n; ++i) {
+    const tgrad_tensor& t = tensors[i];
+    g->kinds[(size_t)i] = Kind{t.numel, t.grad_dtype, t.param_dtype, t.out != nullptr, t.param != nullptr};
+    g->steps = g->steps && (t.param || t.numel == 0);
+  }
+  put(g, tensors, true);
+  k_group_zero<<<dim3(1), dim3(1), 0, g->stream>>>(reinterpret_cast<uint32_t*>(g->ws + l.ticket));
+  if (launched() != TGRAD_OK) {
+    delete g;
+    return TGRAD_ERR_HIP;
+  }
+  *out = g;
+  return TGRAD_OK;
+}
+
+int tgrad_group_bind(tgrad_group* group, const tgrad_tensor* tensors) {
+  if (!group || !tensors) return TGRAD_ERR_INVALID_ARG;
+  for (size_t i = 0; i < group->kinds.size(); ++i) {
+    const Kind& k = group->kinds[i];
+    const tgrad_tensor& t = tensors[i];
+    if (t.numel != k.numel || t.grad_dtype != k.grad_dtype || (t.out != nullptr) != k.out || (t.param != nullptr) != k.param ||
+        (k.param && t.param_dtype != k.param_dtype) || check_tensor(t) != TGRAD_OK)
+      return TGRAD_ERR_INVALID_ARG;
+  }
+  if (pending()) return TGRAD_ERR_HIP;
+  put(group, tensors, false);
+  return launched();
+}
+
+int tgrad_group_grad_norm(tgrad_group* group, float max_norm, const double* add_sumsq_dev, tgrad_norm* norm_dev) {
+  if (!group || !norm_dev || !(max_norm >= 0.f) || (uintptr_t)norm_dev % 8 || (uintptr_t)add_sumsq_dev % 8)
+    return TGRAD_ERR_INVALID_ARG;
+  if (pending()) return TGRAD_ERR_HIP;
+  const int grid = grid_for(group, 4);
+  k_group_sumsq<<<dim3(grid < kMaxSums ? grid : kMaxSums), dim3(kThreads), 0, group->stream>>>(
+      group->entries(), group->pieces(), group->lay.npieces, reinterpret_cast<double*>(group->ws + group->lay.sums),
+      reinterpret_cast<uint32_t*>(group->ws + group->lay.ticket), max_norm, add_sumsq_dev, norm_dev);
+  return launched();
+}
+
+int tgrad_group_scale(tgrad_group* group, const tgrad_norm* norm_dev) {
+  if (!group || !norm_dev || (uintptr_t)norm_dev % 8) return TGRAD_ERR_INVALID_ARG;
+  if (pending()) return TGRAD_ERR_HIP;
+  k_group_scale<<<dim3(grid_for(group, 8)), dim3(kThreads), 0, group->stream>>>(group->entries(), group->pieces(),
+                                                                                group->lay.npieces, norm_dev);
+  return launched();
+}
+
+int tgrad_group_clip(tgrad_group* group, float max_norm, const double* add_sumsq_dev, tgrad_norm* norm_dev) {
+  const int rc = tgrad_group_grad_norm(group, max_norm, add_sumsq_dev, norm_dev);
+  return rc == TGRAD_OK ? tgrad_group_scale(group, norm_dev) : rc;
+}
+
+int tgrad_group_adamw(tgrad_group* group, const tgrad_adamw* hyper, int64_t t, const tgrad_norm* norm_dev) {
+  if (!group || !hyper || t < 0 || !group->steps || (uintptr_t)norm_dev % 8) return TGRAD_ERR_INVALID_ARG;
+  const tgrad_adamw& h = *hyper;
+  if (!(std::isfinite(h.lr) && h.lr >= 0. && h.beta1 >= 0. && h.beta1 < 1. && h.beta2 >= 0. && h.beta2 < 1. &&
+        std::isfinite(h.eps) && h.eps >= 0.) ||
+      h.skip_nonfinite < 0 || h.skip_nonfinite > 1 || (h.skip_nonfinite && !norm_dev))
+    return TGRAD_ERR_INVALID_ARG;
+  if (pending()) return TGRAD_ERR_HIP;
+  const double tau = (double)(t + 1);
+  AdamK k;
+  k.lr = h.lr;
+  k.beta1 = (float)h.beta1;
+  k.beta2 = (float)h.beta2;
+  k.one_beta1 = (float)(1. - h.beta1);
+  k.one_beta2 = (float)(1. - h.beta2);
+  k.inv_c1 = (float)(1. / (1. - std::pow(h.beta1, tau)));
+  k.inv_c2 = (float)(1. / (1. - std::pow(h.beta2, tau)));
+  k.eps = (float)h.eps;
+  k.skip_nonfinite = h.skip_nonfinite != 0;
+  k_group_adamw<<<dim3(grid_for(group, 8)), dim3(kThreads), 0, group->stream>>>(group->entries(), group->pieces(),
+                                                                                group->lay.npieces, k, norm_dev);
+  return launched();
+}
+
+int tgrad_group_destroy(tgrad_group* group) {
+  if (!group) return TGRAD_ERR_INVALID_ARG;
+  delete group;
+  return TGRAD_OK;
+}
+
+}  // extern "C"

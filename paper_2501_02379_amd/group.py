@@ -1,0 +1,172 @@
+"""A group of tensors - gradients, parameters, moments - for the global gradient norm, clipping and AdamW: ctypes binding of the
+tgrad_group_* entry points of include/tgrad.h."""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Sequence
+
+import torch
+
+from . import tgrad as T
+from ._marshal import REAL_TYPES, call, check, refuse
+
+TYPES = {**REAL_TYPES, torch.complex64: T.TGRAD_C64}
+_MOMENTS = (torch.float32, torch.complex64)
+
+
+def _addresses(tensors, n, what, device):
+    if tensors is None:
+        return [None] * n
+    tensors = list(tensors)
+    if len(tensors) != n:
+        refuse("%s: one for every gradient" % what)
+    for t in tensors:
+        if t is not None and (t.device != device or not t.is_contiguous()):
+            refuse("%s: dense tensors on one GPU" % what)
+    return tensors
+
+
+class Group:
+    """Gradients of any shapes and types (float32, bfloat16, float16, complex64) and, for AdamW, their parameters and float32
+    moments; bf16 (re, im) pairs are int16 tensors with a trailing axis of 2, as everywhere in this library.  `exp_avg` has the
+    gradient's shape (complex64, or float32 with a trailing axis of 2, for a complex tensor), `exp_avg_sq` float32 with one number
+    per element.  `outs`: where `tgrad_group_scale` and `tgrad_group_clip` put the scaled gradients (None: in place).
+
+    Every call is enqueued on the stream given here (the device's current one by default) and waits for nothing.  The group
+    keeps its tensors alive.  Results (`tgrad_group_grad_norm`, `tgrad_group_clip`) are a float32 tensor (norm, factor) on the
+    device; the buffer behind it also holds the sum of squares in float64, `group.sumsq(result)`.
+    """
+
+    def __init__(self, grads: Sequence[torch.Tensor], params=None, exp_avg=None, exp_avg_sq=None, outs=None,
+                 lr_scale: Optional[Sequence[float]] = None, weight_decay: Optional[Sequence[float]] = None, stream=None):
+        self.lib = T.load()
+        self.handle = C.c_void_p(None)
+        grads = list(grads)
+        if not grads:
+            refuse("a group has at least one tensor")
+        if not grads[0].is_cuda:
+            refuse("grads: tensors on the GPU")
+        self.device = grads[0].device
+        self.lr_scale, self.weight_decay = lr_scale, weight_decay
+        table = self._table(grads, params, exp_avg, exp_avg_sq, outs)
+        size = C.c_size_t(0)
+        check(self.lib.tgrad_group_query_size(table, len(grads), C.byref(size)), "tgrad_group_query_size")
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(self.stream):
+            self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        call(self.device, self.lib.tgrad_group_init, "tgrad_group_init", C.byref(self.handle), table, len(grads),
+             self.workspace.data_ptr(), self.stream.cuda_stream)
+
+    def _table(self, grads, params, exp_avg, exp_avg_sq, outs):
+        n, dev = len(grads), self.device
+        grads = _addresses(grads, n, "grads", dev)
+        params, exp_avg = _addresses(params, n, "params", dev), _addresses(exp_avg, n, "exp_avg", dev)
+        exp_avg_sq, outs = _addresses(exp_avg_sq, n, "exp_avg_sq", dev), _addresses(outs, n, "outs", dev)
+        lr, wd = self.lr_scale or [1.0] * n, self.weight_decay or [0.0] * n
+        if len(lr) != n or len(wd) != n:
+            refuse("lr_scale, weight_decay: one for every gradient")
+        table = (T.tgrad_tensor * n)()
+        for i in range(n):
+            g, p, m, v, o = grads[i], params[i], exp_avg[i], exp_avg_sq[i], outs[i]
+            if g is None:
+                refuse("grads: a tensor each")
+            numel, kind = self._type(g, "grads")
+            if o is not None and (o.shape != g.shape or o.dtype != g.dtype):
+                refuse("outs: the gradient's shape and type")
+            pkind = kind
+            if p is not None:
+                count, pkind = self._type(p, "params")
+                if pkind == T.TGRAD_F32 and kind in (T.TGRAD_C64, T.TGRAD_CBF16) and p.shape[-1:] == (2,):
+                    count, pkind = p.numel() // 2, T.TGRAD_C64        # complex64 as float32 pairs
+                width = 2 if kind in (T.TGRAD_C64, T.TGRAD_CBF16) else 1
+                if count != numel or m is None or v is None:
+                    refuse("params: the gradient's number of elements, with moments")
+                if m.dtype not in _MOMENTS or m.numel() * (2 if m.is_complex() else 1) != width * numel or \
+                        v.dtype != torch.float32 or v.numel() != numel:
+                    refuse("moments: float32, the parameter's size")
+            elif m is not None or v is not None:
+                refuse("moments belong to parameters")
+            at = [t.data_ptr() if t is not None else None for t in (g, o, p, m, v)]
+            table[i] = T.tgrad_tensor(numel, *at, kind, pkind, lr[i], wd[i])
+        self.tensors = (grads, params, exp_avg, exp_avg_sq, outs)
+        return table
+
+    @staticmethod
+    def _type(t, what):
+        if t.dtype == torch.int16 and t.shape[-1:] == (2,):
+            return t.numel() // 2, T.TGRAD_CBF16
+        if t.dtype not in TYPES:
+            refuse("%s: float32, bfloat16, float16, complex64, or bf16 pairs as int16[..., 2]" % what)
+        return t.numel(), TYPES[t.dtype]
+
+    def tgrad_group_bind(self, grads, params=None, exp_avg=None, exp_avg_sq=None, outs=None) -> None:
+        """The same tensors at new addresses (gradients allocated anew); what is None stays as it is."""
+        old = self.tensors
+        new = [list(x) if x is not None else y for x, y in zip((grads, params, exp_avg, exp_avg_sq, outs), old)]
+        if any(len(x) != len(old[0]) for x in new):
+            refuse("tgrad_group_bind: as many tensors as at init")
+        try:
+            table = self._table(*new)
+            call(self.device, self.lib.tgrad_group_bind, "tgrad_group_bind", self.handle, table)
+        except Exception:
+            self.tensors = old
+            raise
+
+    def _result(self, into):
+        if into is None:
+            if torch.cuda.current_stream(self.device) == self.stream:
+                return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
+            with torch.cuda.stream(self.stream):
+                return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
+        if into.dtype != torch.float32 or into.shape != (2,) or into.storage_offset() != 2 or into.device != self.device:
+            refuse("into: an earlier result")
+        return into
+
+    def tgrad_group_grad_norm(self, max_norm: float, add_sumsq=None, into=None):
+        """-> (norm, factor): global norm of all gradients and min(1, max_norm / (norm + 1e-6)).  `add_sumsq`: a float64 tensor
+        of one element, the sum of squares of gradients that lie elsewhere.  `into`: an earlier result, overwritten."""
+        r = self._result(into)
+        call(self.device, self.lib.tgrad_group_grad_norm, "tgrad_group_grad_norm", self.handle, max_norm, self._add(add_sumsq),
+             r.data_ptr() - 8)
+        return r
+
+    def tgrad_group_clip(self, max_norm: float, add_sumsq=None, into=None):
+        """`tgrad_group_grad_norm`, and the gradients scaled by the factor; -> (norm, factor)."""
+        r = self._result(into)
+        call(self.device, self.lib.tgrad_group_clip, "tgrad_group_clip", self.handle, max_norm, self._add(add_sumsq),
+             r.data_ptr() - 8)
+        return r
+
+    def tgrad_group_scale(self, norm) -> None:
+        """The gradients times the factor of an earlier result."""
+        call(self.device, self.lib.tgrad_group_scale, "tgrad_group_scale", self.handle, self._result(norm).data_ptr() - 8)
+
+    def tgrad_group_adamw(self, t: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, norm=None,
+                          skip_nonfinite: bool = False) -> None:
+        """One AdamW step after `t` others; `norm`: a result whose factor scales the gradients as they are read."""
+        hyper = T.tgrad_adamw(lr, beta1, beta2, eps, int(skip_nonfinite))
+        at = self._result(norm).data_ptr() - 8 if norm is not None else None
+        call(self.device, self.lib.tgrad_group_adamw, "tgrad_group_adamw", self.handle, C.byref(hyper), int(t), at)
+
+    @staticmethod
+    def sumsq(result):
+        """The float64 sum of squares behind a result."""
+        return torch.as_strided(result, (2,), (1,), 0).view(torch.float64)
+
+    def _add(self, t):
+        if t is None:
+            return None
+        if t.dtype != torch.float64 or t.numel() != 1 or t.device != self.device:
+            refuse("add_sumsq: one float64 on the device")
+        return t.data_ptr()
+
+    def tgrad_group_destroy(self) -> None:
+        if self.handle:
+            self.lib.tgrad_group_destroy(self.handle)
+            self.handle = C.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.tgrad_group_destroy()
+        except Exception:
+            pass

@@ -15,6 +15,7 @@ import numpy as np
 
 MAX_NDIM = 6
 TGRAD_C64, TGRAD_CBF16 = 0, 1
+TGRAD_F32, TGRAD_BF16, TGRAD_F16 = 2, 3, 4
 TGRAD_SELECT_TOPK_MAG = 0
 TGRAD_SELECT_RANDOM = 1
 TGRAD_ORDER_US_LR, TGRAD_ORDER_LR_US, TGRAD_ORDER_SUM = 0, 1, 2
@@ -38,6 +39,10 @@ EXPORTS = (
     "tgrad_set_state", "tgrad_set_profiling", "tgrad_get_kernel_times", "tgrad_calibration_copy",
     "tgrad_calibration_mfma", "tgrad_calibration_tile_stream",
     "tgrad_destroy", "tgrad_strerror",
+    "tgrad_group_query_size", "tgrad_group_init", "tgrad_group_bind", "tgrad_group_grad_norm", "tgrad_group_scale",
+    "tgrad_group_clip", "tgrad_group_adamw", "tgrad_group_destroy",
+    "tgrad_token_logprobs", "tgrad_token_logprobs_backward", "tgrad_loss_query_size", "tgrad_policy_loss",
+    "tgrad_preference_loss",
 )
 
 
@@ -64,6 +69,51 @@ class tgrad_config(C.Structure):
         ("warm_restart", C.c_int32),
         ("eig_max_sweeps", C.c_int32),
     ]
+
+
+class tgrad_tensor(C.Structure):
+    _fields_ = [
+        ("numel", C.c_int64),
+        ("grad", C.c_void_p),
+        ("out", C.c_void_p),
+        ("param", C.c_void_p),
+        ("exp_avg", C.c_void_p),
+        ("exp_avg_sq", C.c_void_p),
+        ("grad_dtype", C.c_int32),
+        ("param_dtype", C.c_int32),
+        ("lr_scale", C.c_float),
+        ("weight_decay", C.c_float),
+    ]
+
+
+class tgrad_adamw(C.Structure):
+    _fields_ = [
+        ("lr", C.c_double),
+        ("beta1", C.c_double),
+        ("beta2", C.c_double),
+        ("eps", C.c_double),
+        ("skip_nonfinite", C.c_int32),
+    ]
+
+
+class tgrad_logits(C.Structure):
+    _fields_ = [
+        ("data", C.c_void_p),
+        ("rows", C.c_int64),
+        ("vocab", C.c_int64),
+        ("row_stride", C.c_int64),
+        ("targets", C.c_void_p),
+        ("dtype", C.c_int32),
+        ("temperature", C.c_float),
+    ]
+
+
+class tgrad_policy(C.Structure):
+    _fields_ = [("clip_low", C.c_float), ("clip_high", C.c_float), ("kl_beta", C.c_float)]
+
+
+class tgrad_preference(C.Structure):
+    _fields_ = [("beta", C.c_float), ("label_smoothing", C.c_float)]
 
 
 class TgradError(RuntimeError):
@@ -100,6 +150,21 @@ def load():
     lib.tgrad_calibration_copy.argtypes = [vp, vp, sz, vp]
     lib.tgrad_calibration_mfma.argtypes = [C.c_int, C.c_int64, vp, vp, C.POINTER(C.c_double)]
     lib.tgrad_calibration_tile_stream.argtypes = [vp, sz, C.c_int, C.c_int, vp, C.POINTER(C.c_int64)]
+    lib.tgrad_group_query_size.argtypes = [C.POINTER(tgrad_tensor), C.c_int64, C.POINTER(sz)]
+    lib.tgrad_group_init.argtypes = [C.POINTER(vp), C.POINTER(tgrad_tensor), C.c_int64, vp, vp]
+    lib.tgrad_group_bind.argtypes = [vp, C.POINTER(tgrad_tensor)]
+    lib.tgrad_group_grad_norm.argtypes = [vp, C.c_float, vp, vp]
+    lib.tgrad_group_scale.argtypes = [vp, vp]
+    lib.tgrad_group_clip.argtypes = [vp, C.c_float, vp, vp]
+    lib.tgrad_group_adamw.argtypes = [vp, C.POINTER(tgrad_adamw), C.c_int64, vp]
+    lib.tgrad_group_destroy.argtypes = [vp]
+    lib.tgrad_token_logprobs.argtypes = [C.POINTER(tgrad_logits), vp, vp, vp]
+    lib.tgrad_token_logprobs_backward.argtypes = [C.POINTER(tgrad_logits), vp, vp, vp, C.c_int64, vp]
+    lib.tgrad_loss_query_size.argtypes = [C.c_int64, C.c_int64, C.POINTER(sz)]
+    lib.tgrad_policy_loss.argtypes = [C.POINTER(tgrad_logits), C.POINTER(tgrad_policy), vp, vp, vp, vp, vp, vp, vp, vp, vp,
+                                      C.c_int64, vp]
+    lib.tgrad_preference_loss.argtypes = [C.POINTER(tgrad_logits), C.POINTER(tgrad_preference), C.c_int64, vp, vp, vp, vp, vp,
+                                          vp, vp, vp, vp, C.c_int64, vp]
     lib.tgrad_destroy.argtypes = [vp]
     lib.tgrad_strerror.argtypes = [i32]
     lib.tgrad_strerror.restype = C.c_char_p

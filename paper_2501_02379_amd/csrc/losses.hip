@@ -17,6 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr double kLog2e = 1.4426950408889634;
+constexpr float kLn2 = 0.693147180559945f;
 
 struct Logits {
   const void* x;
@@ -27,95 +28,261 @@ struct Logits {
   float scale2;                           // log2(e) / temperature
 };
 
+// 16 bytes of a row.  Rows start at any element, so these loads and stores are aligned to an element only; the hardware does
+// them as they are (a wavefront's 1024 bytes touch nine cache lines then instead of eight).
+typedef uint32_t Quad __attribute__((ext_vector_type(4)));
+typedef Quad QuadAny __attribute__((aligned(2)));
+
+template <int DT> struct Pack {
+  typedef typename Elem<DT>::raw raw;
+  static constexpr int N = 16 / sizeof(raw);
+  static constexpr uint32_t kLowest = DT == TGRAD_F32 ? 0xFF800000u : DT == TGRAD_BF16 ? 0xFF80FF80u : 0xFC00FC00u;   // -inf
+  static __device__ __forceinline__ Quad load(const raw* p) { return *reinterpret_cast<const QuadAny*>(p); }
+  static __device__ __forceinline__ void store(raw* p, Quad v) { *reinterpret_cast<QuadAny*>(p) = v; }
+  static __device__ __forceinline__ void widen(Quad v, float* f) {
+    if constexpr (DT == TGRAD_F32) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] = __uint_as_float(v[k]);
+    } else if constexpr (DT == TGRAD_BF16) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        f[2 * k] = __uint_as_float(v[k] << 16);
+        f[2 * k + 1] = __uint_as_float(v[k] & 0xFFFF0000u);
+      }
+    } else {
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const h2 h = __builtin_bit_cast(h2, (uint32_t)v[k]);
+        f[2 * k] = (float)h.x;
+        f[2 * k + 1] = (float)h.y;
+      }
+    }
+  }
+  static __device__ __forceinline__ Quad narrow(const float* f) {
+    Quad v;
+    if constexpr (DT == TGRAD_F32) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = __float_as_uint(f[k]);
+    } else if constexpr (DT == TGRAD_BF16) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = bf16_pack(f[2 * k], f[2 * k + 1]);
+    } else {
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        h2 h;
+        h.x = (_Float16)f[2 * k];
+        h.y = (_Float16)f[2 * k + 1];
+        v[k] = __builtin_bit_cast(uint32_t, h);
+      }
+    }
+    return v;
+  }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // one instruction; 0 below 2^-126
+
 // Running maximum and sum of 2^((x - max) scale2).  A maximum of -inf belongs to a sum of nothing, 0; a NaN entry is no maximum and
 // makes the sum NaN, and so does +inf.
 struct Soft {
   float m, s;
 };
 __device__ __forceinline__ float soft_base(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ Soft soft_join(Soft a, Soft b, float scale2) {
-  const float m = fmaxf(a.m, b.m), base = soft_base(m);
-  return Soft{m, a.s * exp2f((a.m - base) * scale2) + b.s * exp2f((b.m - base) * scale2)};
+template <int N>
+__device__ __forceinline__ void soft_add(Soft& a, const float* x, float scale2) {
+  float m = a.m;
+#pragma unroll
+  for (int k = 0; k < N; ++k) m = fmaxf(m, x[k]);
+  const float base = soft_base(m);
+  float s0 = a.s * exp2_fast((a.m - base) * scale2), s1 = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; k += 2) {
+    s0 += exp2_fast((x[k] - base) * scale2);
+    if (k + 1 < N) s1 += exp2_fast((x[k + 1] - base) * scale2);
+  }
+  a = Soft{m, s0 + s1};
 }
-__device__ __forceinline__ Soft soft_add(Soft a, float x, float scale2) {
-  const float m = fmaxf(a.m, x), base = soft_base(m);
-  return Soft{m, a.s * exp2f((a.m - base) * scale2) + exp2f((x - base) * scale2)};
+// Of all T threads, the same in every one.
+template <int T>
+__device__ __forceinline__ Soft soft_all(Soft a, float scale2, Soft* lds) {
+  float m = a.m;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  float s = a.s * exp2_fast((a.m - soft_base(m)) * scale2);
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d);
+  if constexpr (T == kWave) return Soft{m, s};
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = Soft{m, s};
+  __syncthreads();
+  Soft w[T / kWave];
+#pragma unroll
+  for (int i = 0; i < T / kWave; ++i) w[i] = lds[i];
+  m = w[0].m;
+#pragma unroll
+  for (int i = 1; i < T / kWave; ++i) m = fmaxf(m, w[i].m);
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < T / kWave; ++i) s += w[i].s * exp2_fast((w[i].m - soft_base(m)) * scale2);
+  return Soft{m, s};
 }
 
-// What a row needs: maximum and log of the sum, in units of z.
-struct RowSum {
-  float m;                                // maximum of x
-  float log_s;                            // log sum exp((x - m) scale)
+// A row as a workgroup of T threads sees it: `full` pieces of 16 bytes, thread t's are t, t + T, ...; the `rest` elements behind them
+// belong to the first threads, one each.
+template <int DT, int T>
+struct Row {
+  typedef Pack<DT> P;
+  typedef typename P::raw raw;
+  const raw* x;
+  int full, rest;
+  __device__ __forceinline__ Row(const raw* p, int vocab) : x(p), full(vocab / P::N), rest(vocab % P::N) {}
+  // U pieces of every thread, from `first` on; past the end: the last one again (masked in add())
+  template <int U>
+  __device__ __forceinline__ void load(Quad* q, int first) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * T + (int)threadIdx.x;
+      q[u] = P::load(x + (int64_t)(i < full ? i : full - 1) * P::N);
+    }
+    asm volatile("" ::: "memory");        // all of them on their way: the compiler would move each to the branch that uses it
+  }
+  template <int U>
+  __device__ __forceinline__ void add(Soft& a, const Quad* q, int first, float scale2) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = first + u * T;
+      if (at >= full) break;
+      Quad v = q[u];
+      if (at + T > full && at + (int)threadIdx.x >= full) v = Quad{P::kLowest, P::kLowest, P::kLowest, P::kLowest};
+      float f[P::N];
+      P::widen(v, f);
+      soft_add<P::N>(a, f, scale2);
+    }
+  }
+  // pieces first ... end - 1, read and forgotten
+  template <int U>
+  __device__ __forceinline__ void stream(Soft& a, int first, int end, float scale2) const {
+    for (; first < end; first += U * T) {
+      Quad q[U];
+      load<U>(q, first);
+      add<U>(a, q, first, scale2);
+    }
+  }
+  __device__ __forceinline__ void add_rest(Soft& a, float scale2) const {
+    if ((int)threadIdx.x < rest) {
+      const float f = Elem<DT>::widen(x[(int64_t)full * P::N + threadIdx.x]);
+      soft_add<1>(a, &f, scale2);
+    }
+  }
 };
 
-template <int DT>
-__device__ __forceinline__ RowSum row_sum(const typename Elem<DT>::raw* x, int vocab, float scale2, Soft* lds) {
-  Soft a{-INFINITY, 0.f};
-  for (int i = threadIdx.x; i < vocab; i += kThreads) a = soft_add(a, Elem<DT>::widen(x[i]), scale2);
+// Gradient of a row: -q exp2((x - m) scale2) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.
+template <int DT, int T>
+struct RowGradient {
+  typedef Pack<DT> P;
+  typedef typename P::raw raw;
+  raw* out;
+  float m, scale2, q;
+  __device__ __forceinline__ float at(float x) const { return -q * exp2_fast((x - m) * scale2); }
+  __device__ __forceinline__ void piece(Quad v, int i, int full) const {
+    float f[P::N];
+    P::widen(v, f);
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const Soft b{__shfl_xor(a.m, d), __shfl_xor(a.s, d)};
-    a = soft_join(a, b, scale2);
+    for (int k = 0; k < P::N; ++k) f[k] = at(f[k]);
+    if (i < full) P::store(out + (int64_t)i * P::N, P::narrow(f));
   }
-  __syncthreads();
-  if (lane_id() == 0) lds[threadIdx.x / kWave] = a;
-  __syncthreads();
-  a = lds[0];
+  template <int U>
+  __device__ __forceinline__ void pieces(const Row<DT, T>& r, const Quad* v, int first) const {
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) a = soft_join(a, lds[w], scale2);
-  return RowSum{a.m, logf(a.s)};
-}
-
-// dlogits of a row: d (1[v = y] - exp(x scale - lse)) with d = dlogp * scale, given lse = m scale + log_s.
-template <int DT>
-__device__ __forceinline__ void row_gradient(const typename Elem<DT>::raw* x, typename Elem<DT>::raw* out, int vocab, int64_t y,
-                                             float m, float log2_s, float scale2, float d) {
-  for (int i = threadIdx.x; i < vocab; i += kThreads) {
-    const float p = exp2f((Elem<DT>::widen(x[i]) - m) * scale2 - log2_s);
-    out[i] = Elem<DT>::narrow(i == y ? d - d * p : -d * p);
+    for (int u = 0; u < U; ++u) {
+      if (first + u * T >= r.full) break;
+      piece(v[u], first + u * T + (int)threadIdx.x, r.full);
+    }
   }
-}
+  template <int U>
+  __device__ __forceinline__ void stream(const Row<DT, T>& r, int first, int end) const {
+    for (; first < end; first += U * T) {
+      Quad v[U];
+      r.template load<U>(v, first);
+      pieces<U>(r, v, first);
+    }
+  }
+  __device__ __forceinline__ void rest(const Row<DT, T>& r) const {
+    if ((int)threadIdx.x < r.rest) {
+      const int64_t i = (int64_t)r.full * P::N + threadIdx.x;
+      out[i] = Elem<DT>::narrow(at(Elem<DT>::widen(r.x[i])));
+    }
+  }
+  // Behind everything else, by the thread that wrote this element before: its stores keep their order.
+  __device__ __forceinline__ void target(const Row<DT, T>& r, int64_t y, float xy, float d) const {
+    const int piece = (int)(y / P::N);
+    const int owner = piece < r.full ? piece % T : (int)(y - (int64_t)r.full * P::N);
+    if ((int)threadIdx.x == owner) out[y] = Elem<DT>::narrow(d + at(xy));
+  }
+};
 
-template <int DT>
+template <int DT, int T>
 __device__ __forceinline__ void row_zero(typename Elem<DT>::raw* out, int vocab) {
-  for (int i = threadIdx.x; i < vocab; i += kThreads) out[i] = Elem<DT>::narrow(0.f);
+  typedef Pack<DT> P;
+  const int full = vocab / P::N;
+  for (int i = threadIdx.x; i < full; i += T) P::store(out + (int64_t)i * P::N, Quad{0u, 0u, 0u, 0u});
+  if ((int)threadIdx.x < vocab % P::N) out[(int64_t)full * P::N + threadIdx.x] = Elem<DT>::narrow(0.f);
 }
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, float2* stat) {
+// z_y - lse
+__device__ __forceinline__ float row_logp(float xy, Soft a, float scale2) { return ((xy - a.m) * scale2 - log2f(a.s)) * kLn2; }
+
+template <int DT, int T>
+__global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, Soft* stat) {
   typedef typename Elem<DT>::raw raw;
-  __shared__ Soft lds[kWaves];
+  __shared__ Soft lds[T / kWave];
   const int64_t n = blockIdx.x;
   const int64_t y = L.targets[n];
-  const bool live = y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f);
-  RowSum r{0.f, 0.f};
+  Soft a{0.f, 1.f};
   float lp = 0.f, l = 0.f;
-  if (live) {
+  if (y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f)) {
     const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-    r = row_sum<DT>(x, L.vocab, L.scale2, lds);
-    lp = (Elem<DT>::widen(x[y]) - r.m) * L.scale - r.log_s;
-    l = r.m * L.scale + r.log_s;
+    const Row<DT, T> r(x, L.vocab);
+    const float xy = Elem<DT>::widen(x[y]);
+    a = Soft{-INFINITY, 0.f};
+    r.template stream<8>(a, 0, r.full, L.scale2);
+    r.add_rest(a, L.scale2);
+    a = soft_all<T>(a, L.scale2, lds);
+    lp = row_logp(xy, a, L.scale2);
+    l = a.m * L.scale + log2f(a.s) * kLn2;
   }
   if (threadIdx.x == 0) {
     if (logp) logp[n] = lp;
     if (lse) lse[n] = l;
-    if (stat) stat[n] = make_float2(r.m, r.log_s);
+    if (stat) stat[n] = a;
   }
 }
 
-// stat: maximum and log of the sum of every row; lse instead where stat is null (then its rounding is the gradient's error).
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_logprobs_back(Logits L, const float* lse, const float2* stat, const float* dlogp,
-                                                            void* dx, int64_t dstride) {
+// stat: maximum and sum of every row, or null and lse given.
+template <int DT, int T>
+__global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const Soft* stat, const float* dlogp, void* dx,
+                                                     int64_t dstride) {
   typedef typename Elem<DT>::raw raw;
   const int64_t n = blockIdx.x;
   const int64_t y = L.targets[n];
-  const float d = dlogp[n];
   raw* out = static_cast<raw*>(dx) + n * dstride;
-  if (!(y >= 0 && y < L.vocab) || d == 0.f) return row_zero<DT>(out, L.vocab);
+  const float d = dlogp[n] * L.scale;
+  if (!(y >= 0 && y < L.vocab) || d == 0.f) return row_zero<DT, T>(out, L.vocab);
   const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-  const float m = stat ? stat[n].x : 0.f, log_s = stat ? stat[n].y : lse[n];
-  row_gradient<DT>(x, out, L.vocab, y, m, log_s * (float)kLog2e, L.scale2, d * L.scale);
+  const Row<DT, T> r(x, L.vocab);
+  const float xy = Elem<DT>::widen(x[y]);
+  Soft a;
+  if (stat) {
+    a = stat[n];
+  } else {                                // exp(z - lse) = 2^((x - m) scale2) / s with m = lse / scale, but for its rounding, s for that
+    a.m = (float)((double)lse[n] * kLog2e / (double)L.scale2);
+    a.s = (float)exp2((double)lse[n] * kLog2e - (double)a.m * (double)L.scale2);
+  }
+  const RowGradient<DT, T> g{out, a.m, L.scale2, d / a.s};
+  if constexpr (T > kWave) __syncthreads();          // in place: the target's logit is read before anything is written
+  g.template stream<4>(r, 0, r.full);
+  g.rest(r);
+  g.target(r, y, xy, d);
 }
 
 struct PolicyArgs {
@@ -132,35 +299,49 @@ struct PolicyArgs {
   int64_t dstride;
 };
 
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_policy(Logits L, PolicyArgs a) {
+// One workgroup of T threads per row; the last T NV pieces of 16 bytes stay in registers from the sum to the gradient, what lies
+// before them in longer rows is read twice, the second time backwards.
+template <int DT, int T, int NV>
+__global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
   typedef typename Elem<DT>::raw raw;
-  __shared__ Soft lds[kWaves];
+  constexpr int kStream = 4;              // pieces in flight in the part that does not stay
+  __shared__ Soft lds[T / kWave];
   const int64_t n = blockIdx.x;
   const int64_t y = L.targets[n];
   const float w = a.weight[n];
-  const bool live = y >= 0 && y < L.vocab && w != 0.f;
   raw* out = a.dx ? static_cast<raw*>(a.dx) + n * a.dstride : nullptr;
-  if (!live) {
+  if (!(y >= 0 && y < L.vocab && w != 0.f)) {
     if (threadIdx.x == 0) {
       a.each[n] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (a.logp) a.logp[n] = 0.f;
     }
-    if (out) row_zero<DT>(out, L.vocab);
+    if (out) row_zero<DT, T>(out, L.vocab);
     return;
   }
   const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
+  const Row<DT, T> r(x, L.vocab);
   const float xy = Elem<DT>::widen(x[y]);
-  const RowSum r = row_sum<DT>(x, L.vocab, L.scale2, lds);
-  const float logp = (xy - r.m) * L.scale - r.log_s;
-  const float adv = a.advantage[n];
-  const float ratio = expf(logp - a.old_logp[n]);
+  const float adv = a.advantage[n], old = a.old_logp[n], ref = a.ref_logp ? a.ref_logp[n] : 0.f, scale = a.dloss ? *a.dloss : 1.f;
+  Soft sum{-INFINITY, 0.f};
+  Quad held[NV];
+  // a whole number of batches, so that a piece belongs to the same thread whether it stays or not
+  const int over = r.full - T * NV;
+  const int start = over > 0 ? (over + kStream * T - 1) / (kStream * T) * (kStream * T) : 0;
+  r.template stream<kStream>(sum, 0, start, L.scale2);
+  if (start < r.full) {
+    r.template load<NV>(held, start);
+    r.template add<NV>(sum, held, start, L.scale2);
+  }
+  r.add_rest(sum, L.scale2);
+  sum = soft_all<T>(sum, L.scale2, lds);
+  const float logp = row_logp(xy, sum, L.scale2);
+  const float ratio = expf(logp - old);
   const float whole = ratio * adv, cut = fminf(fmaxf(ratio, a.low), a.high) * adv;
   const bool clipped = cut < whole;
   const float pg = clipped ? -cut : -whole;
   float dlogp = clipped ? 0.f : -whole, kl = 0.f;
   if (a.ref_logp) {
-    const float d = a.ref_logp[n] - logp, e = expm1f(d);
+    const float d = ref - logp, e = expm1f(d);
     kl = e - d;
     if (a.kl_beta != 0.f) dlogp -= a.kl_beta * e;
   }
@@ -170,9 +351,13 @@ __global__ __launch_bounds__(kThreads) void k_policy(Logits L, PolicyArgs a) {
     if (a.logp) a.logp[n] = logp;
   }
   if (!out) return;
-  const float d = w * dlogp * (a.dloss ? *a.dloss : 1.f) * L.scale;
-  if (d == 0.f) return row_zero<DT>(out, L.vocab);
-  row_gradient<DT>(x, out, L.vocab, y, r.m, r.log_s * (float)kLog2e, L.scale2, d);
+  const float d = w * dlogp * scale * L.scale;
+  if (d == 0.f) return row_zero<DT, T>(out, L.vocab);
+  const RowGradient<DT, T> g{out, sum.m, L.scale2, d / sum.s};
+  if (start < r.full) g.template pieces<NV>(r, held, start);
+  for (int first = start - kStream * T; first >= 0; first -= kStream * T) g.template stream<kStream>(r, first, first + kStream * T);
+  g.rest(r);
+  g.target(r, y, xy, d);
 }
 
 __global__ __launch_bounds__(kThreads) void k_policy_sums(const float4* each, int64_t rows, float* stats) {
@@ -197,7 +382,7 @@ struct PairArgs {
   const float* weight;
   const float* ref_logp;
   const float* dloss;
-  const float2* stat;
+  const Soft* stat;
   float* dlogp;
   float* rewards;
   float* pair_loss;
@@ -227,9 +412,9 @@ __global__ __launch_bounds__(kThreads) void k_pairs(Logits L, PairArgs a) {
       const float w = a.weight[n];
       const int64_t y = L.targets[n];
       if (w == 0.f || y < 0 || y >= L.vocab) continue;
-      const float2 st = a.stat[n];
+      const Soft st = a.stat[n];
       const float xy = Elem<DT>::widen(static_cast<const raw*>(L.x)[n * L.stride + y]);
-      const double logp = ((double)xy - (double)st.x) * (double)L.scale - (double)st.y;
+      const double logp = (((double)xy - (double)st.m) * (double)L.scale2 - log2((double)st.s)) / kLog2e;
       s += (double)w * (logp - (double)a.ref_logp[n]);
     }
     reward[side] = a.beta * block_sum<kWaves>(s, lds);
@@ -301,6 +486,33 @@ void for_type(int dt, F&& f) {
   else f(std::integral_constant<int, TGRAD_F16>());
 }
 
+template <int DT>
+void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, Soft* stat) {
+  const dim3 grid((uint32_t)L.rows);
+  const int pieces = L.vocab / Pack<DT>::N;
+  if (pieces <= 256) k_logprobs<DT, 64><<<grid, dim3(64), 0, s>>>(L, weight, logp, lse, stat);
+  else if (L.rows > 2 * compute_units()) k_logprobs<DT, 256><<<grid, dim3(256), 0, s>>>(L, weight, logp, lse, stat);
+  else k_logprobs<DT, 1024><<<grid, dim3(1024), 0, s>>>(L, weight, logp, lse, stat);
+}
+
+template <int DT>
+void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, const Soft* stat, const float* dlogp, void* dx, int64_t dstride) {
+  const dim3 grid((uint32_t)L.rows);
+  const int pieces = L.vocab / Pack<DT>::N;
+  if (pieces <= 256) k_logprobs_back<DT, 64><<<grid, dim3(64), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
+  else k_logprobs_back<DT, 256><<<grid, dim3(256), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
+}
+
+template <int DT>
+void launch_policy(hipStream_t s, const Logits& L, const PolicyArgs& a) {
+  const dim3 grid((uint32_t)L.rows);
+  const int pieces = L.vocab / Pack<DT>::N;
+  if (pieces <= 64 * 4) k_policy<DT, 64, 4><<<grid, dim3(64), 0, s>>>(L, a);
+  else if (pieces <= 256 * 8) k_policy<DT, 256, 8><<<grid, dim3(256), 0, s>>>(L, a);
+  else if (pieces <= 512 * 16) k_policy<DT, 512, 16><<<grid, dim3(512), 0, s>>>(L, a);
+  else k_policy<DT, 1024, 16><<<grid, dim3(1024), 0, s>>>(L, a);
+}
+
 // Scratch of the losses.
 struct Scratch {
   size_t each, stat, dlogp, pair_loss, bytes;
@@ -309,7 +521,7 @@ Scratch scratch(int64_t rows, int64_t pairs) {
   Scratch s;
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes); return at; };
-  s.each = s.stat = take((size_t)rows * (pairs ? sizeof(float2) : sizeof(float4)));
+  s.each = s.stat = take((size_t)rows * (pairs ? sizeof(Soft) : sizeof(float4)));
   s.dlogp = take(pairs ? (size_t)rows * sizeof(float) : 0);
   s.pair_loss = take((size_t)pairs * sizeof(float));
   s.bytes = o ? o : kAlign;
@@ -328,8 +540,7 @@ int tgrad_token_logprobs(const tgrad_logits* logits, float* logp, float* lse, vo
   if (pending()) return TGRAD_ERR_HIP;
   if (L.rows == 0 || (!logp && !lse)) return TGRAD_OK;
   for_type(logits->dtype, [&](auto dt) {
-    k_logprobs<dt.value><<<dim3((uint32_t)L.rows), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(L, nullptr, logp, lse,
-                                                                                                            nullptr);
+    launch_logprobs<dt.value>(static_cast<hipStream_t>(hip_stream), L, nullptr, logp, lse, nullptr);
   });
   return launched();
 }
@@ -345,8 +556,7 @@ int tgrad_token_logprobs_backward(const tgrad_logits* logits, const float* lse, 
   if (pending()) return TGRAD_ERR_HIP;
   if (L.rows == 0) return TGRAD_OK;
   for_type(logits->dtype, [&](auto dt) {
-    k_logprobs_back<dt.value><<<dim3((uint32_t)L.rows), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream)>>>(
-        L, lse, nullptr, dlogp, dlogits, dlogits_stride);
+    launch_logprobs_back<dt.value>(static_cast<hipStream_t>(hip_stream), L, lse, nullptr, dlogp, dlogits, dlogits_stride);
   });
   return launched();
 }
@@ -379,7 +589,7 @@ int tgrad_policy_loss(const tgrad_logits* logits, const tgrad_policy* policy, co
   PolicyArgs a{1.f - policy->clip_low, 1.f + policy->clip_high, policy->kl_beta, weight, advantage, old_logp, ref_logp, dloss,
                reinterpret_cast<float4*>(static_cast<char*>(workspace_dev) + sc.each), logp, dlogits, dlogits_stride};
   if (L.rows > 0)
-    for_type(logits->dtype, [&](auto dt) { k_policy<dt.value><<<dim3((uint32_t)L.rows), dim3(kThreads), 0, s>>>(L, a); });
+    for_type(logits->dtype, [&](auto dt) { launch_policy<dt.value>(s, L, a); });
   k_policy_sums<<<dim3(1), dim3(kThreads), 0, s>>>(a.each, L.rows, stats);
   return launched();
 }
@@ -406,7 +616,7 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const Scratch sc = scratch(L.rows, pairs);
   char* ws = static_cast<char*>(workspace_dev);
-  float2* stat = reinterpret_cast<float2*>(ws + sc.stat);
+  Soft* stat = reinterpret_cast<Soft*>(ws + sc.stat);
   float* dlogp = reinterpret_cast<float*>(ws + sc.dlogp);
   float* pair_loss = reinterpret_cast<float*>(ws + sc.pair_loss);
   PairArgs a{seq_start, weight, ref_logp, dloss, stat, dlogp, rewards, pair_loss, preference->beta, preference->label_smoothing, pairs};
@@ -414,12 +624,12 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
     if (L.rows > 0) {
       // rows that lie in no sequence
       k_zero_floats<<<dim3((uint32_t)((L.rows + 255) / 256)), dim3(256), 0, s>>>(dlogp, L.rows);
-      k_logprobs<dt.value><<<dim3((uint32_t)L.rows), dim3(kThreads), 0, s>>>(L, weight, logp, nullptr, stat);
+      launch_logprobs<dt.value>(s, L, weight, logp, nullptr, stat);
     }
     k_pairs<dt.value><<<dim3((uint32_t)pairs), dim3(kThreads), 0, s>>>(L, a);
     k_pair_mean<<<dim3(1), dim3(kThreads), 0, s>>>(pair_loss, pairs, loss);
     if (dlogits && L.rows > 0)
-      k_logprobs_back<dt.value><<<dim3((uint32_t)L.rows), dim3(kThreads), 0, s>>>(L, nullptr, stat, dlogp, dlogits, dlogits_stride);
+      launch_logprobs_back<dt.value>(s, L, nullptr, stat, dlogp, dlogits, dlogits_stride);
   });
   return launched();
 }

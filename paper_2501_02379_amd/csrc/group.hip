@@ -53,17 +53,6 @@ __global__ void k_group_put(PutArgs a, int first, Entry* entries, Piece* pieces)
 
 __global__ void k_group_zero(uint32_t* ticket) { *ticket = 0; }
 
-__device__ __forceinline__ float load_real(const void* p, int real, int64_t i) {
-  if (real == TGRAD_F32) return static_cast<const float*>(p)[i];
-  if (real == TGRAD_BF16) return Elem<TGRAD_BF16>::widen(static_cast<const uint16_t*>(p)[i]);
-  return Elem<TGRAD_F16>::widen(static_cast<const _Float16*>(p)[i]);
-}
-__device__ __forceinline__ void store_real(void* p, int real, int64_t i, float v) {
-  if (real == TGRAD_F32) static_cast<float*>(p)[i] = v;
-  else if (real == TGRAD_BF16) static_cast<uint16_t*>(p)[i] = Elem<TGRAD_BF16>::narrow(v);
-  else static_cast<_Float16*>(p)[i] = Elem<TGRAD_F16>::narrow(v);
-}
-
 // Real numbers of a piece: [first, first + count) of the tensor's.
 struct Span {
   int64_t first;
@@ -75,9 +64,59 @@ __device__ __forceinline__ Span piece_span(const Entry& e, int index, bool cplx)
   return cplx ? Span{at * 2, n * 2} : Span{at, n};
 }
 
+template <typename F>
+__device__ __forceinline__ void for_real(int real, F&& f) {
+  if (real == TGRAD_F32) f(std::integral_constant<int, TGRAD_F32>());
+  else if (real == TGRAD_BF16) f(std::integral_constant<int, TGRAD_BF16>());
+  else f(std::integral_constant<int, TGRAD_F16>());
+}
+
+// U units of four numbers of a thread from unit `first` on; past the end the last one again.
+template <int DT, int U>
+__device__ __forceinline__ void load_units(typename Four<DT>::type* q, const void* base, int64_t at, int first, int units) {
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int i = first + u * kThreads + (int)threadIdx.x;
+    q[u] = *reinterpret_cast<const typename Four<DT>::any*>(static_cast<const typename Elem<DT>::raw*>(base) + at +
+                                                            (int64_t)(i < units ? i : units - 1) * 4);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_unit(void* base, int64_t at, int unit, const float* f) {
+  *reinterpret_cast<typename Four<DT>::any*>(static_cast<typename Elem<DT>::raw*>(base) + at + (int64_t)unit * 4) = Four<DT>::narrow(f);
+}
+// Everything above is on its way before anything below: the compiler would move each load to the branch that uses it.
+__device__ __forceinline__ void loads_issued() { asm volatile("" ::: "memory"); }
+
 // sum |g|^2.  Squares and sums in float64: the square of a float32 is exact there, and no finite gradient overflows.  Every
 // workgroup leaves one partial sum; the last one to come adds them up in the order of the workgroups, so that the result does
 // not depend on which one that is.
+template <int DT>
+__device__ __forceinline__ double piece_sumsq(const void* g, Span s) {
+  constexpr int U = 4;
+  const int units = s.count / 4, rest = s.count % 4;
+  double acc[4] = {0., 0., 0., 0.};
+  for (int first = 0; first < units; first += U * kThreads) {
+    typename Four<DT>::type q[U];
+    load_units<DT, U>(q, g, s.first, first, units);
+    loads_issued();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (first + u * kThreads + (int)threadIdx.x < units) {
+        float f[4];
+        Four<DT>::widen(q[u], f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[k] = fma((double)f[k], (double)f[k], acc[k]);
+      }
+    }
+  }
+  if ((int)threadIdx.x < rest) {
+    const double v = (double)Elem<DT>::widen(static_cast<const typename Elem<DT>::raw*>(g)[s.first + units * 4 + threadIdx.x]);
+    acc[0] = fma(v, v, acc[0]);
+  }
+  return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+}
+
 __global__ __launch_bounds__(kThreads) void k_group_sumsq(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           int64_t npieces, double* sums, uint32_t* ticket, float max_norm,
                                                           const double* add, tgrad_norm* out) {
@@ -86,13 +125,9 @@ __global__ __launch_bounds__(kThreads) void k_group_sumsq(const Entry* __restric
   double acc = 0.;
   for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
     const Piece pc = pieces[p];
-    const Entry e = entries[pc.entry];
-    const int real = real_type(e.grad_dtype);
+    const Entry& e = entries[pc.entry];
     const Span s = piece_span(e, pc.index, complex_type(e.grad_dtype));
-    for (int i = threadIdx.x; i < s.count; i += kThreads) {
-      const double g = (double)load_real(e.grad, real, s.first + i);
-      acc += g * g;
-    }
+    for_real(real_type(e.grad_dtype), [&](auto dt) { acc += piece_sumsq<dt.value>(e.grad, s); });
   }
   acc = block_sum<kWaves>(acc, lds);
   if (threadIdx.x == 0) {
@@ -116,17 +151,41 @@ __global__ __launch_bounds__(kThreads) void k_group_sumsq(const Entry* __restric
   }
 }
 
+template <int DT>
+__device__ __forceinline__ void piece_scale(const void* g, void* out, Span s, float coef) {
+  constexpr int U = 4;
+  const int units = s.count / 4, rest = s.count % 4;
+  for (int first = 0; first < units; first += U * kThreads) {
+    typename Four<DT>::type q[U];
+    load_units<DT, U>(q, g, s.first, first, units);
+    loads_issued();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * kThreads + (int)threadIdx.x;
+      float f[4];
+      Four<DT>::widen(q[u], f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f[k] *= coef;
+      if (i < units) store_unit<DT>(out, s.first, i, f);
+    }
+  }
+  if ((int)threadIdx.x < rest) {
+    typedef typename Elem<DT>::raw raw;
+    const int64_t i = s.first + units * 4 + threadIdx.x;
+    static_cast<raw*>(out)[i] = Elem<DT>::narrow(coef * Elem<DT>::widen(static_cast<const raw*>(g)[i]));
+  }
+}
+
+// Backwards: the gradients that k_group_sumsq has read last are still in the caches.
 __global__ __launch_bounds__(kThreads) void k_group_scale(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           int64_t npieces, const tgrad_norm* norm) {
   const float coef = norm->coef;
-  for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
+  for (int64_t p = npieces - 1 - blockIdx.x; p >= 0; p -= gridDim.x) {
     const Piece pc = pieces[p];
-    const Entry e = entries[pc.entry];
+    const Entry& e = entries[pc.entry];
     if (coef == 1.f && e.out == e.grad) continue;
-    const int real = real_type(e.grad_dtype);
     const Span s = piece_span(e, pc.index, complex_type(e.grad_dtype));
-    for (int i = threadIdx.x; i < s.count; i += kThreads)
-      store_real(e.out, real, s.first + i, coef * load_real(e.grad, real, s.first + i));
+    for_real(real_type(e.grad_dtype), [&](auto dt) { piece_scale<dt.value>(e.grad, e.out, s, coef); });
   }
 }
 
@@ -135,41 +194,112 @@ struct AdamK {
   float beta1, beta2, one_beta1, one_beta2, inv_c1, inv_c2, eps;
   bool skip_nonfinite;
 };
+struct AdamRates {                         // a tensor's
+  float decay, step;                       // 1 - lr wd; lr / (1 - beta1^tau)
+};
+
+// Four numbers: of four real elements, or of two complex ones, whose v are v[0] and v[1].
+template <bool CX>
+__device__ __forceinline__ void adamw_unit(const AdamK& h, AdamRates r, float coef, const float* g, float* p, float* m, float* v) {
+  float gs[4], d[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    gs[k] = coef * g[k];
+    m[k] = h.beta1 * m[k] + h.one_beta1 * gs[k];
+  }
+#pragma unroll
+  for (int k = 0; k < (CX ? 2 : 4); ++k) {
+    const float sq = CX ? gs[2 * k] * gs[2 * k] + gs[2 * k + 1] * gs[2 * k + 1] : gs[k] * gs[k];
+    v[k] = h.beta2 * v[k] + h.one_beta2 * sq;
+    d[k] = r.step / (sqrtf(v[k] * h.inv_c2) + h.eps);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p[k] = r.decay * p[k] - d[CX ? k / 2 : k] * m[k];
+}
+
+template <int GR, int PR, bool CX>
+__device__ __forceinline__ void piece_adamw(const Entry& e, int index, const AdamK& h, AdamRates r, float coef) {
+  constexpr int U = 4;
+  const Span s = piece_span(e, index, CX);
+  const int64_t vfirst = CX ? s.first / 2 : s.first;
+  const int units = s.count / 4, rest = s.count % 4;
+  float* M = static_cast<float*>(e.m);
+  float* V = static_cast<float*>(e.v);
+  for (int first = 0; first < units; first += U * kThreads) {
+    typename Four<GR>::type g[U];
+    typename Four<PR>::type p[U];
+    Quad m[U], v[U];
+    load_units<GR, U>(g, e.grad, s.first, first, units);
+    load_units<PR, U>(p, e.param, s.first, first, units);
+    load_units<TGRAD_F32, U>(m, M, s.first, first, units);
+    if constexpr (CX) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = first + u * kThreads + (int)threadIdx.x;
+        const Duo w = *reinterpret_cast<const DuoAny*>(V + vfirst + (int64_t)(i < units ? i : units - 1) * 2);
+        v[u] = Quad{w[0], w[1], 0u, 0u};
+      }
+    } else {
+      load_units<TGRAD_F32, U>(v, V, vfirst, first, units);
+    }
+    loads_issued();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * kThreads + (int)threadIdx.x;
+      if (i < units) {
+        float fg[4], fp[4], fm[4], fv[4];
+        Four<GR>::widen(g[u], fg);
+        Four<PR>::widen(p[u], fp);
+        Four<TGRAD_F32>::widen(m[u], fm);
+        Four<TGRAD_F32>::widen(v[u], fv);
+        adamw_unit<CX>(h, r, coef, fg, fp, fm, fv);
+        store_unit<PR>(e.param, s.first, i, fp);
+        store_unit<TGRAD_F32>(M, s.first, i, fm);
+        if constexpr (CX) *reinterpret_cast<DuoAny*>(V + vfirst + (int64_t)i * 2) = Duo{__float_as_uint(fv[0]), __float_as_uint(fv[1])};
+        else store_unit<TGRAD_F32>(V, vfirst, i, fv);
+      }
+    }
+  }
+  // up to three real elements, or one complex element, by one thread each
+  constexpr int W = CX ? 2 : 1;
+  if ((int)threadIdx.x < rest / W) {
+    const int64_t i = s.first + units * 4 + (int64_t)threadIdx.x * W, iv = vfirst + units * 4 / W + threadIdx.x;
+    const typename Elem<GR>::raw* G = static_cast<const typename Elem<GR>::raw*>(e.grad);
+    typename Elem<PR>::raw* P = static_cast<typename Elem<PR>::raw*>(e.param);
+    float fg[4] = {0.f, 0.f, 0.f, 0.f}, fp[4] = {0.f, 0.f, 0.f, 0.f}, fm[4] = {0.f, 0.f, 0.f, 0.f}, fv[4] = {1.f, 1.f, 1.f, 1.f};
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      fg[k] = Elem<GR>::widen(G[i + k]);
+      fp[k] = Elem<PR>::widen(P[i + k]);
+      fm[k] = M[i + k];
+    }
+    fv[0] = V[iv];
+    adamw_unit<CX>(h, r, coef, fg, fp, fm, fv);
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      P[i + k] = Elem<PR>::narrow(fp[k]);
+      M[i + k] = fm[k];
+    }
+    V[iv] = fv[0];
+  }
+}
 
 __global__ __launch_bounds__(kThreads) void k_group_adamw(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           int64_t npieces, AdamK h, const tgrad_norm* norm) {
   const float coef = norm ? norm->coef : 1.f;
   if (h.skip_nonfinite && !(fabsf(norm->norm) < INFINITY)) return;
-  for (int64_t p = blockIdx.x; p < npieces; p += gridDim.x) {
-    const Piece pc = pieces[p];
-    const Entry e = entries[pc.entry];
-    const bool cplx = complex_type(e.grad_dtype);
-    const int gr = real_type(e.grad_dtype), pr = real_type(e.param_dtype);
+  for (int64_t q = npieces - 1 - blockIdx.x; q >= 0; q -= gridDim.x) {
+    const Piece pc = pieces[q];
+    const Entry& e = entries[pc.entry];
     const double lr = h.lr * (double)e.lr_scale;
-    const float decay = (float)(1. - lr * (double)e.weight_decay), step = (float)(lr * (double)h.inv_c1);
-    const Span s = piece_span(e, pc.index, false);
-    float* M = static_cast<float*>(e.m);
-    float* V = static_cast<float*>(e.v);
-    for (int k = threadIdx.x; k < s.count; k += kThreads) {
-      const int64_t i = s.first + k;
-      if (!cplx) {
-        const float g = coef * load_real(e.grad, gr, i);
-        const float m = h.beta1 * M[i] + h.one_beta1 * g, v = h.beta2 * V[i] + h.one_beta2 * (g * g);
-        M[i] = m;
-        V[i] = v;
-        store_real(e.param, pr, i, decay * load_real(e.param, pr, i) - step * m / (sqrtf(v * h.inv_c2) + h.eps));
-      } else {
-        const float gx = coef * load_real(e.grad, gr, 2 * i), gy = coef * load_real(e.grad, gr, 2 * i + 1);
-        const float mx = h.beta1 * M[2 * i] + h.one_beta1 * gx, my = h.beta1 * M[2 * i + 1] + h.one_beta1 * gy;
-        const float v = h.beta2 * V[i] + h.one_beta2 * (gx * gx + gy * gy);
-        M[2 * i] = mx;
-        M[2 * i + 1] = my;
-        V[i] = v;
-        const float d = step / (sqrtf(v * h.inv_c2) + h.eps);
-        store_real(e.param, pr, 2 * i, decay * load_real(e.param, pr, 2 * i) - d * mx);
-        store_real(e.param, pr, 2 * i + 1, decay * load_real(e.param, pr, 2 * i + 1) - d * my);
-      }
-    }
+    const AdamRates r{(float)(1. - lr * (double)e.weight_decay), (float)(lr * (double)h.inv_c1)};
+    const bool cplx = complex_type(e.grad_dtype);
+    for_real(real_type(e.grad_dtype), [&](auto g) {
+      for_real(real_type(e.param_dtype), [&](auto p) {
+        if (!cplx) piece_adamw<g.value, p.value, false>(e, pc.index, h, r, coef);
+        else if constexpr (g.value != TGRAD_F16 && p.value != TGRAD_F16) piece_adamw<g.value, p.value, true>(e, pc.index, h, r, coef);
+      });
+    });
   }
 }
 
@@ -337,7 +467,7 @@ int tgrad_group_grad_norm(tgrad_group* group, float max_norm, const double* add_
   if (!group || !norm_dev || !(max_norm >= 0.f) || (uintptr_t)norm_dev % 8 || (uintptr_t)add_sumsq_dev % 8)
     return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
-  const int grid = grid_for(group, 4);
+  const int grid = grid_for(group, 8);
   k_group_sumsq<<<dim3(grid < kMaxSums ? grid : kMaxSums), dim3(kThreads), 0, group->stream>>>(
       group->entries(), group->pieces(), group->lay.npieces, reinterpret_cast<double*>(group->ws + group->lay.sums),
       reinterpret_cast<uint32_t*>(group->ws + group->lay.ticket), max_norm, add_sumsq_dev, norm_dev);

@@ -33,8 +33,13 @@ template <int DT> struct Pack {
   typedef typename Elem<DT>::raw raw;
   static constexpr int N = 16 / sizeof(raw);
   static constexpr uint32_t kLowest = DT == TGRAD_F32 ? 0xFF800000u : DT == TGRAD_BF16 ? 0xFF80FF80u : 0xFC00FC00u;   // -inf
-  static __device__ __forceinline__ Quad load(const raw* p) { return *reinterpret_cast<const QuadAny*>(p); }
-  static __device__ __forceinline__ void store(raw* p, Quad v) { *reinterpret_cast<QuadAny*>(p) = v; }
+  // LAST: not read again soon
+  template <bool LAST>
+  static __device__ __forceinline__ Quad load(const raw* p) {
+    const QuadAny* q = reinterpret_cast<const QuadAny*>(p);
+    return LAST ? __builtin_nontemporal_load(q) : *q;
+  }
+  static __device__ __forceinline__ void store(raw* p, Quad v) { __builtin_nontemporal_store(v, reinterpret_cast<QuadAny*>(p)); }
   static __device__ __forceinline__ void widen(Quad v, float* f) {
     if constexpr (DT == TGRAD_F32) {
       Four<DT>::widen(v, f);
@@ -99,35 +104,70 @@ __device__ __forceinline__ Soft soft_all(Soft a, float scale2, Soft* lds) {
   return Soft{m, s};
 }
 
-// A row as a workgroup of T threads sees it: `full` pieces of 16 bytes from its first element on, of which thread t's are t, t + T, ...,
-// and `odd` elements behind them, which belong to the first threads, one each.  Where the row lies in memory has no part in it, so
-// results are the same bits at any address.  (Pieces from a 16-byte boundary on are faster where rows of two-byte elements start at
-// odd ones: 1464 such rows of 100003 scored in 187 us instead of 222; at multiples of 4 bytes there is no difference.)
-template <int DT, int T>
+// A piece in flight.  ODD: rows of two-byte elements that start in the upper half of a four-byte word are read from that word on, five
+// words for a piece, and shifted into place where they are used: loads of 16 bytes that are not aligned to 4 take twice as long (4096
+// rows of 100003 bf16 numbers, every other row such a one, scored in 176 us, now 134; stores do not mind).  The first and the last word
+// of such a row may lie across its ends by one element, which is not used.
+template <bool ODD> struct Flight {
+  Quad v;
+  uint32_t more;
+  __device__ __forceinline__ Quad settle() const {
+    return Quad{__builtin_amdgcn_alignbit(v[1], v[0], 16), __builtin_amdgcn_alignbit(v[2], v[1], 16), __builtin_amdgcn_alignbit(v[3], v[2], 16),
+                __builtin_amdgcn_alignbit(more, v[3], 16)};
+  }
+};
+template <> struct Flight<false> {
+  Quad v;
+  __device__ __forceinline__ Quad settle() const { return v; }
+};
+
+// A row as a workgroup of T threads sees it: `head` elements, `full` pieces of 16 bytes, of which thread t's are t, t + T, ..., and a last
+// few elements; those outside the pieces (`odd` of them) belong to the first threads, one each.
+// Sums take head = 0: where the row lies in memory has then no part in their order, and they are the same bits at any address.
+template <int DT, int T, bool ODD = false>
 struct Row {
   typedef Pack<DT> P;
   typedef typename P::raw raw;
-  const raw* x;
-  int full, odd;
-  __device__ __forceinline__ Row(const raw* p, int vocab) : x(p), full(vocab / P::N), odd(vocab % P::N) {}
-  __device__ __forceinline__ int64_t odd_at() const { return (int64_t)full * P::N + threadIdx.x; }
+  typedef Flight<ODD> F;
+  const raw* x;                           // the first piece
+  int head, full, odd;
+  __device__ __forceinline__ Row(const raw* p, int vocab, int up = 0) {
+    head = up < vocab ? up : vocab;
+    full = (vocab - head) / P::N;
+    odd = vocab - full * P::N;
+    x = p + head;
+  }
+  // elements from p to the next 16-byte boundary
+  static __device__ __forceinline__ int to_boundary(const raw* p) { return (int)((0u - (uint32_t)(uintptr_t)p) & 15u) / (int)sizeof(raw); }
+  // this thread's odd element, counted from the first piece
+  __device__ __forceinline__ int64_t odd_at() const {
+    const int t = (int)threadIdx.x;
+    return t < head ? t - head : (int64_t)full * P::N + (t - head);
+  }
   // U pieces of every thread, from `first` on; past the end: the last one again (masked in add())
-  template <int U>
-  __device__ __forceinline__ void load(Quad* q, int first) const {
+  template <int U, bool LAST>
+  __device__ __forceinline__ void load(F* q, int first) const {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = first + u * T + (int)threadIdx.x;
-      q[u] = P::load(x + (int64_t)(i < full ? i : full - 1) * P::N);
+      const raw* p = x + (int64_t)(i < full ? i : full - 1) * P::N;
+      if constexpr (ODD) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p - 1);
+        q[u].v = P::template load<LAST>(p - 1);
+        q[u].more = w[4];
+      } else {
+        q[u].v = P::template load<LAST>(p);
+      }
     }
     asm volatile("" ::: "memory");        // all of them on their way: the compiler would move each to the branch that uses it
   }
   template <int U>
-  __device__ __forceinline__ void add(Soft& a, const Quad* q, int first, float scale2) const {
+  __device__ __forceinline__ void add(Soft& a, F* q, int first, float scale2) const {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int at = first + u * T;
       if (at >= full) break;
-      Quad v = q[u];
+      Quad v = q[u].v = q[u].settle();
       if (at + T > full && at + (int)threadIdx.x >= full) v = Quad{P::kLowest, P::kLowest, P::kLowest, P::kLowest};
       float f[P::N];
       P::widen(v, f);
@@ -135,11 +175,11 @@ struct Row {
     }
   }
   // pieces first ... end - 1, read and forgotten
-  template <int U>
+  template <int U, bool LAST>
   __device__ __forceinline__ void stream(Soft& a, int first, int end, float scale2) const {
     for (; first < end; first += U * T) {
-      Quad q[U];
-      load<U>(q, first);
+      F q[U];
+      load<U, LAST>(q, first);
       add<U>(a, q, first, scale2);
     }
   }
@@ -152,11 +192,12 @@ struct Row {
 };
 
 // Gradient of a row: -q exp2((x - m) scale2) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.
-template <int DT, int T>
+template <int DT, int T, bool ODD = false>
 struct RowGradient {
   typedef Pack<DT> P;
   typedef typename P::raw raw;
-  raw* out;
+  typedef Row<DT, T, ODD> R;
+  raw* out;                               // where the first piece's gradient goes
   float m, scale2, q;
   __device__ __forceinline__ float at(float x) const { return -q * exp2_fast((x - m) * scale2); }
   __device__ __forceinline__ void piece(Quad v, int i, int full) const {
@@ -166,49 +207,63 @@ struct RowGradient {
     for (int k = 0; k < P::N; ++k) f[k] = at(f[k]);
     if (i < full) P::store(out + (int64_t)i * P::N, P::narrow(f));
   }
+  // pieces that add() has settled
   template <int U>
-  __device__ __forceinline__ void pieces(const Row<DT, T>& r, const Quad* v, int first) const {
+  __device__ __forceinline__ void pieces(const R& r, const typename R::F* v, int first) const {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (first + u * T >= r.full) break;
-      piece(v[u], first + u * T + (int)threadIdx.x, r.full);
+      piece(v[u].v, first + u * T + (int)threadIdx.x, r.full);
     }
   }
   template <int U>
-  __device__ __forceinline__ void stream(const Row<DT, T>& r, int first, int end) const {
+  __device__ __forceinline__ void stream(const R& r, int first, int end) const {
     for (; first < end; first += U * T) {
-      Quad v[U];
-      r.template load<U>(v, first);
+      typename R::F v[U];
+      r.template load<U, true>(v, first);
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u].v = v[u].settle();
       pieces<U>(r, v, first);
     }
   }
-  __device__ __forceinline__ void odd(const Row<DT, T>& r) const {
+  __device__ __forceinline__ void odd(const R& r) const {
     if ((int)threadIdx.x < r.odd) {
       const int64_t i = r.odd_at();
       out[i] = Elem<DT>::narrow(at(Elem<DT>::widen(r.x[i])));
     }
   }
   // Behind everything else, by the thread that wrote this element before: its stores keep their order.
-  __device__ __forceinline__ void target(const Row<DT, T>& r, int64_t y, float xy, float d) const {
-    const int piece = (int)(y / P::N);
-    const int owner = piece < r.full ? piece % T : (int)(y % P::N);
-    if ((int)threadIdx.x == owner) out[y] = Elem<DT>::narrow(d + at(xy));
+  __device__ __forceinline__ void target(const R& r, int64_t y, float xy, float d) const {
+    const int64_t i = y - r.head, behind = i - (int64_t)r.full * P::N;
+    const int owner = i < 0 ? (int)y : behind < 0 ? (int)(i / P::N) % T : r.head + (int)behind;
+    if ((int)threadIdx.x == owner) out[i] = Elem<DT>::narrow(d + at(xy));
   }
 };
 
 template <int DT, int T>
 __device__ __forceinline__ void row_zero(typename Elem<DT>::raw* out, int vocab) {
-  typedef Pack<DT> P;
-  const Row<DT, T> r(out, vocab);
-  for (int i = threadIdx.x; i < r.full; i += T) P::store(out + (int64_t)i * P::N, Quad{0u, 0u, 0u, 0u});
-  if ((int)threadIdx.x < r.odd) out[r.odd_at()] = Elem<DT>::narrow(0.f);
+  const Row<DT, T> r(out, vocab, Row<DT, T>::to_boundary(out));
+  typename Elem<DT>::raw* body = out + r.head;
+  for (int i = threadIdx.x; i < r.full; i += T) Pack<DT>::store(body + (int64_t)i * Pack<DT>::N, Quad{0u, 0u, 0u, 0u});
+  if ((int)threadIdx.x < r.odd) body[r.odd_at()] = Elem<DT>::narrow(0.f);
+}
+
+// f(true) for a row of two-byte elements that starts in the upper half of a four-byte word, f(false) for any other.
+template <int DT, typename F>
+__device__ __forceinline__ void with_parity(const typename Elem<DT>::raw* x, F&& f) {
+  if constexpr (DT != TGRAD_F32) {
+    if ((uintptr_t)x & 2) return f(std::true_type());
+  }
+  f(std::false_type());
 }
 
 // z_y - lse
 __device__ __forceinline__ float row_logp(float xy, Soft a, float scale2) { return ((xy - a.m) * scale2 - log2f(a.s)) * kLn2; }
 
-// stat and dlogp (zero for the rows that lie in no sequence) are for the kernels behind this one in a preference loss; null elsewhere.
-template <int DT, int T>
+// AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
+// rows that lie in no sequence) are.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
+// numbers, a quarter of them ignored: 151 us without it, 136 with it, 5.9 TB/s).
+template <int DT, int T, bool AGAIN>
 __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, Soft* stat, float* dlogp) {
   typedef typename Elem<DT>::raw raw;
   __shared__ Soft lds[T / kWave];
@@ -218,11 +273,13 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, f
   float lp = 0.f, l = 0.f;
   if (y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f)) {
     const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-    const Row<DT, T> r(x, L.vocab);
     const float xy = Elem<DT>::widen(x[y]);
     a = Soft{-INFINITY, 0.f};
-    r.template stream<8>(a, 0, r.full, L.scale2);
-    r.add_odd(a, L.scale2);
+    with_parity<DT>(x, [&](auto odd) {
+      const Row<DT, T, odd.value> r(x, L.vocab);
+      r.template stream<8, !AGAIN>(a, 0, r.full, L.scale2);
+      r.add_odd(a, L.scale2);
+    });
     a = soft_all<T>(a, L.scale2, lds);
     lp = row_logp(xy, a, L.scale2);
     l = a.m * L.scale + log2f(a.s) * kLn2;
@@ -230,25 +287,26 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, f
   if (threadIdx.x == 0) {
     if (logp) logp[n] = lp;
     if (lse) lse[n] = l;
-    if (stat) {
+    if constexpr (AGAIN) {
       stat[n] = a;
       dlogp[n] = 0.f;
     }
   }
 }
 
-// stat: maximum and sum of every row, or null and lse given.
+// stat: maximum and sum of every row, or null and lse given.  Rows backwards: what was read last lies in the caches.  Pieces start at
+// 16-byte boundaries of the gradient.
 template <int DT, int T>
 __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const Soft* stat, const float* dlogp, void* dx,
                                                      int64_t dstride) {
   typedef typename Elem<DT>::raw raw;
-  const int64_t n = blockIdx.x;
+  const int64_t n = (int64_t)gridDim.x - 1 - blockIdx.x;
   const int64_t y = L.targets[n];
   raw* out = static_cast<raw*>(dx) + n * dstride;
   const float d = dlogp[n] * L.scale;
   if (!(y >= 0 && y < L.vocab) || d == 0.f) return row_zero<DT, T>(out, L.vocab);
   const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-  const Row<DT, T> r(x, L.vocab);
+  const Row<DT, T> r(x, L.vocab, Row<DT, T>::to_boundary(out));
   const float xy = Elem<DT>::widen(x[y]);
   Soft a;
   if (stat) {
@@ -257,7 +315,7 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
     a.m = (float)((double)lse[n] * kLog2e / (double)L.scale2);
     a.s = (float)exp2((double)lse[n] * kLog2e - (double)a.m * (double)L.scale2);
   }
-  const RowGradient<DT, T> g{out, a.m, L.scale2, d / a.s};
+  const RowGradient<DT, T> g{out + r.head, a.m, L.scale2, d / a.s};
   if constexpr (T > kWave) __syncthreads();          // in place: the target's logit is read before anything is written
   g.template stream<4>(r, 0, r.full);
   g.odd(r);
@@ -278,37 +336,22 @@ struct PolicyArgs {
   int64_t dstride;
 };
 
-// One workgroup of T threads per row; the last T NV pieces of 16 bytes stay in registers from the sum to the gradient, what lies
-// before them in longer rows is read twice, the second time backwards.
-template <int DT, int T, int NV>
-__global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
-  typedef typename Elem<DT>::raw raw;
+template <int DT, int T, int NV, bool ODD>
+__device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a, int64_t n, int64_t y, float w, const typename Elem<DT>::raw* x,
+                                           typename Elem<DT>::raw* out, Soft* lds) {
   constexpr int kStream = 4;              // pieces in flight in the part that does not stay
-  __shared__ Soft lds[T / kWave];
-  const int64_t n = blockIdx.x;
-  const int64_t y = L.targets[n];
-  const float w = a.weight[n];
-  raw* out = a.dx ? static_cast<raw*>(a.dx) + n * a.dstride : nullptr;
-  if (!(y >= 0 && y < L.vocab && w != 0.f)) {
-    if (threadIdx.x == 0) {
-      a.each[n] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (a.logp) a.logp[n] = 0.f;
-    }
-    if (out) row_zero<DT, T>(out, L.vocab);
-    return;
-  }
-  const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-  const Row<DT, T> r(x, L.vocab);
+  typedef Row<DT, T, ODD> R;
+  const R r(x, L.vocab);
   const float xy = Elem<DT>::widen(x[y]);
   const float adv = a.advantage[n], old = a.old_logp[n], ref = a.ref_logp ? a.ref_logp[n] : 0.f, scale = a.dloss ? *a.dloss : 1.f;
   Soft sum{-INFINITY, 0.f};
-  Quad held[NV];
+  typename R::F held[NV];
   // a whole number of batches, so that a piece belongs to the same thread whether it stays or not
   const int over = r.full - T * NV;
   const int start = over > 0 ? (over + kStream * T - 1) / (kStream * T) * (kStream * T) : 0;
-  r.template stream<kStream>(sum, 0, start, L.scale2);
+  r.template stream<kStream, false>(sum, 0, start, L.scale2);
   if (start < r.full) {
-    r.template load<NV>(held, start);
+    r.template load<NV, true>(held, start);
     r.template add<NV>(sum, held, start, L.scale2);
   }
   r.add_odd(sum, L.scale2);
@@ -332,11 +375,33 @@ __global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
   if (!out) return;
   const float d = w * dlogp * scale * L.scale;
   if (d == 0.f) return row_zero<DT, T>(out, L.vocab);
-  const RowGradient<DT, T> g{out, sum.m, L.scale2, d / sum.s};
+  const RowGradient<DT, T, ODD> g{out, sum.m, L.scale2, d / sum.s};
   if (start < r.full) g.template pieces<NV>(r, held, start);
   for (int first = start - kStream * T; first >= 0; first -= kStream * T) g.template stream<kStream>(r, first, first + kStream * T);
   g.odd(r);
   g.target(r, y, xy, d);
+}
+
+// One workgroup of T threads per row; the last T NV pieces of 16 bytes stay in registers from the sum to the gradient, what lies
+// before them in longer rows is read twice, the second time backwards.
+template <int DT, int T, int NV>
+__global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
+  typedef typename Elem<DT>::raw raw;
+  __shared__ Soft lds[T / kWave];
+  const int64_t n = blockIdx.x;
+  const int64_t y = L.targets[n];
+  const float w = a.weight[n];
+  raw* out = a.dx ? static_cast<raw*>(a.dx) + n * a.dstride : nullptr;
+  if (!(y >= 0 && y < L.vocab && w != 0.f)) {
+    if (threadIdx.x == 0) {
+      a.each[n] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (a.logp) a.logp[n] = 0.f;
+    }
+    if (out) row_zero<DT, T>(out, L.vocab);
+    return;
+  }
+  const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
+  with_parity<DT>(x, [&](auto odd) { policy_row<DT, T, NV, odd.value>(L, a, n, y, w, x, out, lds); });
 }
 
 __global__ __launch_bounds__(1024) void k_policy_sums(const float4* each, int64_t rows, float* stats) {
@@ -460,13 +525,13 @@ void for_type(int dt, F&& f) {
   else f(std::integral_constant<int, TGRAD_F16>());
 }
 
-template <int DT>
+template <int DT, bool AGAIN>
 void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, Soft* stat, float* dlogp) {
   const dim3 grid((uint32_t)L.rows);
   const int pieces = L.vocab / Pack<DT>::N;
-  if (pieces <= 256) k_logprobs<DT, 64><<<grid, dim3(64), 0, s>>>(L, weight, logp, lse, stat, dlogp);
-  else if (L.rows > 2 * compute_units()) k_logprobs<DT, 256><<<grid, dim3(256), 0, s>>>(L, weight, logp, lse, stat, dlogp);
-  else k_logprobs<DT, 1024><<<grid, dim3(1024), 0, s>>>(L, weight, logp, lse, stat, dlogp);
+  if (pieces <= 256) k_logprobs<DT, 64, AGAIN><<<grid, dim3(64), 0, s>>>(L, weight, logp, lse, stat, dlogp);
+  else if (L.rows > 2 * compute_units()) k_logprobs<DT, 256, AGAIN><<<grid, dim3(256), 0, s>>>(L, weight, logp, lse, stat, dlogp);
+  else k_logprobs<DT, 1024, AGAIN><<<grid, dim3(1024), 0, s>>>(L, weight, logp, lse, stat, dlogp);
 }
 
 template <int DT>
@@ -474,7 +539,7 @@ void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, cons
   const dim3 grid((uint32_t)L.rows);
   const int pieces = L.vocab / Pack<DT>::N;
   if (pieces <= 256) k_logprobs_back<DT, 64><<<grid, dim3(64), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
-  else k_logprobs_back<DT, 256><<<grid, dim3(256), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
+  else k_logprobs_back<DT, 512><<<grid, dim3(512), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
 }
 
 template <int DT>
@@ -514,7 +579,7 @@ int tgrad_token_logprobs(const tgrad_logits* logits, float* logp, float* lse, vo
   if (pending()) return TGRAD_ERR_HIP;
   if (L.rows == 0 || (!logp && !lse)) return TGRAD_OK;
   for_type(logits->dtype, [&](auto dt) {
-    launch_logprobs<dt.value>(static_cast<hipStream_t>(hip_stream), L, nullptr, logp, lse, nullptr, nullptr);
+    launch_logprobs<dt.value, false>(static_cast<hipStream_t>(hip_stream), L, nullptr, logp, lse, nullptr, nullptr);
   });
   return launched();
 }
@@ -596,7 +661,7 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
   PairArgs a{seq_start, weight, ref_logp, dloss, stat, dlogp, rewards, pair_loss, preference->beta, preference->label_smoothing, pairs};
   for_type(logits->dtype, [&](auto dt) {
     if (L.rows > 0)
-      launch_logprobs<dt.value>(s, L, weight, logp, nullptr, stat, dlogp);
+      launch_logprobs<dt.value, true>(s, L, weight, logp, nullptr, stat, dlogp);
     k_pairs<dt.value><<<dim3((uint32_t)pairs), dim3(kThreads), 0, s>>>(L, a);
     k_pair_mean<<<dim3(1), dim3(kThreads), 0, s>>>(pair_loss, pairs, loss);
     if (dlogits && L.rows > 0)

@@ -5,6 +5,7 @@
 // d loss / d logp times (1[v = y] - exp(z_v - lse)) / temperature.  Exponentials are those of 2, of (x - max) log2(e) / temperature.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "launch_util.h"
@@ -260,21 +261,28 @@ __device__ __forceinline__ void with_parity(const typename Elem<DT>::raw* x, F&&
 // z_y - lse
 __device__ __forceinline__ float row_logp(float xy, Soft a, float scale2) { return ((xy - a.m) * scale2 - log2f(a.s)) * kLn2; }
 
+// What a preference loss keeps of a row.
+struct RowStat {
+  float m, s;                             // maximum, sum
+  float xy;                               // the target's logit
+  float live;                             // 0: ignored
+};
+
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
 // rows that lie in no sequence) are.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
 // numbers, a quarter of them ignored: 151 us without it, 136 with it, 5.9 TB/s).
 template <int DT, int T, bool AGAIN>
-__global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, Soft* stat, float* dlogp) {
+__global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
   typedef typename Elem<DT>::raw raw;
   __shared__ Soft lds[T / kWave];
   const int64_t n = blockIdx.x;
   const int64_t y = L.targets[n];
-  Soft a{0.f, 1.f};
-  float lp = 0.f, l = 0.f;
-  if (y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f)) {
+  const bool live = y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f);
+  Soft a{-INFINITY, 0.f};
+  float xy = 0.f, lp = 0.f, l = 0.f;
+  if (live) {
     const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
-    const float xy = Elem<DT>::widen(x[y]);
-    a = Soft{-INFINITY, 0.f};
+    xy = Elem<DT>::widen(x[y]);
     with_parity<DT>(x, [&](auto odd) {
       const Row<DT, T, odd.value> r(x, L.vocab);
       r.template stream<8, !AGAIN>(a, 0, r.full, L.scale2);
@@ -288,38 +296,73 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, f
     if (logp) logp[n] = lp;
     if (lse) lse[n] = l;
     if constexpr (AGAIN) {
-      stat[n] = a;
+      stat[n] = RowStat{a.m, a.s, xy, live ? 1.f : 0.f};
       dlogp[n] = 0.f;
     }
   }
 }
 
-// stat: maximum and sum of every row, or null and lse given.  Rows backwards: what was read last lies in the caches.  Pieces start at
-// 16-byte boundaries of the gradient.
-template <int DT, int T>
-__global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const Soft* stat, const float* dlogp, void* dx,
-                                                     int64_t dstride) {
+struct PairMean {
+  const float* pair_loss;
+  int64_t pairs;
+  float* loss;
+};
+template <int T>
+__device__ __forceinline__ void pair_mean(const PairMean& a) {
+  __shared__ double lds[T / kWave];
+  double s = 0.;
+  for (int64_t p = threadIdx.x; p < a.pairs; p += T) s += (double)a.pair_loss[p];
+  s = block_sum<T / kWave>(s, lds);
+  if (threadIdx.x == 0) *a.loss = (float)(s / (double)a.pairs);
+}
+
+// stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread (a workgroup per
+// row, in a loop: 1464 rows of 100003 float16 numbers 365 us, now 300).  Pieces start at 16-byte boundaries of the gradient.  The first
+// workgroup forms the mean over `pairs` pairs besides.
+template <int DT, int T, int U>
+__global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
+                                                     int64_t dstride, int parts, PairMean mean) {
   typedef typename Elem<DT>::raw raw;
-  const int64_t n = (int64_t)gridDim.x - 1 - blockIdx.x;
+  if (blockIdx.x == 0 && mean.pairs > 0) pair_mean<T>(mean);
+  const uint32_t row = blockIdx.x / (uint32_t)parts;
+  const int part = (int)(blockIdx.x - row * (uint32_t)parts);
+  const int64_t n = row;
   const int64_t y = L.targets[n];
   raw* out = static_cast<raw*>(dx) + n * dstride;
   const float d = dlogp[n] * L.scale;
-  if (!(y >= 0 && y < L.vocab) || d == 0.f) return row_zero<DT, T>(out, L.vocab);
   const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
   const Row<DT, T> r(x, L.vocab, Row<DT, T>::to_boundary(out));
-  const float xy = Elem<DT>::widen(x[y]);
+  const int first = part * U * T;
+  if (!(y >= 0 && y < L.vocab) || d == 0.f) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = first + u * T + (int)threadIdx.x;
+      if (i < r.full) Pack<DT>::store(out + r.head + (int64_t)i * Pack<DT>::N, Quad{0u, 0u, 0u, 0u});
+    }
+    if (part == 0 && (int)threadIdx.x < r.odd) out[r.head + r.odd_at()] = Elem<DT>::narrow(0.f);
+    return;
+  }
   Soft a;
   if (stat) {
-    a = stat[n];
+    a = Soft{stat[n].m, stat[n].s};
   } else {                                // exp(z - lse) = 2^((x - m) scale2) / s with m = lse / scale, but for its rounding, s for that
     a.m = (float)((double)lse[n] * kLog2e / (double)L.scale2);
     a.s = (float)exp2((double)lse[n] * kLog2e - (double)a.m * (double)L.scale2);
   }
   const RowGradient<DT, T> g{out + r.head, a.m, L.scale2, d / a.s};
+  // the target's element: by the thread that writes it (again) behind the others
+  const int64_t i = y - r.head;
+  const int piece = i >= 0 && i < (int64_t)r.full * Pack<DT>::N ? (int)(i / Pack<DT>::N) : -1;
+  const bool here = piece >= 0 ? piece >= first && piece < first + U * T : part == 0;
+  const float xy = here ? Elem<DT>::widen(x[y]) : 0.f;
   if constexpr (T > kWave) __syncthreads();          // in place: the target's logit is read before anything is written
-  g.template stream<4>(r, 0, r.full);
-  g.odd(r);
-  g.target(r, y, xy, d);
+  if (first < r.full) {
+    typename Row<DT, T>::F v[U];
+    r.template load<U, true>(v, first);
+    g.template pieces<U>(r, v, first);
+  }
+  if (part == 0) g.odd(r);
+  if (here) g.target(r, y, xy, d);
 }
 
 struct PolicyArgs {
@@ -426,7 +469,7 @@ struct PairArgs {
   const float* weight;
   const float* ref_logp;
   const float* dloss;
-  const Soft* stat;
+  const RowStat* stat;
   float* dlogp;
   float* rewards;
   float* pair_loss;
@@ -438,9 +481,7 @@ __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.) + log1
 
 // One workgroup per pair: both sums of log ratios, the pair's loss, and the gradient of every log-probability in it.  In float64:
 // log ratios are small differences of large numbers, and there are few rows.
-template <int DT>
-__global__ __launch_bounds__(kThreads) void k_pairs(Logits L, PairArgs a) {
-  typedef typename Elem<DT>::raw raw;
+__global__ __launch_bounds__(kThreads) void k_pairs(int64_t rows, float scale2, PairArgs a) {
   __shared__ double lds[kWaves];
   const int64_t p = blockIdx.x;
   double reward[2];
@@ -449,17 +490,15 @@ __global__ __launch_bounds__(kThreads) void k_pairs(Logits L, PairArgs a) {
   for (int side = 0; side < 2; ++side) {
     const int64_t i = p + side * a.pairs;
     const int64_t f = a.start[i], t = a.start[i + 1];
-    from[side] = f < 0 ? 0 : f < L.rows ? f : L.rows;
-    to[side] = t < from[side] ? from[side] : t < L.rows ? t : L.rows;
+    from[side] = f < 0 ? 0 : f < rows ? f : rows;
+    to[side] = t < from[side] ? from[side] : t < rows ? t : rows;
     double s = 0.;
     for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += kThreads) {
-      const float w = a.weight[n];
-      const int64_t y = L.targets[n];
-      if (w == 0.f || y < 0 || y >= L.vocab) continue;
-      const Soft st = a.stat[n];
-      const float xy = Elem<DT>::widen(static_cast<const raw*>(L.x)[n * L.stride + y]);
-      const double logp = (((double)xy - (double)st.m) * (double)L.scale2 - log2((double)st.s)) / kLog2e;
-      s += (double)w * (logp - (double)a.ref_logp[n]);
+      const float w = a.weight[n], ref = a.ref_logp[n];
+      const RowStat st = a.stat[n];
+      if (st.live == 0.f) continue;
+      const double logp = (((double)st.xy - (double)st.m) * (double)scale2 - log2((double)st.s)) / kLog2e;
+      s += (double)w * (logp - (double)ref);
     }
     reward[side] = a.beta * block_sum<kWaves>(s, lds);
   }
@@ -479,13 +518,7 @@ __global__ __launch_bounds__(kThreads) void k_pairs(Logits L, PairArgs a) {
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_pair_mean(const float* pair_loss, int64_t pairs, float* loss) {
-  __shared__ double lds[kWaves];
-  double s = 0.;
-  for (int64_t p = threadIdx.x; p < pairs; p += kThreads) s += (double)pair_loss[p];
-  s = block_sum<kWaves>(s, lds);
-  if (threadIdx.x == 0) *loss = (float)(s / (double)pairs);
-}
+__global__ __launch_bounds__(kThreads) void k_pair_mean(PairMean mean) { pair_mean<kThreads>(mean); }
 
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
@@ -526,7 +559,7 @@ void for_type(int dt, F&& f) {
 }
 
 template <int DT, bool AGAIN>
-void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, Soft* stat, float* dlogp) {
+void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
   const dim3 grid((uint32_t)L.rows);
   const int pieces = L.vocab / Pack<DT>::N;
   if (pieces <= 256) k_logprobs<DT, 64, AGAIN><<<grid, dim3(64), 0, s>>>(L, weight, logp, lse, stat, dlogp);
@@ -534,12 +567,30 @@ void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float*
   else k_logprobs<DT, 1024, AGAIN><<<grid, dim3(1024), 0, s>>>(L, weight, logp, lse, stat, dlogp);
 }
 
+template <int DT, int T, int U>
+void launch_logprobs_back_as(hipStream_t s, const Logits& L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
+                             int64_t dstride, PairMean mean) {
+  const int64_t pieces = L.vocab / Pack<DT>::N;
+  const int64_t parts = std::max<int64_t>(1, (pieces + U * T - 1) / (U * T));
+  // whole rows per launch, as many as a grid holds
+  const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / parts);
+  for (int64_t at = 0; at < L.rows; at += most) {
+    Logits some = L;
+    some.rows = std::min(L.rows - at, most);
+    some.x = static_cast<const typename Elem<DT>::raw*>(L.x) + at * L.stride;
+    some.targets = L.targets + at;
+    k_logprobs_back<DT, T, U><<<dim3((uint32_t)(some.rows * parts)), dim3(T), 0, s>>>(
+        some, lse ? lse + at : nullptr, stat ? stat + at : nullptr, dlogp + at, static_cast<typename Elem<DT>::raw*>(dx) + at * dstride,
+        dstride, (int)parts, mean);
+    mean.pairs = 0;
+  }
+}
+
 template <int DT>
-void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, const Soft* stat, const float* dlogp, void* dx, int64_t dstride) {
-  const dim3 grid((uint32_t)L.rows);
-  const int pieces = L.vocab / Pack<DT>::N;
-  if (pieces <= 256) k_logprobs_back<DT, 64><<<grid, dim3(64), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
-  else k_logprobs_back<DT, 512><<<grid, dim3(512), 0, s>>>(L, lse, stat, dlogp, dx, dstride);
+void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
+                          int64_t dstride, PairMean mean) {
+  if (L.vocab / Pack<DT>::N <= 256) launch_logprobs_back_as<DT, 64, 4>(s, L, lse, stat, dlogp, dx, dstride, mean);
+  else launch_logprobs_back_as<DT, 256, 2>(s, L, lse, stat, dlogp, dx, dstride, mean);
 }
 
 template <int DT>
@@ -560,7 +611,7 @@ Scratch scratch(int64_t rows, int64_t pairs) {
   Scratch s;
   size_t o = 0;
   auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes); return at; };
-  s.each = s.stat = take((size_t)rows * (pairs ? sizeof(Soft) : sizeof(float4)));
+  s.each = s.stat = take((size_t)rows * (pairs ? sizeof(RowStat) : sizeof(float4)));
   s.dlogp = take(pairs ? (size_t)rows * sizeof(float) : 0);
   s.pair_loss = take((size_t)pairs * sizeof(float));
   s.bytes = o ? o : kAlign;
@@ -595,7 +646,7 @@ int tgrad_token_logprobs_backward(const tgrad_logits* logits, const float* lse, 
   if (pending()) return TGRAD_ERR_HIP;
   if (L.rows == 0) return TGRAD_OK;
   for_type(logits->dtype, [&](auto dt) {
-    launch_logprobs_back<dt.value>(static_cast<hipStream_t>(hip_stream), L, lse, nullptr, dlogp, dlogits, dlogits_stride);
+    launch_logprobs_back<dt.value>(static_cast<hipStream_t>(hip_stream), L, lse, nullptr, dlogp, dlogits, dlogits_stride, PairMean{nullptr, 0, nullptr});
   });
   return launched();
 }
@@ -655,17 +706,16 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const Scratch sc = scratch(L.rows, pairs);
   char* ws = static_cast<char*>(workspace_dev);
-  Soft* stat = reinterpret_cast<Soft*>(ws + sc.stat);
+  RowStat* stat = reinterpret_cast<RowStat*>(ws + sc.stat);
   float* dlogp = reinterpret_cast<float*>(ws + sc.dlogp);
   float* pair_loss = reinterpret_cast<float*>(ws + sc.pair_loss);
   PairArgs a{seq_start, weight, ref_logp, dloss, stat, dlogp, rewards, pair_loss, preference->beta, preference->label_smoothing, pairs};
+  const PairMean mean{pair_loss, pairs, loss};
   for_type(logits->dtype, [&](auto dt) {
-    if (L.rows > 0)
-      launch_logprobs<dt.value, true>(s, L, weight, logp, nullptr, stat, dlogp);
-    k_pairs<dt.value><<<dim3((uint32_t)pairs), dim3(kThreads), 0, s>>>(L, a);
-    k_pair_mean<<<dim3(1), dim3(kThreads), 0, s>>>(pair_loss, pairs, loss);
-    if (dlogits && L.rows > 0)
-      launch_logprobs_back<dt.value>(s, L, nullptr, stat, dlogp, dlogits, dlogits_stride);
+    if (L.rows > 0) launch_logprobs<dt.value, true>(s, L, weight, logp, nullptr, stat, dlogp);
+    k_pairs<<<dim3((uint32_t)pairs), dim3(kThreads), 0, s>>>(L.rows, L.scale2, a);
+    if (dlogits && L.rows > 0) launch_logprobs_back<dt.value>(s, L, nullptr, stat, dlogp, dlogits, dlogits_stride, mean);
+    else k_pair_mean<<<dim3(1), dim3(kThreads), 0, s>>>(mean);
   });
   return launched();
 }

@@ -61,48 +61,85 @@ template <int DT> struct Pack {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }   // one instruction; 0 below 2^-126
 
-// Running maximum and sum of 2^((x - max) scale2).  A maximum of -inf belongs to a sum of nothing, 0; a NaN entry is no maximum and
-// makes the sum NaN, and so does +inf.
+// A running sum of 2^(x scale2 - b), b the largest x scale2 so far, rounded, or -kReach if that is more: one fused multiply-add an
+// exponent.  (b is a float32, so its rounding is no error: the sum is relative to that very number.)  -inf, and masks of the type's
+// lowest value, add 0; a NaN makes the sum NaN, and so does +inf.  Rows whose maximum lies beyond kReach either way, where an exponent
+// would lose its fraction, are summed again (wide).
+constexpr float kReach = 1048576.f;
 struct Soft {
-  float m, s;
+  float b, s;
 };
-__device__ __forceinline__ float soft_base(float m) { return m == -INFINITY ? 0.f : m; }
 template <int N>
 __device__ __forceinline__ void soft_add(Soft& a, const float* x, float scale2) {
-  float m = a.m;
+  float m = x[0];
 #pragma unroll
-  for (int k = 0; k < N; ++k) m = fmaxf(m, x[k]);
-  const float base = soft_base(m);
-  float s0 = a.s * exp2_fast((a.m - base) * scale2), s1 = 0.f;
+  for (int k = 1; k < N; ++k) m = fmaxf(m, x[k]);
+  const float b = fmaxf(a.b, m * scale2);
+  float s0 = a.s * exp2_fast(a.b - b), s1 = 0.f;
 #pragma unroll
   for (int k = 0; k < N; k += 2) {
-    s0 += exp2_fast((x[k] - base) * scale2);
-    if (k + 1 < N) s1 += exp2_fast((x[k + 1] - base) * scale2);
+    s0 += exp2_fast(fmaf(x[k], scale2, -b));
+    if (k + 1 < N) s1 += exp2_fast(fmaf(x[k + 1], scale2, -b));
   }
-  a = Soft{m, s0 + s1};
+  a = Soft{b, s0 + s1};
 }
 // Of all T threads, the same in every one.
 template <int T>
-__device__ __forceinline__ Soft soft_all(Soft a, float scale2, Soft* lds) {
-  float m = a.m;
+__device__ __forceinline__ Soft soft_all(Soft a, Soft* lds) {
+  float b = a.b;
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  float s = a.s * exp2_fast((a.m - soft_base(m)) * scale2);
+  for (int d = 1; d < kWave; d <<= 1) b = fmaxf(b, __shfl_xor(b, d));
+  float s = a.s * exp2_fast(a.b - b);
 #pragma unroll
   for (int d = 1; d < kWave; d <<= 1) s += __shfl_xor(s, d);
-  if constexpr (T == kWave) return Soft{m, s};
-  if (lane_id() == 0) lds[threadIdx.x / kWave] = Soft{m, s};
+  if constexpr (T == kWave) return Soft{b, s};
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = Soft{b, s};
   __syncthreads();
   Soft w[T / kWave];
 #pragma unroll
   for (int i = 0; i < T / kWave; ++i) w[i] = lds[i];
-  m = w[0].m;
+  b = w[0].b;
 #pragma unroll
-  for (int i = 1; i < T / kWave; ++i) m = fmaxf(m, w[i].m);
+  for (int i = 1; i < T / kWave; ++i) b = fmaxf(b, w[i].b);
   s = 0.f;
 #pragma unroll
-  for (int i = 0; i < T / kWave; ++i) s += w[i].s * exp2_fast((w[i].m - soft_base(m)) * scale2);
-  return Soft{m, s};
+  for (int i = 0; i < T / kWave; ++i) s += w[i].s * exp2_fast(w[i].b - b);
+  return Soft{b, s};
+}
+
+// Sum of a row: of 2^(x scale2 - ref), or of 2^((x - ref) scale2) where it is wide.
+struct RowSum {
+  float ref, s;
+  bool wide;
+  // z_y - lse, lse in units of log2
+  __device__ __forceinline__ float above(float x, float scale2) const { return wide ? (x - ref) * scale2 : fmaf(x, scale2, -ref); }
+  __device__ __forceinline__ float logp(float xy, float scale2) const { return (above(xy, scale2) - log2f(s)) * kLn2; }
+  __device__ __forceinline__ float lse(float scale, float scale2) const {
+    return wide ? ref * scale + log2f(s) * kLn2 : (ref + log2f(s)) * kLn2;
+  }
+};
+
+// The whole row again, one element at a time, relative to its maximum: exponents are exact at the maximum whatever its size.
+template <int DT, int T>
+__device__ __forceinline__ RowSum wide_sum(const typename Elem<DT>::raw* x, int vocab, float scale2, Soft* lds) {
+  float m = -INFINITY, s = 0.f;
+  for (int i = threadIdx.x; i < vocab; i += T) m = fmaxf(m, Elem<DT>::widen(x[i]));
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  __syncthreads();
+  if (lane_id() == 0) lds[threadIdx.x / kWave].b = m;
+  __syncthreads();
+  for (int i = 0; i < T / kWave; ++i) m = fmaxf(m, lds[i].b);
+  for (int i = threadIdx.x; i < vocab; i += T) s += exp2_fast((Elem<DT>::widen(x[i]) - m) * scale2);
+  s = block_sum<T / kWave>(s, &lds->s);
+  return RowSum{m, s, true};
+}
+
+template <int DT, int T>
+__device__ __forceinline__ RowSum row_sum(Soft a, const typename Elem<DT>::raw* x, int vocab, float scale2, Soft* lds) {
+  a = soft_all<T>(a, lds);
+  if (a.b > -kReach && a.b < kReach) return RowSum{a.b, a.s, false};
+  return wide_sum<DT, T>(x, vocab, scale2, lds);
 }
 
 // A piece in flight.  ODD: rows of two-byte elements that start in the upper half of a four-byte word are read from that word on, five
@@ -162,17 +199,22 @@ struct Row {
     }
     asm volatile("" ::: "memory");        // all of them on their way: the compiler would move each to the branch that uses it
   }
+  // two pieces at a time: one step of the running maximum for both
   template <int U>
   __device__ __forceinline__ void add(Soft& a, F* q, int first, float scale2) const {
+    static_assert(U % 2 == 0, "pieces are added in pairs");
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; u += 2) {
       const int at = first + u * T;
       if (at >= full) break;
-      Quad v = q[u].v = q[u].settle();
-      if (at + T > full && at + (int)threadIdx.x >= full) v = Quad{P::kLowest, P::kLowest, P::kLowest, P::kLowest};
-      float f[P::N];
-      P::widen(v, f);
-      soft_add<P::N>(a, f, scale2);
+      float f[2 * P::N];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        Quad v = q[u + k].v = q[u + k].settle();
+        if (at + 2 * T > full && at + k * T + (int)threadIdx.x >= full) v = Quad{P::kLowest, P::kLowest, P::kLowest, P::kLowest};
+        P::widen(v, f + k * P::N);
+      }
+      soft_add<2 * P::N>(a, f, scale2);
     }
   }
   // pieces first ... end - 1, read and forgotten
@@ -192,21 +234,38 @@ struct Row {
   }
 };
 
-// Gradient of a row: -q exp2((x - m) scale2) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.
+// Gradient of a row: -q 2^(x scale2 - ref) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.  For two-byte
+// types q is part of the exponent, and its sign that of the rounded result: the exponent's rounding is 2^-19 of it at most, where the
+// result's own is 2^-12.
 template <int DT, int T, bool ODD = false>
 struct RowGradient {
   typedef Pack<DT> P;
   typedef typename P::raw raw;
   typedef Row<DT, T, ODD> R;
   raw* out;                               // where the first piece's gradient goes
-  float m, scale2, q;
-  __device__ __forceinline__ float at(float x) const { return -q * exp2_fast((x - m) * scale2); }
+  RowSum sum;
+  float scale2, q, ref;
+  uint32_t sign;
+  __device__ __forceinline__ RowGradient(raw* o, RowSum r, float scale2_, float d)
+      : out(o), sum(r), scale2(scale2_), q(d / r.s), ref(r.ref - log2f(fabsf(q))), sign(q > 0.f ? 0x80008000u : 0u) {}
+  __device__ __forceinline__ float at(float x) const { return -q * exp2_fast(sum.above(x, scale2)); }
   __device__ __forceinline__ void piece(Quad v, int i, int full) const {
     float f[P::N];
     P::widen(v, f);
+    if constexpr (DT == TGRAD_F32) {
 #pragma unroll
-    for (int k = 0; k < P::N; ++k) f[k] = at(f[k]);
-    if (i < full) P::store(out + (int64_t)i * P::N, P::narrow(f));
+      for (int k = 0; k < P::N; ++k) f[k] = -q * exp2_fast(fmaf(f[k], scale2, -sum.ref));
+    } else {
+#pragma unroll
+      for (int k = 0; k < P::N; ++k) f[k] = exp2_fast(fmaf(f[k], scale2, -ref));
+    }
+    Quad w = P::narrow(f);
+    if constexpr (DT != TGRAD_F32) w = w ^ sign;
+    if (i < full) P::store(out + (int64_t)i * P::N, w);
+  }
+  // elements first ... end - 1 of a row that was summed wide
+  __device__ __forceinline__ void wide(const raw* x, raw* row, int64_t first, int64_t end) const {
+    for (int64_t i = first + threadIdx.x; i < end; i += T) row[i] = Elem<DT>::narrow(at(Elem<DT>::widen(x[i])));
   }
   // pieces that add() has settled
   template <int U>
@@ -258,14 +317,12 @@ __device__ __forceinline__ void with_parity(const typename Elem<DT>::raw* x, F&&
   f(std::false_type());
 }
 
-// z_y - lse
-__device__ __forceinline__ float row_logp(float xy, Soft a, float scale2) { return ((xy - a.m) * scale2 - log2f(a.s)) * kLn2; }
-
 // What a preference loss keeps of a row.
+enum { ROW_IGNORED = 0, ROW_PLAIN = 1, ROW_WIDE = 2 };
 struct RowStat {
-  float m, s;                             // maximum, sum
+  float ref, s;                           // its sum
   float xy;                               // the target's logit
-  float live;                             // 0: ignored
+  int kind;
 };
 
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
@@ -278,25 +335,26 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, f
   const int64_t n = blockIdx.x;
   const int64_t y = L.targets[n];
   const bool live = y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f);
-  Soft a{-INFINITY, 0.f};
+  RowSum r{0.f, 1.f, false};
   float xy = 0.f, lp = 0.f, l = 0.f;
   if (live) {
     const raw* x = static_cast<const raw*>(L.x) + n * L.stride;
     xy = Elem<DT>::widen(x[y]);
     with_parity<DT>(x, [&](auto odd) {
-      const Row<DT, T, odd.value> r(x, L.vocab);
-      r.template stream<8, !AGAIN>(a, 0, r.full, L.scale2);
-      r.add_odd(a, L.scale2);
+      const Row<DT, T, odd.value> row(x, L.vocab);
+      Soft a{-kReach, 0.f};
+      row.template stream<8, !AGAIN>(a, 0, row.full, L.scale2);
+      row.add_odd(a, L.scale2);
+      r = row_sum<DT, T>(a, x, L.vocab, L.scale2, lds);
     });
-    a = soft_all<T>(a, L.scale2, lds);
-    lp = row_logp(xy, a, L.scale2);
-    l = a.m * L.scale + log2f(a.s) * kLn2;
+    lp = r.logp(xy, L.scale2);
+    l = r.lse(L.scale, L.scale2);
   }
   if (threadIdx.x == 0) {
     if (logp) logp[n] = lp;
     if (lse) lse[n] = l;
     if constexpr (AGAIN) {
-      stat[n] = RowStat{a.m, a.s, xy, live ? 1.f : 0.f};
+      stat[n] = RowStat{r.ref, r.s, xy, !live ? ROW_IGNORED : r.wide ? ROW_WIDE : ROW_PLAIN};
       dlogp[n] = 0.f;
     }
   }
@@ -342,14 +400,16 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
     if (part == 0 && (int)threadIdx.x < r.odd) out[r.head + r.odd_at()] = Elem<DT>::narrow(0.f);
     return;
   }
-  Soft a;
+  RowSum sum;
   if (stat) {
-    a = Soft{stat[n].m, stat[n].s};
-  } else {                                // exp(z - lse) = 2^((x - m) scale2) / s with m = lse / scale, but for its rounding, s for that
-    a.m = (float)((double)lse[n] * kLog2e / (double)L.scale2);
-    a.s = (float)exp2((double)lse[n] * kLog2e - (double)a.m * (double)L.scale2);
+    sum = RowSum{stat[n].ref, stat[n].s, stat[n].kind == ROW_WIDE};
+  } else {                                // a reference near lse, and what its rounding leaves
+    const double l2 = (double)lse[n] * kLog2e;
+    sum.wide = !(fabs(l2) < (double)kReach);
+    sum.ref = (float)(sum.wide ? l2 / (double)L.scale2 : l2);
+    sum.s = (float)exp2(l2 - (sum.wide ? (double)sum.ref * (double)L.scale2 : (double)sum.ref));
   }
-  const RowGradient<DT, T> g{out + r.head, a.m, L.scale2, d / a.s};
+  const RowGradient<DT, T> g(out + r.head, sum, L.scale2, d);
   // the target's element: by the thread that writes it (again) behind the others
   const int64_t i = y - r.head;
   const int piece = i >= 0 && i < (int64_t)r.full * Pack<DT>::N ? (int)(i / Pack<DT>::N) : -1;
@@ -357,9 +417,15 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
   const float xy = here ? Elem<DT>::widen(x[y]) : 0.f;
   if constexpr (T > kWave) __syncthreads();          // in place: the target's logit is read before anything is written
   if (first < r.full) {
-    typename Row<DT, T>::F v[U];
-    r.template load<U, true>(v, first);
-    g.template pieces<U>(r, v, first);
+    if (sum.wide) {
+      const int last = first + U * T < r.full ? first + U * T : r.full;
+      g.wide(r.x, g.out, (int64_t)first * Pack<DT>::N, (int64_t)last * Pack<DT>::N);
+      if constexpr (T > kWave) __syncthreads();      // the target's element is another thread's here
+    } else {
+      typename Row<DT, T>::F v[U];
+      r.template load<U, true>(v, first);
+      g.template pieces<U>(r, v, first);
+    }
   }
   if (part == 0) g.odd(r);
   if (here) g.target(r, y, xy, d);
@@ -387,19 +453,19 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
   const R r(x, L.vocab);
   const float xy = Elem<DT>::widen(x[y]);
   const float adv = a.advantage[n], old = a.old_logp[n], ref = a.ref_logp ? a.ref_logp[n] : 0.f, scale = a.dloss ? *a.dloss : 1.f;
-  Soft sum{-INFINITY, 0.f};
+  Soft run{-kReach, 0.f};
   typename R::F held[NV];
   // a whole number of batches, so that a piece belongs to the same thread whether it stays or not
   const int over = r.full - T * NV;
   const int start = over > 0 ? (over + kStream * T - 1) / (kStream * T) * (kStream * T) : 0;
-  r.template stream<kStream, false>(sum, 0, start, L.scale2);
+  r.template stream<kStream, false>(run, 0, start, L.scale2);
   if (start < r.full) {
     r.template load<NV, true>(held, start);
-    r.template add<NV>(sum, held, start, L.scale2);
+    r.template add<NV>(run, held, start, L.scale2);
   }
-  r.add_odd(sum, L.scale2);
-  sum = soft_all<T>(sum, L.scale2, lds);
-  const float logp = row_logp(xy, sum, L.scale2);
+  r.add_odd(run, L.scale2);
+  const RowSum sum = row_sum<DT, T>(run, x, L.vocab, L.scale2, lds);
+  const float logp = sum.logp(xy, L.scale2);
   const float ratio = expf(logp - old);
   const float whole = ratio * adv, cut = fminf(fmaxf(ratio, a.low), a.high) * adv;
   const bool clipped = cut < whole;
@@ -418,10 +484,15 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
   if (!out) return;
   const float d = w * dlogp * scale * L.scale;
   if (d == 0.f) return row_zero<DT, T>(out, L.vocab);
-  const RowGradient<DT, T, ODD> g{out, sum.m, L.scale2, d / sum.s};
-  if (start < r.full) g.template pieces<NV>(r, held, start);
-  for (int first = start - kStream * T; first >= 0; first -= kStream * T) g.template stream<kStream>(r, first, first + kStream * T);
-  g.odd(r);
+  const RowGradient<DT, T, ODD> g(out, sum, L.scale2, d);
+  if (sum.wide) {
+    g.wide(x, out, 0, L.vocab);
+    if constexpr (T > kWave) __syncthreads();        // the target's element is another thread's here
+  } else {
+    if (start < r.full) g.template pieces<NV>(r, held, start);
+    for (int first = start - kStream * T; first >= 0; first -= kStream * T) g.template stream<kStream>(r, first, first + kStream * T);
+    g.odd(r);
+  }
   g.target(r, y, xy, d);
 }
 
@@ -496,8 +567,10 @@ __global__ __launch_bounds__(kThreads) void k_pairs(int64_t rows, float scale2, 
     for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += kThreads) {
       const float w = a.weight[n], ref = a.ref_logp[n];
       const RowStat st = a.stat[n];
-      if (st.live == 0.f) continue;
-      const double logp = (((double)st.xy - (double)st.m) * (double)scale2 - log2((double)st.s)) / kLog2e;
+      if (st.kind == ROW_IGNORED) continue;
+      const double above = st.kind == ROW_WIDE ? ((double)st.xy - (double)st.ref) * (double)scale2
+                                               : (double)st.xy * (double)scale2 - (double)st.ref;
+      const double logp = (above - log2((double)st.s)) / kLog2e;
       s += (double)w * (logp - (double)ref);
     }
     reward[side] = a.beta * block_sum<kWaves>(s, lds);

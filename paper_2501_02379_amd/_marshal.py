@@ -26,7 +26,13 @@ def on_stream(f):
     return run
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def stream_of(device) -> int:
+    """The handle of the device's current stream (without a Stream object around it where torch offers that: 0.2 us instead of 2)."""
+    if _raw_stream is not None:
+        return _raw_stream(device.index)
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -34,7 +40,7 @@ def vector(t, n, dtype, device, what):
     """Address of a dense vector of n elements (None stays None); anything else is refused."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or t.get_device() != device.index or not t.is_contiguous():
         refuse("%s: %s[%d], dense, on the logits' device" % (what, dtype, n))
     return t.data_ptr()
 

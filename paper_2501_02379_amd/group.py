@@ -8,7 +8,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import tgrad as T
-from ._marshal import REAL_TYPES, call, check, refuse
+from ._marshal import REAL_TYPES, call, check, refuse, stream_of
 
 TYPES = {**REAL_TYPES, torch.complex64: T.TGRAD_C64}
 _MOMENTS = (torch.float32, torch.complex64)
@@ -114,7 +114,7 @@ class Group:
 
     def _result(self, into):
         if into is None:
-            if torch.cuda.current_stream(self.device) == self.stream:
+            if stream_of(self.device) == self.stream.cuda_stream:
                 return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
             with torch.cuda.stream(self.stream):
                 return torch.empty(4, dtype=torch.float32, device=self.device)[2:]

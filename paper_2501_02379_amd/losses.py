@@ -7,6 +7,7 @@ allocator on that stream.  The gradient with respect to the logits goes on throu
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -46,19 +47,26 @@ def _describe(logits, targets, temperature):
 def _gradient(logits, out):
     """Where the gradient goes, and its row stride: `out` (logits itself is allowed) or a new tensor."""
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or \
             (out.shape[1] > 1 and out.stride(1) != 1):
         refuse("out: the logits' shape, type and device, with dense rows")
     return out, (out.stride(0) if out.shape[0] > 1 else out.shape[1])
 
 
-def _scratch(logits, pairs):
+@functools.lru_cache(maxsize=1024)
+def _scratch_floats(rows, pairs):
     n = C.c_size_t(0)
-    rc = T.load().tgrad_loss_query_size(logits.shape[0], pairs, C.byref(n))
+    rc = T.load().tgrad_loss_query_size(rows, pairs, C.byref(n))
     if rc != T.TGRAD_OK:
         raise T.TgradError(rc, "tgrad_loss_query_size")
-    return torch.empty(n.value, dtype=torch.uint8, device=logits.device)
+    return n.value // 4
+
+
+def _floats(logits, pairs, *sizes):
+    """The scratch of a loss and its float32 outputs, one allocation for all of them."""
+    scratch = _scratch_floats(logits.shape[0], pairs)
+    return torch.empty(scratch + sum(sizes), dtype=torch.float32, device=logits.device).split_with_sizes((scratch,) + sizes)
 
 
 @on_stream
@@ -67,7 +75,7 @@ def tgrad_token_logprobs(logits, targets, *, temperature: float = 1.0):
     Rows whose target lies outside the vocabulary (-100, say) have 0 in both and are not read."""
     d = _describe(logits, targets, temperature)
     out = torch.empty(2, d.rows, dtype=torch.float32, device=logits.device)
-    logp, lse = out[0], out[1]
+    logp, lse = out.unbind(0)
     call(logits.device, T.load().tgrad_token_logprobs, "tgrad_token_logprobs", C.byref(d), logp.data_ptr(), lse.data_ptr(),
          stream_of(logits.device))
     return logp, lse
@@ -94,9 +102,7 @@ def tgrad_policy_loss(logits, targets, weight, advantage, old_logp, ref_logp=Non
     d = _describe(logits, targets, temperature)
     dev, rows = logits.device, d.rows
     dx, stride = _gradient(logits, out) if backward else (None, 0)
-    ws = _scratch(logits, 0)
-    small = torch.empty(4 + rows, dtype=torch.float32, device=dev)
-    stats, logp = small[:4], small[4:]
+    ws, stats, logp = _floats(logits, 0, 4, rows)
     hyper = T.tgrad_policy(clip_low, clip_high, kl_beta)
     call(dev, T.load().tgrad_policy_loss, "tgrad_policy_loss", C.byref(d), C.byref(hyper),
          vector(weight, rows, torch.float32, dev, "weight"), vector(advantage, rows, torch.float32, dev, "advantage"),
@@ -117,13 +123,11 @@ def tgrad_preference_loss(logits, targets, weight, ref_logp, seq_start, *, beta:
         refuse("seq_start: int64[2 pairs + 1]")
     pairs = seq_start.shape[0] // 2
     dx, stride = _gradient(logits, out) if backward else (None, 0)
-    ws = _scratch(logits, pairs)
-    small = torch.empty(1 + 2 * pairs + rows, dtype=torch.float32, device=dev)
-    loss, rewards, logp = small[0], small[1:1 + 2 * pairs], small[1 + 2 * pairs:]
+    ws, loss, rewards, logp = _floats(logits, pairs, 1, 2 * pairs, rows)
     hyper = T.tgrad_preference(beta, label_smoothing)
     call(dev, T.load().tgrad_preference_loss, "tgrad_preference_loss", C.byref(d), C.byref(hyper), pairs,
          vector(seq_start, 2 * pairs + 1, torch.int64, dev, "seq_start"), vector(weight, rows, torch.float32, dev, "weight"),
          vector(ref_logp, rows, torch.float32, dev, "ref_logp"), vector(dloss, 1, torch.float32, dev, "dloss"), ws.data_ptr(),
          loss.data_ptr(), rewards.data_ptr(), logp.data_ptr(), dx.data_ptr() if backward else None, stride,
          stream_of(dev))
-    return PreferenceLoss(loss, rewards, logp, dx)
+    return PreferenceLoss(loss[0], rewards, logp, dx)

@@ -198,6 +198,16 @@ int tgrad_refresh_factors(tgrad_ctx* ctx, const void* grad_dev);
 int tgrad_step(tgrad_ctx* ctx, void* weight_dev, const void* grad_dev);
 
 /*
+ * Multiply the gradient of every later `tgrad_step` of this context by a number that lies on the device when the step runs: the
+ * factor that clips a global norm (tgrad_norm.coef below), an inverse loss scale.  The gradient itself is neither rewritten nor read
+ * once more: its compressed parts, which are linear in it, are scaled before AdamUpdate.  The support and the factors of a refresh come from the
+ * gradient as it is; a positive factor changes neither, up to rounding.  SPARSE_G and CORE_G report scaled values.
+ *  scale_dev  device pointer to one float32, read by every step, or NULL: no scaling (as after tgrad_init).
+ * Errors: INVALID_ARG.
+ */
+int tgrad_set_grad_scale(tgrad_ctx* ctx, const float* scale_dev);
+
+/*
  * tgrad_step for callers that cannot allocate device memory and cannot hold a context: code under
  * HIP graph capture, tight serving loops, harnesses that forbid hipMalloc.  It does what
  * `tgrad_step` does for a context at step count t (refresh first when t % cfg.refresh_every == 0,
@@ -314,8 +324,8 @@ int tgrad_destroy(tgrad_ctx* ctx);
  *
  * The loss at its head (token log-probabilities, a clipped policy loss with a KL term, a preference loss; value and gradient
  * with respect to the logits), the global norm of all gradients, clipping, and AdamW for the parameters that have no
- * low-rank part.  The clip factor stays on the device: tgrad_group_adamw applies it to what it reads, so that clipping needs no
- * pass over the gradients.
+ * low-rank part.  The clip factor stays on the device: tgrad_group_adamw and, after tgrad_set_grad_scale, tgrad_step apply it to
+ * what they read, so that clipping needs no pass over the gradients.
  *
  * Real element types, beside TGRAD_C64 and TGRAD_CBF16.
  */

@@ -51,6 +51,7 @@ struct Core2Adam {
   float* v;             // second moments
   float2* g_out;        // compressed gradient, written for the state accessors
   float beta1, beta2, inv_c1, inv_c2, eps;
+  const float* scale;   // what the gradient is multiplied by, or null
 };
 
 constexpr int kSlot = 2 * 4 * 64;            // floats of a wavefront's partial P in LDS: [comp][r][lane]
@@ -196,6 +197,10 @@ __global__ __launch_bounds__(kThreads) void k_core2(Core2Args a, Core2Adam ad) {
       gre += pr[w * kSlot];
       gim += pi[w * kSlot];
     }
+    if (ad.scale) {
+      gre *= *ad.scale;
+      gim *= *ad.scale;
+    }
     float2 m = mm;
     m.x = ad.beta1 * m.x + (1.f - ad.beta1) * gre;
     m.y = ad.beta1 * m.y + (1.f - ad.beta1) * gim;
@@ -278,11 +283,11 @@ bool core2_kernel_fits(int I0, int I1, int M0, int M1, int64_t Cc) {
 
 void launch_core2(hipStream_t s, const float2* x, const float2* U0, const float2* U1, int I0, int I1, int M0, int M1,
                   int64_t Cc, float2* m, float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2,
-                  float eps, float2* z) {
+                  float eps, const float* scale, float2* z) {
   if (Cc <= 0) return;
   const size_t lds = core2_lds(I1);
   Core2Args a{reinterpret_cast<const float*>(x), reinterpret_cast<float*>(z), U0, U1, I0, I1, M0, M1, (int)Cc};
-  Core2Adam ad{m, v, g_out, beta1, beta2, inv_c1, inv_c2, eps};
+  Core2Adam ad{m, v, g_out, beta1, beta2, inv_c1, inv_c2, eps, scale};
   allow_lds(k_core2, lds);
   k_core2<<<dim3((unsigned)((Cc + 7) / 8 * 8)), dim3(kThreads), lds, s>>>(a, ad);
 }

@@ -525,6 +525,7 @@ struct CoreAdam {
   float* v;             // second moments
   float2* g_out;        // compressed gradient, written for the state accessors
   float beta1, beta2, inv_c1, inv_c2, eps;
+  const float* scale;   // what the gradient is multiplied by, or null
 };
 constexpr int kCoreSteps = 4;             // steps of four rows of x per wavefront: one operand, all of them for K <= 16 waves
 
@@ -680,6 +681,10 @@ __global__ __launch_bounds__(64 * W) void k_core(const float* x, const float2* _
         for (int w = 0; w < W; ++w) {
           gre += pr[w * kPart];
           gim += pi[w * kPart];
+        }
+        if (ad.scale) {
+          gre *= *ad.scale;
+          gim *= *ad.scale;
         }
         float2 m = mm[q];
         m.x = ad.beta1 * m.x + (1.f - ad.beta1) * gre;
@@ -894,10 +899,10 @@ bool core_kernel_fits(int K, int M, int64_t B) {
 // Last compression stage + AdamUpdate on the core + first reconstruction stage (mode 1: the tensor
 // before is (K, B), the tensor after is (K, B) again, the core in between (M, B)).
 void launch_core(hipStream_t s, const float2* x, const float2* U, int rn, int K, int M, int64_t B, float2* m,
-                 float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2, float eps,
+                 float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2, float eps, const float* scale,
                  float2* z) {
   if (B <= 0) return;
-  CoreAdam ad{m, v, g_out, beta1, beta2, inv_c1, inv_c2, eps};
+  CoreAdam ad{m, v, g_out, beta1, beta2, inv_c1, inv_c2, eps, scale};
   const float* xf = reinterpret_cast<const float*>(x);
   float* zf = reinterpret_cast<float*>(z);
   const int64_t groups = (B + 15) / 16;

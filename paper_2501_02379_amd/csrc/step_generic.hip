@@ -59,6 +59,15 @@ __global__ __launch_bounds__(kThreads) void k_contract(const void* __restrict__ 
   out[o] = acc;
 }
 
+// x <- x *scale: compressed quantities of a gradient that is to be clipped.
+__global__ void k_scale_values(float2* __restrict__ x, int64_t n, const float* __restrict__ scale) {
+  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= n) return;
+  const float s = *scale;
+  const float2 v = x[i];
+  x[i] = make_float2(v.x * s, v.y * s);
+}
+
 // AdamUpdate on the compressed low-rank gradient (appendix algorithm "Adam with low-rank tensor
 // decomposition": M, V from |R conj R|, bias correction, N = M^ / (sqrt(V^) + eps)).
 __global__ void k_adam_core(const float2* __restrict__ r, float2* __restrict__ m, float* __restrict__ v,
@@ -229,6 +238,11 @@ void launch_contract(hipStream_t s, const void* x, int x_dtype, const uint32_t* 
     TGRAD_GO(TGRAD_C64, false, false);
   }
 #undef TGRAD_GO
+}
+
+void launch_scale_values(hipStream_t s, float2* x, int64_t n, const float* scale) {
+  if (n <= 0) return;
+  k_scale_values<<<dim3(blocks_for(n, 256)), dim3(256), 0, s>>>(x, n, scale);
 }
 
 void launch_adam_core(hipStream_t s, const float2* r, float2* m, float* v, float2* n_out, int64_t C,

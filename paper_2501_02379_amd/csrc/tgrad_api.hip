@@ -33,7 +33,7 @@ const char* const kKernelNames[KID_COUNT] = {
     "mask_from_indices",
     "tile_offsets", "gram", "gram_reduce", "eig_jacobi", "factor_pack",
     "gather", "project_first", "project", "adam_core", "backproject", "update", "sparse_update",
-    "hooi_project", "core", "residual"};
+    "hooi_project", "core", "residual", "grad_scale"};
 
 struct Plan {
   int N = 0;
@@ -354,6 +354,7 @@ struct tgrad_ctx {
   bool have_indices;
   bool have_factor[kMaxNdim];
   bool have_hist;                 // the last refresh has counted its gradient's non-finite entries
+  const float* grad_scale;        // what tgrad_step multiplies the gradient by (device), or null
   int launch_status;              // first failed kernel launch of the current call (TGRAD_OK = none)
   bool profiling;
   std::vector<EventPair> events;
@@ -703,6 +704,14 @@ int do_step(tgrad_ctx* c, void* weight, const void* g) {
     src = last = dst;
   }
 
+  // A gradient that is to be scaled: everything so far is linear in it, so its compressed parts are scaled instead, the sparse
+  // values here and the core where it is formed (k_core, k_core2) or here as well.
+  if (c->grad_scale) {
+    Scope sc_(c, KID_SCALE);
+    launch_scale_values(s, gs, p.k, c->grad_scale);
+    if (!p.fuse_core2 && !p.fuse_core) launch_scale_values(s, core_g, p.C, c->grad_scale);
+  }
+
   // AdamUpdate on the core; tau = t + 1
   const double tau = (double)(c->t + 1);
   const double corr1 = 1.0 / (1.0 - std::pow((double)cf.beta1, tau)), corr2 = 1.0 / (1.0 - std::pow((double)cf.beta2, tau));
@@ -737,7 +746,7 @@ int do_step(tgrad_ctx* c, void* weight, const void* g) {
     Scope sc_(c, KID_CORE);
     launch_core2(s, src, c->st<float2>(p.st_U[0]), c->st<float2>(p.st_U[1]), (int)p.shape[0], (int)p.shape[1], p.rank[0],
                  p.rank[1], p.proj[N - 2].B, c->st<float2>(p.st_ml), c->st<float>(p.st_vl), core_g, cf.beta1, cf.beta2,
-                 inv_c1, inv_c2, cf.eps, last);
+                 inv_c1, inv_c2, cf.eps, c->grad_scale, last);
     zsrc = last;
     first_back = 2;
   } else if (p.fuse_core) {
@@ -745,7 +754,7 @@ int do_step(tgrad_ctx* c, void* weight, const void* g) {
     const Stage& sg = p.proj[N - 1];
     Scope sc_(c, KID_CORE);
     launch_core(s, src, c->st<float2>(p.st_U[0]), p.rank[0], sg.K, sg.M, sg.B, c->st<float2>(p.st_ml),
-                c->st<float>(p.st_vl), core_g, cf.beta1, cf.beta2, inv_c1, inv_c2, cf.eps, pair[1] ? pair[0] : last);
+                c->st<float>(p.st_vl), core_g, cf.beta1, cf.beta2, inv_c1, inv_c2, cf.eps, c->grad_scale, pair[1] ? pair[0] : last);
     zsrc = pair[1] ? pair[0] : last;
     first_back = 1;
   } else {
@@ -935,6 +944,7 @@ int tgrad_init(tgrad_ctx** out, const tgrad_config* cfg, void* state_dev, void* 
   c->have_indices = false;
   for (int n = 0; n < kMaxNdim; ++n) c->have_factor[n] = false;
   c->have_hist = false;
+  c->grad_scale = nullptr;
   c->launch_status = TGRAD_OK;
   c->profiling = false;
   for (int i = 0; i < KID_COUNT; ++i) {
@@ -975,6 +985,12 @@ int tgrad_step(tgrad_ctx* ctx, void* weight_dev, const void* grad_dev) {
   return do_step(ctx, weight_dev, grad_dev);
 }
 
+int tgrad_set_grad_scale(tgrad_ctx* ctx, const float* scale_dev) {
+  if (!ctx || (uintptr_t)scale_dev % 4) return TGRAD_ERR_INVALID_ARG;
+  ctx->grad_scale = scale_dev;
+  return TGRAD_OK;
+}
+
 int tgrad_step_static(const tgrad_config* cfg, void* state_dev, int64_t t, void* weight_dev,
                       const void* grad_dev, void* hip_stream) {
   int rc = validate(cfg);
@@ -1002,6 +1018,7 @@ int tgrad_step_static(const tgrad_config* cfg, void* state_dev, int64_t t, void*
   c.have_indices = true;                                          // the caller's contract for t % T != 0
   for (int n = 0; n < kMaxNdim; ++n) c.have_factor[n] = true;
   c.have_hist = false;
+  c.grad_scale = nullptr;
   c.launch_status = TGRAD_OK;
   c.profiling = false;
   if (error_pending_on_entry()) return TGRAD_ERR_HIP;

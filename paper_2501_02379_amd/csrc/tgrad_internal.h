@@ -39,7 +39,7 @@ enum KernelId {
   KID_MASK_FROM_IDX,
   KID_TILE_OFFSETS, KID_GRAM, KID_GRAM_REDUCE, KID_EIG, KID_FACTOR_PACK,
   KID_GATHER, KID_PROJECT_FIRST, KID_PROJECT, KID_ADAM_CORE, KID_BACKPROJECT, KID_UPDATE,
-  KID_SPARSE_UPDATE, KID_HOOI_PROJECT, KID_CORE, KID_RESIDUAL, KID_COUNT
+  KID_SPARSE_UPDATE, KID_HOOI_PROJECT, KID_CORE, KID_RESIDUAL, KID_SCALE, KID_COUNT
 };
 
 struct Launch {                            // what every launcher needs
@@ -84,6 +84,7 @@ void launch_gather(hipStream_t s, const void* g, int dtype, const int32_t* omega
                    float2* out);
 void launch_contract(hipStream_t s, const void* x, int x_dtype, const uint32_t* mask,
                      const float2* U, int In, int rn, bool project, const Stage& st, float2* out);
+void launch_scale_values(hipStream_t s, float2* x, int64_t n, const float* scale);
 void launch_adam_core(hipStream_t s, const float2* r, float2* m, float* v, float2* n_out, int64_t C,
                       float beta1, float beta2, float inv_c1, float inv_c2, float eps);
 void launch_sparse_adam(hipStream_t s, float2* gs, int64_t k, float2* m, float* v, float beta1, float beta2,
@@ -107,12 +108,12 @@ void launch_mid(hipStream_t s, const float2* x, const float2* U, int rn, bool pr
                 float2* out);
 bool core_kernel_fits(int K, int M, int64_t B);
 void launch_core(hipStream_t s, const float2* x, const float2* U, int rn, int K, int M, int64_t B, float2* m,
-                 float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2, float eps,
+                 float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2, float eps, const float* scale,
                  float2* z);
 bool core2_kernel_fits(int I0, int I1, int M0, int M1, int64_t Cc);
 void launch_core2(hipStream_t s, const float2* x, const float2* U0, const float2* U1, int I0, int I1, int M0, int M1,
                   int64_t Cc, float2* m, float* v, float2* g_out, float beta1, float beta2, float inv_c1, float inv_c2,
-                  float eps, float2* z);
+                  float eps, const float* scale, float2* z);
 void launch_pack_fused_factor(hipStream_t s, const float2* U, int I2, int r, float2* fpad, float2* ut);
 void launch_lproj(hipStream_t s, const void* g, int dtype, const int32_t* omega, const uint32_t* tile_start,
                   float2* gs, const float2* U, int rn, const Stage& st, int W, float2* out, int fused_I2,

@@ -38,7 +38,7 @@ EXPORTS = (
     "tgrad_query_sizes", "tgrad_init", "tgrad_refresh_factors", "tgrad_step", "tgrad_step_static", "tgrad_get_state", "tgrad_check",
     "tgrad_set_state", "tgrad_set_profiling", "tgrad_get_kernel_times", "tgrad_calibration_copy",
     "tgrad_calibration_mfma", "tgrad_calibration_tile_stream",
-    "tgrad_destroy", "tgrad_strerror",
+    "tgrad_destroy", "tgrad_strerror", "tgrad_set_grad_scale",
     "tgrad_group_query_size", "tgrad_group_init", "tgrad_group_bind", "tgrad_group_grad_norm", "tgrad_group_scale",
     "tgrad_group_clip", "tgrad_group_adamw", "tgrad_group_destroy",
     "tgrad_token_logprobs", "tgrad_token_logprobs_backward", "tgrad_loss_query_size", "tgrad_policy_loss",
@@ -141,6 +141,7 @@ def load():
     lib.tgrad_refresh_factors.argtypes = [vp, vp]
     lib.tgrad_step.argtypes = [vp, vp, vp]
     lib.tgrad_step_static.argtypes = [C.POINTER(tgrad_config), vp, C.c_int64, vp, vp, vp]
+    lib.tgrad_set_grad_scale.argtypes = [vp, vp]
     lib.tgrad_get_state.argtypes = [vp, i32, vp, sz]
     lib.tgrad_set_state.argtypes = [vp, i32, vp, sz]
     lib.tgrad_check.argtypes = [vp, C.POINTER(C.c_int64)]
@@ -249,6 +250,17 @@ class Context:
         rc = self.lib.tgrad_step(self.handle, _ptr(weight), _ptr(grad))
         if rc != TGRAD_OK:
             raise TgradError(rc, "tgrad_step")
+
+    def tgrad_set_grad_scale(self, scale) -> None:
+        """Later steps multiply the gradient by `scale`, one float32 on the device (the factor of a group's norm, `norm[1]`), read
+        when the step runs; None: no scaling.  The context keeps the tensor alive."""
+        import torch
+        if scale is not None and (scale.dtype != torch.float32 or scale.numel() != 1 or scale.device.type != "cuda"):
+            raise TgradError(TGRAD_ERR_INVALID_ARG, "tgrad_set_grad_scale")
+        rc = self.lib.tgrad_set_grad_scale(self.handle, _ptr(scale) if scale is not None else None)
+        if rc != TGRAD_OK:
+            raise TgradError(rc, "tgrad_set_grad_scale")
+        self.grad_scale = scale
 
     # ---- state ---------------------------------------------------------------------------
     def _item_array(self, what: int) -> np.ndarray:

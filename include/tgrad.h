@@ -420,7 +420,7 @@ int tgrad_group_destroy(tgrad_group* group);
 typedef struct {
   const void* data;         /* device pointer: TGRAD_F32, TGRAD_BF16 or TGRAD_F16, rows of `vocab` consecutive elements */
   int64_t rows;             /* 0..2^31-1 */
-  int64_t vocab;            /* 1..2^31-1 */
+  int64_t vocab;            /* 1..2^30-1 */
   int64_t row_stride;       /* elements from one row to the next, >= vocab */
   const int64_t* targets;   /* device pointer, int64[rows] */
   int32_t dtype;
@@ -485,7 +485,7 @@ typedef struct {
  *   loss = mean over pairs of -(1 - s) log sigma(h) - s log sigma(-h);  dlogits = dloss d loss / d logits.
  * A sequence without rows, or whose weights are all 0, has R = 0.
  *  seq_start  device pointer, int64[2 pairs + 1], ascending; bounds outside 0 .. rows are taken as the nearest inside.
- *             Rows in no sequence have no gradient.  pairs >= 1.
+ *             Rows in no sequence have no gradient.  1 <= pairs < 2^24.
  *  weight, ref_logp  device pointers, float32[rows]; rows of weight 0 are ignored.
  *  dloss, workspace_dev (tgrad_loss_query_size(rows, pairs)), logp, dlogits  as for tgrad_policy_loss.
  *  loss       device pointer, one float32.

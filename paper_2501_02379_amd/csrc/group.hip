@@ -420,6 +420,16 @@ void put(tgrad_group* g, const tgrad_tensor* t, bool table) {
   }
 }
 
+// f(pieces, workgroups) for parts of the table, the last one first, whose launches stay below 2^32 threads.
+template <typename F>
+void by_pieces(const tgrad_group* g, F&& f) {
+  constexpr int64_t kMost = (((int64_t)1 << 32) - 1) / kThreads;
+  for (int64_t end = g->lay.npieces; end > 0; end -= kMost) {
+    const int64_t first = end > kMost ? end - kMost : 0;
+    f(g->pieces() + first, (uint32_t)(end - first));
+  }
+}
+
 int sum_grid(const tgrad_group* g) {
   const int64_t most = std::min<int64_t>(compute_units() * 4, kMaxSums);
   return (int)std::max<int64_t>(1, std::min(g->lay.npieces, most));
@@ -507,8 +517,9 @@ int tgrad_group_grad_norm(tgrad_group* group, float max_norm, const double* add_
 int tgrad_group_scale(tgrad_group* group, const tgrad_norm* norm_dev) {
   if (!group || !norm_dev || (uintptr_t)norm_dev % 8) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
-  if (group->lay.npieces == 0) return TGRAD_OK;
-  k_group_scale<<<dim3((uint32_t)group->lay.npieces), dim3(kThreads), 0, group->stream>>>(group->entries(), group->pieces(), norm_dev);
+  by_pieces(group, [&](const Piece* pieces, uint32_t grid) {
+    k_group_scale<<<dim3(grid), dim3(kThreads), 0, group->stream>>>(group->entries(), pieces, norm_dev);
+  });
   return launched();
 }
 
@@ -536,8 +547,9 @@ int tgrad_group_adamw(tgrad_group* group, const tgrad_adamw* hyper, int64_t t, c
   k.inv_c2 = (float)(1. / (1. - std::pow(h.beta2, tau)));
   k.eps = (float)h.eps;
   k.skip_nonfinite = h.skip_nonfinite != 0;
-  if (group->lay.npieces == 0) return TGRAD_OK;
-  k_group_adamw<<<dim3((uint32_t)group->lay.npieces), dim3(kThreads), 0, group->stream>>>(group->entries(), group->pieces(), k, norm_dev);
+  by_pieces(group, [&](const Piece* pieces, uint32_t grid) {
+    k_group_adamw<<<dim3(grid), dim3(kThreads), 0, group->stream>>>(group->entries(), pieces, k, norm_dev);
+  });
   return launched();
 }
 

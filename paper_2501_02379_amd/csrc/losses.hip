@@ -24,6 +24,7 @@ struct Logits {
   const void* x;
   int64_t rows, stride;
   const int64_t* targets;
+  int64_t first;                          // the row of a launch's first workgroup
   int vocab;
   float scale;                            // 1 / temperature
   float scale2;                           // log2(e) / temperature
@@ -332,7 +333,7 @@ template <int DT, int T, bool AGAIN>
 __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
   typedef typename Elem<DT>::raw raw;
   __shared__ Soft lds[T / kWave];
-  const int64_t n = blockIdx.x;
+  const int64_t n = L.first + blockIdx.x;
   const int64_t y = L.targets[n];
   const bool live = y >= 0 && y < L.vocab && (!weight || weight[n] != 0.f);
   RowSum r{0.f, 1.f, false};
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
   if (blockIdx.x == 0 && mean.pairs > 0) pair_mean<T>(mean);
   const uint32_t row = blockIdx.x / (uint32_t)parts;
   const int part = (int)(blockIdx.x - row * (uint32_t)parts);
-  const int64_t n = row;
+  const int64_t n = L.first + row;
   const int64_t y = L.targets[n];
   raw* out = static_cast<raw*>(dx) + n * dstride;
   const float d = dlogp[n] * L.scale;
@@ -502,7 +503,7 @@ template <int DT, int T, int NV>
 __global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
   typedef typename Elem<DT>::raw raw;
   __shared__ Soft lds[T / kWave];
-  const int64_t n = blockIdx.x;
+  const int64_t n = L.first + blockIdx.x;
   const int64_t y = L.targets[n];
   const float w = a.weight[n];
   raw* out = a.dx ? static_cast<raw*>(a.dx) + n * a.dstride : nullptr;
@@ -606,14 +607,14 @@ int check_logits(const tgrad_logits* l, Logits* out) {
   if (!l) return TGRAD_ERR_INVALID_ARG;
   if (l->dtype != TGRAD_F32 && l->dtype != TGRAD_BF16 && l->dtype != TGRAD_F16) return TGRAD_ERR_INVALID_ARG;
   constexpr int64_t kMost = ((int64_t)1 << 31) - 1;
-  if (l->rows < 0 || l->rows > kMost || l->vocab < 1 || l->vocab > kMost || l->row_stride < l->vocab) return TGRAD_ERR_INVALID_ARG;
+  if (l->rows < 0 || l->rows > kMost || l->vocab < 1 || l->vocab > kMost / 2 || l->row_stride < l->vocab) return TGRAD_ERR_INVALID_ARG;
   if (l->rows > 0 && l->row_stride > (((int64_t)1 << 62) / l->rows)) return TGRAD_ERR_INVALID_ARG;
   if (!(l->temperature > 0.f) || !std::isfinite(l->temperature)) return TGRAD_ERR_INVALID_ARG;
   const double inv = 1. / (double)l->temperature;
   if (!std::isfinite((float)(inv * kLog2e)) || (float)inv == 0.f) return TGRAD_ERR_INVALID_ARG;
   if (l->rows > 0 && (!l->data || !l->targets)) return TGRAD_ERR_INVALID_ARG;
   if ((uintptr_t)l->data % (uintptr_t)real_bytes(l->dtype) || (uintptr_t)l->targets % 8) return TGRAD_ERR_INVALID_ARG;
-  *out = Logits{l->data, l->rows, l->row_stride, l->targets, (int)l->vocab, (float)inv, (float)(inv * kLog2e)};
+  *out = Logits{l->data, l->rows, l->row_stride, l->targets, 0, (int)l->vocab, (float)inv, (float)(inv * kLog2e)};
   return TGRAD_OK;
 }
 
@@ -631,13 +632,29 @@ void for_type(int dt, F&& f) {
   else f(std::integral_constant<int, TGRAD_F16>());
 }
 
+// f(first, rows) for parts of the rows whose launches, `groups` workgroups of T threads a row, stay below 2^32 threads.
+template <typename F>
+void by_rows(const Logits& L, int T, int64_t groups, F&& f) {
+  const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 32) - 1) / (T * groups));
+  for (int64_t at = 0; at < L.rows; at += most) {
+    Logits some = L;
+    some.first = at;
+    f(some, (uint32_t)(std::min(L.rows - at, most) * groups));
+  }
+}
+
+// Threads of a row: a wavefront where it has no more than four pieces for each of its lanes; otherwise 256, or 1024 where there are
+// fewer rows than compute units (a call behind another, 1024 / 256 threads: 64 rows of 131072 bf16 numbers 10.8 / 14.6 us, one of 131072
+// float32 numbers 12.4 / 18.9, 300 rows of 131072 bf16 numbers 23.3 / 21.1).
 template <int DT, bool AGAIN>
 void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
-  const dim3 grid((uint32_t)L.rows);
   const int pieces = L.vocab / Pack<DT>::N;
-  if (pieces <= 256) k_logprobs<DT, 64, AGAIN><<<grid, dim3(64), 0, s>>>(L, weight, logp, lse, stat, dlogp);
-  else if (L.rows > 2 * compute_units()) k_logprobs<DT, 256, AGAIN><<<grid, dim3(256), 0, s>>>(L, weight, logp, lse, stat, dlogp);
-  else k_logprobs<DT, 1024, AGAIN><<<grid, dim3(1024), 0, s>>>(L, weight, logp, lse, stat, dlogp);
+  const int T = pieces <= 256 ? 64 : L.rows > compute_units() ? 256 : 1024;
+  by_rows(L, T, 1, [&](const Logits& some, uint32_t grid) {
+    if (T == 64) k_logprobs<DT, 64, AGAIN><<<dim3(grid), dim3(64), 0, s>>>(some, weight, logp, lse, stat, dlogp);
+    else if (T == 256) k_logprobs<DT, 256, AGAIN><<<dim3(grid), dim3(256), 0, s>>>(some, weight, logp, lse, stat, dlogp);
+    else k_logprobs<DT, 1024, AGAIN><<<dim3(grid), dim3(1024), 0, s>>>(some, weight, logp, lse, stat, dlogp);
+  });
 }
 
 template <int DT, int T, int U>
@@ -645,18 +662,10 @@ void launch_logprobs_back_as(hipStream_t s, const Logits& L, const float* lse, c
                              int64_t dstride, PairMean mean) {
   const int64_t pieces = L.vocab / Pack<DT>::N;
   const int64_t parts = std::max<int64_t>(1, (pieces + U * T - 1) / (U * T));
-  // whole rows per launch, as many as a grid holds
-  const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / parts);
-  for (int64_t at = 0; at < L.rows; at += most) {
-    Logits some = L;
-    some.rows = std::min(L.rows - at, most);
-    some.x = static_cast<const typename Elem<DT>::raw*>(L.x) + at * L.stride;
-    some.targets = L.targets + at;
-    k_logprobs_back<DT, T, U><<<dim3((uint32_t)(some.rows * parts)), dim3(T), 0, s>>>(
-        some, lse ? lse + at : nullptr, stat ? stat + at : nullptr, dlogp + at, static_cast<typename Elem<DT>::raw*>(dx) + at * dstride,
-        dstride, (int)parts, mean);
+  by_rows(L, T, parts, [&](const Logits& some, uint32_t grid) {
+    k_logprobs_back<DT, T, U><<<dim3(grid), dim3(T), 0, s>>>(some, lse, stat, dlogp, dx, dstride, (int)parts, mean);
     mean.pairs = 0;
-  }
+  });
 }
 
 template <int DT>
@@ -666,15 +675,22 @@ void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, cons
   else launch_logprobs_back_as<DT, 256, 2>(s, L, lse, stat, dlogp, dx, dstride, mean);
 }
 
+template <int DT, int T, int NV>
+void launch_policy_as(hipStream_t s, const Logits& L, const PolicyArgs& a) {
+  by_rows(L, T, 1, [&](const Logits& some, uint32_t grid) { k_policy<DT, T, NV><<<dim3(grid), dim3(T), 0, s>>>(some, a); });
+}
+
+// The fewest threads whose registers hold the row: several rows then share a compute unit, and one loads while another computes.
 template <int DT>
 void launch_policy(hipStream_t s, const Logits& L, const PolicyArgs& a) {
-  const dim3 grid((uint32_t)L.rows);
   const int pieces = L.vocab / Pack<DT>::N;
-  if (pieces <= 64 * 4) k_policy<DT, 64, 4><<<grid, dim3(64), 0, s>>>(L, a);
-  else if (pieces <= 256 * 8) k_policy<DT, 256, 8><<<grid, dim3(256), 0, s>>>(L, a);
-  else if (pieces <= 512 * 16) k_policy<DT, 512, 16><<<grid, dim3(512), 0, s>>>(L, a);
-  else k_policy<DT, 1024, 16><<<grid, dim3(1024), 0, s>>>(L, a);
+  if (pieces <= 64 * 4) launch_policy_as<DT, 64, 4>(s, L, a);
+  else if (pieces <= 256 * 8) launch_policy_as<DT, 256, 8>(s, L, a);
+  else if (pieces <= 512 * 16) launch_policy_as<DT, 512, 16>(s, L, a);
+  else launch_policy_as<DT, 1024, 16>(s, L, a);
 }
+
+constexpr int64_t kMostPairs = (int64_t)1 << 24;   // a workgroup of 256 threads for each
 
 // Scratch of the losses.
 struct Scratch {
@@ -725,7 +741,7 @@ int tgrad_token_logprobs_backward(const tgrad_logits* logits, const float* lse, 
 }
 
 int tgrad_loss_query_size(int64_t rows, int64_t pairs, size_t* workspace_bytes) {
-  if (!workspace_bytes || rows < 0 || rows >= ((int64_t)1 << 31) || pairs < 0 || pairs >= ((int64_t)1 << 30)) return TGRAD_ERR_INVALID_ARG;
+  if (!workspace_bytes || rows < 0 || rows >= ((int64_t)1 << 31) || pairs < 0 || pairs >= kMostPairs) return TGRAD_ERR_INVALID_ARG;
   *workspace_bytes = scratch(rows, pairs).bytes;
   return TGRAD_OK;
 }
@@ -767,7 +783,7 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
   if (!preference || !(preference->beta > 0.f) || !std::isfinite(preference->beta) || !(preference->label_smoothing >= 0.f) ||
       !(preference->label_smoothing <= 0.5f))
     return TGRAD_ERR_INVALID_ARG;
-  if (pairs < 1 || pairs >= ((int64_t)1 << 30) || !seq_start || (uintptr_t)seq_start % 8) return TGRAD_ERR_INVALID_ARG;
+  if (pairs < 1 || pairs >= kMostPairs || !seq_start || (uintptr_t)seq_start % 8) return TGRAD_ERR_INVALID_ARG;
   if (!workspace_dev || (uintptr_t)workspace_dev % kAlign || !float_ptr(loss) || !float_ptr(rewards)) return TGRAD_ERR_INVALID_ARG;
   if (L.rows > 0 && (!float_ptr(weight) || !float_ptr(ref_logp))) return TGRAD_ERR_INVALID_ARG;
   if (!float_ptr_or_null(dloss) || !float_ptr_or_null(logp)) return TGRAD_ERR_INVALID_ARG;

@@ -442,3 +442,27 @@ def test_the_bindings_refuse():
                 lambda: losses.tgrad_preference_loss(x, y, w, w, torch.zeros(3, dtype=torch.int64, device=DEV), beta=0.0)):
         with pytest.raises(T.TgradError):
             bad()
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^26 + 300 rows of three numbers: a wavefront each is more than 2^32 threads."""
+    rows, vocab = (1 << 26) + 300, 3
+    x = torch.zeros(rows, vocab, dtype=torch.float16, device=DEV)
+    y = torch.full((rows,), -100, device=DEV)
+    live = torch.tensor([0, 1, (1 << 26) - 2, (1 << 26) - 1, 1 << 26, rows - 1])
+    y[live.to(DEV)] = 1
+    x[live.to(DEV)] = torch.tensor([0.0, 1.0, -1.0], dtype=torch.float16, device=DEV)
+    logp, _ = losses.tgrad_token_logprobs(x, y)
+    want = 1.0 - math.log(math.exp(0.0) + math.exp(1.0) + math.exp(-1.0))
+    assert int(torch.count_nonzero(logp)) == len(live) and bool(((logp[live.to(DEV)] - want).abs() < 1e-6).all())
+    ones = torch.ones(rows, device=DEV)
+    r = losses.tgrad_policy_loss(x, y, ones, ones, logp)
+    assert abs(float(r.stats[0]) + len(live)) < 1e-5
+    p = torch.softmax(x[live.to(DEV)].double(), 1).cpu()
+    p[:, 1] -= 1
+    assert bool(((r.dlogits[live.to(DEV)].double().cpu() - p).abs() < 1e-3).all())
+    assert int(torch.count_nonzero(r.dlogits)) == 3 * len(live)
+    start = torch.tensor([0, 2, rows], device=DEV)
+    q = losses.tgrad_preference_loss(x, y, ones, torch.zeros_like(logp), start)
+    assert int(torch.count_nonzero(q.dlogits)) == 3 * len(live)
+    assert bool((torch.sign(q.dlogits[live.to(DEV), 1]).cpu() == torch.tensor([-1, -1, 1, 1, 1, 1])).all())

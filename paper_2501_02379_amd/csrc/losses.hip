@@ -235,9 +235,7 @@ struct Row {
   }
 };
 
-// Gradient of a row: -q 2^(x scale2 - ref) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.  For two-byte
-// types q is part of the exponent, and its sign that of the rounded result: the exponent's rounding is 2^-19 of it at most, where the
-// result's own is 2^-12.
+// Gradient of a row: -q 2^(x scale2 - ref) with q = d / sum, and d more at the target, d = d loss / d z_y / temperature.
 template <int DT, int T, bool ODD = false>
 struct RowGradient {
   typedef Pack<DT> P;
@@ -245,24 +243,15 @@ struct RowGradient {
   typedef Row<DT, T, ODD> R;
   raw* out;                               // where the first piece's gradient goes
   RowSum sum;
-  float scale2, q, ref;
-  uint32_t sign;
-  __device__ __forceinline__ RowGradient(raw* o, RowSum r, float scale2_, float d)
-      : out(o), sum(r), scale2(scale2_), q(d / r.s), ref(r.ref - log2f(fabsf(q))), sign(q > 0.f ? 0x80008000u : 0u) {}
+  float scale2, q;
+  __device__ __forceinline__ RowGradient(raw* o, RowSum r, float scale2_, float d) : out(o), sum(r), scale2(scale2_), q(d / r.s) {}
   __device__ __forceinline__ float at(float x) const { return -q * exp2_fast(sum.above(x, scale2)); }
   __device__ __forceinline__ void piece(Quad v, int i, int full) const {
     float f[P::N];
     P::widen(v, f);
-    if constexpr (DT == TGRAD_F32) {
 #pragma unroll
-      for (int k = 0; k < P::N; ++k) f[k] = -q * exp2_fast(fmaf(f[k], scale2, -sum.ref));
-    } else {
-#pragma unroll
-      for (int k = 0; k < P::N; ++k) f[k] = exp2_fast(fmaf(f[k], scale2, -ref));
-    }
-    Quad w = P::narrow(f);
-    if constexpr (DT != TGRAD_F32) w = w ^ sign;
-    if (i < full) P::store(out + (int64_t)i * P::N, w);
+    for (int k = 0; k < P::N; ++k) f[k] = -q * exp2_fast(fmaf(f[k], scale2, -sum.ref));
+    if (i < full) P::store(out + (int64_t)i * P::N, P::narrow(f));
   }
   // elements first ... end - 1 of a row that was summed wide
   __device__ __forceinline__ void wide(const raw* x, raw* row, int64_t first, int64_t end) const {

@@ -466,3 +466,48 @@ def test_more_rows_than_one_launch_takes():
     q = losses.tgrad_preference_loss(x, y, ones, torch.zeros_like(logp), start)
     assert int(torch.count_nonzero(q.dlogits)) == 3 * len(live)
     assert bool((torch.sign(q.dlogits[live.to(DEV), 1]).cpu() == torch.tensor([-1, -1, 1, 1, 1, 1])).all())
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.01])
+@pytest.mark.parametrize("offset", [300.0, -5000.0, 30000.0, -60000.0, 3e6, -3e6, 1e30, -1e30, 3e38])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_far_from_zero(dtype, offset, temperature):
+    """Only differences within a row count, wherever the row lies: entries equal to the offset, one step of the type below it, and
+    far below.  In the bounds |z| is then the distance to the row's maximum, of entries that are not negligible."""
+    if dtype == "f16" and abs(offset) > 65000:
+        pytest.skip("beyond float16")
+    for vocab in (50, 3001, 20002):
+        g = torch.Generator().manual_seed(vocab)
+        top = torch.tensor(offset).to(TYPES[dtype][0])
+        low = torch.tensor(-math.inf).to(top.dtype)
+        below = torch.nextafter(top, low) if dtype != "bf16" else (top.double() * (1 - math.copysign(2.0 ** -7, offset))).to(top.dtype)
+        pick = torch.randint(0, 3, (4, vocab), generator=g)
+        x = torch.where(pick == 0, top, torch.where(pick == 1, below, (below.double() - abs(float(below)) * 0.1).to(top.dtype)))
+        x = torch.where(torch.isfinite(x), x, below)
+        y = torch.randint(0, vocab, (4,), generator=g)
+        x[torch.arange(4), y] = top
+        shift = x.double().amax(1, keepdim=True)                        # the reference too, relative to the maximum
+        xs = x.double() - shift
+        z, lse, logp, _ = scores(xs, y, temperature)
+        lse = lse + shift[:, 0] / float(np.float32(temperature))
+        near = torch.clamp(z, min=-200)
+        e = logp_bound(near, logp)
+        xd, yd = x.to(DEV), y.to(DEV)
+        got, got_lse = losses.tgrad_token_logprobs(xd, yd, temperature=temperature)
+        assert bool(((got.cpu().double() - logp).abs() <= e).all())
+        if float(lse.abs().max()) < 3.4e38:                            # a float32 holds it
+            assert bool(((got_lse.cpu().double() - lse).abs() <= e + 4 * U * lse.abs()).all())
+        w = torch.ones(4, device=DEV)
+        r = losses.tgrad_policy_loss(xd, yd, w, w, got, temperature=temperature)
+        d = -torch.exp(r.logp.cpu().double() - got.cpu().double()) / float(np.float32(temperature))
+        gr, p = gradient(near, torch.logsumexp(near, 1), y, d)
+        close_gradient(r.dlogits, gr, p, d, near, logp, y, dtype, d_error=8 * U * d.abs())
+        start = torch.tensor([0, 2, 4], device=DEV)
+        q = losses.tgrad_preference_loss(xd, yd, w, (logp - 0.3).float().to(DEV), start, temperature=temperature)
+        assert bool(((q.logp.cpu().double() - logp).abs() <= e).all()) and bool(((r.logp.cpu().double() - logp).abs() <= e).all())
+        s = preference_reference(xs, y, w, (logp - 0.3).float(), start, 0.1, 0.0, temperature)[3] / float(np.float32(temperature))
+        gr, p = gradient(near, torch.logsumexp(near, 1), y, s)
+        close_gradient(q.dlogits, gr, p, s, near, logp, y, dtype, d_error=s.abs() * (8 * U + 0.4 * float(e.max())))
+        inplace = xd.clone()
+        losses.tgrad_policy_loss(inplace, yd, w, w, got, temperature=temperature, out=inplace)
+        assert torch.equal(inplace, r.dlogits)

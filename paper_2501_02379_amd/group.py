@@ -3,6 +3,7 @@ tgrad_group_* entry points of include/tgrad.h."""
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -11,19 +12,33 @@ from . import tgrad as T
 from ._marshal import REAL_TYPES, call, check, refuse, stream_of
 
 TYPES = {**REAL_TYPES, torch.complex64: T.TGRAD_C64}
-_MOMENTS = (torch.float32, torch.complex64)
 
 
-def _addresses(tensors, n, what, device):
+_ENTRY = struct.Struct("=q5Q2i2f")        # tgrad_tensor
+assert _ENTRY.size == C.sizeof(T.tgrad_tensor)
+
+
+def _tensors(tensors, n, what, index):
+    """n tensors (or None) on GPU `index`, dense."""
     if tensors is None:
         return [None] * n
     tensors = list(tensors)
     if len(tensors) != n:
         refuse("%s: one for every gradient" % what)
     for t in tensors:
-        if t is not None and (t.device != device or not t.is_contiguous()):
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
             refuse("%s: dense tensors on one GPU" % what)
     return tensors
+
+
+def _type(t, what):
+    """Elements and type code."""
+    kind = TYPES.get(t.dtype)
+    if kind is not None:
+        return t.numel(), kind
+    if t.dtype is torch.int16 and t.shape[-1:] == (2,):
+        return t.numel() // 2, T.TGRAD_CBF16
+    refuse("%s: float32, bfloat16, float16, complex64, or bf16 pairs as int16[..., 2]" % what)
 
 
 class Group:
@@ -58,46 +73,43 @@ class Group:
              self.workspace.data_ptr(), self.stream.cuda_stream)
 
     def _table(self, grads, params, exp_avg, exp_avg_sq, outs):
-        n, dev = len(grads), self.device
-        grads = _addresses(grads, n, "grads", dev)
-        params, exp_avg = _addresses(params, n, "params", dev), _addresses(exp_avg, n, "exp_avg", dev)
-        exp_avg_sq, outs = _addresses(exp_avg_sq, n, "exp_avg_sq", dev), _addresses(outs, n, "outs", dev)
+        n, index = len(grads), self.device.index
+        grads = _tensors(grads, n, "grads", index)
+        params, exp_avg = _tensors(params, n, "params", index), _tensors(exp_avg, n, "exp_avg", index)
+        exp_avg_sq, outs = _tensors(exp_avg_sq, n, "exp_avg_sq", index), _tensors(outs, n, "outs", index)
         lr, wd = self.lr_scale or [1.0] * n, self.weight_decay or [0.0] * n
         if len(lr) != n or len(wd) != n:
             refuse("lr_scale, weight_decay: one for every gradient")
-        table = (T.tgrad_tensor * n)()
-        for i in range(n):
-            g, p, m, v, o = grads[i], params[i], exp_avg[i], exp_avg_sq[i], outs[i]
+        entries = []
+        for g, p, m, v, o, scale, decay in zip(grads, params, exp_avg, exp_avg_sq, outs, lr, wd):
             if g is None:
                 refuse("grads: a tensor each")
-            numel, kind = self._type(g, "grads")
-            if o is not None and (o.shape != g.shape or o.dtype != g.dtype):
+            numel, kind = _type(g, "grads")
+            if o is not None and (o.dtype is not g.dtype or o.shape != g.shape):
                 refuse("outs: the gradient's shape and type")
             pkind = kind
             if p is not None:
-                count, pkind = self._type(p, "params")
-                if pkind == T.TGRAD_F32 and kind in (T.TGRAD_C64, T.TGRAD_CBF16) and p.shape[-1:] == (2,):
-                    count, pkind = p.numel() // 2, T.TGRAD_C64        # complex64 as float32 pairs
-                width = 2 if kind in (T.TGRAD_C64, T.TGRAD_CBF16) else 1
+                cplx = kind == T.TGRAD_C64 or kind == T.TGRAD_CBF16
+                count, pkind = _type(p, "params")
+                if cplx and pkind == T.TGRAD_F32 and p.shape[-1:] == (2,):
+                    count, pkind = count // 2, T.TGRAD_C64            # complex64 as float32 pairs
                 if count != numel or m is None or v is None:
                     refuse("params: the gradient's number of elements, with moments")
-                if m.dtype not in _MOMENTS or m.numel() * (2 if m.is_complex() else 1) != width * numel or \
-                        v.dtype != torch.float32 or v.numel() != numel:
+                if m.dtype is torch.complex64:
+                    size = 2 * m.numel()
+                else:
+                    size = m.numel() if m.dtype is torch.float32 else -1
+                if size != (2 * numel if cplx else numel) or v.dtype is not torch.float32 or v.numel() != numel:
                     refuse("moments: float32, the parameter's size")
             elif m is not None or v is not None:
                 refuse("moments belong to parameters")
-            at = [t.data_ptr() if t is not None else None for t in (g, o, p, m, v)]
-            table[i] = T.tgrad_tensor(numel, *at, kind, pkind, lr[i], wd[i])
+            try:
+                entries.append(_ENTRY.pack(numel, g.data_ptr(), 0 if o is None else o.data_ptr(), 0 if p is None else p.data_ptr(),
+                                           0 if m is None else m.data_ptr(), 0 if v is None else v.data_ptr(), kind, pkind, scale, decay))
+            except (OverflowError, struct.error):
+                refuse("lr_scale, weight_decay: float32 numbers")
         self.tensors = (grads, params, exp_avg, exp_avg_sq, outs)
-        return table
-
-    @staticmethod
-    def _type(t, what):
-        if t.dtype == torch.int16 and t.shape[-1:] == (2,):
-            return t.numel() // 2, T.TGRAD_CBF16
-        if t.dtype not in TYPES:
-            refuse("%s: float32, bfloat16, float16, complex64, or bf16 pairs as int16[..., 2]" % what)
-        return t.numel(), TYPES[t.dtype]
+        return (T.tgrad_tensor * n).from_buffer_copy(b"".join(entries))
 
     def tgrad_group_bind(self, grads, params=None, exp_avg=None, exp_avg_sq=None, outs=None) -> None:
         """The same tensors at new addresses (gradients allocated anew); what is None stays as it is."""

@@ -485,7 +485,7 @@ typedef struct {
  *   loss = mean over pairs of -(1 - s) log sigma(h) - s log sigma(-h);  dlogits = dloss d loss / d logits.
  * A sequence without rows, or whose weights are all 0, has R = 0.
  *  seq_start  device pointer, int64[2 pairs + 1], ascending; bounds outside 0 .. rows are taken as the nearest inside.
- *             Rows in no sequence have no gradient.  1 <= pairs < 2^24.
+ *             Rows in no sequence have no gradient.  1 <= pairs < 2^22.
  *  weight, ref_logp  device pointers, float32[rows]; rows of weight 0 are ignored.
  *  dloss, workspace_dev (tgrad_loss_query_size(rows, pairs)), logp, dlogits  as for tgrad_policy_loss.
  *  loss       device pointer, one float32.

@@ -308,18 +308,18 @@ __device__ __forceinline__ void with_parity(const typename Elem<DT>::raw* x, F&&
 }
 
 // What a preference loss keeps of a row.
-enum { ROW_IGNORED = 0, ROW_PLAIN = 1, ROW_WIDE = 2 };
 struct RowStat {
+  double gap;                             // w (logp - ref_logp); 0 for an ignored row
   float ref, s;                           // its sum
-  float xy;                               // the target's logit
-  int kind;
+  int32_t wide;
 };
 
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
-// rows that lie in no sequence) are.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
+// rows that lie in no sequence) are.  The log ratio is formed in float64 from the sum itself: it is a small difference of large numbers.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
 // numbers, a quarter of them ignored: 151 us without it, 136 with it, 5.9 TB/s).
 template <int DT, int T, bool AGAIN>
-__global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
+__global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
+                                                float* dlogp) {
   typedef typename Elem<DT>::raw raw;
   __shared__ Soft lds[T / kWave];
   const int64_t n = L.first + blockIdx.x;
@@ -344,7 +344,12 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, f
     if (logp) logp[n] = lp;
     if (lse) lse[n] = l;
     if constexpr (AGAIN) {
-      stat[n] = RowStat{r.ref, r.s, xy, !live ? ROW_IGNORED : r.wide ? ROW_WIDE : ROW_PLAIN};
+      double gap = 0.;
+      if (live) {
+        const double above = r.wide ? ((double)xy - (double)r.ref) * (double)L.scale2 : (double)xy * (double)L.scale2 - (double)r.ref;
+        gap = (double)weight[n] * ((above - log2((double)r.s)) / kLog2e - (double)ref_logp[n]);
+      }
+      stat[n] = RowStat{gap, r.ref, r.s, r.wide};
       dlogp[n] = 0.f;
     }
   }
@@ -392,7 +397,7 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
   }
   RowSum sum;
   if (stat) {
-    sum = RowSum{stat[n].ref, stat[n].s, stat[n].kind == ROW_WIDE};
+    sum = RowSum{stat[n].ref, stat[n].s, stat[n].wide != 0};
   } else {                                // a reference near lse, and what its rounding leaves
     const double l2 = (double)lse[n] * kLog2e;
     sum.wide = !(fabs(l2) < (double)kReach);
@@ -538,7 +543,6 @@ __global__ __launch_bounds__(1024) void k_policy_sums(const float4* each, int64_
 struct PairArgs {
   const int64_t* start;
   const float* weight;
-  const float* ref_logp;
   const float* dloss;
   const RowStat* stat;
   float* dlogp;
@@ -550,12 +554,13 @@ struct PairArgs {
 
 __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.) + log1p(exp(-fabs(x))); }
 
-// One workgroup per pair: both sums of log ratios, the pair's loss, and the gradient of every log-probability in it.  In float64:
-// log ratios are small differences of large numbers, and there are few rows.
-__global__ __launch_bounds__(kThreads) void k_pairs(int64_t rows, float scale2, PairArgs a) {
-  __shared__ double lds[kWaves];
+// One workgroup per pair: both sums of log ratios, in float64, the pair's loss, and the gradient of every log-probability in it.
+constexpr int kPairThreads = 512;
+__global__ __launch_bounds__(kPairThreads) void k_pairs(int64_t rows, PairArgs a) {
+  __shared__ double lds[kPairThreads / kWave];
+  constexpr int U = 4;                    // rows of a thread in flight
   const int64_t p = blockIdx.x;
-  double reward[2];
+  double sum[2] = {0., 0.};
   int64_t from[2], to[2];
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
@@ -563,29 +568,29 @@ __global__ __launch_bounds__(kThreads) void k_pairs(int64_t rows, float scale2, 
     const int64_t f = a.start[i], t = a.start[i + 1];
     from[side] = f < 0 ? 0 : f < rows ? f : rows;
     to[side] = t < from[side] ? from[side] : t < rows ? t : rows;
-    double s = 0.;
-    for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += kThreads) {
-      const float w = a.weight[n], ref = a.ref_logp[n];
-      const RowStat st = a.stat[n];
-      if (st.kind == ROW_IGNORED) continue;
-      const double above = st.kind == ROW_WIDE ? ((double)st.xy - (double)st.ref) * (double)scale2
-                                               : (double)st.xy * (double)scale2 - (double)st.ref;
-      const double logp = (above - log2((double)st.s)) / kLog2e;
-      s += (double)w * (logp - (double)ref);
-    }
-    reward[side] = a.beta * block_sum<kWaves>(s, lds);
   }
-  const double h = reward[0] - reward[1];
+#pragma unroll
+  for (int side = 0; side < 2; ++side)
+    for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += U * kPairThreads) {
+      double gap[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) gap[u] = a.stat[n + u * kPairThreads < to[side] ? n + u * kPairThreads : n].gap;
+#pragma unroll
+      for (int u = 0; u < U; ++u) sum[side] += n + u * kPairThreads < to[side] ? gap[u] : 0.;
+    }
+  const double chosen = a.beta * block_sum<kPairThreads / kWave>(sum[0], lds);
+  const double rejected = a.beta * block_sum<kPairThreads / kWave>(sum[1], lds);
+  const double h = chosen - rejected;
   const double dh = a.beta * (a.smoothing / (1. + exp(-h)) - (1. - a.smoothing) / (1. + exp(h))) / (double)a.pairs *
                     (a.dloss ? (double)*a.dloss : 1.);
   if (threadIdx.x == 0) {
-    a.rewards[p] = (float)reward[0];
-    a.rewards[p + a.pairs] = (float)reward[1];
+    a.rewards[p] = (float)chosen;
+    a.rewards[p + a.pairs] = (float)rejected;
     a.pair_loss[p] = (float)((1. - a.smoothing) * softplus(-h) + a.smoothing * softplus(h));
   }
 #pragma unroll
   for (int side = 0; side < 2; ++side)
-    for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += kThreads) {
+    for (int64_t n = from[side] + threadIdx.x; n < to[side]; n += kPairThreads) {
       const float w = a.weight[n];
       a.dlogp[n] = w == 0.f ? 0.f : (float)((side ? -dh : dh) * (double)w);
     }
@@ -646,13 +651,14 @@ void by_rows(const Logits& L, int T, int64_t groups, F&& f) {
 // fewer rows than compute units (a call behind another, 1024 / 256 threads: 64 rows of 131072 bf16 numbers 10.8 / 14.6 us, one of 131072
 // float32 numbers 12.4 / 18.9, 300 rows of 131072 bf16 numbers 23.3 / 21.1).
 template <int DT, bool AGAIN>
-void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, float* logp, float* lse, RowStat* stat, float* dlogp) {
+void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
+                     float* dlogp) {
   const int pieces = L.vocab / Pack<DT>::N;
   const int T = pieces <= 256 ? 64 : L.rows > compute_units() ? 256 : 1024;
   by_rows(L, T, 1, [&](const Logits& some, uint32_t grid) {
-    if (T == 64) k_logprobs<DT, 64, AGAIN><<<dim3(grid), dim3(64), 0, s>>>(some, weight, logp, lse, stat, dlogp);
-    else if (T == 256) k_logprobs<DT, 256, AGAIN><<<dim3(grid), dim3(256), 0, s>>>(some, weight, logp, lse, stat, dlogp);
-    else k_logprobs<DT, 1024, AGAIN><<<dim3(grid), dim3(1024), 0, s>>>(some, weight, logp, lse, stat, dlogp);
+    if (T == 64) k_logprobs<DT, 64, AGAIN><<<dim3(grid), dim3(64), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
+    else if (T == 256) k_logprobs<DT, 256, AGAIN><<<dim3(grid), dim3(256), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
+    else k_logprobs<DT, 1024, AGAIN><<<dim3(grid), dim3(1024), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
   });
 }
 
@@ -694,7 +700,7 @@ void launch_policy(hipStream_t s, const Logits& L, const PolicyArgs& a) {
   else launch_policy_as<DT, 1024, 16>(s, L, a);
 }
 
-constexpr int64_t kMostPairs = (int64_t)1 << 24;   // a workgroup of 256 threads for each
+constexpr int64_t kMostPairs = (int64_t)1 << 22;   // a workgroup for each
 
 // Scratch of the losses.
 struct Scratch {
@@ -723,7 +729,7 @@ int tgrad_token_logprobs(const tgrad_logits* logits, float* logp, float* lse, vo
   if (pending()) return TGRAD_ERR_HIP;
   if (L.rows == 0 || (!logp && !lse)) return TGRAD_OK;
   for_type(logits->dtype, [&](auto dt) {
-    launch_logprobs<dt.value, false>(static_cast<hipStream_t>(hip_stream), L, nullptr, logp, lse, nullptr, nullptr);
+    launch_logprobs<dt.value, false>(static_cast<hipStream_t>(hip_stream), L, nullptr, nullptr, logp, lse, nullptr, nullptr);
   });
   return launched();
 }
@@ -802,11 +808,11 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
   RowStat* stat = reinterpret_cast<RowStat*>(ws + sc.stat);
   float* dlogp = reinterpret_cast<float*>(ws + sc.dlogp);
   float* pair_loss = reinterpret_cast<float*>(ws + sc.pair_loss);
-  PairArgs a{seq_start, weight, ref_logp, dloss, stat, dlogp, rewards, pair_loss, preference->beta, preference->label_smoothing, pairs};
+  PairArgs a{seq_start, weight, dloss, stat, dlogp, rewards, pair_loss, preference->beta, preference->label_smoothing, pairs};
   const PairMean mean{pair_loss, pairs, loss};
   for_type(logits->dtype, [&](auto dt) {
-    if (L.rows > 0) launch_logprobs<dt.value, true>(s, L, weight, logp, nullptr, stat, dlogp);
-    k_pairs<<<dim3((uint32_t)pairs), dim3(kThreads), 0, s>>>(L.rows, L.scale2, a);
+    if (L.rows > 0) launch_logprobs<dt.value, true>(s, L, weight, ref_logp, logp, nullptr, stat, dlogp);
+    k_pairs<<<dim3((uint32_t)pairs), dim3(kPairThreads), 0, s>>>(L.rows, a);
     if (dlogits && L.rows > 0) launch_logprobs_back<dt.value>(s, L, nullptr, stat, dlogp, dlogits, dlogits_stride, mean);
     else k_pair_mean<<<dim3(1), dim3(kThreads), 0, s>>>(mean);
   });

@@ -74,7 +74,8 @@ __device__ __forceinline__ void for_real(int real, F&& f) {
 }
 
 // U units of four numbers of a thread from unit `first` on; past the end the last one again.  LAST: nobody reads them again soon; with
-// that hint on loads and stores, scaling 136 M complex64 takes 335 us instead of 400, AdamW of 478 M numbers 2190 instead of 2310.
+// that hint on loads and stores, norm and scaling of 136 M complex64 take 545 us instead of 608, norm and AdamW of 478 M numbers 2365 instead of
+// 2488.
 template <int DT, int U, bool LAST>
 __device__ __forceinline__ void load_units(typename Four<DT>::type* q, const void* base, int64_t at, int first, int units) {
 #pragma unroll
@@ -93,7 +94,7 @@ __device__ __forceinline__ void store_unit(void* base, int64_t at, int unit, con
 // Everything above is on its way before anything below: the compiler would move each load to the branch that uses it.
 __device__ __forceinline__ void loads_issued() { asm volatile("" ::: "memory"); }
 
-// sum |g|^2.  Squares and sums in float64: the square of a float32 is exact there, and no finite gradient overflows.  Every
+// sum |g|^2, bounded by the read (136 M complex64: 181 us, 5.7 to 6 TB/s).  Squares and sums in float64: the square of a float32 is exact there, and no finite gradient overflows.  Every
 // workgroup leaves one partial sum; the last one to come adds them up in the order of the workgroups, so that the result does
 // not depend on which one that is.
 template <int DT>
@@ -145,8 +146,9 @@ __device__ __forceinline__ void finish_norm(const NormArgs& a, int n, double* ld
   }
 }
 
-// FINISH: the last workgroup to come does k_group_norm's work; which one that is does not change the result.  For few workgroups:
-// the counter costs every one of them some 50 ns at the same address, behind one another (2048 of them: 90 us of 290), k_group_norm a launch.
+// FINISH: the last workgroup to come does k_group_norm's work; which one that is does not change the result.  For few workgroups: the
+// counter, with what it makes visible, costs every one of them some 50 ns, mostly behind one another (2048 of them: 90 us of 290; counters
+// in two levels were no better), k_group_norm a launch.
 template <bool FINISH>
 __global__ __launch_bounds__(kThreads) void k_group_sumsq(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           int64_t npieces, NormArgs a) {
@@ -204,8 +206,8 @@ __device__ __forceinline__ void piece_scale(const void* g, void* out, Span s, fl
   }
 }
 
-// One workgroup per piece: workgroups that stay for more of them, one piece behind the other, are slower (AdamW of 478 M numbers
-// 2500 us instead of 2310).
+// One workgroup per piece: workgroups that stay for more of them, one piece behind the other, are slower (norm and AdamW of
+// 478 M numbers 2690 us instead of 2488).  136 M complex64: 371 us, 5.9 TB/s, a copy's rate.
 __global__ __launch_bounds__(kThreads) void k_group_scale(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           const tgrad_norm* norm) {
   const float coef = norm->coef;
@@ -311,7 +313,8 @@ __device__ __forceinline__ void piece_adamw(const Entry& e, int index, const Ada
   }
 }
 
-// Backwards: what k_group_sumsq has read last is still in the caches (norm and step of 478 M numbers 2320 us, forwards 2343).
+// Seven streams, 26 to 28 bytes a number: 478 M numbers with bf16 gradients in 1940 to 2170 us, 6.4 to 5.7 TB/s.  Backwards: what k_group_sumsq has
+// read last is still in the caches (norm and step 2320 us, forwards 2343).
 __global__ __launch_bounds__(kThreads) void k_group_adamw(const Entry* __restrict__ entries, const Piece* __restrict__ pieces, AdamK h,
                                                           const tgrad_norm* norm) {
   const float coef = norm ? norm->coef : 1.f;

@@ -2,7 +2,8 @@
 // with a KL term, the preference loss on paired log ratios, and their gradients with respect to the logits.
 //
 // Both losses depend on a row through logp = z_y - lse, lse = log sum_v exp z_v (z = x / temperature), alone, so the gradient is
-// d loss / d logp times (1[v = y] - exp(z_v - lse)) / temperature.  Exponentials are those of 2, of (x - max) log2(e) / temperature.
+// d loss / d logp times (1[v = y] - exp(z_v - lse)) / temperature.  There are some ten operations for every two to eight bytes: memory bounds
+// all of it, and what counts is how often a row is read, how many bytes are on their way, and that arithmetic goes on under them.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -145,7 +146,7 @@ __device__ __forceinline__ RowSum row_sum(Soft a, const typename Elem<DT>::raw* 
 
 // A piece in flight.  ODD: rows of two-byte elements that start in the upper half of a four-byte word are read from that word on, five
 // words for a piece, and shifted into place where they are used: loads of 16 bytes that are not aligned to 4 take twice as long (4096
-// rows of 100003 bf16 numbers, every other row such a one, scored in 176 us, now 134; stores do not mind).  The first and the last word
+// rows of 100003 bf16 numbers, every other row such a one, scored in 175 us, now 128; stores do not mind).  The first and the last word
 // of such a row may lie across its ends by one element, which is not used.
 template <bool ODD> struct Flight {
   Quad v;
@@ -316,7 +317,7 @@ struct RowStat {
 
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
 // rows that lie in no sequence) are.  The log ratio is formed in float64 from the sum itself: it is a small difference of large numbers.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
-// numbers, a quarter of them ignored: 151 us without it, 136 with it, 5.9 TB/s).
+// numbers, a quarter of them ignored: 151 us without it, 136 with it; now 127, 6.35 TB/s).  8 pieces of every thread are on their way.
 template <int DT, int T, bool AGAIN>
 __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
                                                 float* dlogp) {
@@ -369,8 +370,9 @@ __device__ __forceinline__ void pair_mean(const PairMean& a) {
   if (threadIdx.x == 0) *a.loss = (float)(s / (double)a.pairs);
 }
 
-// stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread (a workgroup per
-// row, in a loop: 1464 rows of 100003 float16 numbers 365 us, now 300).  Pieces start at 16-byte boundaries of the gradient.  The first
+// stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread (a
+// workgroup per row, in a loop: a loss on 5721 rows of 100003 float16 numbers 563 us, so 501; the gradient alone now 305 us, 6.4 TB/s with
+// what the memory-side cache still has).  Pieces start at 16-byte boundaries of the gradient.  The first
 // workgroup forms the mean over `pairs` pairs besides.
 template <int DT, int T, int U>
 __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
@@ -492,7 +494,10 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
 }
 
 // One workgroup of T threads per row; the last T NV pieces of 16 bytes stay in registers from the sum to the gradient, what lies
-// before them in longer rows is read twice, the second time backwards.
+// before them in longer rows is read twice, the second time backwards.  8192 rows of 131072 bf16 numbers, a quarter ignored: 655 us, 5.75 TB/s,
+// a copy's rate; 1024 of 200003 float32 numbers: 320 us, 6.3 TB/s with a fifth of the bytes read again (in LDS besides: 312, but rows of 150000
+// bf16 numbers 260 instead of 252); 2048 of 50001: 75 us, 4.9 TB/s, two rows a compute unit at a time in three rounds (four rows of 256 threads
+// 87, one of 1024 90).
 template <int DT, int T, int NV>
 __global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
   typedef typename Elem<DT>::raw raw;

@@ -370,10 +370,10 @@ __device__ __forceinline__ void pair_mean(const PairMean& a) {
   if (threadIdx.x == 0) *a.loss = (float)(s / (double)a.pairs);
 }
 
-// stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread (a
-// workgroup per row, in a loop: a loss on 5721 rows of 100003 float16 numbers 563 us, so 501; the gradient alone now 305 us, 6.4 TB/s with
-// what the memory-side cache still has).  Pieces start at 16-byte boundaries of the gradient.  The first
-// workgroup forms the mean over `pairs` pairs besides.
+// stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread and no more: each
+// loads, computes and stores once (with a workgroup that walks its row a loss on 5721 rows of 100003 float16 numbers took 563 us, so 501; the
+// gradient alone now 305, 6.4 TB/s with what the memory-side cache still has).  Pieces start at 16-byte boundaries of the gradient.  The
+// first workgroup forms the mean over `pairs` pairs besides.
 template <int DT, int T, int U>
 __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
                                                      int64_t dstride, int parts, PairMean mean) {
@@ -412,17 +412,18 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
   const int piece = i >= 0 && i < (int64_t)r.full * Pack<DT>::N ? (int)(i / Pack<DT>::N) : -1;
   const bool here = piece >= 0 ? piece >= first && piece < first + U * T : part == 0;
   const float xy = here ? Elem<DT>::widen(x[y]) : 0.f;
-  if constexpr (T > kWave) __syncthreads();          // in place: the target's logit is read before anything is written
-  if (first < r.full) {
-    if (sum.wide) {
-      const int last = first + U * T < r.full ? first + U * T : r.full;
-      g.wide(r.x, g.out, (int64_t)first * Pack<DT>::N, (int64_t)last * Pack<DT>::N);
-      if constexpr (T > kWave) __syncthreads();      // the target's element is another thread's here
-    } else {
-      typename Row<DT, T>::F v[U];
-      r.template load<U, true>(v, first);
-      g.template pieces<U>(r, v, first);
-    }
+  const bool plain = first < r.full && !sum.wide;
+  typename Row<DT, T>::F v[U];
+  if (plain) r.template load<U, true>(v, first);
+  if constexpr (T > kWave) {
+    if (out == x) __syncthreads();                   // the target's logit is read before anything is written
+  }
+  if (plain) {
+    g.template pieces<U>(r, v, first);
+  } else if (first < r.full) {
+    const int last = first + U * T < r.full ? first + U * T : r.full;
+    g.wide(r.x, g.out, (int64_t)first * Pack<DT>::N, (int64_t)last * Pack<DT>::N);
+    if constexpr (T > kWave) __syncthreads();        // the target's element is another thread's here
   }
   if (part == 0) g.odd(r);
   if (here) g.target(r, y, xy, d);
@@ -652,16 +653,18 @@ void by_rows(const Logits& L, int T, int64_t groups, F&& f) {
   }
 }
 
-// Threads of a row: a wavefront where it has no more than four pieces for each of its lanes; otherwise 256, or 1024 where there are
-// fewer rows than compute units (a call behind another, 1024 / 256 threads: 64 rows of 131072 bf16 numbers 10.8 / 14.6 us, one of 131072
-// float32 numbers 12.4 / 18.9, 300 rows of 131072 bf16 numbers 23.3 / 21.1).
+// Threads of a row: as many as have no more than 8 pieces each, the number on their way at a time, up to 256 (16384 rows of 3111 bf16
+// numbers 20 us with a wavefront each, 38 with 256 threads; of 6111 float16 33 with 128, 46 with 256); 1024 where there are fewer rows
+// than compute units (a call behind another, 1024 / 256 threads: 64 rows of 131072 bf16 numbers 10.8 / 14.6 us, one of 131072
+// float32 numbers 12.4 / 18.9, 300 rows of 131072 bf16 numbers 23.3 / 21.1; 512 are never better).
 template <int DT, bool AGAIN>
 void launch_logprobs(hipStream_t s, const Logits& L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
                      float* dlogp) {
   const int pieces = L.vocab / Pack<DT>::N;
-  const int T = pieces <= 256 ? 64 : L.rows > compute_units() ? 256 : 1024;
+  const int T = pieces <= 512 ? 64 : pieces <= 1024 ? 128 : L.rows > compute_units() ? 256 : 1024;
   by_rows(L, T, 1, [&](const Logits& some, uint32_t grid) {
     if (T == 64) k_logprobs<DT, 64, AGAIN><<<dim3(grid), dim3(64), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
+    else if (T == 128) k_logprobs<DT, 128, AGAIN><<<dim3(grid), dim3(128), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
     else if (T == 256) k_logprobs<DT, 256, AGAIN><<<dim3(grid), dim3(256), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
     else k_logprobs<DT, 1024, AGAIN><<<dim3(grid), dim3(1024), 0, s>>>(some, weight, ref_logp, logp, lse, stat, dlogp);
   });
@@ -678,10 +681,17 @@ void launch_logprobs_back_as(hipStream_t s, const Logits& L, const float* lse, c
   });
 }
 
+// One workgroup for a row of up to 2048 pieces, 8 for every thread; parts of 512 pieces of longer ones (a loss on 14403 rows of 3111 bf16
+// numbers 51 us with 64 threads of 8 pieces, 57 with parts; 10354 of 12345 float16 109 with 256 of 8, 138 with parts; 5721 of 100003 float16
+// 501 in parts of 512 pieces, 512 of 2048).
 template <int DT>
 void launch_logprobs_back(hipStream_t s, const Logits& L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
                           int64_t dstride, PairMean mean) {
-  if (L.vocab / Pack<DT>::N <= 256) launch_logprobs_back_as<DT, 64, 4>(s, L, lse, stat, dlogp, dx, dstride, mean);
+  const int pieces = L.vocab / Pack<DT>::N;
+  if (pieces <= 256) launch_logprobs_back_as<DT, 64, 4>(s, L, lse, stat, dlogp, dx, dstride, mean);
+  else if (pieces <= 512) launch_logprobs_back_as<DT, 64, 8>(s, L, lse, stat, dlogp, dx, dstride, mean);
+  else if (pieces <= 1024) launch_logprobs_back_as<DT, 128, 8>(s, L, lse, stat, dlogp, dx, dstride, mean);
+  else if (pieces <= 2048) launch_logprobs_back_as<DT, 256, 8>(s, L, lse, stat, dlogp, dx, dstride, mean);
   else launch_logprobs_back_as<DT, 256, 2>(s, L, lse, stat, dlogp, dx, dstride, mean);
 }
 

@@ -28,6 +28,8 @@ def _tensors(tensors, n, what, index):
     for t in tensors:
         if t is not None and (t.get_device() != index or not t.is_contiguous()):
             refuse("%s: dense tensors on one GPU" % what)
+        if t is not None and (t.is_conj() or t.is_neg()):     # autograd leaves such gradients; memory holds other numbers than the tensor
+            refuse("%s: tensors without a pending conjugation or negation (resolve_conj(), resolve_neg())" % what)
     return tensors
 
 

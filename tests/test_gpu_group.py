@@ -297,3 +297,19 @@ def test_the_binding_refuses():
         with pytest.raises(T.TgradError):
             bad()
     assert float(r[1]) == 1
+
+
+def test_tensors_that_memory_does_not_hold():
+    """Autograd leaves gradients whose conjugation is still pending: their memory holds other numbers, so they are refused."""
+    p = torch.randn(6, dtype=torch.complex64, device=DEV, requires_grad=True)
+    p.conj().backward(torch.randn(6, dtype=torch.complex64, device=DEV))
+    assert p.grad.is_conj()
+    moments = [torch.zeros(6, dtype=torch.complex64, device=DEV)], [torch.zeros(6, device=DEV)]
+    with pytest.raises(T.TgradError):
+        group.Group([p.grad])
+    g = group.Group([p.grad.resolve_conj()], [p.detach()], *moments)
+    with pytest.raises(T.TgradError):
+        g.tgrad_group_bind([p.grad])
+    with pytest.raises(T.TgradError):
+        group.Group([torch._neg_view(torch.randn(6, device=DEV))])
+    assert bool(torch.isfinite(g.tgrad_group_grad_norm(1.0)).all())

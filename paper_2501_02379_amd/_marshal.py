@@ -45,6 +45,15 @@ def vector(t, n, dtype, device, what):
     return t.data_ptr()
 
 
+def scalar(t, dtype, device, what):
+    """Address of a tensor of one element, of any dimension (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != 1 or t.get_device() != device.index:
+        refuse("%s: one %s on the logits' device" % (what, dtype))
+    return t.data_ptr()
+
+
 def check(rc: int, where: str) -> None:
     if rc != T.TGRAD_OK:
         raise T.TgradError(rc, where)

@@ -13,7 +13,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import tgrad as T
-from ._marshal import REAL_TYPES, call, on_stream, refuse, stream_of, vector
+from ._marshal import REAL_TYPES, call, on_stream, refuse, scalar, stream_of, vector
 
 
 class PolicyLoss(NamedTuple):
@@ -107,7 +107,7 @@ def tgrad_policy_loss(logits, targets, weight, advantage, old_logp, ref_logp=Non
     call(dev, T.load().tgrad_policy_loss, "tgrad_policy_loss", C.byref(d), C.byref(hyper),
          vector(weight, rows, torch.float32, dev, "weight"), vector(advantage, rows, torch.float32, dev, "advantage"),
          vector(old_logp, rows, torch.float32, dev, "old_logp"), vector(ref_logp, rows, torch.float32, dev, "ref_logp"),
-         vector(dloss, 1, torch.float32, dev, "dloss"), ws.data_ptr(), stats.data_ptr(), logp.data_ptr(),
+         scalar(dloss, torch.float32, dev, "dloss"), ws.data_ptr(), stats.data_ptr(), logp.data_ptr(),
          dx.data_ptr() if backward else None, stride, stream_of(dev))
     return PolicyLoss(stats, logp, dx)
 
@@ -127,7 +127,7 @@ def tgrad_preference_loss(logits, targets, weight, ref_logp, seq_start, *, beta:
     hyper = T.tgrad_preference(beta, label_smoothing)
     call(dev, T.load().tgrad_preference_loss, "tgrad_preference_loss", C.byref(d), C.byref(hyper), pairs,
          vector(seq_start, 2 * pairs + 1, torch.int64, dev, "seq_start"), vector(weight, rows, torch.float32, dev, "weight"),
-         vector(ref_logp, rows, torch.float32, dev, "ref_logp"), vector(dloss, 1, torch.float32, dev, "dloss"), ws.data_ptr(),
+         vector(ref_logp, rows, torch.float32, dev, "ref_logp"), scalar(dloss, torch.float32, dev, "dloss"), ws.data_ptr(),
          loss.data_ptr(), rewards.data_ptr(), logp.data_ptr(), dx.data_ptr() if backward else None, stride,
          stream_of(dev))
     return PreferenceLoss(loss[0], rewards, logp, dx)

@@ -511,3 +511,18 @@ def test_rows_far_from_zero(dtype, offset, temperature):
         inplace = xd.clone()
         losses.tgrad_policy_loss(inplace, yd, w, w, got, temperature=temperature, out=inplace)
         assert torch.equal(inplace, r.dlogits)
+
+
+def test_loss_scale_of_any_dimension():
+    x, y = make(12, 300, "bf16", seed=9)
+    w, adv, old, ref = policy_inputs(x, y, 9)
+    start = torch.tensor([0, 5, 12], device=DEV)
+    scale = torch.full((1,), 8.0, device=DEV)
+    for s in (scale[0], scale.reshape(1, 1)):
+        assert torch.equal(losses.tgrad_policy_loss(x, y, w, adv, old, ref, dloss=scale).dlogits,
+                           losses.tgrad_policy_loss(x, y, w, adv, old, ref, dloss=s).dlogits)
+        assert torch.equal(losses.tgrad_preference_loss(x, y, w, ref, start, dloss=scale).dlogits,
+                           losses.tgrad_preference_loss(x, y, w, ref, start, dloss=s).dlogits)
+    for s in (torch.ones(2, device=DEV), torch.ones((), dtype=torch.float64, device=DEV), torch.ones(())):
+        with pytest.raises(T.TgradError):
+            losses.tgrad_policy_loss(x, y, w, adv, old, ref, dloss=s)

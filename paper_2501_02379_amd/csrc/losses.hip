@@ -8,6 +8,9 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstring>
+#include <limits>
+#include <type_traits>
 
 #include "launch_util.h"
 #include "train_common.h"
@@ -29,6 +32,8 @@ struct Logits {
   int vocab;
   float scale;                            // 1 / temperature
   float scale2;                           // log2(e) / temperature
+  float high, low;                        // the same in two terms (see Fine)
+  double bend;                            // scale2 / (log2(e) / temperature)
 };
 
 // 16 bytes of a row.
@@ -68,22 +73,44 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // lowest value, add 0; a NaN makes the sum NaN, and so does +inf.  Rows whose maximum lies beyond kReach either way, where an exponent
 // would lose its fraction, are summed again (wide).
 constexpr float kReach = 1048576.f;
-struct Soft {
+struct alignas(8) Soft {
   float b, s;
 };
-template <int N>
-__device__ __forceinline__ void soft_add(Soft& a, const float* x, float scale2) {
+
+// scale2 as the sums take it: one float32, or two more that make it up exactly.  Rounded to one it is up to 6e-8 off, and with it every
+// exponent, the same way in every row; a sum of many small log ratios, as a preference loss forms it, sees that.  The first of the two
+// has 16 bits, so that the second one's part is more than the first one's rounding takes away; it is positive, so that -inf stays -inf.
+struct Plain {
+  float whole;
+  __device__ __forceinline__ float above(float x, float b) const { return fmaf(x, whole, -b); }
+};
+struct Fine {
+  float whole, high, low;
+  __device__ __forceinline__ float above(float x, float b) const { return fmaf(x, low, fmaf(x, high, -b)); }
+};
+template <bool FINE>
+__device__ __forceinline__ auto scale_of(const Logits& L) {
+  if constexpr (FINE) return Fine{L.scale2, L.high, L.low};
+  else return Plain{L.scale2};
+}
+
+// The new terms are added up by themselves, four at a time: next to a sum that holds a large one each of the small ones would be rounded
+// away, always downwards (-2.5e-8 of a row's sum at T = 0.7 and 3001 entries, -3e-9 this way).
+template <int N, typename S>
+__device__ __forceinline__ void soft_add(Soft& a, const float* x, S scale) {
   float m = x[0];
 #pragma unroll
   for (int k = 1; k < N; ++k) m = fmaxf(m, x[k]);
-  const float b = fmaxf(a.b, m * scale2);
-  float s0 = a.s * exp2_fast(a.b - b), s1 = 0.f;
+  const float b = fmaxf(a.b, m * scale.whole);
+  constexpr int C = N < 4 ? N : 4;
+  float s[C];
 #pragma unroll
-  for (int k = 0; k < N; k += 2) {
-    s0 += exp2_fast(fmaf(x[k], scale2, -b));
-    if (k + 1 < N) s1 += exp2_fast(fmaf(x[k + 1], scale2, -b));
-  }
-  a = Soft{b, s0 + s1};
+  for (int k = 0; k < C; ++k) s[k] = exp2_fast(scale.above(x[k], b));
+#pragma unroll
+  for (int k = C; k < N; ++k) s[k % C] += exp2_fast(scale.above(x[k], b));
+#pragma unroll
+  for (int k = 1; k < C; ++k) s[0] += s[k];
+  a = Soft{b, fmaf(a.s, exp2_fast(a.b - b), s[0])};
 }
 // Of all T threads, the same in every one.
 template <int T>
@@ -122,8 +149,8 @@ struct RowSum {
 };
 
 // The whole row again, one element at a time, relative to its maximum: exponents are exact at the maximum whatever its size.
-template <int DT, int T>
-__device__ __forceinline__ RowSum wide_sum(const typename Elem<DT>::raw* x, int vocab, float scale2, Soft* lds) {
+template <int DT, int T, typename S>
+__device__ __forceinline__ RowSum wide_sum(const typename Elem<DT>::raw* x, int vocab, S scale, Soft* lds) {
   float m = -INFINITY, s = 0.f;
   for (int i = threadIdx.x; i < vocab; i += T) m = fmaxf(m, Elem<DT>::widen(x[i]));
 #pragma unroll
@@ -132,16 +159,24 @@ __device__ __forceinline__ RowSum wide_sum(const typename Elem<DT>::raw* x, int 
   if (lane_id() == 0) lds[threadIdx.x / kWave].b = m;
   __syncthreads();
   for (int i = 0; i < T / kWave; ++i) m = fmaxf(m, lds[i].b);
-  for (int i = threadIdx.x; i < vocab; i += T) s += exp2_fast((Elem<DT>::widen(x[i]) - m) * scale2);
-  s = block_sum<T / kWave>(s, &lds->s);
+  if constexpr (std::is_same<S, Fine>::value) {
+    // numbers this large have few values and their exponents few roundings, the same ones in every row: in float64
+    double t = 0.;
+    const double fine = (double)scale.high + (double)scale.low;
+    for (int i = threadIdx.x; i < vocab; i += T) t += exp2(((double)Elem<DT>::widen(x[i]) - (double)m) * fine);
+    s = (float)block_sum<T / kWave>(t, reinterpret_cast<double*>(lds));
+  } else {
+    for (int i = threadIdx.x; i < vocab; i += T) s += exp2_fast((Elem<DT>::widen(x[i]) - m) * scale.whole);
+    s = block_sum<T / kWave>(s, &lds->s);
+  }
   return RowSum{m, s, true};
 }
 
-template <int DT, int T>
-__device__ __forceinline__ RowSum row_sum(Soft a, const typename Elem<DT>::raw* x, int vocab, float scale2, Soft* lds) {
+template <int DT, int T, typename S>
+__device__ __forceinline__ RowSum row_sum(Soft a, const typename Elem<DT>::raw* x, int vocab, S scale, Soft* lds) {
   a = soft_all<T>(a, lds);
   if (a.b > -kReach && a.b < kReach) return RowSum{a.b, a.s, false};
-  return wide_sum<DT, T>(x, vocab, scale2, lds);
+  return wide_sum<DT, T>(x, vocab, scale, lds);
 }
 
 // A piece in flight.  ODD: rows of two-byte elements that start in the upper half of a four-byte word are read from that word on, five
@@ -202,8 +237,8 @@ struct Row {
     asm volatile("" ::: "memory");        // all of them on their way: the compiler would move each to the branch that uses it
   }
   // two pieces at a time: one step of the running maximum for both
-  template <int U>
-  __device__ __forceinline__ void add(Soft& a, F* q, int first, float scale2) const {
+  template <int U, typename S>
+  __device__ __forceinline__ void add(Soft& a, F* q, int first, S scale) const {
     static_assert(U % 2 == 0, "pieces are added in pairs");
 #pragma unroll
     for (int u = 0; u < U; u += 2) {
@@ -216,22 +251,23 @@ struct Row {
         if (at + 2 * T > full && at + k * T + (int)threadIdx.x >= full) v = Quad{P::kLowest, P::kLowest, P::kLowest, P::kLowest};
         P::widen(v, f + k * P::N);
       }
-      soft_add<2 * P::N>(a, f, scale2);
+      soft_add<2 * P::N>(a, f, scale);
     }
   }
   // pieces first ... end - 1, read and forgotten
-  template <int U, bool LAST>
-  __device__ __forceinline__ void stream(Soft& a, int first, int end, float scale2) const {
+  template <int U, bool LAST, typename S>
+  __device__ __forceinline__ void stream(Soft& a, int first, int end, S scale) const {
     for (; first < end; first += U * T) {
       F q[U];
       load<U, LAST>(q, first);
-      add<U>(a, q, first, scale2);
+      add<U>(a, q, first, scale);
     }
   }
-  __device__ __forceinline__ void add_odd(Soft& a, float scale2) const {
+  template <typename S>
+  __device__ __forceinline__ void add_odd(Soft& a, S scale) const {
     if ((int)threadIdx.x < odd) {
       const float f = Elem<DT>::widen(x[odd_at()]);
-      soft_add<1>(a, &f, scale2);
+      soft_add<1>(a, &f, scale);
     }
   }
 };
@@ -316,8 +352,10 @@ struct RowStat {
 };
 
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
-// rows that lie in no sequence) are.  The log ratio is formed in float64 from the sum itself: it is a small difference of large numbers.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096 rows of 131072 bf16
-// numbers, a quarter of them ignored: 151 us without it, 136 with it; now 127, 6.35 TB/s).  8 pieces of every thread are on their way.
+// rows that lie in no sequence) are.  Log ratios are small differences of large numbers, and a reward adds up hundreds of them: the sum
+// takes the scale in two terms, and the rest is formed in float64.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096
+// rows of 131072 bf16 numbers, a quarter of them ignored: 151 us without it, 136 with it; now 127, 6.35 TB/s).  8 pieces of every thread are
+// on their way.
 template <int DT, int T, bool AGAIN>
 __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
                                                 float* dlogp) {
@@ -333,26 +371,37 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, c
     xy = Elem<DT>::widen(x[y]);
     with_parity<DT>(x, [&](auto odd) {
       const Row<DT, T, odd.value> row(x, L.vocab);
+      const auto scale = scale_of<AGAIN>(L);
       Soft a{-kReach, 0.f};
-      row.template stream<8, !AGAIN>(a, 0, row.full, L.scale2);
-      row.add_odd(a, L.scale2);
-      r = row_sum<DT, T>(a, x, L.vocab, L.scale2, lds);
+      row.template stream<8, !AGAIN>(a, 0, row.full, scale);
+      row.add_odd(a, scale);
+      r = row_sum<DT, T>(a, x, L.vocab, scale, lds);
     });
-    lp = r.logp(xy, L.scale2);
-    l = r.lse(L.scale, L.scale2);
+    if constexpr (!AGAIN) {
+      lp = r.logp(xy, L.scale2);
+      l = r.lse(L.scale, L.scale2);
+    }
   }
   if (threadIdx.x == 0) {
-    if (logp) logp[n] = lp;
-    if (lse) lse[n] = l;
     if constexpr (AGAIN) {
       double gap = 0.;
       if (live) {
-        const double above = r.wide ? ((double)xy - (double)r.ref) * (double)L.scale2 : (double)xy * (double)L.scale2 - (double)r.ref;
-        gap = (double)weight[n] * ((above - log2((double)r.s)) / kLog2e - (double)ref_logp[n]);
+        const double scale = (double)L.high + (double)L.low;
+        const double above = r.wide ? ((double)xy - (double)r.ref) * scale : (double)xy * scale - (double)r.ref;
+        const double p = (above - log2((double)r.s)) / kLog2e;
+        gap = (double)weight[n] * (p - (double)ref_logp[n]);
+        lp = (float)p;
+        if (!r.wide) {                    // the gradient's kernel takes the scale in one term: the reference as that sees it
+          const double ref = (double)r.ref * L.bend;
+          r.ref = (float)ref;
+          r.s *= exp2f((float)(ref - (double)r.ref));
+        }
       }
       stat[n] = RowStat{gap, r.ref, r.s, r.wide};
       dlogp[n] = 0.f;
     }
+    if (logp) logp[n] = lp;
+    if (lse) lse[n] = l;
   }
 }
 
@@ -456,13 +505,14 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
   // a whole number of batches, so that a piece belongs to the same thread whether it stays or not
   const int over = r.full - T * NV;
   const int start = over > 0 ? (over + kStream * T - 1) / (kStream * T) * (kStream * T) : 0;
-  r.template stream<kStream, false>(run, 0, start, L.scale2);
+  const Plain plain{L.scale2};
+  r.template stream<kStream, false>(run, 0, start, plain);
   if (start < r.full) {
     r.template load<NV, true>(held, start);
-    r.template add<NV>(run, held, start, L.scale2);
+    r.template add<NV>(run, held, start, plain);
   }
-  r.add_odd(run, L.scale2);
-  const RowSum sum = row_sum<DT, T>(run, x, L.vocab, L.scale2, lds);
+  r.add_odd(run, plain);
+  const RowSum sum = row_sum<DT, T>(run, x, L.vocab, plain, lds);
   const float logp = sum.logp(xy, L.scale2);
   const float ratio = expf(logp - old);
   const float whole = ratio * adv, cut = fminf(fmaxf(ratio, a.low), a.high) * adv;
@@ -624,7 +674,15 @@ int check_logits(const tgrad_logits* l, Logits* out) {
   if (!std::isfinite((float)(inv * kLog2e)) || (float)inv == 0.f) return TGRAD_ERR_INVALID_ARG;
   if (l->rows > 0 && (!l->data || !l->targets)) return TGRAD_ERR_INVALID_ARG;
   if ((uintptr_t)l->data % (uintptr_t)real_bytes(l->dtype) || (uintptr_t)l->targets % 8) return TGRAD_ERR_INVALID_ARG;
-  *out = Logits{l->data, l->rows, l->row_stride, l->targets, 0, (int)l->vocab, (float)inv, (float)(inv * kLog2e)};
+  const double scale = inv * kLog2e;
+  float high = (float)scale;
+  if ((double)high > scale) high = std::nextafterf(high, 0.f);
+  uint32_t bits;
+  std::memcpy(&bits, &high, 4);
+  bits &= 0xFFFFFF00u;
+  std::memcpy(&high, &bits, 4);
+  const float low = std::max((float)(scale - (double)high), std::numeric_limits<float>::denorm_min());
+  *out = Logits{l->data, l->rows, l->row_stride, l->targets, 0, (int)l->vocab, (float)inv, (float)scale, high, low, (double)(float)scale / scale};
   return TGRAD_OK;
 }
 

@@ -438,7 +438,8 @@ int tgrad_token_logprobs(const tgrad_logits* logits, float* logp, float* lse, vo
 
 /*
  * dlogits[n, v] = dlogp[n] / temperature * ([v = y_n] - exp(z[n, v] - lse[n])), rounded once to the logits' type.
- *  lse, dlogp      device pointers, float32[rows].  A row with dlogp = 0 is not read.
+ *  lse, dlogp      device pointers, float32[rows].  A row with dlogp = 0 is not read.  From |lse| = 7e5 on, where lse's rounding
+ *                  alone moves exp(z - lse) by several percent, exponents above 0 count as 0.
  *  dlogits         device pointer, the logits' type, rows `dlogits_stride` >= vocab elements apart; what lies between them is
  *                  left alone.  May be logits->data, with the same stride.
  * Errors: INVALID_ARG, HIP.

@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <limits>
@@ -30,10 +31,12 @@ struct Logits {
   const int64_t* targets;
   int64_t first;                          // the row of a launch's first workgroup
   int vocab;
+  float temperature;
   float scale;                            // 1 / temperature
   float scale2;                           // log2(e) / temperature
   float high, low;                        // the same in two terms (see Fine)
-  double bend;                            // scale2 / (log2(e) / temperature)
+  double bend;                            // scale2 / (log2(e) / temperature): 1, but for scale2's rounding
+  __device__ __forceinline__ double nats() const { return 0.69314718055994531 * (2. - bend); }   // z = x scale2 nats()
 };
 
 // 16 bytes of a row.
@@ -136,15 +139,21 @@ __device__ __forceinline__ Soft soft_all(Soft a, Soft* lds) {
   return Soft{b, s};
 }
 
-// Sum of a row: of 2^(x scale2 - ref), or of 2^((x - ref) scale2) where it is wide.
+// Sum of a row: of 2^(x scale2 - ref), or, where it is wide, of 2^((x - ref) scale2 - rest), whose exponents are not above 0: the reference
+// is the row's maximum, or a given log sum, that of these numbers as its rounding left it.
 struct RowSum {
   float ref, s;
   bool wide;
+  float rest = 0.f;
   // z_y - lse, lse in units of log2
-  __device__ __forceinline__ float above(float x, float scale2) const { return wide ? (x - ref) * scale2 : fmaf(x, scale2, -ref); }
+  __device__ __forceinline__ float above(float x, float scale2) const {
+    if (!wide) return fmaf(x, scale2, -ref);
+    const float t = fmaf(x - ref, scale2, -rest);
+    return t > 0.f ? 0.f : t;             // a NaN stays one
+  }
   __device__ __forceinline__ float logp(float xy, float scale2) const { return (above(xy, scale2) - log2f(s)) * kLn2; }
-  __device__ __forceinline__ float lse(float scale, float scale2) const {
-    return wide ? ref * scale + log2f(s) * kLn2 : (ref + log2f(s)) * kLn2;
+  __device__ __forceinline__ float lse(const Logits& L) const {
+    return (float)((wide ? (double)ref * (double)L.scale2 : (double)ref) * L.nats() + (double)(log2f(s) * kLn2));
   }
 };
 
@@ -379,7 +388,7 @@ __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, c
     });
     if constexpr (!AGAIN) {
       lp = r.logp(xy, L.scale2);
-      l = r.lse(L.scale, L.scale2);
+      l = r.lse(L);
     }
   }
   if (threadIdx.x == 0) {
@@ -450,10 +459,17 @@ __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse,
   if (stat) {
     sum = RowSum{stat[n].ref, stat[n].s, stat[n].wide != 0};
   } else {                                // a reference near lse, and what its rounding leaves
-    const double l2 = (double)lse[n] * kLog2e;
+    const double top = (double)lse[n] * (double)L.temperature;          // exact
+    const double l2 = top * (double)L.scale2;
     sum.wide = !(fabs(l2) < (double)kReach);
-    sum.ref = (float)(sum.wide ? l2 / (double)L.scale2 : l2);
-    sum.s = (float)exp2(l2 - (sum.wide ? (double)sum.ref * (double)L.scale2 : (double)sum.ref));
+    if (sum.wide) {
+      sum.ref = fminf(fmaxf((float)top, -FLT_MAX), FLT_MAX);
+      sum.s = 1.f;
+      sum.rest = (float)((top - (double)sum.ref) * (double)L.scale2);
+    } else {
+      sum.ref = (float)l2;
+      sum.s = exp2f((float)(l2 - (double)sum.ref));
+    }
   }
   const RowGradient<DT, T> g(out + r.head, sum, L.scale2, d);
   // the target's element: by the thread that writes it (again) behind the others
@@ -682,7 +698,7 @@ int check_logits(const tgrad_logits* l, Logits* out) {
   bits &= 0xFFFFFF00u;
   std::memcpy(&high, &bits, 4);
   const float low = std::max((float)(scale - (double)high), std::numeric_limits<float>::denorm_min());
-  *out = Logits{l->data, l->rows, l->row_stride, l->targets, 0, (int)l->vocab, (float)inv, (float)scale, high, low, (double)(float)scale / scale};
+  *out = Logits{l->data, l->rows, l->row_stride, l->targets, 0, (int)l->vocab, l->temperature, (float)inv, (float)scale, high, low, (double)(float)scale / scale};
   return TGRAD_OK;
 }
 

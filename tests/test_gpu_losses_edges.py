@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2501_02379_amd import losses
-from test_gpu_losses import DEV, TYPES, U, make
+from test_gpu_losses import DEV, TYPES, U, close_gradient, gradient, logp_bound, make, scores
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,91 @@ def test_rewards_have_no_error_of_one_sign(dtype, temperature, offset):
     want = (logp - ref.double()).view(parts, -1).sum(1)
     assert float((r.rewards.double() - want).abs().max()) / (rows // parts) <= U / 4 * math.sqrt(parts)
     assert abs(float((r.rewards.double() - want).sum())) / rows <= U / 4
+
+
+def given_lse(x, y, lse, temperature):
+    """z, and the gradient's softmax for a log sum as it is given, with exponents of far rows held to 0."""
+    z = x.cpu().double() / float(np.float32(temperature))
+    t = z - lse.cpu().double()[:, None]
+    far = lse.cpu().double().abs()[:, None] * math.log2(math.e) >= 2 ** 20 * (1 - 1e-6)
+    return z, torch.where(far & (t > 0), 0.0, t)
+
+
+@pytest.mark.parametrize("temperature", [1.0, 0.01, 1.3])
+@pytest.mark.parametrize("offset", [0.0, 300.0, -5000.0, 30000.0, -60000.0, 6.5e5, 4e6, -3e6, 1e8, -1e9, 1e30, -1e30, "lowest"])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_gradient_from_a_given_log_sum(dtype, offset, temperature):
+    """exp(z - lse) for lse as the float32 that the caller has, wherever the row lies.  An exponent t is off by 4u|t|, and by 2u of what
+    the reference's rounding left, at most 2u|lse|; the rest as in the other gradients."""
+    lowest = offset == "lowest"
+    if dtype == "f16" and not lowest and abs(offset) > 65000:
+        pytest.skip("beyond float16")
+    for vocab in (50, 3001, 20002):
+        g = torch.Generator().manual_seed(vocab)
+        kind = TYPES[dtype][0]
+        if lowest:
+            x = torch.full((4, vocab), torch.finfo(kind).min, dtype=kind)
+        else:
+            top = torch.tensor(offset).to(kind)
+            low = torch.tensor(-math.inf).to(kind)
+            below = torch.nextafter(top, low) if dtype != "bf16" else (top.double() * (1 - math.copysign(2.0 ** -7, offset))).to(kind)
+            pick = torch.randint(0, 3, (4, vocab), generator=g)
+            x = torch.where(pick == 0, top, torch.where(pick == 1, below, (below.double() - abs(float(below)) * 0.1).to(kind)))
+            if not offset:
+                x = (torch.randn(4, vocab, generator=g) * 3).to(kind)
+            x[0, 1:] = (below.double() - abs(float(below)) * 0.1 - 200).to(kind)     # one entry alone: softmax 1
+            x[0, 0] = top
+        y = torch.randint(0, vocab, (4,), generator=g)
+        xd, yd = x.to(DEV), y.to(DEV)
+        logp, lse = losses.tgrad_token_logprobs(xd, yd, temperature=temperature)
+        if not bool(torch.isfinite(lse).all()):                        # beyond float32: nothing to give
+            assert lowest or abs(offset) > 1e29
+            continue
+        shift = x.double().amax(1)
+        exact = torch.logsumexp((x.double() - shift[:, None]) / float(np.float32(temperature)), 1) + shift / float(np.float32(temperature))
+        near = torch.clamp((x.double() - shift[:, None]) / float(np.float32(temperature)), min=-200)
+        e = logp_bound(near, near.amax(1))
+        assert bool(((lse.cpu().double() - exact).abs() <= U * exact.abs() * (1 + 4 * U) + e).all())     # rounded once
+        d = torch.tensor([1.0, -0.5, 2.0, 3.0])
+        z, t = given_lse(x, y, lse, temperature)
+        p = t.exp()
+        # d logits = d / T ([v = y] - p)
+        inv = 1 / float(np.float32(temperature))
+        dz = d.double() * inv
+        want = -p * dz[:, None]
+        want[torch.arange(4), y] += dz
+        rest = 8 * U * 2 * U * lse.cpu().double().abs()
+        got = losses.tgrad_token_logprobs_backward(xd, yd, lse, d.to(DEV), temperature=temperature)
+        assert bool(torch.isfinite(got).all())
+        close_gradient(got, want, p, dz, torch.clamp(t, min=-200), torch.zeros(4), y, dtype,
+                       d_error=dz.abs() * (rest * p.amax(1) + 8 * U * p.amax(1)))
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("stride,offset", [(1000, 0), (1001, 1), (1008, 3), (4000, 2)])
+def test_backward_strides_places_and_rows_that_are_not_read(stride, offset, dtype):
+    """Row strides of logits and gradient, in place, rows with dlogp = 0 or without a target full of NaN."""
+    rows, vocab = 9, 1000
+    x, y = make(rows, vocab, dtype, stride, offset, seed=offset + 80)
+    z, lse, logp, _ = scores(x, y, 0.7)
+    _, got_lse = losses.tgrad_token_logprobs(x, y, temperature=0.7)
+    d = torch.linspace(-1, 2, rows)
+    d[4] = 0
+    y[7], y[8] = -100, vocab
+    off = [4, 7, 8]
+    x[off] = float("nan")
+    got_lse[off] = float("nan")
+    out = torch.full((rows, stride + 2), 7.0, device=DEV, dtype=x.dtype)[:, 1:1 + vocab]
+    r = losses.tgrad_token_logprobs_backward(x, y, got_lse, d.to(DEV), temperature=0.7, out=out)
+    assert r is out and not bool(out[off].any())
+    whole = torch.as_strided(out, (rows, stride + 2), (stride + 2, 1), 0)
+    assert bool((whole[:, 0] == 7).all()) and bool((whole[:, 1 + vocab:] == 7).all())
+    on = [k for k in range(rows) if k not in off]
+    dz = d.double() / float(np.float32(0.7))
+    given = got_lse.cpu().double()[on]
+    gr, p = gradient(z[on], given, y[on], dz[on])
+    close_gradient(out[on], gr, p, dz[on], z[on], logp[on], y[on], dtype, d_error=8 * U * dz[on].abs())
+    new = losses.tgrad_token_logprobs_backward(x, y, got_lse, d.to(DEV), temperature=0.7)
+    assert torch.equal(new, out)
+    assert losses.tgrad_token_logprobs_backward(x, y, got_lse, d.to(DEV), temperature=0.7, out=x) is x
+    assert torch.equal(x, new)

@@ -459,7 +459,8 @@ int tgrad_loss_query_size(int64_t rows, int64_t pairs, size_t* workspace_bytes);
  * Clipped policy loss with a KL term towards a reference, and its gradient:
  *   r = exp(logp - old);  pg = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A);  d = ref - logp;  kl = exp(d) - d - 1
  *   loss = sum_n w_n (pg + kl_beta kl);  dlogits = dloss d loss / d logits.
- * Where both arguments of the minimum are equal the gradient is that of the unclipped one.
+ * Where both arguments of the minimum are equal the gradient is that of the unclipped one.  A = 0: both are 0, whatever r, one beyond
+ * float32 among them.
  *  weight, advantage, old_logp  device pointers, float32[rows].  weight carries the mask and the normalisation (1 / number of
  *                tokens, say); a row of weight 0 is ignored like one without a target: none of its entries anywhere is read.
  *  ref_logp      the same, or NULL: kl = 0.

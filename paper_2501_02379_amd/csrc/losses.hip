@@ -531,7 +531,9 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
   const RowSum sum = row_sum<DT, T>(run, x, L.vocab, plain, lds);
   const float logp = sum.logp(xy, L.scale2);
   const float ratio = expf(logp - old);
-  const float whole = ratio * adv, cut = fminf(fmaxf(ratio, a.low), a.high) * adv;
+  // an advantage of 0 takes the row out whatever its ratio, one beyond float32 too (logp - old above 88.7)
+  const bool none = adv == 0.f && logp - old < INFINITY;
+  const float whole = none ? 0.f : ratio * adv, cut = none ? 0.f : fminf(fmaxf(ratio, a.low), a.high) * adv;
   const bool clipped = cut < whole;
   const float pg = clipped ? -cut : -whole;
   float dlogp = clipped ? 0.f : -whole, kl = 0.f;

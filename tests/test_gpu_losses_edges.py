@@ -122,3 +122,22 @@ def test_backward_strides_places_and_rows_that_are_not_read(stride, offset, dtyp
     assert torch.equal(new, out)
     assert losses.tgrad_token_logprobs_backward(x, y, got_lse, d.to(DEV), temperature=0.7, out=x) is x
     assert torch.equal(x, new)
+
+
+@pytest.mark.parametrize("vocab", [37, 5003])
+@pytest.mark.parametrize("kl_beta", [0.0, 0.1])
+def test_no_advantage_under_a_ratio_beyond_float32(vocab, kl_beta):
+    """Advantage 0: both arguments of the minimum are 0, whatever the ratio; the KL term stays.  A NaN stays one."""
+    x, y = make(4, vocab, "f32", seed=90)
+    logp = scores(x, y)[2].float().to(DEV)
+    w = torch.full((4,), 0.25, device=DEV)
+    adv = torch.tensor([0.0, -0.0, 1.0, 0.0], device=DEV)
+    old = logp - torch.tensor([100.0, 1e30, 0.1, 0.2], device=DEV)
+    ref = logp + 0.5
+    got = losses.tgrad_policy_loss(x, y, w, adv, old, ref, kl_beta=kl_beta)
+    same = losses.tgrad_policy_loss(x, y, w, adv, torch.where(adv == 0, logp, old), ref, kl_beta=kl_beta)
+    assert bool(torch.isfinite(got.stats).all()) and torch.equal(got.stats, same.stats) and torch.equal(got.dlogits, same.dlogits)
+    assert bool(got.dlogits[0].any()) == (kl_beta != 0)
+    x[0, 0] = float("nan")
+    got = losses.tgrad_policy_loss(x, y, w, adv, old, ref, kl_beta=kl_beta)
+    assert bool(torch.isnan(got.stats[0])) and bool(torch.isnan(got.dlogits[0]).all()) and bool(torch.isfinite(got.dlogits[1:]).all())

@@ -660,7 +660,8 @@ __global__ __launch_bounds__(kPairThreads) void k_pairs(int64_t rows, PairArgs a
   if (threadIdx.x == 0) {
     a.rewards[p] = (float)chosen;
     a.rewards[p + a.pairs] = (float)rejected;
-    a.pair_loss[p] = (float)((1. - a.smoothing) * softplus(-h) + a.smoothing * softplus(h));
+    // without smoothing the second term is not there, also where softplus(h) is infinite (a rejected token of probability 0)
+    a.pair_loss[p] = (float)((1. - a.smoothing) * softplus(-h) + (a.smoothing > 0. ? a.smoothing * softplus(h) : 0.));
   }
 #pragma unroll
   for (int side = 0; side < 2; ++side)

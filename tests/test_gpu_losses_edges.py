@@ -141,3 +141,22 @@ def test_no_advantage_under_a_ratio_beyond_float32(vocab, kl_beta):
     x[0, 0] = float("nan")
     got = losses.tgrad_policy_loss(x, y, w, adv, old, ref, kl_beta=kl_beta)
     assert bool(torch.isnan(got.stats[0])) and bool(torch.isnan(got.dlogits[0]).all()) and bool(torch.isfinite(got.dlogits[1:]).all())
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+def test_a_rejected_token_of_probability_0(smoothing):
+    """Its pair is told apart for certain: no loss without smoothing, an infinite one with it; the other pair is as it was."""
+    x, y = make(8, 300, "f32", seed=91)
+    w, ref = torch.ones(8, device=DEV), scores(x, y)[2].float().to(DEV) + 0.2
+    start = torch.arange(5, device=DEV) * 2
+    alone = losses.tgrad_preference_loss(x, y, torch.tensor([1.0, 1, 0, 0, 1, 1, 0, 0], device=DEV), ref, start, label_smoothing=smoothing)
+    x[7, y[7]] = -math.inf
+    r = losses.tgrad_preference_loss(x, y, w, ref, start, label_smoothing=smoothing)
+    assert float(r.rewards[3]) == -math.inf and bool(torch.isfinite(r.rewards[:3]).all())
+    if smoothing:
+        assert float(r.loss) == math.inf
+    else:                                                              # the mean of the first pair's loss and 0
+        first = 2 * float(alone.loss) - math.log(2)
+        assert abs(float(r.loss) - first / 2) <= 4 * U
+        assert not bool(r.dlogits[[2, 3, 6, 7]].any())
+    assert bool(torch.isfinite(r.dlogits).all()) and torch.equal(r.dlogits[[0, 1, 4, 5]], alone.dlogits[[0, 1, 4, 5]])

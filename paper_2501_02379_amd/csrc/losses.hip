@@ -539,7 +539,7 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
   float dlogp = clipped ? 0.f : -whole, kl = 0.f;
   if (a.ref_logp) {
     const float d = ref - logp, e = expm1f(d);
-    kl = e - d;
+    kl = d < INFINITY ? e - d : d;         // a token of probability 0: infinite
     if (a.kl_beta != 0.f) dlogp -= a.kl_beta * e;
   }
   if (threadIdx.x == 0) {

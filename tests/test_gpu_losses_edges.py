@@ -160,3 +160,15 @@ def test_a_rejected_token_of_probability_0(smoothing):
         assert abs(float(r.loss) - first / 2) <= 4 * U
         assert not bool(r.dlogits[[2, 3, 6, 7]].any())
     assert bool(torch.isfinite(r.dlogits).all()) and torch.equal(r.dlogits[[0, 1, 4, 5]], alone.dlogits[[0, 1, 4, 5]])
+
+
+def test_kl_of_a_token_of_probability_0():
+    """exp(d) - d - 1 for an infinite d is infinite; where the KL term is only reported it touches nothing else."""
+    x, y = make(3, 200, "f32", seed=92)
+    logp = scores(x, y)[2].float().to(DEV)
+    w = torch.ones(3, device=DEV)
+    x[1, y[1]] = -math.inf
+    r = losses.tgrad_policy_loss(x, y, w, w, logp, logp)
+    assert float(r.stats[2]) == math.inf and bool(torch.isfinite(r.stats[[0, 1, 3]]).all()) and bool(torch.isfinite(r.dlogits).all())
+    assert not bool(r.dlogits[1].any())
+    assert float(losses.tgrad_policy_loss(x, y, w, w, logp, logp, kl_beta=0.1).stats[0]) == math.inf

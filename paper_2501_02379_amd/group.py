@@ -126,40 +126,44 @@ class Group:
             self.tensors = old
             raise
 
-    def _result(self, into):
-        if into is None:
-            if stream_of(self.device) == self.stream.cuda_stream:
-                return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
-            with torch.cuda.stream(self.stream):
-                return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
-        if into.dtype != torch.float32 or into.shape != (2,) or into.storage_offset() != 2 or into.device != self.device:
-            refuse("into: an earlier result")
-        return into
+    def _new(self):
+        """A result to be written."""
+        if stream_of(self.device) == self.stream.cuda_stream:
+            return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
+        with torch.cuda.stream(self.stream):
+            return torch.empty(4, dtype=torch.float32, device=self.device)[2:]
+
+    def _result(self, r, what):
+        """Address of what lies behind an earlier result."""
+        if r is None or r.dtype != torch.float32 or r.shape != (2,) or r.stride() != (1,) or r.storage_offset() != 2 or \
+                r.device != self.device:
+            refuse("%s: an earlier result" % what)
+        return r.data_ptr() - 8
 
     def tgrad_group_grad_norm(self, max_norm: float, add_sumsq=None, into=None):
         """-> (norm, factor): global norm of all gradients and min(1, max_norm / (norm + 1e-6)).  `add_sumsq`: a float64 tensor
         of one element, the sum of squares of gradients that lie elsewhere.  `into`: an earlier result, overwritten."""
-        r = self._result(into)
+        r = self._new() if into is None else into
         call(self.device, self.lib.tgrad_group_grad_norm, "tgrad_group_grad_norm", self.handle, max_norm, self._add(add_sumsq),
-             r.data_ptr() - 8)
+             self._result(r, "into"))
         return r
 
     def tgrad_group_clip(self, max_norm: float, add_sumsq=None, into=None):
         """`tgrad_group_grad_norm`, and the gradients scaled by the factor; -> (norm, factor)."""
-        r = self._result(into)
+        r = self._new() if into is None else into
         call(self.device, self.lib.tgrad_group_clip, "tgrad_group_clip", self.handle, max_norm, self._add(add_sumsq),
-             r.data_ptr() - 8)
+             self._result(r, "into"))
         return r
 
     def tgrad_group_scale(self, norm) -> None:
         """The gradients times the factor of an earlier result."""
-        call(self.device, self.lib.tgrad_group_scale, "tgrad_group_scale", self.handle, self._result(norm).data_ptr() - 8)
+        call(self.device, self.lib.tgrad_group_scale, "tgrad_group_scale", self.handle, self._result(norm, "norm"))
 
     def tgrad_group_adamw(self, t: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, norm=None,
                           skip_nonfinite: bool = False) -> None:
         """One AdamW step after `t` others; `norm`: a result whose factor scales the gradients as they are read."""
         hyper = T.tgrad_adamw(lr, beta1, beta2, eps, int(skip_nonfinite))
-        at = self._result(norm).data_ptr() - 8 if norm is not None else None
+        at = self._result(norm, "norm") if norm is not None else None
         call(self.device, self.lib.tgrad_group_adamw, "tgrad_group_adamw", self.handle, C.byref(hyper), int(t), at)
 
     @staticmethod

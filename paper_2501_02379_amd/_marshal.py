@@ -40,8 +40,8 @@ def vector(t, n, dtype, device, what):
     """Address of a dense vector of n elements (None stays None); anything else is refused."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or t.get_device() != device.index or not t.is_contiguous():
-        refuse("%s: %s[%d], dense, on the logits' device" % (what, dtype, n))
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or t.get_device() != device.index or not t.is_contiguous() or t.is_neg():
+        refuse("%s: %s[%d], dense, on the logits' device, no pending negation" % (what, dtype, n))
     return t.data_ptr()
 
 
@@ -49,8 +49,8 @@ def scalar(t, dtype, device, what):
     """Address of a tensor of one element, of any dimension (None stays None)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() != 1 or t.get_device() != device.index:
-        refuse("%s: one %s on the logits' device" % (what, dtype))
+    if t.dtype is not dtype or t.numel() != 1 or t.get_device() != device.index or t.is_neg():
+        refuse("%s: one %s on the logits' device, no pending negation" % (what, dtype))
     return t.data_ptr()
 
 

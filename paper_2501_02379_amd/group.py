@@ -136,7 +136,7 @@ class Group:
     def _result(self, r, what):
         """Address of what lies behind an earlier result."""
         if r is None or r.dtype != torch.float32 or r.shape != (2,) or r.stride() != (1,) or r.storage_offset() != 2 or \
-                r.device != self.device:
+                r.device != self.device or r.is_neg():
             refuse("%s: an earlier result" % what)
         return r.data_ptr() - 8
 
@@ -174,8 +174,8 @@ class Group:
     def _add(self, t):
         if t is None:
             return None
-        if t.dtype != torch.float64 or t.numel() != 1 or t.device != self.device:
-            refuse("add_sumsq: one float64 on the device")
+        if t.dtype != torch.float64 or t.numel() != 1 or t.device != self.device or t.is_neg():
+            refuse("add_sumsq: one float64 on the device, no pending negation")
         return t.data_ptr()
 
     def tgrad_group_destroy(self) -> None:

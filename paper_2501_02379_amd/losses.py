@@ -38,8 +38,8 @@ def _describe(logits, targets, temperature):
         refuse("logits: a 2-D float32, bfloat16 or float16 tensor on the GPU")
     rows, vocab = logits.shape
     stride = logits.stride(0) if rows > 1 else vocab
-    if vocab > 1 and logits.stride(1) != 1:
-        refuse("logits: dense rows")
+    if (vocab > 1 and logits.stride(1) != 1) or logits.is_neg():       # memory holds other numbers than a tensor with that pending
+        refuse("logits: dense rows, no pending negation")
     y = vector(targets, rows, torch.int64, logits.device, "targets")
     return T.tgrad_logits(logits.data_ptr(), rows, vocab, stride, y, REAL_TYPES[logits.dtype], temperature)
 
@@ -49,8 +49,8 @@ def _gradient(logits, out):
     if out is None:
         out = torch.empty_like(logits, memory_format=torch.contiguous_format)
     elif out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or \
-            (out.shape[1] > 1 and out.stride(1) != 1):
-        refuse("out: the logits' shape, type and device, with dense rows")
+            (out.shape[1] > 1 and out.stride(1) != 1) or out.is_neg():
+        refuse("out: the logits' shape, type and device, with dense rows, no pending negation")
     return out, (out.stride(0) if out.shape[0] > 1 else out.shape[1])
 
 

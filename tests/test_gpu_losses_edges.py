@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2501_02379_amd import losses
+from paper_2501_02379_amd import group, losses, tgrad as T
 from test_gpu_losses import DEV, TYPES, U, close_gradient, gradient, logp_bound, make, scores
 
 pytestmark = pytest.mark.gpu
@@ -172,3 +172,26 @@ def test_kl_of_a_token_of_probability_0():
     assert float(r.stats[2]) == math.inf and bool(torch.isfinite(r.stats[[0, 1, 3]]).all()) and bool(torch.isfinite(r.dlogits).all())
     assert not bool(r.dlogits[1].any())
     assert float(losses.tgrad_policy_loss(x, y, w, w, logp, logp, kl_beta=0.1).stats[0]) == math.inf
+
+
+def test_pending_negations_are_refused():
+    """The imaginary part of a conjugate is the negative of what its memory holds."""
+    x, y = make(4, 50, "f32", seed=93)
+    w = torch.ones(4, device=DEV)
+    start = torch.tensor([0, 2, 4], device=DEV)
+    neg = lambda t: torch._neg_view(t)  # noqa: E731
+    one = torch.complex(torch.ones(1, device=DEV), torch.ones(1, device=DEV)).conj().imag
+    assert one.is_neg() and float(one) == -1
+    grp = group.Group([w])
+    shape = (8, 8, 8)
+    ctx = T.Context(T.make_config(shape, (2, 2, 2), 5))
+    for bad in (lambda: losses.tgrad_token_logprobs(neg(x), y), lambda: losses.tgrad_token_logprobs_backward(x, y, neg(w), w),
+                lambda: losses.tgrad_token_logprobs_backward(x, y, w, w, out=neg(torch.empty_like(x))),
+                lambda: losses.tgrad_policy_loss(x, y, neg(w), w, w), lambda: losses.tgrad_policy_loss(x, y, w, neg(w), w),
+                lambda: losses.tgrad_policy_loss(x, y, w, w, w, dloss=one),
+                lambda: losses.tgrad_preference_loss(x, y, w, neg(w), start), lambda: losses.tgrad_preference_loss(x, y, w, w, neg(start)),
+                lambda: grp.tgrad_group_grad_norm(1.0, add_sumsq=neg(torch.ones(1, dtype=torch.float64, device=DEV))),
+                lambda: grp.tgrad_group_scale(neg(grp.tgrad_group_grad_norm(1.0))), lambda: ctx.tgrad_set_grad_scale(one)):
+        with pytest.raises(T.TgradError):
+            bad()
+    ctx.tgrad_destroy()

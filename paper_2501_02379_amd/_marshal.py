@@ -14,6 +14,14 @@ def refuse(what: str):
     raise T.TgradError(T.TGRAD_ERR_INVALID_ARG, what)
 
 
+def used_on(stream, tensors):
+    """Tensors of another stream's allocator that kernels on `stream` work on: the caller may let go of them at once, and their memory
+    is not handed out again before those kernels have run."""
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda:
+            t.record_stream(stream)
+
+
 def on_stream(f):
     """Adds `stream=`: the call runs with that stream current, so that what it allocates belongs to it (memory of another stream's
     could still be in use there, and scratch could be handed out again before the kernels have run)."""
@@ -21,8 +29,14 @@ def on_stream(f):
     def run(*args, stream=None, **kw):
         if stream is None:
             return f(*args, **kw)
+        for t in args:
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != stream.device:
+                refuse("stream: one of the logits' device")
         with torch.cuda.stream(stream):
-            return f(*args, **kw)
+            result = f(*args, **kw)
+        used_on(stream, args)
+        used_on(stream, kw.values())
+        return result
     return run
 
 

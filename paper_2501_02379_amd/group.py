@@ -9,7 +9,7 @@ from typing import Optional, Sequence
 import torch
 
 from . import tgrad as T
-from ._marshal import REAL_TYPES, call, check, refuse, stream_of
+from ._marshal import REAL_TYPES, call, check, refuse, stream_of, used_on
 
 TYPES = {**REAL_TYPES, torch.complex64: T.TGRAD_C64}
 
@@ -50,7 +50,8 @@ class Group:
     per element.  `outs`: where `tgrad_group_scale` and `tgrad_group_clip` put the scaled gradients (None: in place).
 
     Every call is enqueued on the stream given here (the device's current one by default) and waits for nothing.  The group
-    keeps its tensors alive.  Results (`tgrad_group_grad_norm`, `tgrad_group_clip`) are a float32 tensor (norm, factor) on the
+    keeps its tensors alive; where its stream is not the current one they are recorded on it, so that tensors that a bind replaces,
+    or those of a group that is dropped, last until the calls before have run.  Results (`tgrad_group_grad_norm`, `tgrad_group_clip`) are a float32 tensor (norm, factor) on the
     device; the buffer behind it also holds the sum of squares in float64, `group.sumsq(result)`.
     """
 
@@ -69,10 +70,13 @@ class Group:
         size = C.c_size_t(0)
         check(self.lib.tgrad_group_query_size(table, len(grads), C.byref(size)), "tgrad_group_query_size")
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if self.stream.device != self.device:
+            refuse("stream: one of the gradients' device")
         with torch.cuda.stream(self.stream):
             self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
         call(self.device, self.lib.tgrad_group_init, "tgrad_group_init", C.byref(self.handle), table, len(grads),
              self.workspace.data_ptr(), self.stream.cuda_stream)
+        self._used(*self.tensors)
 
     def _table(self, grads, params, exp_avg, exp_avg_sq, outs):
         n, index = len(grads), self.device.index
@@ -125,6 +129,12 @@ class Group:
         except Exception:
             self.tensors = old
             raise
+        self._used(*self.tensors)
+
+    def _used(self, *lists):
+        if stream_of(self.device) != self.stream.cuda_stream:
+            for tensors in lists:
+                used_on(self.stream, tensors)
 
     def _new(self):
         """A result to be written."""
@@ -146,6 +156,7 @@ class Group:
         r = self._new() if into is None else into
         call(self.device, self.lib.tgrad_group_grad_norm, "tgrad_group_grad_norm", self.handle, max_norm, self._add(add_sumsq),
              self._result(r, "into"))
+        self._used((add_sumsq, into))
         return r
 
     def tgrad_group_clip(self, max_norm: float, add_sumsq=None, into=None):
@@ -153,11 +164,13 @@ class Group:
         r = self._new() if into is None else into
         call(self.device, self.lib.tgrad_group_clip, "tgrad_group_clip", self.handle, max_norm, self._add(add_sumsq),
              self._result(r, "into"))
+        self._used((add_sumsq, into))
         return r
 
     def tgrad_group_scale(self, norm) -> None:
         """The gradients times the factor of an earlier result."""
         call(self.device, self.lib.tgrad_group_scale, "tgrad_group_scale", self.handle, self._result(norm, "norm"))
+        self._used((norm,))
 
     def tgrad_group_adamw(self, t: int, *, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, norm=None,
                           skip_nonfinite: bool = False) -> None:
@@ -165,6 +178,7 @@ class Group:
         hyper = T.tgrad_adamw(lr, beta1, beta2, eps, int(skip_nonfinite))
         at = self._result(norm, "norm") if norm is not None else None
         call(self.device, self.lib.tgrad_group_adamw, "tgrad_group_adamw", self.handle, C.byref(hyper), int(t), at)
+        self._used((norm,))
 
     @staticmethod
     def sumsq(result):

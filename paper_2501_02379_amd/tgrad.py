@@ -260,6 +260,8 @@ class Context:
         rc = self.lib.tgrad_set_grad_scale(self.handle, _ptr(scale) if scale is not None else None)
         if rc != TGRAD_OK:
             raise TgradError(rc, "tgrad_set_grad_scale")
+        if scale is not None and self.stream != torch.cuda.current_stream(scale.device):
+            scale.record_stream(self.stream)              # steps that read it may be waiting when the next one replaces it
         self.grad_scale = scale
 
     # ---- state ---------------------------------------------------------------------------

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paper_2501_02379_amd import group, tgrad as T
+from paper_2501_02379_amd import group, losses, tgrad as T
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -25,3 +25,84 @@ def test_scaling_needs_an_earlier_result():
     assert all(torch.equal(a, b) for a, b in zip(g, was))
     grp.tgrad_group_scale(grp.tgrad_group_grad_norm(1.0))
     assert not torch.equal(g[0], was[0])
+
+
+def busy():
+    """A side stream with some tens of milliseconds of waiting in front of what comes next."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    return side
+
+
+def test_replaced_tensors_last_until_the_groups_stream_has_passed():
+    n = 9_700_001
+    x = torch.full((n,), 2.0, device=DEV)
+    want = 2.0 * n ** 0.5
+    torch.cuda.synchronize()
+    side = busy()
+    grp = group.Group([x], stream=side)
+    r = grp.tgrad_group_grad_norm(1.0)
+    at = x.data_ptr()
+    grp.tgrad_group_bind([torch.ones(n, device=DEV)])
+    del x
+    fresh = torch.full((n,), 7.0, device=DEV)
+    assert fresh.data_ptr() != at
+    torch.cuda.synchronize()
+    assert abs(float(r[0]) - want) <= 1e-6 * want
+
+
+def test_tensors_of_a_dropped_group_last_too():
+    n = 9_800_003
+    x, m, v, g = (torch.full((n,), k, device=DEV) for k in (1.0, 0.0, 0.0, 3.0))
+    torch.cuda.synchronize()
+    side = busy()
+    grp = group.Group([g], [x], [m], [v], stream=side)
+    grp.tgrad_group_adamw(0, lr=1e-2)
+    at = {t.data_ptr() for t in (m, v, g)}
+    del grp, m, v, g
+    fresh = [torch.full((n,), 7.0, device=DEV) for _ in range(3)]
+    assert not at & {t.data_ptr() for t in fresh}
+    torch.cuda.synchronize()
+    assert bool(((x - 0.99).abs() < 1e-6).all()) and all(bool((t == 7).all()) for t in fresh)
+
+
+def test_arguments_of_a_loss_on_another_stream_last():
+    rows, vocab = 503, 20_011
+    x = torch.zeros(rows, vocab, device=DEV)
+    y = torch.zeros(rows, dtype=torch.int64, device=DEV)
+    torch.cuda.synchronize()
+    side = busy()
+    logp, _ = losses.tgrad_token_logprobs(x, targets=y, stream=side)
+    at = x.data_ptr()
+    del x
+    fresh = torch.randn(rows, vocab, device=DEV)
+    assert fresh.data_ptr() != at
+    torch.cuda.synchronize()
+    assert bool(((logp + math.log(vocab)).abs() < 1e-5).all())
+
+
+def test_a_replaced_factor_lasts():
+    shape = (16, 16, 8, 5)
+    side = torch.cuda.Stream()
+    w, g = torch.zeros(*shape, 2, device=DEV), torch.randn(*shape, 2, device=DEV)
+    ctx = T.Context(T.make_config(shape, (8, 8, 4, 3), 103), stream=side)
+    torch.cuda.synchronize()
+    ctx.tgrad_step(w, g)                                               # loads the kernels: what follows takes the host less than the wait
+    scale = torch.full((1,), 0.5, device=DEV)
+    at = scale.data_ptr()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    ctx.tgrad_set_grad_scale(scale)
+    ctx.tgrad_step(w, g)
+    done = torch.cuda.Event()
+    done.record(side)
+    ctx.tgrad_set_grad_scale(None)
+    del scale
+    fresh = [torch.zeros(1, device=DEV) for _ in range(64)]
+    assert not done.query()                                            # or this test shows nothing
+    assert at not in {t.data_ptr() for t in fresh}
+    torch.cuda.synchronize()
+    ctx.tgrad_destroy()

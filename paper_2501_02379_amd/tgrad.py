@@ -252,10 +252,11 @@ class Context:
             raise TgradError(rc, "tgrad_step")
 
     def tgrad_set_grad_scale(self, scale) -> None:
-        """Later steps multiply the gradient by `scale`, one float32 on the device (the factor of a group's norm, `norm[1]`), read
+        """Later steps multiply the gradient by `scale`, one float32 on the context's device (the factor of a group's norm, `norm[1]`), read
         when the step runs; None: no scaling.  The context keeps the tensor alive."""
         import torch
-        if scale is not None and (scale.dtype != torch.float32 or scale.numel() != 1 or scale.device.type != "cuda" or scale.is_neg()):
+        if scale is not None and (scale.dtype != torch.float32 or scale.numel() != 1 or scale.is_neg() or
+                                  scale.get_device() != self.state_buf.get_device()):
             raise TgradError(TGRAD_ERR_INVALID_ARG, "tgrad_set_grad_scale")
         rc = self.lib.tgrad_set_grad_scale(self.handle, _ptr(scale) if scale is not None else None)
         if rc != TGRAD_OK:

@@ -156,3 +156,22 @@ def test_bindings_refuse_tensors_that_do_not_fit():
         group.Group([])
     with pytest.raises(T.TgradError):
         group.Group([x])
+
+
+def test_a_factor_on_another_gpu_is_refused():
+    """The library is not reached: a pointer to another GPU's memory would be read by every later step."""
+    from types import SimpleNamespace as N
+
+    import torch
+
+    class Scale:
+        dtype, device = torch.float32, torch.device("cuda", 1)
+        numel, is_neg, data_ptr = (lambda self: 1), (lambda self: False), (lambda self: 4096)
+        get_device = lambda self: 1  # noqa: E731
+
+    reached = []
+    ctx = N(lib=N(tgrad_set_grad_scale=lambda *a: reached.append(a) or T.TGRAD_ERR_INVALID_ARG), handle=None,
+            state_buf=N(get_device=lambda: 0))
+    with pytest.raises(T.TgradError):
+        T.Context.tgrad_set_grad_scale(ctx, Scale())
+    assert not reached

@@ -139,7 +139,7 @@ __device__ __forceinline__ void finish_norm(const NormArgs& a, int n, double* ld
   if (threadIdx.x == 0) {
     if (a.add) acc += *a.add;
     const float norm = (float)sqrt(acc);
-    const float c = a.max_norm / (norm + 1e-6f);
+    const float c = norm == INFINITY ? 0.f : a.max_norm / (norm + 1e-6f);   // for max_norm = INFINITY too (no clipping)
     a.out->sumsq = acc;
     a.out->norm = norm;
     a.out->coef = c > 1.f ? 1.f : c;      // a NaN stays one

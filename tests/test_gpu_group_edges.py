@@ -106,3 +106,16 @@ def test_a_replaced_factor_lasts():
     assert at not in {t.data_ptr() for t in fresh}
     torch.cuda.synchronize()
     ctx.tgrad_destroy()
+
+
+def test_an_unbounded_norm():
+    """max_norm = inf only measures: factor 1, and still 0 for an infinite norm, NaN for a NaN."""
+    x = torch.full((300,), 1e4, device=DEV)
+    grp = group.Group([x])
+    assert float(grp.tgrad_group_grad_norm(math.inf)[1]) == 1
+    for bad in (math.inf, -math.inf):
+        x[7] = bad
+        norm, coef = grp.tgrad_group_grad_norm(math.inf).tolist()
+        assert norm == math.inf and coef == 0
+    x[9] = math.nan
+    assert all(math.isnan(k) for k in grp.tgrad_group_grad_norm(math.inf).tolist())

@@ -83,7 +83,8 @@ class Group:
         grads = _tensors(grads, n, "grads", index)
         params, exp_avg = _tensors(params, n, "params", index), _tensors(exp_avg, n, "exp_avg", index)
         exp_avg_sq, outs = _tensors(exp_avg_sq, n, "exp_avg_sq", index), _tensors(outs, n, "outs", index)
-        lr, wd = self.lr_scale or [1.0] * n, self.weight_decay or [0.0] * n
+        lr = self.lr_scale if self.lr_scale is not None else [1.0] * n
+        wd = self.weight_decay if self.weight_decay is not None else [0.0] * n
         if len(lr) != n or len(wd) != n:
             refuse("lr_scale, weight_decay: one for every gradient")
         entries = []

@@ -2,6 +2,7 @@
 works on them."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -119,3 +120,19 @@ def test_an_unbounded_norm():
         assert norm == math.inf and coef == 0
     x[9] = math.nan
     assert all(math.isnan(k) for k in grp.tgrad_group_grad_norm(math.inf).tolist())
+
+
+def test_rates_and_decays_of_any_sequence():
+    """Arrays and tuples as well as lists; an empty one is not one for every gradient."""
+    def step(lr_scale, weight_decay):
+        p, g = [torch.ones(50, device=DEV), torch.ones(60, device=DEV)], [torch.ones(50, device=DEV), torch.ones(60, device=DEV)]
+        m, v = [torch.zeros_like(t) for t in p], [torch.zeros_like(t) for t in p]
+        group.Group(g, p, m, v, lr_scale=lr_scale, weight_decay=weight_decay).tgrad_group_adamw(0, lr=0.1)
+        return torch.cat(p)
+
+    want = step([1.0, 0.5], [0.0, 0.25])
+    assert torch.equal(step(np.array([1.0, 0.5]), np.array([0.0, 0.25], dtype=np.float32)), want)
+    assert torch.equal(step((1.0, 0.5), torch.tensor([0.0, 0.25])), want)
+    for bad in (([], None), (None, ()), ([1.0], None)):
+        with pytest.raises(T.TgradError):
+            step(*bad)

@@ -253,7 +253,8 @@ class Context:
 
     def tgrad_set_grad_scale(self, scale) -> None:
         """Later steps multiply the gradient by `scale`, one float32 on the context's device (the factor of a group's norm, `norm[1]`), read
-        when the step runs; None: no scaling.  The context keeps the tensor alive."""
+        when the step runs; None: no scaling.  The context keeps the tensor alive.  A step under a factor or gradient that is not
+        finite is not skipped, and its weights and moments are lost: where that may happen read the norm first (`float(norm[0])`)."""
         import torch
         if scale is not None and (scale.dtype != torch.float32 or scale.numel() != 1 or scale.is_neg() or
                                   scale.get_device() != self.state_buf.get_device()):

@@ -136,3 +136,38 @@ def test_rates_and_decays_of_any_sequence():
     for bad in (([], None), (None, ()), ([1.0], None)):
         with pytest.raises(T.TgradError):
             step(*bad)
+
+
+def test_an_overflowed_step_left_out_for_both_kinds_of_parameter():
+    """The norm read on the host in front of tgrad_step, skip_nonfinite for the rest: weights and moments as if the gradient had not been."""
+    shape, steps = (16, 16, 8, 5), 6
+    gen = torch.Generator().manual_seed(3)
+    spectral = [torch.randn(*shape, 2, generator=gen) for _ in range(steps)]
+    dense = [torch.randn(3000, generator=gen) for _ in range(steps)]
+
+    def train(overflow):
+        ctx = T.Context(T.make_config(shape, (8, 8, 4, 3), 103, lr=1e-2, refresh_every=2))
+        w, p = torch.ones(*shape, 2, device=DEV), torch.ones(3000, device=DEV)
+        gs, gd = torch.zeros_like(w), torch.zeros_like(p)
+        m, v = torch.zeros_like(p), torch.zeros_like(p)
+        every, rest = group.Group([gs, gd]), group.Group([gd], [p], [m], [v])
+        norm = every.tgrad_group_grad_norm(1.0)
+        ctx.tgrad_set_grad_scale(norm[1:])
+        t = 0
+        for k in range(steps):
+            for bad in ((True, False) if overflow and k in (0, 3) else (False,)):
+                gs.copy_(spectral[k])
+                gd.copy_(dense[k])
+                if bad:
+                    gs[1, 2, 3, 4, 0] = gd[5] = math.inf
+                every.tgrad_group_grad_norm(1.0, into=norm)
+                rest.tgrad_group_adamw(t, lr=1e-2, norm=norm, skip_nonfinite=True)
+                if math.isfinite(float(norm[0])):
+                    ctx.tgrad_step(w, gs)
+                    t += 1
+        got = [w, p, m, v] + [torch.from_numpy(ctx.tgrad_get_state(s)) for s in (T.STATE_CORE_M, T.STATE_CORE_V, T.STATE_SPARSE_M)]
+        ctx.tgrad_destroy()
+        return got
+
+    for a, b in zip(train(True), train(False)):
+        assert torch.equal(a, b) and bool(torch.isfinite(torch.view_as_real(a) if a.is_complex() else a).all())

@@ -29,13 +29,12 @@ def on_stream(f):
     def run(*args, stream=None, **kw):
         if stream is None:
             return f(*args, **kw)
-        for t in args:
+        for t in (*args, *kw.values()):
             if isinstance(t, torch.Tensor) and t.is_cuda and t.device != stream.device:
                 refuse("stream: one of the logits' device")
         with torch.cuda.stream(stream):
             result = f(*args, **kw)
-        used_on(stream, args)
-        used_on(stream, kw.values())
+        used_on(stream, (*args, *kw.values()))
         return result
     return run
 

@@ -171,3 +171,13 @@ def test_an_overflowed_step_left_out_for_both_kinds_of_parameter():
 
     for a, b in zip(train(True), train(False)):
         assert torch.equal(a, b) and bool(torch.isfinite(torch.view_as_real(a) if a.is_complex() else a).all())
+
+
+def test_streams_of_another_gpu_are_refused():
+    from types import SimpleNamespace
+    other = SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
+    x, y = torch.zeros(3, 5, device=DEV), torch.zeros(3, dtype=torch.int64, device=DEV)
+    for bad in (lambda: losses.tgrad_token_logprobs(x, y, stream=other), lambda: losses.tgrad_token_logprobs(logits=x, targets=y, stream=other),
+                lambda: group.Group([x], stream=other)):
+        with pytest.raises(T.TgradError):
+            bad()

@@ -200,12 +200,13 @@ int tgrad_step(tgrad_ctx* ctx, void* weight_dev, const void* grad_dev);
 /*
  * Multiply the gradient of every later `tgrad_step` of this context by a number that lies on the device when the step runs: the
  * factor that clips a global norm (tgrad_norm.coef below), an inverse loss scale.  The gradient itself is neither rewritten nor read
- * once more: its compressed parts, which are linear in it, are scaled before AdamUpdate.  The support and the factors of a refresh come from the
- * gradient as it is; a positive factor changes neither, up to rounding.  SPARSE_G and CORE_G report scaled values.
- * There is no skip here as tgrad_group_adamw has it (skip_nonfinite): a NaN factor, or an infinite entry under the factor 0 that an infinite
- * norm gives, makes moments and weight NaN, and a refresh on such a gradient leaves a support and factors of no use to the steps behind it.
- * A program whose gradients may overflow (float16 under a loss scale) reads tgrad_norm.norm on the host in front of tgrad_step, and leaves
- * the step out where it is not finite.  tgrad_step_static takes no factor: give it a scaled gradient (tgrad_group_scale).
+ * once more: its compressed parts, which are linear in it, are scaled before AdamUpdate.  The support and the factors of a refresh
+ * come from the gradient as it is; a positive factor changes neither, up to rounding.  SPARSE_G and CORE_G report scaled values.
+ * There is no skip here as tgrad_group_adamw has it (skip_nonfinite): a NaN factor, or an infinite entry under the factor 0 that an
+ * infinite norm gives, makes moments and weight NaN, and a refresh on such a gradient leaves a support and factors of no use to the
+ * steps behind it.  A program whose gradients may overflow (float16 under a loss scale) reads tgrad_norm.norm on the host in front of
+ * tgrad_step, and leaves the step out where it is not finite.
+ * tgrad_step_static takes no factor: give it a scaled gradient (tgrad_group_scale).
  *  scale_dev  device pointer to one float32, read by every step, or NULL: no scaling (as after tgrad_init).
  * Errors: INVALID_ARG.
  */

@@ -73,9 +73,9 @@ __device__ __forceinline__ void for_real(int real, F&& f) {
   else f(std::integral_constant<int, TGRAD_F16>());
 }
 
-// U units of four numbers of a thread from unit `first` on; past the end the last one again.  LAST: nobody reads them again soon; with
-// that hint on loads and stores, norm and scaling of 136 M complex64 take 545 us instead of 608, norm and AdamW of 478 M numbers 2365 instead of
-// 2488.
+// U units of four numbers of a thread from unit `first` on; past the end the last one again.  LAST: nobody reads them again soon.  With
+// that hint on loads and stores norm and scaling of 136 M complex64 took 545 us instead of 608, norm and AdamW of 478 M numbers 2365
+// instead of 2488.
 template <int DT, int U, bool LAST>
 __device__ __forceinline__ void load_units(typename Four<DT>::type* q, const void* base, int64_t at, int first, int units) {
 #pragma unroll
@@ -94,9 +94,9 @@ __device__ __forceinline__ void store_unit(void* base, int64_t at, int unit, con
 // Everything above is on its way before anything below: the compiler would move each load to the branch that uses it.
 __device__ __forceinline__ void loads_issued() { asm volatile("" ::: "memory"); }
 
-// sum |g|^2, bounded by the read (136 M complex64: 181 us, 5.7 to 6 TB/s).  Squares and sums in float64: the square of a float32 is exact there, and no finite gradient overflows.  Every
-// workgroup leaves one partial sum; the last one to come adds them up in the order of the workgroups, so that the result does
-// not depend on which one that is.
+// sum |g|^2, bounded by the read: 136 M complex64 in 181 to 183 us, 5.7 TB/s and what the caches give besides.  Squares and sums in float64:
+// the square of a float32 is exact there, and no finite gradient overflows.  Every workgroup leaves one partial sum; the last one to come
+// adds them up in the order of the workgroups, so that the result does not depend on which one that is.
 template <int DT>
 __device__ __forceinline__ double piece_sumsq(const void* g, Span s) {
   constexpr int U = 4;
@@ -207,7 +207,7 @@ __device__ __forceinline__ void piece_scale(const void* g, void* out, Span s, fl
 }
 
 // One workgroup per piece: workgroups that stay for more of them, one piece behind the other, are slower (norm and AdamW of
-// 478 M numbers 2690 us instead of 2488).  136 M complex64: 371 us, 5.9 TB/s, a copy's rate.
+// 478 M numbers 2690 us instead of 2488).  136 M complex64: 382 to 385 us, 5.7 TB/s.
 __global__ __launch_bounds__(kThreads) void k_group_scale(const Entry* __restrict__ entries, const Piece* __restrict__ pieces,
                                                           const tgrad_norm* norm) {
   const float coef = norm->coef;
@@ -313,8 +313,8 @@ __device__ __forceinline__ void piece_adamw(const Entry& e, int index, const Ada
   }
 }
 
-// Seven streams, 26 to 28 bytes a number: 478 M numbers with bf16 gradients in 1940 to 2170 us, 6.4 to 5.7 TB/s.  Backwards: what k_group_sumsq has
-// read last is still in the caches (norm and step 2320 us, forwards 2343).
+// Seven streams, 26 to 28 bytes a number: 478 M numbers with bf16 gradients in 2180 to 2200 us behind the norm, 5.7 TB/s.  Backwards: what
+// k_group_sumsq has read last is still in the caches (norm and step 2320 us, forwards 2343).
 __global__ __launch_bounds__(kThreads) void k_group_adamw(const Entry* __restrict__ entries, const Piece* __restrict__ pieces, AdamK h,
                                                           const tgrad_norm* norm) {
   const float coef = norm ? norm->coef : 1.f;

@@ -362,9 +362,10 @@ struct RowStat {
 
 // AGAIN: the logits are read again soon, by the kernels behind this one in a preference loss, for which stat and dlogp (zero for the
 // rows that lie in no sequence) are.  Log ratios are small differences of large numbers, and a reward adds up hundreds of them: the sum
-// takes the scale in two terms, and the rest is formed in float64.  Elsewhere this is the last read, and the hint for that is worth 10 % (4096
-// rows of 131072 bf16 numbers, a quarter of them ignored: 151 us without it, 136 with it; now 127, 6.35 TB/s).  8 pieces of every thread are
-// on their way.
+// takes the scale in two terms, and the rest is formed in float64.  (With it 5721 rows of 100003 float16 numbers are scored in 156 us, without
+// it in 154; a whole loss on short rows, 9000 bf16 numbers each, takes 2 % longer.)  Elsewhere this is the last read, and the hint for that
+// is worth 10 %: 4096 rows of 131072 bf16 numbers, a quarter of them ignored, 136 us with it, 151 without; now 125, 6.4 TB/s.  8 pieces of
+// every thread are on their way.
 template <int DT, int T, bool AGAIN>
 __global__ __launch_bounds__(T) void k_logprobs(Logits L, const float* weight, const float* ref_logp, float* logp, float* lse, RowStat* stat,
                                                 float* dlogp) {
@@ -429,8 +430,8 @@ __device__ __forceinline__ void pair_mean(const PairMean& a) {
 }
 
 // stat: what every row's sum was, or null and lse given.  `parts` workgroups of T threads share a row, U pieces a thread and no more: each
-// loads, computes and stores once (with a workgroup that walks its row a loss on 5721 rows of 100003 float16 numbers took 563 us, so 501; the
-// gradient alone now 305, 6.4 TB/s with what the memory-side cache still has).  Pieces start at 16-byte boundaries of the gradient.  The
+// loads, computes and stores once (with a workgroup that walks its row a loss on 5721 rows of 100003 float16 numbers took 563 us, so
+// 501; the gradient alone now 321, 6.2 TB/s with what the memory-side cache still has).  Pieces start at 16-byte boundaries of the gradient.  The
 // first workgroup forms the mean over `pairs` pairs besides.
 template <int DT, int T, int U>
 __global__ __launch_bounds__(T) void k_logprobs_back(Logits L, const float* lse, const RowStat* stat, const float* dlogp, void* dx,
@@ -563,10 +564,10 @@ __device__ __forceinline__ void policy_row(const Logits& L, const PolicyArgs& a,
 }
 
 // One workgroup of T threads per row; the last T NV pieces of 16 bytes stay in registers from the sum to the gradient, what lies
-// before them in longer rows is read twice, the second time backwards.  8192 rows of 131072 bf16 numbers, a quarter ignored: 655 us, 5.75 TB/s,
-// a copy's rate; 1024 of 200003 float32 numbers: 320 us, 6.3 TB/s with a fifth of the bytes read again (in LDS besides: 312, but rows of 150000
-// bf16 numbers 260 instead of 252); 2048 of 50001: 75 us, 4.9 TB/s, two rows a compute unit at a time in three rounds (four rows of 256 threads
-// 87, one of 1024 90).
+// before them in longer rows is read twice, the second time backwards.  8192 rows of 131072 bf16 numbers, a quarter ignored: 662 us,
+// 5.7 TB/s, a copy's rate.  1024 of 200003 float32 numbers: 327 us, 6.2 TB/s with a fifth of the bytes read again (in LDS besides 3 % less,
+// but rows of 150000 bf16 numbers 260 instead of 252).  2048 of 50001 bf16 numbers: 75 us, 4.9 TB/s, two rows a compute unit at a time in
+// three rounds (four rows of 256 threads 87, one of 1024 90).
 template <int DT, int T, int NV>
 __global__ __launch_bounds__(T) void k_policy(Logits L, PolicyArgs a) {
   typedef typename Elem<DT>::raw raw;

@@ -119,7 +119,9 @@ class Group:
         return (T.tgrad_tensor * n).from_buffer_copy(b"".join(entries))
 
     def tgrad_group_bind(self, grads, params=None, exp_avg=None, exp_avg_sq=None, outs=None) -> None:
-        """The same tensors at new addresses (gradients allocated anew); what is None stays as it is."""
+        """The same tensors at new addresses (gradients allocated anew); what is None stays as it is.  Every tensor is checked and every
+        entry written again, 1.6 us a tensor on the host, 2.3 with parameters and moments: gradient buffers that stay where they are
+        (`zero_grad(set_to_none=False)`) need none of it."""
         old = self.tensors
         new = [list(x) if x is not None else y for x, y in zip((grads, params, exp_avg, exp_avg_sq, outs), old)]
         if any(len(x) != len(old[0]) for x in new):

@@ -1,0 +1,368 @@
+"""A block of a model in 8 bits, as measurable cases: its products, what it keeps for the backward pass, and the norms around it.
+
+`linear` quantises tokens as they come and multiplies the codes with a weight that lies in 8 bits, a scale for each token and channel;
+`gradients` are that product's two backward products, which read the 8-bit codes that were kept; `activation` is the nonlinearity
+between two products with its checkpoint in 8 bits and the backward pass from it; `norm` joins a block's output to the residual
+stream (norm, gate, residual scale) and norms the sum for the next block, forward alone where tokens are served and with the
+backward pass where a model is trained.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+EPS = 1e-6
+MOST_PRODUCT = 8192 * 8192 * 8192                         # multiplications of the largest product
+MOST_VALUES = 8192 * 28672                                # elements of the largest activation and norm
+
+
+def _linear(name, op, tokens, inner, outer, dtype, pad=0):
+    """tokens x inner times inner x outer; `pad`: elements between the token rows."""
+    c = {"op": op, "tokens": tokens, "inner": inner, "outer": outer, "dtype": dtype, "pad": pad}
+    return {**c, "name": name} if name else c
+
+
+def _activation(name, tokens, width, dtype, act, gated, group, quantize=False):
+    """`gated`: a second matrix of the same size that the activation is multiplied with, beside it in memory; `group`: columns to a
+    scale of the checkpoint; `quantize`: the result in 8 bits for the next product."""
+    c = {"op": "activation", "tokens": tokens, "width": width, "dtype": dtype, "act": act, "gated": gated, "group": group,
+         "quantize": quantize}
+    return {**c, "name": name} if name else c
+
+
+def _norm(name, tokens, width, stream, dtype, shared, centered=False, train=True, quantize=False, weights="f32"):
+    """`stream`: type of the residual stream, `dtype`: of the block's input and output; `shared`: tokens to a row of the gate."""
+    c = {"op": "norm", "tokens": tokens, "width": width, "stream": stream, "dtype": dtype, "shared": shared, "centered": centered,
+         "train": train, "quantize": quantize, "weights": weights}
+    return {**c, "name": name} if name else c
+
+
+def listed():
+    return [
+        # one token of one sequence served: latency
+        _linear("linear_token", "linear", 1, 4096, 4096, "bf16"),
+        # a few sequences served together, odd sizes
+        _linear("linear_decode_odd", "linear", 23, 8190, 10007, "f16", pad=6),
+        # a training or prefill step
+        _linear("linear_large", "linear", 8192, 8192, 8192, "bf16"),
+        # ordinary fine-tuning step of a small layer, single precision, odd sizes
+        _linear("gradients_odd_f32", "gradients", 2051, 1537, 1025, "f32"),
+        # points of many fields through a narrow layer: a long sum into a small weight
+        _linear("gradients_long", "gradients", 131072, 512, 768, "f16"),
+        # the largest
+        _linear("gradients_large", "gradients", 8192, 8192, 8192, "bf16"),
+        # the pointwise part of a small neural operator
+        _activation("activation_small", 257, 1021, "f32", "gelu", False, 128),
+        # a gated feed-forward block in training, its result quantised for the product behind it
+        _activation("activation_large", 8192, 28672, "bf16", "silu", True, 128, quantize=True),
+        # between two blocks of one served token: latency
+        _norm("norm_token", 1, 4096, "bf16", "bf16", 1, train=False),
+        # a chunk of tokens served, stream in single precision, the norm's result quantised for the product behind it
+        _norm("norm_quantized", 4096, 5120, "f32", "bf16", 4096, train=False, quantize=True),
+        # a few sequences of a small model, a gate for each sequence, mean taken off, odd width
+        _norm("norm_train_odd", 1000, 1537, "f32", "f32", 250, centered=True),
+        # an ordinary large training step, one gate for all tokens
+        _norm("norm_train_large", 8192, 8192, "bf16", "bf16", 8192, weights="bf16"),
+    ]
+
+
+def _log(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    op = rng.choice(["linear", "linear", "gradients", "activation", "norm", "norm"])
+    dtype = rng.choice(["bf16", "bf16", "f16", "f32"])
+    if op in ("linear", "gradients"):
+        inner, outer = _log(rng, 64, 12000), _log(rng, 64, 12000)
+        if rng.random() < 0.5:
+            inner, outer = -(-inner // 64) * 64, -(-outer // 64) * 64
+        most = MOST_PRODUCT // (inner * outer * (4 if dtype == "f32" else 1))
+        return _linear(None, op, _log(rng, 1, min(32768, most)), inner, outer, dtype, rng.choice([0, 0, 3, 8]))
+    if op == "activation":
+        width = _log(rng, 60, 30000)
+        if rng.random() < 0.5:
+            width = -(-width // 32) * 32
+        return _activation(None, _log(rng, 1, min(32768, MOST_VALUES // (2 * width))), width, dtype, rng.choice(["silu", "gelu"]),
+                           rng.random() < 0.5, rng.choice([32, 64, 128, 128, 256]), rng.random() < 0.3 and dtype != "f32")
+    width = _log(rng, 60, 16000)
+    if rng.random() < 0.5:
+        width = -(-width // 32) * 32
+    tokens = _log(rng, 1, min(32768, MOST_VALUES // (4 * width)))
+    train = rng.random() < 0.6
+    return _norm(None, tokens, width, rng.choice([dtype, "f32"]), dtype, rng.choice([1, max(1, tokens // 3), tokens]), rng.random() < 0.4,
+                 train, dtype != "f32" and not train and rng.random() < 0.5, rng.choice(["f32", dtype]))
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------------
+
+def _quantise(v, group):
+    """(codes, scales) of a matrix, for `group` columns together (0: the whole row): the scale is the largest magnitude over 127, a
+    code the exact quotient rounded to nearest even.  The quotient is taken in 64 bits where 32 could cross a border: 127 times a
+    two-byte number is exact in 32, and a quotient of two such lies on a border or clear of it."""
+    rows, cols = v.shape
+    g = group or cols
+    wide = v.float() if v.dtype != torch.float32 else v.double()
+    wide = torch.nn.functional.pad(wide, (0, -cols % g)).view(rows, -1, g)
+    top = wide.abs().amax(2, keepdim=True)
+    codes = torch.round(wide * 127 / torch.where(top > 0, top, 1)).to(torch.int8)
+    return codes.view(rows, -1)[:, :cols], (top[..., 0].double() / 127).float()
+
+
+def _values(codes, scale, group):
+    """What codes stand for, in 32 bits."""
+    g = group or codes.shape[1]
+    return codes.float() * scale.repeat_interleave(g, 1)[:, :codes.shape[1]]
+
+
+def _rows16(codes):
+    """Codes in rows that start at multiples of 16 bytes, as a program lays its weights out once."""
+    rows, cols = codes.shape
+    laid = torch.zeros(rows, -(-cols // 16) * 16, dtype=torch.int8, device=DEV)
+    laid[:, :cols] = codes
+    return laid[:, :cols]
+
+
+def _randn(gen, rows, cols, spread=1.0, outliers=False):
+    x = torch.randn(rows, cols, device=DEV, generator=gen) * spread
+    if outliers:                                          # a few channels of activations are much larger than the rest
+        x[:, torch.randint(0, cols, (max(1, cols // 200),), device=DEV, generator=gen)] *= 6
+    return x
+
+
+def _strided(x, dtype, pad):
+    flat = torch.zeros(x.shape[0], x.shape[1] + pad, dtype=dtype, device=DEV)
+    flat[:, :x.shape[1]] = x
+    return flat[:, :x.shape[1]]
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    s = dict(case)
+    t = TYPES[case["dtype"]]
+    if case["op"] in ("linear", "gradients"):
+        n, k, m = case["tokens"], case["inner"], case["outer"]
+        w, ws = _quantise(_randn(gen, m, k, 1 / math.sqrt(k)), 0)
+        x = _randn(gen, n, k, outliers=True)
+        s.update(w=_rows16(w), w_scale=ws)
+        if case["op"] == "linear":
+            s["x"] = _strided(x, t, case["pad"])
+        else:
+            c, cs = _quantise(x.to(t), 0)
+            s.update(x8=_rows16(c), x_scale=cs, dy=_strided(_randn(gen, n, m, 0.1), t, case["pad"]))
+    elif case["op"] == "activation":
+        n, f = case["tokens"], case["width"]
+        both = _randn(gen, n, 2 * f if case["gated"] else f, 1.5, outliers=True).to(t)
+        s.update(x=both[:, :f], gate=both[:, f:] if case["gated"] else None, dy=_randn(gen, n, f, 0.1).to(t))
+    else:
+        n, d, u, wt = case["tokens"], case["width"], TYPES[case["stream"]], TYPES[case["weights"]]
+        s.update(x=_randn(gen, n, d, 2.0, outliers=True).to(u), block=_randn(gen, n, d, 0.7).to(t),
+                 gate=(0.5 + 0.2 * _randn(gen, -(-n // case["shared"]), d)).to(t), scale=0.7,
+                 post=(1 + 0.1 * _randn(gen, 1, d)[0]).to(wt), pre=(1 + 0.1 * _randn(gen, 1, d)[0]).to(wt))
+        if case["train"]:
+            s.update(dx=_randn(gen, n, d, 0.1).to(u), dh=_randn(gen, n, d, 0.1).to(t))
+    return s
+
+
+# ---- the plain forms --------------------------------------------------------------------------------------------------------
+
+def _plain_linear(s):
+    codes, scale = _quantise(s["x"], 0)
+    product = codes.float() @ s["w"].float().t()
+    return [(product * scale * s["w_scale"].view(1, -1)).to(s["x"].dtype)]
+
+
+def _plain_gradients(s):
+    dy = s["dy"].float()
+    dx = dy @ _values(s["w"], s["w_scale"], 0)
+    dw = dy.t() @ _values(s["x8"], s["x_scale"], 0)
+    return [dx.to(s["dy"].dtype), dw.to(s["dy"].dtype)]
+
+
+def _act(name, v):
+    """An activation and its derivative."""
+    if name == "silu":
+        p = 1 / (1 + torch.exp(-v))
+        return v * p, p * (1 + v * (1 - p))
+    p = 0.5 * (1 + torch.erf(v * math.sqrt(0.5)))
+    return v * p, p + v * torch.exp(-0.5 * v * v) / math.sqrt(2 * math.pi)
+
+
+def _plain_activation(s):
+    t = s["x"].dtype
+    y, _ = _act(s["act"], s["x"].float())
+    if s["gated"]:
+        y = y * s["gate"].float()
+    y = _values(*_quantise(y, 0), 0).to(t) if s["quantize"] else y.to(t)
+    a, da = _act(s["act"], _values(*_quantise(s["x"], s["group"]), s["group"]))
+    dy = s["dy"].float()
+    if not s["gated"]:
+        return [y, (dy * da).to(t)]
+    g = _values(*_quantise(s["gate"], s["group"]), s["group"])
+    return [y, (dy * g * da).to(t), (dy * a).to(t)]
+
+
+def _normed(v, centered):
+    if centered:
+        v = v - v.mean(1, keepdim=True)
+    inv = torch.rsqrt(v.square().mean(1, keepdim=True) + EPS)
+    return v * inv, inv
+
+
+def _norm_back(u, n, inv, centered):
+    r = u - n * (u * n).mean(1, keepdim=True)
+    if centered:
+        r = r - u.mean(1, keepdim=True)
+    return r * inv
+
+
+def _plain_norm(s):
+    t, u, c = s["block"].dtype, s["x"].dtype, s["centered"]
+    shared = s["shared"]
+    gate = s["gate"].float().repeat_interleave(shared, 0)[:s["tokens"]]
+    post, pre = s["post"].float(), s["pre"].float()
+    nb, ib = _normed(s["block"].float(), c)
+    x = (s["x"].float() + s["scale"] * gate * (nb * post)).to(u)
+    nx, ix = _normed(x.float(), c)
+    h = nx * pre
+    h = _values(*_quantise(h, 0), 0).to(t) if s["quantize"] else h.to(t)
+    if not s["train"]:
+        return [x, h]
+    dh = s["dh"].float()
+    dx = s["dx"].float() + _norm_back(dh * pre, nx, ix, c)
+    d = s["scale"] * dx
+    db = _norm_back(d * gate * post, nb, ib, c)
+    dgate = d * nb * post
+    if shared > 1:
+        dgate = torch.nn.functional.pad(dgate, (0, 0, 0, -s["tokens"] % shared)).view(-1, shared, s["width"]).sum(1)
+    return [x, h, dx.to(u), db.to(t), dgate.to(t), (d * gate * nb).sum(0), (dh * nx).sum(0)]
+
+
+# ---- the framework's operators ----------------------------------------------------------------------------------------------
+
+def _own(s):
+    from paper_2501_02379_amd import act8, norms
+    if s["op"] == "linear":
+        return [act8.tgrad_int8_linear(s["x"], act8.Codes(s["w"], s["w_scale"], 0)).y]
+    if s["op"] == "gradients":
+        dx = act8.tgrad_int8_grad_input(s["dy"], act8.Codes(s["w"], s["w_scale"], 0))
+        return [dx, act8.tgrad_int8_grad_weight(s["dy"], act8.Codes(s["x8"], s["x_scale"], 0))]
+    if s["op"] == "activation":
+        a = act8.tgrad_activation(s["x"], s["gate"], act=s["act"], group=s["group"], quantize=s["quantize"])
+        y = act8.tgrad_dequantize(a.y, s["x"].dtype) if s["quantize"] else a.y
+        dx, dgate = act8.tgrad_activation_backward(s["dy"], a.x8, a.gate8, act=s["act"])
+        return [y, dx, dgate] if s["gated"] else [y, dx]
+    shared = {"gate": s["gate"], "rows_per_gate": s["shared"], "scale": s["scale"], "post_weight": s["post"], "pre_weight": s["pre"],
+              "centered": s["centered"]}
+    r = norms.tgrad_block_norm(s["x"], s["block"], eps=EPS, quantize=s["quantize"], **shared)
+    h = act8.tgrad_dequantize(r.h, s["block"].dtype) if s["quantize"] else r.h
+    if not s["train"]:
+        return [r.x, h]
+    g = norms.tgrad_block_norm_backward(s["dx"], s["dh"], r.x, s["block"], stats=r.stats, **shared)
+    return [r.x, h, g.dx, g.dblock, g.dgate, g.dpost, g.dpre]
+
+
+def run(state):
+    if own:
+        return _own(state)
+    return {"linear": _plain_linear, "gradients": _plain_gradients, "activation": _plain_activation, "norm": _plain_norm}[state["op"]](state)
+
+
+# ---- what a pass cannot do without ------------------------------------------------------------------------------------------
+
+def work(case):
+    b = BYTES[case["dtype"]]
+    if case["op"] in ("linear", "gradients"):
+        n, k, m = case["tokens"], case["inner"], case["outer"]
+        if case["op"] == "linear":
+            return {"bytes": n * k * b + m * k + 4 * m + n * m * b, "flops": 2 * n * k * m}
+        return {"bytes": n * m * b + n * k + m * k + 4 * (n + m) + (n * k + m * k) * b, "flops": 4 * n * k * m}
+    n = case["tokens"]
+    if case["op"] == "activation":
+        f = case["width"]
+        parts = 2 if case["gated"] else 1
+        return {"bytes": n * f * b * (2 * parts + 2), "flops": 30 * n * f * parts}
+    d = case["width"]
+    u, w = BYTES[case["stream"]], BYTES[case["weights"]]
+    gate = -(-n // case["shared"]) * d * b
+    forward = n * d * (2 * u + 2 * b) + gate + 2 * d * w
+    backward = n * d * (2 * u + 2 * b) + gate + 8 * d if case["train"] else 0
+    return {"bytes": forward + backward, "flops": n * d * (40 if case["train"] else 14)}
+
+
+# ---- the definitions in 64 bits ---------------------------------------------------------------------------------------------
+
+def _exact_codes(x, group=0):
+    """What the codes of x stand for: steps of the largest magnitude / 127, the scale held in 32 bits."""
+    x = x.double()
+    out = torch.empty_like(x)
+    step = group or max(1, x.shape[1])
+    for a in range(0, x.shape[1], step):
+        part = x[:, a:a + step]
+        top = part.abs().max(1, keepdim=True).values
+        code = (127 * part / top.clamp(min=1e-300)).round()
+        out[:, a:a + step] = code * (top / 127).float().double()
+    return out
+
+
+def _exact_held(s, codes, scale):
+    return s[codes].double() * s[scale].double()
+
+
+def _exact_act(name, x):
+    if name == "silu":
+        y = x * torch.sigmoid(x)
+        return y, torch.sigmoid(x) + y * torch.sigmoid(-x)
+    cdf = torch.special.ndtr(x)
+    return x * cdf, cdf + x * (-0.5 * x ** 2).exp() * (2 * math.pi) ** -0.5
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "linear":
+        return [_exact_codes(s["x"]) @ _exact_held(s, "w", "w_scale").t().contiguous()]
+    if case["op"] == "gradients":
+        dy = s["dy"].double()
+        return [dy @ _exact_held(s, "w", "w_scale"), dy.t().contiguous() @ _exact_held(s, "x8", "x_scale")]
+    if case["op"] == "activation":
+        f, gate = _exact_act(case["act"], s["x"].double())[0], s["gate"]
+        y = f if gate is None else f * gate.double()
+        if case["quantize"]:
+            y = _exact_codes(y)
+        f, slope = _exact_act(case["act"], _exact_codes(s["x"], case["group"]))
+        dy = s["dy"].double()
+        if gate is None:
+            return [y, dy * slope]
+        return [y, dy * slope * _exact_codes(gate, case["group"]), dy * f]
+    n, shared = case["tokens"], case["shared"]
+    gate = s["gate"].double()[torch.arange(n, device=DEV) // shared]
+    post, pre, b = s["post"].double(), s["pre"].double(), s["block"].double()
+
+    def spread(v):
+        mean = v.mean(1, keepdim=True) if case["centered"] else torch.zeros(len(v), 1, dtype=v.dtype, device=DEV)
+        return mean, ((v - mean).pow(2).mean(1, keepdim=True) + EPS).pow(-0.5)
+
+    mb, rb = spread(b)
+    unit_b = (b - mb) * rb
+    x = s["x"].double() + 0.7 * gate * post * unit_b
+    held = x.to(TYPES[case["stream"]]).double()            # what the stream holds is what the next norm reads
+    mx, rx = spread(held)
+    unit_x = (held - mx) * rx
+    h = _exact_codes(unit_x * pre) if case["quantize"] else unit_x * pre
+    if not case["train"]:
+        return [x, h]
+
+    def through(grad, unit, r):
+        off = grad.mean(1, keepdim=True) if case["centered"] else 0.0
+        return r * (grad - off - unit * (grad * unit).mean(1, keepdim=True))
+
+    dh = s["dh"].double()
+    dx = s["dx"].double() + through(dh * pre, unit_x, rx)
+    dgate = torch.zeros_like(s["gate"], dtype=torch.float64).index_add_(0, torch.arange(n, device=DEV) // shared, 0.7 * dx * post * unit_b)
+    return [x, h, dx, through(0.7 * dx * gate * post, unit_b, rb), dgate, (0.7 * dx * gate * unit_b).sum(0), (dh * unit_x).sum(0)]

@@ -249,10 +249,10 @@ def _plain_norm(s):
 def _own(s):
     from paper_2501_02379_amd import act8, norms
     if s["op"] == "linear":
-        return [act8.tgrad_int8_linear(s["x"], act8.Codes(s["w"], s["w_scale"], 0)).y]
+        return [act8.tgrad_codes_linear(s["x"], act8.Codes(s["w"], s["w_scale"], 0)).y]
     if s["op"] == "gradients":
-        dx = act8.tgrad_int8_grad_input(s["dy"], act8.Codes(s["w"], s["w_scale"], 0))
-        return [dx, act8.tgrad_int8_grad_weight(s["dy"], act8.Codes(s["x8"], s["x_scale"], 0))]
+        dx = act8.tgrad_codes_grad_input(s["dy"], act8.Codes(s["w"], s["w_scale"], 0))
+        return [dx, act8.tgrad_codes_grad_weight(s["dy"], act8.Codes(s["x8"], s["x_scale"], 0))]
     if s["op"] == "activation":
         a = act8.tgrad_activation(s["x"], s["gate"], act=s["act"], group=s["group"], quantize=s["quantize"])
         y = act8.tgrad_dequantize(a.y, s["x"].dtype) if s["quantize"] else a.y

@@ -504,6 +504,147 @@ int tgrad_preference_loss(const tgrad_logits* logits, const tgrad_preference* pr
                           void* workspace_dev, float* loss, float* rewards, float* logp, void* dlogits,
                           int64_t dlogits_stride, void* hip_stream);
 
+/*
+ * ---- A block of the model in 8 bits: its products, what it keeps for the backward pass, the norms around it ----------------
+ *
+ * With the optimizer's moments compressed, a training step's memory is its activations.  These calls keep them as 8-bit codes that
+ * the forward products are taken of and that the backward pass reads as they are.  Each takes the stream to enqueue on
+ * (NULL = the default stream), waits for nothing and allocates nothing; outputs overlap neither each other nor inputs unless it is said.
+ */
+
+/* rows x cols numbers.  Rows of consecutive elements, any alignment of the element type. */
+typedef struct {
+  void* data;           /* device pointer; may be NULL where rows is 0 */
+  int64_t rows;         /* 0..2^31-1 */
+  int64_t cols;         /* 1..2^30 */
+  int64_t row_stride;   /* elements from one row to the next, >= cols; what lies between rows is neither read nor written */
+  int32_t dtype;        /* TGRAD_F32, TGRAD_BF16 or TGRAD_F16 */
+} tgrad_matrix;
+
+/*
+ * rows x cols numbers in 8 bits: value = code * scale (in float32).  With a the largest magnitude of a group, scale = a / 127 and code =
+ * 127 v / a, the exact quotient rounded to nearest even: -127..127.  (Scales end where 127 times one is finite.)  A group whose largest magnitude is below 2^-119 is all
+ * zeros, with scale 0; one with an infinity or NaN in it has scale NaN and codes 0, so that all its values are NaN.
+ */
+typedef struct {
+  void* codes;          /* device pointer, int8; rows that start at multiples of 16 bytes are read fastest */
+  float* scale;         /* device pointer, float32[rows][ceil(cols / group)], dense */
+  int64_t rows, cols;   /* as above */
+  int64_t row_stride;   /* bytes from one row to the next, >= cols */
+  int32_t group;        /* columns that share a scale, counted from a row's first: 32, 64, 128, 256, 512; 0: the whole row */
+} tgrad_codes;
+
+/* Codes and scales of x.  x and out have the same rows and cols.  Errors: INVALID_ARG, HIP. */
+int tgrad_quantize(const tgrad_matrix* x, const tgrad_codes* out, void* hip_stream);
+
+/* The values that codes stand for, rounded once to out's type.  Errors: INVALID_ARG, HIP. */
+int tgrad_dequantize(const tgrad_codes* codes, const tgrad_matrix* out, void* hip_stream);
+
+enum { TGRAD_CODES_MATMUL = 0, TGRAD_CODES_LINEAR = 1, TGRAD_CODES_GRAD_INPUT = 2, TGRAD_CODES_GRAD_WEIGHT = 3 };
+#define TGRAD_CODES_MAX_INNER 131072   /* longest sum of products of codes that int32 holds: 127^2 2^17 < 2^31 */
+
+/* Bytes of scratch of the four calls below, for tokens x inner times inner x outer.  Host-only.  Errors: INVALID_ARG. */
+int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes);
+
+/*
+ * y[t, n] = x.scale[t] w.scale[n] sum_k x.code[t, k] w.code[n, k].  The sum is exact (int32); it is converted and multiplied in float32
+ * and rounded once to y's type.
+ *  x              tokens x inner, group 0; inner <= TGRAD_CODES_MAX_INNER.  Codes are -127..127, as tgrad_quantize writes them.
+ *  w              outer x inner, group 0: the weight, a row for each output.
+ *  y              tokens x outer.
+ *  workspace_dev  device pointer, >= tgrad_codes_query_size, 256-byte aligned.
+ * Errors: INVALID_ARG, UNSUPPORTED (inner), HIP.
+ */
+int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* workspace_dev, void* hip_stream);
+
+/*
+ * tgrad_quantize of x into `keep` (group 0), then tgrad_codes_matmul of it, with the same results; for a few tokens in one launch.
+ *  keep   receives the codes of x, for the backward pass.  NULL: not kept.
+ */
+int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_codes* keep, const tgrad_matrix* y,
+                      void* workspace_dev, void* hip_stream);
+
+/*
+ * The product's gradients, with the gradient of a code's value taken as that of the number it was made from:
+ *   dx[t, k] = sum_n dy[t, n] w[n, k]     dw[n, k] = sum_t dy[t, n] x[t, k]
+ * w and x are the values of codes, in groups of any size.  bf16 and float16: values are rounded to dy's type (a value beyond float16's
+ * range is infinite), products are exact and added up in float32.  float32: dy times a code's scale is split into three bf16 parts, which keep 24 bits (below
+ * 2^-110 the last ones are lost; an infinity becomes NaN), codes are exact.
+ *  dx, dw  dy's type, or TGRAD_F32; rounded once.  The order of the sums depends on the sizes alone.
+ *  workspace_dev  as above.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream);
+int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream);
+
+enum { TGRAD_ACT_SILU = 0, TGRAD_ACT_GELU = 1 };   /* x / (1 + exp(-x)); x (1 + erf(x / sqrt(2))) / 2 */
+
+/*
+ * y = act(x), or act(x) * gate, in float32, and the checkpoint that its backward pass needs.
+ *  gate       the same size and type as x, or NULL.
+ *  y, y8      one of them: the result in x's type, or as codes for the next product (group 0).
+ *  x8, gate8  receive the codes of x and gate, in groups of 32..512 columns.  Both NULL: no checkpoint; gate8 goes with gate.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_activation(const tgrad_matrix* x, const tgrad_matrix* gate, int act, const tgrad_matrix* y, const tgrad_codes* y8,
+                     const tgrad_codes* x8, const tgrad_codes* gate8, void* hip_stream);
+
+/*
+ * dx = dy act'(x) [* gate] and dgate = dy act(x), of the values that the checkpoint stands for.
+ *  gate8, dgate  both or neither.  dx and dgate have dy's size and type.
+ * Errors: INVALID_ARG, HIP.
+ */
+int tgrad_activation_backward(const tgrad_matrix* dy, const tgrad_codes* x8, const tgrad_codes* gate8, int act, const tgrad_matrix* dx,
+                              const tgrad_matrix* dgate, void* hip_stream);
+
+/* The norms after and before a block and what joins them.  norm(v) = (v - m) / sqrt(mean((v - m)^2) + eps), m = mean(v) or 0. */
+typedef struct {
+  const void* post_weight;   /* device pointer, [cols]: norm of the block's output; NULL: the output goes in as it is */
+  const void* pre_weight;    /* device pointer, [cols]: norm of the sum, for the next block; NULL: none */
+  const void* gate;          /* device pointer, [ceil(rows / rows_per_gate)][cols], the block's type; NULL: 1 */
+  int64_t gate_stride;       /* elements from one row of the gate to the next, >= cols */
+  int64_t rows_per_gate;     /* >= 1: rows 0 .. rows_per_gate - 1 take the gate's first row, and so on */
+  int32_t weight_dtype;      /* type of both weights */
+  float scale;               /* of the residual branch; finite */
+  float eps;                 /* > 0 */
+  int32_t centered;          /* 1: m is the mean; 0: m = 0 */
+} tgrad_block;
+#define TGRAD_NORM_MAX_COLS 32768
+
+/*
+ * x_out = x + scale * gate * (norm(block) * post_weight), rounded to the stream's type;  h = norm(x_out) * pre_weight.
+ *  x, x_out  the residual stream before and after: float32, or the block's type.
+ *  block     the block's output.  NULL: h = norm(x) * pre_weight alone; x_out, post_weight and gate are NULL then.
+ *  h, h8     one of them where there is a pre_weight: the next block's input in the block's type, or as codes (group 0).
+ *  stats     device pointer, float32[rows][4]: mean and factor 1 / sqrt(...) of the block's norm and of the sum's, for the
+ *            backward pass; NULL: not kept.
+ * Statistics are float32.  Errors: INVALID_ARG, UNSUPPORTED (cols > TGRAD_NORM_MAX_COLS), HIP.
+ */
+int tgrad_block_norm(const tgrad_block* desc, const tgrad_matrix* x, const tgrad_matrix* block, const tgrad_matrix* x_out,
+                     const tgrad_matrix* h, const tgrad_codes* h8, float* stats, void* hip_stream);
+
+/* Bytes of scratch of tgrad_block_norm_backward; rows_per_gate: 1 without a gate.  Host-only.  Errors: INVALID_ARG, UNSUPPORTED. */
+int tgrad_block_norm_query_size(int64_t rows, int64_t cols, int64_t rows_per_gate, size_t* workspace_bytes);
+
+/*
+ * Gradients of tgrad_block_norm, for d = its gradient with respect to x_out (all of it, h's share among it):
+ *   dx = d = dx_out + norm'(dh * pre_weight),  dblock = norm'(scale * d * gate * post_weight),
+ *   dgate = sum over its rows of scale * d * norm(block) * post_weight,  dpost = sum of scale * d * gate * norm(block),
+ *   dpre = sum of dh * norm(x_out).
+ *  dx_out  gradient with respect to x_out from elsewhere, the stream's type; NULL: none.
+ *  dh      gradient with respect to h; NULL where there is no pre_weight.
+ *  x_out   as the forward call left it (its x, where there was no block).
+ *  stats   as the forward call left them.
+ *  dx, dblock  the stream's and the block's type; dblock NULL without a block.  dx may be dx_out, with the same stride.
+ *  dgate   the gate's size and type, rows of cols elements, dense; NULL without a gate.
+ *  dpost, dpre   device pointers, float32[cols]; NULL without their weights.
+ *  workspace_dev  device pointer, >= tgrad_block_norm_query_size, 256-byte aligned.
+ * The order of the sums depends on the sizes alone.  Errors: INVALID_ARG, UNSUPPORTED, HIP.
+ */
+int tgrad_block_norm_backward(const tgrad_block* desc, const tgrad_matrix* dx_out, const tgrad_matrix* dh, const tgrad_matrix* x_out,
+                              const tgrad_matrix* block, const float* stats, const tgrad_matrix* dx, const tgrad_matrix* dblock,
+                              void* dgate, float* dpost, float* dpre, void* workspace_dev, void* hip_stream);
+
 /* Static description of a status code. */
 const char* tgrad_strerror(int status);
 

@@ -22,21 +22,28 @@ def used_on(stream, tensors):
             t.record_stream(stream)
 
 
-def on_stream(f):
-    """Adds `stream=`: the call runs with that stream current, so that what it allocates belongs to it (memory of another stream's
-    could still be in use there, and scratch could be handed out again before the kernels have run)."""
-    @functools.wraps(f)
-    def run(*args, stream=None, **kw):
-        if stream is None:
-            return f(*args, **kw)
-        for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != stream.device:
-                refuse("stream: one of the logits' device")
-        with torch.cuda.stream(stream):
-            result = f(*args, **kw)
-        used_on(stream, (*args, *kw.values()))
-        return result
-    return run
+def on_stream_with(parts):
+    """A decorator that adds `stream=`: the call runs with that stream current, so that what it allocates belongs to it (memory of another
+    stream's could still be in use there, and scratch could be handed out again before the kernels have run).  `parts(argument)`: the
+    tensors of an argument that is none itself."""
+    def add(f):
+        @functools.wraps(f)
+        def run(*args, stream=None, **kw):
+            if stream is None:
+                return f(*args, **kw)
+            given = [t for a in (*args, *kw.values()) for t in ((a,) if isinstance(a, torch.Tensor) else parts(a))]
+            for t in given:
+                if t.is_cuda and t.device != stream.device:
+                    refuse("stream: one of the arguments' device")
+            with torch.cuda.stream(stream):
+                result = f(*args, **kw)
+            used_on(stream, given)
+            return result
+        return run
+    return add
+
+
+on_stream = on_stream_with(lambda a: ())
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)

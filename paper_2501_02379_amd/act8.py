@@ -1,0 +1,248 @@
+"""Activations and weights in 8 bits: ctypes binding of the quantising, product and activation entry points of include/tgrad.h.
+
+Matrices are 2-D tensors on the GPU, float32, bfloat16 or float16, with dense rows (any stride from row to row).  A call enqueues
+its kernels on the device's current stream, or on `stream=`, and waits for nothing; outputs and scratch come from torch's
+allocator on that stream, and with `stream=` the arguments are recorded on it, so that they may be let go of at once.
+
+A linear layer trained in 8 bits, with its activation:
+
+    h = tgrad_codes_linear(x, w, keep=True)                    # h.y, and h.x8: what the backward pass needs of x
+    a = tgrad_activation(h.y, act="silu", quantize=True)      # a.y: codes for the next product; a.x8: the checkpoint of h.y
+    ...
+    dh, _ = tgrad_activation_backward(da, a.x8, act="silu")
+    dx, dw = tgrad_codes_grad_input(dh, w), tgrad_codes_grad_weight(dh, h.x8)
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import tgrad as T
+from ._marshal import REAL_TYPES, call, on_stream_with, refuse, stream_of
+
+ACTS = {"silu": T.TGRAD_ACT_SILU, "gelu": T.TGRAD_ACT_GELU}
+
+
+class Codes(NamedTuple):
+    """rows x cols numbers in 8 bits: codes * scale, a scale for `group` columns (0: for the whole row)."""
+    codes: torch.Tensor                   # int8[rows, cols], dense rows
+    scale: torch.Tensor                   # float32[rows, ceil(cols / group)], dense
+    group: int = 0
+
+
+class Linear(NamedTuple):
+    y: torch.Tensor
+    x8: Optional[Codes]
+
+
+class Activation(NamedTuple):
+    y: object                             # a tensor, or Codes where it was asked to quantize
+    x8: Optional[Codes]
+    gate8: Optional[Codes]
+
+
+def describe(x, what, like=None, rows=None, cols=None, dtype=None):
+    """A matrix as the library takes it; anything it does not take is refused."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in REAL_TYPES or not x.is_cuda:
+        refuse(what + ": a 2-D float32, bfloat16 or float16 tensor on the GPU")
+    n, m = x.shape
+    if (m > 1 and x.stride(1) != 1 and n > 0) or x.is_neg():               # memory holds other numbers than a tensor with that pending
+        refuse(what + ": dense rows, no pending negation")
+    if like is not None and x.device != like.device:
+        refuse(what + ": on the other tensors' device")
+    if (rows is not None and n != rows) or (cols is not None and m != cols) or (dtype is not None and x.dtype is not dtype):
+        refuse("%s: %s x %s%s" % (what, "rows" if rows is None else rows, "cols" if cols is None else cols, "" if dtype is None else " of %s" % dtype))
+    return T.tgrad_matrix(x.data_ptr(), n, m, x.stride(0) if n > 1 else m, REAL_TYPES[x.dtype])
+
+
+def describe_codes(c, what, like=None, rows=None, cols=None):
+    if not isinstance(c, Codes) or not isinstance(c.codes, torch.Tensor) or not isinstance(c.scale, torch.Tensor):
+        refuse(what + ": Codes")
+    q, s, g = c
+    if q.dim() != 2 or q.dtype is not torch.int8 or not q.is_cuda or (q.shape[1] > 1 and q.stride(1) != 1 and q.shape[0] > 0):
+        refuse(what + ": int8 codes on the GPU, 2-D, dense rows")
+    n, m = q.shape
+    if s.dtype is not torch.float32 or s.device != q.device or not s.is_contiguous() or s.is_neg() or \
+            s.numel() != n * (1 if not g else -(-m // g) if g > 0 else -1):
+        refuse(what + ": float32 scales, dense, one for each group of columns of each row, on the codes' device, no pending negation")
+    if like is not None and q.device != like.device:
+        refuse(what + ": on the other tensors' device")
+    if (rows is not None and n != rows) or (cols is not None and m != cols):
+        refuse("%s: %s x %s" % (what, "rows" if rows is None else rows, "cols" if cols is None else cols))
+    return T.tgrad_codes(q.data_ptr(), s.data_ptr(), n, m, q.stride(0) if n > 1 else m, g)
+
+
+def new_codes(rows, cols, group, device) -> Codes:
+    """Memory for codes, rows at multiples of 16 bytes."""
+    pitch = -(-cols // 16) * 16
+    codes = torch.empty(rows, pitch, dtype=torch.int8, device=device)
+    return Codes(codes[:, :cols] if pitch != cols else codes,
+                 torch.empty(rows, -(-cols // group) if group else 1, dtype=torch.float32, device=device), group)
+
+
+def _result(out, what, like, rows, cols, dtype):
+    """`out`, checked, or a new tensor, and its description."""
+    if out is None:
+        out = torch.empty(rows, cols, dtype=dtype, device=like.device)
+    return out, describe(out, what, like, rows, cols, dtype)
+
+
+@functools.lru_cache(maxsize=4096)
+def _scratch_bytes(op, tokens, inner, outer):
+    n = C.c_size_t(0)
+    rc = T.load().tgrad_codes_query_size(op, tokens, inner, outer, C.byref(n))
+    if rc != T.TGRAD_OK:
+        raise T.TgradError(rc, "tgrad_codes_query_size")
+    return n.value
+
+
+def _scratch(op, tokens, inner, outer, device):
+    return torch.empty(_scratch_bytes(op, tokens, inner, outer), dtype=torch.uint8, device=device)
+
+
+def _group(group):
+    if group not in (0, 32, 64, 128, 256, 512):
+        refuse("group: 0 (the whole row), 32, 64, 128, 256 or 512 columns")
+    return group
+
+
+def _act(act):
+    if act not in ACTS:
+        refuse("act: one of " + ", ".join(ACTS))
+    return ACTS[act]
+
+
+_on_stream = on_stream_with(lambda a: [t for t in a if isinstance(t, torch.Tensor)] if isinstance(a, Codes) else ())
+
+
+@_on_stream
+def tgrad_quantize(x, *, group: int = 0, out: Optional[Codes] = None) -> Codes:
+    """x in 8 bits, a scale for `group` columns (0: the whole row).  `out`: where the codes go."""
+    d = describe(x, "x")
+    if out is None:
+        out = new_codes(d.rows, d.cols, _group(group), x.device)
+    elif isinstance(out, Codes) and out.group != group:
+        refuse("out: codes in groups of `group` columns")
+    call(x.device, T.load().tgrad_quantize, "tgrad_quantize", C.byref(d), C.byref(describe_codes(out, "out", x, d.rows, d.cols)),
+         stream_of(x.device))
+    return out
+
+
+@_on_stream
+def tgrad_dequantize(codes: Codes, dtype=torch.float32, *, out=None):
+    """The values that codes stand for, rounded once to `dtype`."""
+    c = describe_codes(codes, "codes")
+    if dtype not in REAL_TYPES:
+        refuse("dtype: float32, bfloat16 or float16")
+    out, d = _result(out, "out", codes.codes, c.rows, c.cols, dtype)
+    call(out.device, T.load().tgrad_dequantize, "tgrad_dequantize", C.byref(c), C.byref(d), stream_of(out.device))
+    return out
+
+
+@_on_stream
+def tgrad_codes_matmul(x: Codes, weight: Codes, *, dtype=torch.bfloat16, out=None):
+    """x (tokens x inner) times weight (outer x inner) transposed, both codes with a scale a row: tokens x outer in `dtype`."""
+    c = describe_codes(x, "x")
+    w = describe_codes(weight, "weight", x.codes, cols=c.cols)
+    if dtype not in REAL_TYPES:
+        refuse("dtype: float32, bfloat16 or float16")
+    dev = x.codes.device
+    y, d = _result(out, "out", x.codes, c.rows, w.rows, dtype)
+    ws = _scratch(T.TGRAD_CODES_MATMUL, c.rows, c.cols, w.rows, dev)
+    call(dev, T.load().tgrad_codes_matmul, "tgrad_codes_matmul", C.byref(c), C.byref(w), C.byref(d), ws.data_ptr(), stream_of(dev))
+    return y
+
+
+@_on_stream
+def tgrad_codes_linear(x, weight: Codes, *, keep: bool = False, dtype=None, out=None) -> Linear:
+    """x in 8 bits, a scale for each token, times weight transposed.  keep: x's codes come back too, for the backward pass.  `dtype`: of
+    the result (x's)."""
+    d = describe(x, "x")
+    w = describe_codes(weight, "weight", x, cols=d.cols)
+    dev = x.device
+    dtype = dtype or x.dtype
+    if dtype not in REAL_TYPES:
+        refuse("dtype: float32, bfloat16 or float16")
+    y, e = _result(out, "out", x, d.rows, w.rows, dtype)
+    x8 = new_codes(d.rows, d.cols, 0, dev) if keep else None
+    ws = _scratch(T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows, dev)
+    call(dev, T.load().tgrad_codes_linear, "tgrad_codes_linear", C.byref(d), C.byref(w), C.byref(describe_codes(x8, "keep")) if keep else None,
+         C.byref(e), ws.data_ptr(), stream_of(dev))
+    return Linear(y, x8)
+
+
+@_on_stream
+def tgrad_codes_grad_input(dy, weight: Codes, *, dtype=None, out=None):
+    """Gradient of a product with respect to its input: dy (tokens x outer) times the values of weight (outer x inner).  `dtype`: of the
+    result, dy's or float32."""
+    return _gradient("tgrad_codes_grad_input", T.TGRAD_CODES_GRAD_INPUT, dy, weight, dtype, out)
+
+
+@_on_stream
+def tgrad_codes_grad_weight(dy, x: Codes, *, dtype=None, out=None):
+    """Gradient of a product with respect to its weight: dy (tokens x outer) transposed, times the values of x (tokens x inner)."""
+    return _gradient("tgrad_codes_grad_weight", T.TGRAD_CODES_GRAD_WEIGHT, dy, x, dtype, out)
+
+
+def _gradient(name, op, dy, codes, dtype, out):
+    d = describe(dy, "dy")
+    dev = dy.device
+    dtype = dtype or dy.dtype
+    if dtype not in (dy.dtype, torch.float32):
+        refuse("dtype: dy's or float32")
+    if op == T.TGRAD_CODES_GRAD_INPUT:
+        c = describe_codes(codes, "weight", dy, rows=d.cols)
+        tokens, outer, rows = d.rows, c.rows, d.rows
+    else:
+        c = describe_codes(codes, "x", dy, rows=d.rows)
+        tokens, outer, rows = d.rows, d.cols, d.cols
+    out, e = _result(out, "out", dy, rows, c.cols, dtype)
+    ws = _scratch(op, tokens, c.cols, outer, dev)
+    call(dev, getattr(T.load(), name), name, C.byref(d), C.byref(c), C.byref(e), ws.data_ptr(), stream_of(dev))
+    return out
+
+
+@_on_stream
+def tgrad_activation(x, gate=None, *, act: str = "silu", group: int = 128, keep: bool = True, quantize: bool = False,
+                     out=None) -> Activation:
+    """act(x), or act(x) * gate, with the checkpoint of x and gate in 8 bits (`keep`), in groups of `group` columns.  quantize: the
+    result as codes with a scale a row, for the next product.  act: "silu" or "gelu" (with erf)."""
+    d = describe(x, "x")
+    dev, code = x.device, _act(act)
+    g = describe(gate, "gate", x, d.rows, d.cols, x.dtype) if gate is not None else None
+    if keep and not _group(group):
+        refuse("group: 32, 64, 128, 256 or 512 columns")
+    if quantize:
+        y = new_codes(d.rows, d.cols, 0, dev) if out is None else out
+        e = describe_codes(y, "out", x, d.rows, d.cols)
+    else:
+        y, e = _result(out, "out", x, d.rows, d.cols, x.dtype)
+    x8 = new_codes(d.rows, d.cols, group, dev) if keep else None
+    gate8 = new_codes(d.rows, d.cols, group, dev) if keep and g is not None else None
+    ref = lambda c: C.byref(describe_codes(c, "checkpoint")) if c is not None else None  # noqa: E731
+    call(dev, T.load().tgrad_activation, "tgrad_activation", C.byref(d), C.byref(g) if g is not None else None, code,
+         None if quantize else C.byref(e), C.byref(e) if quantize else None, ref(x8), ref(gate8), stream_of(dev))
+    return Activation(y, x8, gate8)
+
+
+@_on_stream
+def tgrad_activation_backward(dy, x8: Codes, gate8: Optional[Codes] = None, *, act: str = "silu", out=None, gate_out=None):
+    """-> (dx, dgate) from the checkpoint; dgate is None where there was no gate."""
+    d = describe(dy, "dy")
+    dev, code = dy.device, _act(act)
+    c = describe_codes(x8, "x8", dy, d.rows, d.cols)
+    dx, e = _result(out, "out", dy, d.rows, d.cols, dy.dtype)
+    if gate8 is None:
+        if gate_out is not None:
+            refuse("gate_out: only with gate8")
+        call(dev, T.load().tgrad_activation_backward, "tgrad_activation_backward", C.byref(d), C.byref(c), None, code, C.byref(e), None,
+             stream_of(dev))
+        return dx, None
+    b = describe_codes(gate8, "gate8", dy, d.rows, d.cols)
+    dgate, f = _result(gate_out, "gate_out", dy, d.rows, d.cols, dy.dtype)
+    call(dev, T.load().tgrad_activation_backward, "tgrad_activation_backward", C.byref(d), C.byref(c), C.byref(b), code, C.byref(e),
+         C.byref(f), stream_of(dev))
+    return dx, dgate

@@ -1,0 +1,268 @@
+// What the files of a block in 8 bits share (act8.hip, norms.hip, int8mm.hip): matrices and codes as kernels see them, rows in units of eight
+// numbers, the rounding of a code, checks of arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "launch_util.h"
+#include "train_common.h"
+
+namespace tgrad {
+
+constexpr size_t kScratchAlign = 256;
+
+struct Mat {
+  char* data;
+  int64_t stride;                         // bytes from one row to the next
+  __device__ __forceinline__ char* row(int64_t r) const { return data + r * stride; }
+};
+
+struct Codes8 {
+  int8_t* codes;
+  float* scale;
+  int64_t stride;
+  int64_t groups;                         // scales of a row
+  int shift;                              // log2 of a group's columns; 31: the whole row
+};
+
+typedef Duo DuoByte __attribute__((aligned(1)));
+typedef Quad QuadByte __attribute__((aligned(1)));
+
+// Eight consecutive numbers of a real type, as they lie in memory.
+template <int DT> struct Eight {
+  typedef typename Elem<DT>::raw raw;
+  static constexpr int kQuads = DT == TGRAD_F32 ? 2 : 1;
+  Quad q[kQuads];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kQuads; ++i) q[i] = Quad{0, 0, 0, 0};
+  }
+  // `n` of them are there (at least 8: all); the others count as 0.
+  __device__ __forceinline__ void load(const char* at, int n) {
+    const raw* p = reinterpret_cast<const raw*>(at);
+    if (n >= 8) {
+#pragma unroll
+      for (int i = 0; i < kQuads; ++i) q[i] = reinterpret_cast<const QuadAny*>(p)[i];
+    } else {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = i < n ? Elem<DT>::widen(p[i]) : 0.f;
+      set(f);
+    }
+  }
+  __device__ __forceinline__ void store(char* at, int n) const {
+    raw* p = reinterpret_cast<raw*>(at);
+    if (n >= 8) {
+#pragma unroll
+      for (int i = 0; i < kQuads; ++i) reinterpret_cast<QuadAny*>(p)[i] = q[i];
+    } else {
+      float f[8];
+      get(f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < n) p[i] = Elem<DT>::narrow(f[i]);
+    }
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    if constexpr (DT == TGRAD_F32) {
+      Four<DT>::widen(q[0], f);
+      Four<DT>::widen(q[1], f + 4);
+    } else {
+      Four<DT>::widen(Duo{q[0][0], q[0][1]}, f);
+      Four<DT>::widen(Duo{q[0][2], q[0][3]}, f + 4);
+    }
+  }
+  __device__ __forceinline__ void set(const float* f) {
+    if constexpr (DT == TGRAD_F32) {
+      q[0] = Four<DT>::narrow(f);
+      q[1] = Four<DT>::narrow(f + 4);
+    } else {
+      const Duo a = Four<DT>::narrow(f), b = Four<DT>::narrow(f + 4);
+      q[0] = Quad{a[0], a[1], b[0], b[1]};
+    }
+  }
+};
+
+// Eight numbers of a vector whose type is known at run time only (the same for every thread).
+__device__ __forceinline__ void load_weights(const void* w, int dt, int64_t at, int n, float* f) {
+  if (dt == TGRAD_F32) {
+    Eight<TGRAD_F32> e;
+    e.load(static_cast<const char*>(w) + at * 4, n);
+    e.get(f);
+  } else if (dt == TGRAD_BF16) {
+    Eight<TGRAD_BF16> e;
+    e.load(static_cast<const char*>(w) + at * 2, n);
+    e.get(f);
+  } else {
+    Eight<TGRAD_F16> e;
+    e.load(static_cast<const char*>(w) + at * 2, n);
+    e.get(f);
+  }
+}
+
+// The bits of the largest magnitude: magnitudes order like their bit patterns, with infinity and then NaN above all numbers.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+__device__ __forceinline__ uint32_t largest(const float* f) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = max(m, magnitude(f[i]));
+  return m;
+}
+// ... over neighbouring lanes, `lanes` a power of two up to 64
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t m, int lanes) {
+  for (int d = 1; d < lanes; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+  return m;
+}
+// ... over a workgroup of WAVES wavefronts
+template <int WAVES>
+__device__ __forceinline__ uint32_t largest_of_block(uint32_t m, uint32_t* lds) {
+  m = largest_of_lanes(m, kWave);
+  if constexpr (WAVES == 1) return m;
+  __syncthreads();
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = m;
+  __syncthreads();
+  m = lds[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) m = max(m, lds[w]);
+  return m;
+}
+
+// How a group is rounded, from the bits of its largest magnitude a.  The factor 127 / a is finite and normal where a is 2^-119 at least.
+struct Rounding {
+  float scale, factor, top;
+};
+__device__ __forceinline__ Rounding rounding_of(uint32_t top_bits) {
+  const float a = __uint_as_float(top_bits);
+  Rounding r;
+  r.top = a;
+  if (top_bits >= 0x7F800000u) {          // an infinity or NaN
+    r.scale = __uint_as_float(0x7FC00000u);
+    r.factor = 0.f;
+  } else if (a < 0x1p-119f) {
+    r.scale = 0.f;
+    r.factor = 0.f;
+  } else {
+    r.scale = fminf(a / 127.f, 0x1.0204060000000p+121f);      // the largest scale with a finite 127 * scale: a / 127 rounds up at float32's end
+    r.factor = 127.f / a;
+  }
+  return r;
+}
+
+// The code of v: 127 v / a, rounded to nearest even as the exact quotient is.  v * factor is off by two roundings, 127 * 2^-23 = 1.6e-5 of
+// a code at most, so it decides but for quotients within 1e-4 of a border; there 254 |v| is compared with an odd multiple of
+// a, both exact in float64 (32 bits each).  Halves are no rare case: v = a / 2 is one, in two-byte types a common one.
+__device__ __forceinline__ int code_of(float v, const Rounding& r) {
+  const float q = v * r.factor;
+  float n = rintf(q);
+  if (fabsf(fabsf(q - n) - 0.5f) < 1e-4f) {
+    const float below = floorf(fabsf(q));          // the border is below + 0.5, or within 1e-4 of it on either side
+    const double twice = 254. * (double)fabsf(v), border = (2. * (double)below + 1.) * (double)r.top;
+    const float up = twice > border ? below + 1.f : twice < border ? below : 2.f * floorf(0.5f * (below + 1.f));
+    n = copysignf(up, v);
+  }
+  return r.factor == 0.f ? 0 : (int)n;
+}
+
+// Eight codes as the two dwords that memory holds.
+__device__ __forceinline__ Duo pack_codes(const int* c) {
+  Duo d;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    d[i] = ((uint32_t)c[4 * i] & 0xFFu) | (((uint32_t)c[4 * i + 1] & 0xFFu) << 8) | (((uint32_t)c[4 * i + 2] & 0xFFu) << 16) |
+           ((uint32_t)c[4 * i + 3] << 24);
+  return d;
+}
+__device__ __forceinline__ Duo codes_of(const float* f, const Rounding& r) {
+  int c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = code_of(f[i], r);
+  return pack_codes(c);
+}
+__device__ __forceinline__ void store_codes(int8_t* p, Duo d, int n) {
+  if (n >= 8) {
+    *reinterpret_cast<DuoByte*>(p) = d;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (int8_t)(d[i / 4] >> (8 * (i % 4)));
+  }
+}
+__device__ __forceinline__ Duo load_codes(const int8_t* p, int n) {
+  Duo d = {0, 0};
+  if (n >= 8) {
+    d = *reinterpret_cast<const DuoByte*>(p);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) d[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
+  }
+  return d;
+}
+// v as the float32 that it is.  (A product that is then narrowed to float16 becomes one v_fma_mixlo_f16, which rounds once, otherwise: every result
+// is to be the same whichever kernel computes it.)
+__device__ __forceinline__ float in_float32(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ void widen_codes(Duo d, float scale, float* f) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = in_float32((float)(int8_t)(d[i / 4] >> (8 * (i % 4))) * scale);
+}
+
+// A sum of products of codes as a number: one conversion, two products.
+__device__ __forceinline__ float scaled(int sum, float sx, float sw) { return in_float32(in_float32((float)sum * sx) * sw); }
+
+// ---- host ---------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1, kMostCols = (int64_t)1 << 30;
+
+inline bool is_real(int dt) { return dt == TGRAD_F32 || dt == TGRAD_BF16 || dt == TGRAD_F16; }
+
+inline bool extents_ok(int64_t rows, int64_t cols, int64_t stride) {
+  return rows >= 0 && rows <= kMostRows && cols >= 1 && cols <= kMostCols && stride >= cols && stride <= ((int64_t)1 << 60) / std::max<int64_t>(rows, 1);
+}
+inline bool good(const tgrad_matrix* m) {
+  return m && is_real(m->dtype) && extents_ok(m->rows, m->cols, m->row_stride) && (m->data || m->rows == 0) &&
+         (uintptr_t)m->data % (uintptr_t)real_bytes(m->dtype) == 0;
+}
+inline bool good(const tgrad_codes* c) {
+  if (!c || !extents_ok(c->rows, c->cols, c->row_stride)) return false;
+  if (c->group != 0 && c->group != 32 && c->group != 64 && c->group != 128 && c->group != 256 && c->group != 512) return false;
+  return (c->rows == 0 || (c->codes && c->scale)) && (uintptr_t)c->scale % 4 == 0;
+}
+inline bool same_size(const tgrad_matrix* a, int64_t rows, int64_t cols) { return a->rows == rows && a->cols == cols; }
+inline bool same_size(const tgrad_codes* a, int64_t rows, int64_t cols) { return a->rows == rows && a->cols == cols; }
+
+inline Mat mat(const tgrad_matrix* m) {
+  return m ? Mat{static_cast<char*>(m->data), m->row_stride * real_bytes(m->dtype)} : Mat{nullptr, 0};
+}
+inline Codes8 codes8(const tgrad_codes* c) {
+  if (!c) return Codes8{nullptr, nullptr, 0, 0, 31};
+  const int shift = c->group ? __builtin_ctz((unsigned)c->group) : 31;
+  return Codes8{static_cast<int8_t*>(c->codes), c->scale, c->row_stride, c->group ? (c->cols + c->group - 1) / c->group : 1, shift};
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? TGRAD_OK : TGRAD_ERR_HIP; }
+inline bool pending() { return hipPeekAtLastError() != hipSuccess; }
+
+template <typename F>
+void for_real(int dt, F&& f) {
+  if (dt == TGRAD_F32) f(std::integral_constant<int, TGRAD_F32>());
+  else if (dt == TGRAD_BF16) f(std::integral_constant<int, TGRAD_BF16>());
+  else f(std::integral_constant<int, TGRAD_F16>());
+}
+
+// f(first, rows) for parts of the rows whose launches, `groups` workgroups of T threads a row, stay below 2^32 threads.
+template <typename F>
+void rows_in_launches(int64_t rows, int T, int64_t groups, F&& f) {
+  const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 32) - 1) / (T * groups));
+  for (int64_t at = 0; at < rows; at += most) f(at, std::min(rows - at, most));
+}
+
+}  // namespace tgrad

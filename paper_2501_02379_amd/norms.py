@@ -1,0 +1,137 @@
+"""The norms after and before a block, with the gate and the scale of its residual branch: ctypes binding of the tgrad_block_norm entry
+points of include/tgrad.h.  Matrices, streams and memory as in `act8`.
+
+    r = tgrad_block_norm(x, block, post_weight=wa, gate=g, rows_per_gate=n, scale=a, pre_weight=wb)
+    # r.x = x + a * g * (norm(block) * wa), r.h = norm(r.x) * wb
+    d = tgrad_block_norm_backward(dx, dh, r.x, block, stats=r.stats, post_weight=wa, gate=g, rows_per_gate=n, scale=a, pre_weight=wb)
+"""
+from __future__ import annotations
+
+import ctypes as C
+import functools
+import math
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import act8
+from . import tgrad as T
+from ._marshal import REAL_TYPES, call, refuse, stream_of
+
+
+class BlockNorm(NamedTuple):
+    x: torch.Tensor                       # the stream behind the block (x itself where there is no block)
+    h: object                             # the next block's input: a tensor, Codes, or None without a pre_weight
+    stats: Optional[torch.Tensor]         # float32[rows, 4], for the backward pass
+
+
+class BlockNormGrads(NamedTuple):
+    dx: torch.Tensor
+    dblock: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]         # the gate's size and type
+    dpost: Optional[torch.Tensor]         # float32[cols]
+    dpre: Optional[torch.Tensor]
+
+
+def _describe(x, block, dtype, post, pre, gate, rows_per_gate, scale, eps, centered):
+    rows, cols = x.shape
+    weights = [w for w in (post, pre) if w is not None]
+    for w in weights:
+        if w.dim() != 1 or w.shape[0] != cols or w.dtype not in REAL_TYPES or w.device != x.device or not w.is_contiguous() or w.is_neg() or \
+                w.dtype is not weights[0].dtype:
+            refuse("post_weight, pre_weight: [cols], dense, float32, bfloat16 or float16, both of one type, on x's device")
+    if block is None and (post is not None or gate is not None or pre is None):
+        refuse("without a block there is a pre_weight, and neither post_weight nor gate")
+    if rows_per_gate < 1:
+        refuse("rows_per_gate: at least 1")
+    if gate is not None:
+        g = act8.describe(gate, "gate", x, -(-rows // rows_per_gate), cols, dtype)
+    if not (math.isfinite(scale) and math.isfinite(eps) and eps > 0):
+        refuse("scale: finite; eps: above 0, finite")
+    return T.tgrad_block(post.data_ptr() if post is not None else None, pre.data_ptr() if pre is not None else None,
+                         gate.data_ptr() if gate is not None else None, g.row_stride if gate is not None else 0, rows_per_gate,
+                         REAL_TYPES[weights[0].dtype] if weights else T.TGRAD_F32, scale, eps, 1 if centered else 0)
+
+
+@functools.lru_cache(maxsize=1024)
+def _scratch_bytes(rows, cols, rows_per_gate):
+    n = C.c_size_t(0)
+    rc = T.load().tgrad_block_norm_query_size(rows, cols, rows_per_gate, C.byref(n))
+    if rc != T.TGRAD_OK:
+        raise T.TgradError(rc, "tgrad_block_norm_query_size")
+    return n.value
+
+
+def _ref(d):
+    return None if d is None else C.byref(d)
+
+
+def _types(x, dtype):
+    if x.dtype not in (dtype, torch.float32):
+        refuse("x: float32, or the block's type")
+
+
+@act8._on_stream
+def tgrad_block_norm(x, block=None, *, post_weight=None, gate=None, rows_per_gate: int = 1, scale: float = 1.0, pre_weight=None,
+                     eps: float = 1e-6, centered: bool = False, quantize: bool = False, dtype=None, keep: bool = True) -> BlockNorm:
+    """x + scale * gate * (norm(block) * post_weight), and norm of that * pre_weight.  Without post_weight the block goes in as it is;
+    without pre_weight there is no h; without a block h is x's norm.  quantize: h as codes with a scale a row.  `dtype`: of h, where there is no
+    block (x's).  keep=False: no stats.  centered: the mean is taken off first."""
+    d = act8.describe(x, "x")
+    dev = x.device
+    b = act8.describe(block, "block", x, d.rows, d.cols) if block is not None else None
+    if block is not None and dtype not in (None, block.dtype):
+        refuse("dtype: the block's")
+    dtype = block.dtype if block is not None else dtype or x.dtype
+    if dtype not in REAL_TYPES:
+        refuse("dtype: float32, bfloat16 or float16")
+    _types(x, dtype)
+    desc = _describe(x, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, eps, centered)
+    out, o = act8._result(None, "x", x, d.rows, d.cols, x.dtype) if block is not None else (x, None)
+    h = e = c = None
+    if pre_weight is not None and quantize:
+        h = act8.new_codes(d.rows, d.cols, 0, dev)
+        c = act8.describe_codes(h, "h")
+    elif pre_weight is not None:
+        h, e = act8._result(None, "h", x, d.rows, d.cols, dtype)
+    elif quantize:
+        refuse("quantize: with a pre_weight")
+    stats = torch.empty(d.rows, 4, dtype=torch.float32, device=dev) if keep else None
+    call(dev, T.load().tgrad_block_norm, "tgrad_block_norm", C.byref(desc), C.byref(d), _ref(b), _ref(o), _ref(e), _ref(c),
+         stats.data_ptr() if keep else None, stream_of(dev))
+    return BlockNorm(out, h, stats)
+
+
+@act8._on_stream
+def tgrad_block_norm_backward(dx, dh, x, block=None, *, stats, post_weight=None, gate=None, rows_per_gate: int = 1, scale: float = 1.0,
+                              pre_weight=None, centered: bool = False) -> BlockNormGrads:
+    """Gradients for `dx`, the gradient with respect to the stream behind the block from elsewhere (None: none), and `dh` with respect to h
+    (None without a pre_weight).  x: the stream behind the block, as the forward call returned it; the other arguments as they were there."""
+    o = act8.describe(x, "x")
+    dev = x.device
+    rows, cols = o.rows, o.cols
+    b = act8.describe(block, "block", x, rows, cols) if block is not None else None
+    if (dh is None) != (pre_weight is None):
+        refuse("dh: with a pre_weight")
+    dtype = block.dtype if block is not None else dh.dtype if dh is not None else x.dtype
+    if dtype not in REAL_TYPES:
+        refuse("dh: float32, bfloat16 or float16")
+    _types(x, dtype)
+    desc = _describe(x, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, 1.0, centered)
+    a = act8.describe(dx, "dx", x, rows, cols, x.dtype) if dx is not None else None
+    u = act8.describe(dh, "dh", x, rows, cols, dtype) if dh is not None else None
+    if stats is None or stats.dtype is not torch.float32 or tuple(stats.shape) != (rows, 4) or stats.device != dev or not stats.is_contiguous() or \
+            stats.is_neg() or stats.data_ptr() % 16:
+        refuse("stats: float32[rows, 4] of the forward call")
+    new = lambda *shape, t: torch.empty(*shape, dtype=t, device=dev)  # noqa: E731
+    gx = new(rows, cols, t=x.dtype)
+    gb = new(rows, cols, t=dtype) if block is not None else None
+    gg = new(*gate.shape, t=dtype) if gate is not None else None
+    gpost = new(cols, t=torch.float32) if post_weight is not None else None
+    gpre = new(cols, t=torch.float32) if pre_weight is not None else None
+    ws = new(_scratch_bytes(rows, cols, rows_per_gate if gate is not None else 1), t=torch.uint8)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    call(dev, T.load().tgrad_block_norm_backward, "tgrad_block_norm_backward", C.byref(desc), _ref(a), _ref(u), C.byref(o), _ref(b),
+         stats.data_ptr(), C.byref(act8.describe(gx, "dx")), C.byref(act8.describe(gb, "dblock")) if gb is not None else None, at(gg),
+         at(gpost), at(gpre), ws.data_ptr(), stream_of(dev))
+    return BlockNormGrads(gx, gb, gg, gpost, gpre)

@@ -20,6 +20,9 @@ TGRAD_SELECT_TOPK_MAG = 0
 TGRAD_SELECT_RANDOM = 1
 TGRAD_ORDER_US_LR, TGRAD_ORDER_LR_US, TGRAD_ORDER_SUM = 0, 1, 2
 
+TGRAD_CODES_MATMUL, TGRAD_CODES_LINEAR, TGRAD_CODES_GRAD_INPUT, TGRAD_CODES_GRAD_WEIGHT = 0, 1, 2, 3
+TGRAD_ACT_SILU, TGRAD_ACT_GELU = 0, 1
+
 TGRAD_OK = 0
 TGRAD_ERR_INVALID_ARG = -1
 TGRAD_ERR_UNSUPPORTED = -2
@@ -43,6 +46,9 @@ EXPORTS = (
     "tgrad_group_clip", "tgrad_group_adamw", "tgrad_group_destroy",
     "tgrad_token_logprobs", "tgrad_token_logprobs_backward", "tgrad_loss_query_size", "tgrad_policy_loss",
     "tgrad_preference_loss",
+    "tgrad_quantize", "tgrad_dequantize", "tgrad_codes_query_size", "tgrad_codes_matmul", "tgrad_codes_linear", "tgrad_codes_grad_input",
+    "tgrad_codes_grad_weight", "tgrad_activation", "tgrad_activation_backward", "tgrad_block_norm", "tgrad_block_norm_query_size",
+    "tgrad_block_norm_backward",
 )
 
 
@@ -116,6 +122,29 @@ class tgrad_preference(C.Structure):
     _fields_ = [("beta", C.c_float), ("label_smoothing", C.c_float)]
 
 
+class tgrad_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64), ("dtype", C.c_int32)]
+
+
+class tgrad_codes(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int64), ("row_stride", C.c_int64),
+                ("group", C.c_int32)]
+
+
+class tgrad_block(C.Structure):
+    _fields_ = [
+        ("post_weight", C.c_void_p),
+        ("pre_weight", C.c_void_p),
+        ("gate", C.c_void_p),
+        ("gate_stride", C.c_int64),
+        ("rows_per_gate", C.c_int64),
+        ("weight_dtype", C.c_int32),
+        ("scale", C.c_float),
+        ("eps", C.c_float),
+        ("centered", C.c_int32),
+    ]
+
+
 class TgradError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -166,6 +195,19 @@ def load():
                                       C.c_int64, vp]
     lib.tgrad_preference_loss.argtypes = [C.POINTER(tgrad_logits), C.POINTER(tgrad_preference), C.c_int64, vp, vp, vp, vp, vp,
                                           vp, vp, vp, vp, C.c_int64, vp]
+    mat, cod, blk = C.POINTER(tgrad_matrix), C.POINTER(tgrad_codes), C.POINTER(tgrad_block)
+    lib.tgrad_quantize.argtypes = [mat, cod, vp]
+    lib.tgrad_dequantize.argtypes = [cod, mat, vp]
+    lib.tgrad_codes_query_size.argtypes = [i32, C.c_int64, C.c_int64, C.c_int64, C.POINTER(sz)]
+    lib.tgrad_codes_matmul.argtypes = [cod, cod, mat, vp, vp]
+    lib.tgrad_codes_linear.argtypes = [mat, cod, cod, mat, vp, vp]
+    lib.tgrad_codes_grad_input.argtypes = [mat, cod, mat, vp, vp]
+    lib.tgrad_codes_grad_weight.argtypes = [mat, cod, mat, vp, vp]
+    lib.tgrad_activation.argtypes = [mat, mat, i32, mat, cod, cod, cod, vp]
+    lib.tgrad_activation_backward.argtypes = [mat, cod, cod, i32, mat, mat, vp]
+    lib.tgrad_block_norm.argtypes = [blk, mat, mat, mat, mat, cod, vp, vp]
+    lib.tgrad_block_norm_query_size.argtypes = [C.c_int64, C.c_int64, C.c_int64, C.POINTER(sz)]
+    lib.tgrad_block_norm_backward.argtypes = [blk, mat, mat, mat, mat, vp, mat, mat, vp, vp, vp, vp, vp]
     lib.tgrad_destroy.argtypes = [vp]
     lib.tgrad_strerror.argtypes = [i32]
     lib.tgrad_strerror.restype = C.c_char_p

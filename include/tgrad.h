@@ -553,7 +553,7 @@ int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer,
  *  w              outer x inner, group 0: the weight, a row for each output.
  *  y              tokens x outer.
  *  workspace_dev  device pointer, >= tgrad_codes_query_size, 256-byte aligned.
- * Errors: INVALID_ARG, UNSUPPORTED (inner), HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (inner; 2^33 results), HIP.
  */
 int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* workspace_dev, void* hip_stream);
 
@@ -570,9 +570,9 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
  * w and x are the values of codes, in groups of any size.  bf16 and float16: values are rounded to dy's type (a value beyond float16's
  * range is infinite), products are exact and added up in float32.  float32: dy times a code's scale is split into three bf16 parts, which keep 24 bits (below
  * 2^-110 the last ones are lost; an infinity becomes NaN), codes are exact.
- *  dx, dw  dy's type, or TGRAD_F32; rounded once.  The order of the sums depends on the sizes alone.
+ *  dx, dw  dy's type, or TGRAD_F32; rounded once.  The order of the sums depends on sizes and alignment alone.
  *  workspace_dev  as above.
- * Errors: INVALID_ARG, HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (2^33 results), HIP.
  */
 int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream);
 int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream);

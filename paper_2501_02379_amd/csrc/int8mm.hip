@@ -9,16 +9,18 @@ void launch_quantize(hipStream_t s, const tgrad_matrix* x, const tgrad_codes* ou
 
 namespace {
 
-// ---- codes times codes: 64 x 64 results a workgroup, 4 x 4 a thread, v_dot4_i32_i8 ------------------------------------------------
+// ---- codes times codes: tiles of results, v_mfma_i32_16x16x64_i8 ----------------------------------------------------------------------
 
-constexpr int kStep = 64;                 // bytes of the sum that are staged at a time
-constexpr int kPitch = kStep + 4;         // an odd number of dwords: rows start in different banks
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef __amdgpu_buffer_rsrc_t Ref;
+
+constexpr int kStep = 128;                // bytes of the sum in memory on the chip at a time: a row of it is 8 chunks of 16
 
 __device__ __forceinline__ Quad load16(const int8_t* p, int64_t n) {
   Quad q = {0, 0, 0, 0};
   if (n >= 16) {
     q = *reinterpret_cast<const QuadByte*>(p);
-  } else {
+  } else if (n > 0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i < n) q[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
@@ -26,41 +28,275 @@ __device__ __forceinline__ Quad load16(const int8_t* p, int64_t n) {
   return q;
 }
 
-template <int OT>
-__global__ __launch_bounds__(256) void k_int8_tile(Codes8 x, Codes8 w, int64_t tokens, int64_t outer, int inner, Mat y) {
-  __shared__ uint32_t xs[64 * kPitch / 4], ws[64 * kPitch / 4];
-  const int64_t t0 = (int64_t)blockIdx.y * 64, n0 = (int64_t)blockIdx.x * 64;
-  const int r = threadIdx.x / 4, seg = threadIdx.x % 4;
-  const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
-  int acc[4][4] = {};
-  for (int k0 = 0; k0 < inner; k0 += kStep) {
-    const int at = k0 + seg * 16;
-    Quad a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-    if (t0 + r < tokens) a = load16(x.codes + (t0 + r) * x.stride + at, inner - at);
-    if (n0 + r < outer) b = load16(w.codes + (n0 + r) * w.stride + at, inner - at);
-    __syncthreads();
+// Memory from p on, for loads that go straight to LDS: 16 bytes a lane, the lanes' one behind the other.
+__device__ __forceinline__ Ref ref(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, 0x7FFFFFF8, 0x00020000); }
+__device__ __forceinline__ void to_lds(const Ref& g, char* l, int each, int all) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(g, (__attribute__((address_space(3))) void*)l, 16, each, all, 0, 0);
+}
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+
+// A launch's workgroups go round the 8 dies; here each die gets neighbouring tiles, in bands of 4 tiles of rows, so that those at work at a time
+// share what its L2 holds.  -> (tile of rows, tile of columns)
+__device__ __forceinline__ int2 tile_of(int id, int total, int tiles_c) {
+  const int q = total / 8, r = total % 8, die = id % 8;
+  id = die * q + min(die, r) + id / 8;
+  const int band = id / (4 * tiles_c), in = id % (4 * tiles_c), tall = min(4, total / tiles_c - band * 4);
+  return make_int2(band * 4 + in % tall, in / tall);
+}
+
+// y[t][n] = sum_k x[t][k] w[n][k].  WT x WN wavefronts, each FT x FN results of 16 x 16.  A step's 128 bytes of every row lie in LDS, chunk c of row r
+// at chunk c ^ (r % 8), so that eight rows' loads of one chunk meet eight banks; `BUFS` steps are there or on their way.  One
+// barrier a step: it says that everyone's part of this step has arrived and that everyone is done with the step before, whose place is filled
+// next.  OT < 0: sums go to `part`, [split][tokens][outer], and are added up by k_add_parts.
+// STAGED: rows that do not start at multiples of 16 bytes go through registers.
+// 8192^3: 457 us, 2400 TOP/s with 4 x 2 wavefronts of 4 x 8 results (2 x 4 of 8 x 4: 519; four wavefronts of 8 x 8: 582; 128 x 128 tiles, two
+// workgroups a compute unit: 546).
+template <int WT, int WN, int FT, int FN, int BUFS, bool STAGED, int OT>
+__global__ __launch_bounds__(WT * WN * 64) void k_codes_tiles(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int* part, int tiles_n, int tiles,
+                                                              int steps_a_split) {
+  constexpr int T = WT * WN * 64, BT = WT * FT * 16, BN = WN * FN * 16, kBytes = (BT + BN) * kStep;
+  constexpr int kLoads = kBytes / 16 / T, kLoadsN = BN * kStep / 16 / T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int split = blockIdx.x / tiles;
+  const int2 tile = tile_of(blockIdx.x % tiles, tiles, tiles_n);
+  const int t0 = tile.x * BT, n0 = tile.y * BN;
+  const int8_t* xp = x.codes + (int64_t)t0 * x.stride;
+  const int8_t* wp = w.codes + (int64_t)n0 * w.stride;
+  const int first = split * steps_a_split, last = min(first + steps_a_split, (inner + kStep - 1) / kStep);
+  const int whole = STAGED ? first : min(last, inner / kStep);        // steps that go straight to LDS
+
+  // this thread's chunks of a step: row (rows beyond the matrix are its last one again, and are not stored) and column
+  auto row_of = [&](int i) {
+    const int r = (i * T + (int)threadIdx.x) / 8;
+    return i < kLoadsN ? min(r, outer - 1 - n0) : min(r - BN, tokens - 1 - t0);
+  };
+  const int chunk = ((int)threadIdx.x % 8 ^ (int)threadIdx.x / 8 % 8) * 16;
+  int each[kLoads];
+  if constexpr (!STAGED) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      xs[r * (kPitch / 4) + seg * 4 + i] = a[i];
-      ws[r * (kPitch / 4) + seg * 4 + i] = b[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kStep / 4; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          acc[i][j] = __builtin_amdgcn_sdot4((int)xs[(tr + 16 * i) * (kPitch / 4) + k], (int)ws[(tc + 16 * j) * (kPitch / 4) + k], acc[i][j], false);
+    for (int i = 0; i < kLoads; ++i) each[i] = row_of(i) * (int)(i < kLoadsN ? w.stride : x.stride) + chunk;
   }
+  const Ref xr = ref(xp), wr = ref(wp);
+  auto fill = [&](int s) {
+    char* l = lds + (s - first) % BUFS * kBytes + wave * kWave * 16;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kLoads; ++i) to_lds(i < kLoadsN ? wr : xr, l + i * T * 16, each[i], s * kStep);
+  };
+  Quad held[kLoads];
+  auto read = [&](int s) {
+    const int at = s * kStep + chunk;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t t = t0 + tr + 16 * i, n = n0 + tc + 16 * j;
-      if (t < tokens && n < outer)
-        reinterpret_cast<typename Elem<OT>::raw*>(y.row(t))[n] = Elem<OT>::narrow(scaled(acc[i][j], x.scale[t], w.scale[n]));
+    for (int i = 0; i < kLoads; ++i) held[i] = load16((i < kLoadsN ? wp + row_of(i) * w.stride : xp + row_of(i) * x.stride) + at, inner - at);
+  };
+  auto place = [&](int s) {
+    char* l = lds + (s - first) % BUFS * kBytes + threadIdx.x * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<Quad*>(l + i * T * 16) = held[i];
+  };
+
+  i32x4 acc[FN][FT] = {};
+  const int wn = wave % WN, wt = wave / WN;
+  auto multiply = [&](int s) {
+    const char* l = lds + (s - first) % BUFS * kBytes;
+    const char* nl = l + (wn * FN * 16 + lane % 16) * kStep;
+    const char* tl = l + (BN + wt * FT * 16 + lane % 16) * kStep;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      i32x4 a[FN], b[FT];
+      const int c = ((k * 4 + lane / 16) ^ (lane % 8)) * 16;
+#pragma unroll
+      for (int i = 0; i < FN; ++i) a[i] = *reinterpret_cast<const i32x4*>(nl + i * 16 * kStep + c);
+#pragma unroll
+      for (int j = 0; j < FT; ++j) b[j] = *reinterpret_cast<const i32x4*>(tl + j * 16 * kStep + c);
+#pragma unroll
+      for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
     }
+  };
+
+  if constexpr (STAGED) {
+    read(first);
+    place(first);
+    for (int s = first; s < last; ++s) {
+      if (s + 1 < last) read(s + 1);
+      __syncthreads();
+      multiply(s);
+      if (s + 1 < last) place(s + 1);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < BUFS - 1; ++i)
+      if (first + i < whole) fill(first + i);
+    for (int s = first; s < whole; ++s) {
+      if (s + BUFS - 2 < whole) wait_loads<kLoads * (BUFS - 2)>();
+      else wait_loads<0>();
+      __builtin_amdgcn_s_barrier();
+      if (s + BUFS - 1 < whole) fill(s + BUFS - 1);
+      multiply(s);
+    }
+    if (whole < last) {                   // the sum's end, less than a step
+      read(whole);
+      __syncthreads();
+      place(whole);
+      __syncthreads();
+      multiply(whole);
+    }
+  }
+
+#pragma unroll
+  for (int j = 0; j < FT; ++j) {
+    const int t = t0 + (wt * FT + j) * 16 + lane % 16;
+    if (t >= tokens) continue;
+    const float sx = OT < 0 ? 0.f : x.scale[t];
+#pragma unroll
+    for (int i = 0; i < FN; ++i) {
+      const int n = n0 + (wn * FN + i) * 16 + lane / 16 * 4;
+      if (n >= outer) continue;
+      if constexpr (OT < 0) {
+        int* to = part + ((int64_t)split * tokens + t) * outer + n;
+        if (n + 4 <= outer) {
+          *reinterpret_cast<QuadAny*>(to) = __builtin_bit_cast(Quad, acc[i][j]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < outer) to[r] = acc[i][j][r];
+        }
+      } else {
+        typedef typename Elem<OT>::raw raw;
+        raw* to = reinterpret_cast<raw*>(y.row(t)) + n;
+        if (n + 4 <= outer) {
+          float f[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) f[r] = scaled(acc[i][j][r], sx, w.scale[n + r]);
+          *reinterpret_cast<typename Four<OT>::any*>(to) = Four<OT>::narrow(f);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < outer) to[r] = Elem<OT>::narrow(scaled(acc[i][j][r], sx, w.scale[n + r]));
+        }
+      }
+    }
+  }
+}
+
+// Sums of the splits' sums: four results a thread.
+template <int OT>
+__global__ __launch_bounds__(256) void k_add_parts(const int* __restrict__ part, int splits, int tokens, int outer, const float* sx, const float* sw, Mat y) {
+  const int64_t per = (outer + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int t = (int)(id / per), n = (int)(id % per) * 4;
+  if (t >= tokens) return;
+  const int many = min(4, outer - n);
+  i32x4 sum = {0, 0, 0, 0};
+  for (int s = 0; s < splits; ++s) {
+    const int* from = part + ((int64_t)s * tokens + t) * outer + n;
+    if (many == 4) {
+      sum += __builtin_bit_cast(i32x4, *reinterpret_cast<const QuadAny*>(from));
+    } else {
+      for (int r = 0; r < many; ++r) sum[r] += from[r];
+    }
+  }
+  typedef typename Elem<OT>::raw raw;
+  raw* to = reinterpret_cast<raw*>(y.row(t)) + n;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r < many) to[r] = Elem<OT>::narrow(scaled(sum[r], sx[t], sw[n + r]));
+}
+
+// ---- up to 16 tokens: the weight is read once, straight to registers --------------------------------------------------------------------
+
+constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kAhead = 8;
+constexpr int kFusedTokens = 4, kFusedCodes = 32768, kFusedUnits = 4;      // what one workgroup quantises by the way
+
+// 16 outputs a workgroup; its wavefronts share the sum, and a matrix instruction takes 64 bytes of 16 rows of the weight and of all tokens.
+// XT >= 0: the tokens come as numbers; every workgroup quantises them into LDS for itself while its first loads of the weight are on their way, which
+// spares a launch; the first one writes what is kept.
+template <int XT, int OT>
+__global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, bool keep, Codes8 w, int tokens, int outer, int inner, Mat y) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];          // sums, scales, then codes of the tokens
+  int (*sums)[kWave][4] = reinterpret_cast<int (*)[kWave][4]>(lds);
+  float* sx = reinterpret_cast<float*>(lds + sizeof(int) * kFewWaves * kWave * 4);
+  uint32_t* tops = reinterpret_cast<uint32_t*>(sx + 16);
+  char* codes = reinterpret_cast<char*>(tops + kFewWaves);
+  const int wave = threadIdx.x / kWave, lane = lane_id();
+  const int n0 = blockIdx.x * 16;
+  const int8_t* wrow = w.codes + (int64_t)min(n0 + lane % 16, outer - 1) * w.stride;
+  const int pieces = (inner + 63) / 64, a_wave = (pieces + kFewWaves - 1) / kFewWaves;
+  const int first = min(wave * a_wave, pieces), last = min(first + a_wave, pieces);
+  const int mine = lane / 16 * 16;
+  Quad a[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) {
+    const int at = (first + i) * 64 + mine;
+    a[i] = load16(wrow + at, first + i < last ? inner - at : 0);
+  }
+  const int pitch = (inner + 63) / 64 * 64;
+  const int8_t* xrow;
+  if constexpr (XT >= 0) {
+    constexpr int es = sizeof(typename Elem<XT>::raw);
+    const int units = pitch / 8;
+    for (int t = 0; t < tokens; ++t) {
+      Eight<XT> held[kFusedUnits];
+      float f[8];
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < kFusedUnits; ++i) {
+        const int u = threadIdx.x + i * kFewThreads;
+        held[i].clear();
+        if (u * 8 < inner) held[i].load(xm.row(t) + (int64_t)u * 8 * es, inner - u * 8);
+        held[i].get(f);
+        top = max(top, largest(f));
+      }
+      const Rounding r = rounding_of(largest_of_block<kFewWaves>(top, tops));
+      if (threadIdx.x == 0) {
+        sx[t] = r.scale;
+        if (keep && blockIdx.x == 0) x.scale[t] = r.scale;
+      }
+#pragma unroll
+      for (int i = 0; i < kFusedUnits; ++i) {
+        const int u = threadIdx.x + i * kFewThreads;
+        held[i].get(f);
+        if (u < units) {
+          const Duo d = codes_of(f, r);
+          *reinterpret_cast<Duo*>(codes + t * pitch + u * 8) = d;
+          if (keep && blockIdx.x == 0 && u * 8 < inner) store_codes(x.codes + t * x.stride + u * 8, d, inner - u * 8);
+        }
+      }
+    }
+    __syncthreads();
+    xrow = nullptr;
+  } else {
+    if (threadIdx.x < (uint32_t)tokens) sx[threadIdx.x] = x.scale[threadIdx.x];
+    xrow = x.codes + (int64_t)min(lane % 16, tokens - 1) * x.stride;
+  }
+  const char* lrow = codes + min(lane % 16, tokens - 1) * pitch;
+  i32x4 acc = {0, 0, 0, 0};
+  for (int p = first; p < last; p += kAhead) {
+    Quad b[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = (p + i) * 64 + mine;
+      if constexpr (XT >= 0) b[i] = p + i < last ? *reinterpret_cast<const Quad*>(lrow + at) : Quad{0, 0, 0, 0};
+      else b[i] = load16(xrow + at, p + i < last ? inner - at : 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a[i]), __builtin_bit_cast(i32x4, b[i]), acc, 0, 0, 0);
+      const int at = (p + kAhead + i) * 64 + mine;
+      a[i] = load16(wrow + at, p + kAhead + i < last ? inner - at : 0);
+    }
+  }
+  *reinterpret_cast<i32x4*>(sums[wave][lane]) = acc;
+  __syncthreads();
+  // lane l of a wavefront has token l % 16 and outputs 4 (l / 16) .. + 3
+  if (threadIdx.x < 256) {
+    const int t = threadIdx.x / 16, n = threadIdx.x % 16;
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kFewWaves; ++i) sum += sums[i][n / 4 * 16 + t][n % 4];
+    if (t < tokens && n0 + n < outer) reinterpret_cast<typename Elem<OT>::raw*>(y.row(t))[n0 + n] = Elem<OT>::narrow(scaled(sum, sx[t], w.scale[n0 + n]));
+  }
 }
 
 // ---- gradients: 64 x 64 results a workgroup, 4 x 4 a thread, float32 ---------------------------------------------------------------
@@ -109,15 +345,87 @@ __global__ __launch_bounds__(256) void k_grad_tile(Mat dy, Codes8 c, int64_t row
 
 size_t aligned(size_t n) { return (n + kScratchAlign - 1) / kScratchAlign * kScratchAlign; }
 
+size_t few_lds(int64_t tokens, int64_t inner) {
+  return sizeof(int) * kFewWaves * kWave * 4 + 16 * 4 + kFewWaves * 4 + (size_t)tokens * ((inner + 63) / 64 * 64);
+}
+
 // Codes of x that nobody keeps: rows of a multiple of 16 bytes, and a scale each.
 int64_t scratch_stride(int64_t inner) { return (inner + 15) / 16 * 16; }
 size_t scratch_codes(int64_t tokens, int64_t inner) { return aligned((size_t)tokens * scratch_stride(inner)) + aligned((size_t)tokens * 4); }
 
-void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y) {
-  for_real(y->dtype, [&](auto t) {
-    k_int8_tile<decltype(t)::value><<<dim3((uint32_t)((y->cols + 63) / 64), (uint32_t)((y->rows + 63) / 64)), dim3(256), 0, s>>>(
-        codes8(x), codes8(w), y->rows, y->cols, (int)x->cols, mat(y));
-  });
+// How a product of more than 16 tokens is cut.
+struct Cut {
+  int tile;                               // 256, 128 or 64 results on a side
+  int tiles_n, tiles, splits, steps;      // steps of kStep bytes to a split
+};
+// Codes that go straight to LDS: 16-byte rows, and offsets of 32 bits within a tile.
+bool straight(const void* p, int64_t stride) { return (uintptr_t)p % 16 == 0 && stride % 16 == 0 && stride <= ((int64_t)1 << 22); }
+// Tiles of 256 x 256 where they fill three quarters of the compute units (one workgroup each), of 128 x 128 otherwise, of 64 x 64 for up to 64 tokens, where
+// it is the weight's bytes that count.  The sum is split where there are fewer tiles than two (four of 64 x 64) for every compute unit.
+// (2048 x 8192 x 2048: 96 us in tiles of 256, 48 of 128; 1024 x 4096 x 4096: 56 and 29; 4096^3: 69 and 75.)
+Cut cut_of(int64_t tokens, int64_t outer, int64_t inner, bool direct) {
+  auto tiles = [&](int64_t b) { return ((tokens + b - 1) / b) * ((outer + b - 1) / b); };
+  Cut c;
+  c.tile = tokens <= 64 ? 64 : direct && tiles(256) >= 192 ? 256 : 128;
+  c.tiles_n = (int)((outer + c.tile - 1) / c.tile);
+  c.tiles = (int)std::min<int64_t>(tiles(c.tile), kMostRows);
+  const int64_t steps = (inner + kStep - 1) / kStep, want = c.tile == 256 ? 1 : c.tile == 128 ? 512 : 1024;
+  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(want / c.tiles, steps / 4));
+  c.steps = (int)((steps + splits - 1) / splits);
+  c.splits = (int)((steps + c.steps - 1) / c.steps);
+  return c;
+}
+constexpr int64_t kFew = 16;
+size_t part_bytes(int64_t tokens, int64_t outer, int64_t inner) {
+  if (tokens <= kFew) return 0;
+  size_t most = 0;
+  for (bool direct : {false, true}) {
+    const Cut c = cut_of(tokens, outer, inner, direct);
+    if (c.splits > 1) most = std::max(most, (size_t)c.splits * tokens * outer * 4);
+  }
+  return aligned(most);
+}
+
+template <int WT, int WN, int FT, int FN, int BUFS, bool STAGED, int OT>
+void launch_tiles_as(hipStream_t s, const Cut& c, const Codes8& x, const Codes8& w, const tgrad_matrix* y, int inner, int* part) {
+  constexpr size_t bytes = (size_t)(WT * FT + WN * FN) * 16 * kStep * BUFS;
+  auto k = k_codes_tiles<WT, WN, FT, FN, BUFS, STAGED, OT>;
+  allow_lds(k, bytes);
+  k<<<dim3((uint32_t)(c.tiles * c.splits)), dim3(WT * WN * 64), bytes, s>>>(x, w, (int)y->rows, (int)y->cols, inner, mat(y), part, c.tiles_n, c.tiles, c.steps);
+}
+template <bool STAGED, int OT>
+void launch_tiles(hipStream_t s, const Cut& c, const Codes8& x, const Codes8& w, const tgrad_matrix* y, int inner, int* part) {
+  if (c.tile == 64) launch_tiles_as<2, 2, 2, 2, STAGED ? 2 : 3, STAGED, OT>(s, c, x, w, y, inner, part);
+  else if (STAGED || c.tile == 128) launch_tiles_as<2, 2, 4, 4, 2, STAGED, OT>(s, c, x, w, y, inner, part);
+  else if constexpr (OT >= 0) launch_tiles_as<4, 2, 4, 8, 2, false, OT>(s, c, x, w, y, inner, part);
+}
+
+void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* parts) {
+  const Codes8 cx = codes8(x), cw = codes8(w);
+  const int inner = (int)x->cols;
+  if (y->rows <= kFew) {
+    for_real(y->dtype, [&](auto t) {
+      k_codes_few<-1, decltype(t)::value><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(0, 0), s>>>(
+          Mat{nullptr, 0}, cx, false, cw, (int)y->rows, (int)y->cols, inner, mat(y));
+    });
+    return;
+  }
+  const bool direct = straight(x->codes, x->row_stride) && straight(w->codes, w->row_stride);
+  const Cut c = cut_of(y->rows, y->cols, inner, direct);
+  int* part = static_cast<int*>(parts);
+  if (c.splits > 1) {
+    if (direct) launch_tiles<false, -1>(s, c, cx, cw, y, inner, part);
+    else launch_tiles<true, -1>(s, c, cx, cw, y, inner, part);
+    const int64_t threads = y->rows * ((y->cols + 3) / 4);
+    for_real(y->dtype, [&](auto t) {
+      k_add_parts<decltype(t)::value><<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, s>>>(part, c.splits, (int)y->rows, (int)y->cols, x->scale, w->scale, mat(y));
+    });
+  } else {
+    for_real(y->dtype, [&](auto t) {
+      if (direct) launch_tiles<false, decltype(t)::value>(s, c, cx, cw, y, inner, nullptr);
+      else launch_tiles<true, decltype(t)::value>(s, c, cx, cw, y, inner, nullptr);
+    });
+  }
 }
 
 template <bool WEIGHT>
@@ -130,6 +438,9 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
     else k_grad_tile<DT, TGRAD_F32, WEIGHT><<<grid, dim3(256), 0, s>>>(mat(dy), codes8(c), out->rows, out->cols, sum, mat(out));
   });
 }
+
+// A launch has fewer than 2^32 threads.
+bool too_many(const tgrad_matrix* y) { return ((y->rows + 63) / 64) * ((y->cols + 63) / 64) >= ((int64_t)1 << 21); }
 
 bool scratch_ok(const void* p) { return p && (uintptr_t)p % kScratchAlign == 0; }
 
@@ -151,17 +462,22 @@ extern "C" {
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes) {
   if (!workspace_bytes || op < TGRAD_CODES_MATMUL || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
   if (!extents_ok(tokens, inner, inner) || !extents_ok(outer, inner, inner)) return TGRAD_ERR_INVALID_ARG;
-  *workspace_bytes = kScratchAlign + (op == TGRAD_CODES_LINEAR ? scratch_codes(tokens, inner) : 0);
+  size_t n = kScratchAlign;
+  if (op == TGRAD_CODES_MATMUL || op == TGRAD_CODES_LINEAR) {
+    if (inner <= TGRAD_CODES_MAX_INNER && tokens > 0) n += part_bytes(tokens, outer, inner);
+    if (op == TGRAD_CODES_LINEAR) n += scratch_codes(tokens, inner);
+  }
+  *workspace_bytes = n;
   return TGRAD_OK;
 }
 
 int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* workspace_dev, void* hip_stream) {
   if (!good(x) || !good(w) || !good(y) || x->group || w->group || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
   if (x->cols != w->cols || !same_size(y, x->rows, w->rows)) return TGRAD_ERR_INVALID_ARG;
-  if (x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
+  if (too_many(y) || x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
   if (pending()) return TGRAD_ERR_HIP;
   if (y->rows == 0) return TGRAD_OK;
-  launch_product(static_cast<hipStream_t>(hip_stream), x, w, y);
+  launch_product(static_cast<hipStream_t>(hip_stream), x, w, y, workspace_dev);
   return launched();
 }
 
@@ -170,15 +486,24 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
   if (!good(x) || !good(w) || !good(y) || w->group || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
   if (x->cols != w->cols || !same_size(y, x->rows, w->rows)) return TGRAD_ERR_INVALID_ARG;
   if (keep && (!good(keep) || keep->group || !same_size(keep, x->rows, x->cols))) return TGRAD_ERR_INVALID_ARG;
-  if (x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
+  if (too_many(y) || x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
   if (pending()) return TGRAD_ERR_HIP;
   if (y->rows == 0) return TGRAD_OK;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  char* ws = static_cast<char*>(workspace_dev) + kScratchAlign;
-  tgrad_codes own{ws, reinterpret_cast<float*>(ws + aligned((size_t)x->rows * scratch_stride(x->cols))), x->rows, x->cols, scratch_stride(x->cols), 0};
+  if (x->rows <= kFusedTokens && x->rows * x->cols <= kFusedCodes && x->cols <= kFewThreads * 8 * kFusedUnits) {
+    for_real(x->dtype, [&](auto xt) {
+      for_real(y->dtype, [&](auto yt) {
+        k_codes_few<decltype(xt)::value, decltype(yt)::value><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(x->rows, x->cols), s>>>(
+            mat(x), codes8(keep), keep != nullptr, codes8(w), (int)y->rows, (int)y->cols, (int)x->cols, mat(y));
+      });
+    });
+    return launched();
+  }
+  char* own_codes = static_cast<char*>(workspace_dev) + part_bytes(y->rows, y->cols, x->cols);
+  tgrad_codes own{own_codes, reinterpret_cast<float*>(own_codes + aligned((size_t)x->rows * scratch_stride(x->cols))), x->rows, x->cols, scratch_stride(x->cols), 0};
   const tgrad_codes* c = keep ? keep : &own;
   launch_quantize(s, x, c);
-  launch_product(s, c, w, y);
+  launch_product(s, c, w, y, workspace_dev);
   return launched();
 }
 

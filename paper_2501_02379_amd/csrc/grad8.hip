@@ -1,0 +1,558 @@
+// The two gradients of a product with codes: sums over s of dy's numbers times codes' values, dx[t][k] = sum_n dy[t][n] w[n][k] and
+// dw[n][k] = sum_t dy[t][n] x[t][k].
+//
+// Both have the codes' rows along the sum, so that codes and, for dw, dy lie across it: a matrix instruction wants eight
+// neighbours along the sum in a lane, and LDS gives them with transposing loads.  Codes are widened on their way to LDS (cvt, mul, half a pack for each), once for each
+// tile of results that they go into.
+#include "tiles8.h"
+
+using namespace tgrad;
+
+namespace {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+template <int DT>
+__device__ __forceinline__ v4f mfma_of(Quad a, Quad b, v4f c) {
+  if constexpr (DT == TGRAD_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// A tile that lies across the sum: rows along the sum, `W` two-byte numbers each, block b (16 numbers, 32 bytes) of row s at block b ^ bend(s): a
+// transposing load's 16 lanes take a block of four rows, 0 to 3 modulo 4, and these then meet all banks.
+__device__ __forceinline__ int bend(int s) { return (s & 3) | ((s >> 1) & 4); }
+// Rows 8 g .. 8 g + 7 of block b, column l % 16, for lane l = 16 g + ...
+template <int W>
+__device__ __forceinline__ Quad across(const char* tile, int s0, int block, int lane) {
+  const int s = s0 + lane / 16 * 8 + lane % 16 / 4;
+  const char* p = tile + s * (W * 2) + (block ^ bend(s)) * 32 + lane % 4 * 8;
+  typedef __attribute__((address_space(3))) s16x4* At;
+  const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p));
+  const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p + 4 * W * 2));        // bend(s + 4) = bend(s)
+  const Duo l = __builtin_bit_cast(Duo, lo), h = __builtin_bit_cast(Duo, hi);
+  return Quad{l[0], l[1], h[0], h[1]};
+}
+
+// Eight two-byte numbers of which n are there.
+template <int DT>
+__device__ __forceinline__ Quad load8(const char* p, int64_t n) {
+  Eight<DT> e;
+  e.clear();
+  if (n > 0) e.load(p, (int)min(n, (int64_t)8));
+  return e.q[0];
+}
+
+// Sixteen codes times a scale, as two-byte numbers.
+template <int DT>
+__device__ __forceinline__ void widen16(Quad c, float scale, Quad* out) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float f[8];
+    widen_codes(Duo{c[2 * h], c[2 * h + 1]}, scale, f);
+    Eight<DT> e;
+    e.set(f);
+    out[h] = e.q[0];
+  }
+}
+
+// A result's four neighbours in a row, of the type OT (float32 sums of a split where OT < 0).
+template <int OT>
+__device__ __forceinline__ void store4(char* row, int64_t c, int64_t cols, v4f v) {
+  constexpr int RT = OT < 0 ? TGRAD_F32 : OT;
+  typedef typename Elem<RT>::raw raw;
+  raw* to = reinterpret_cast<raw*>(row) + c;
+  const float f[4] = {v[0], v[1], v[2], v[3]};
+  if (c + 4 <= cols) {
+    *reinterpret_cast<typename Four<RT>::any*>(to) = Four<RT>::narrow(f);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (c + r < cols) to[r] = Elem<RT>::narrow(f[r]);
+  }
+}
+
+struct Grad {
+  Mat dy;
+  Codes8 c;
+  Mat out;                                // [split][rows][cols] in float32 where the sum is split
+  int64_t sum;
+  int rows, cols;                         // of the result
+  int tiles_c, tiles, steps;              // steps of a split
+};
+
+// ---- two-byte dy ----------------------------------------------------------------------------------------------------------------------
+
+constexpr int kStep = 64;                 // of the sum in LDS at a time
+
+// WR x WC wavefronts, each FR x FC results of 16 x 16; two steps in LDS, one barrier a step.  WEIGHT: dy lies across the sum, else along it (rows of
+// 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end and where STAGED (rows that do not start at
+// multiples of 16 bytes); codes go through registers, a step ahead.
+template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT, bool STAGED>
+__global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
+  constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
+  constexpr int kDy = BR * kStep * 2, kBytes = kDy + BC * kStep * 2;
+  constexpr int kLoads = kDy / 16 / T, kCodes = BC * kStep / 16 / T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int split = blockIdx.x / a.tiles;
+  const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
+  const int r0 = tile.x * BR, c0 = tile.y * BC;
+  const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep - 1) / kStep);
+  const int64_t whole = STAGED ? last : min(last, a.sum / kStep);
+  auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
+
+  // this thread's chunks of dy: row of the tile and chunk of eight numbers
+  auto part = [&](int i, int& row, int& chunk) {
+    const int id = i * T + (int)threadIdx.x;
+    if constexpr (WEIGHT) {
+      row = id / (BR / 8);
+      const int c = id % (BR / 8);
+      chunk = ((c / 2) ^ bend(row)) * 2 + c % 2;
+    } else {
+      row = id / 8;
+      chunk = (id % 8) ^ (row % 8);
+    }
+  };
+  int each[kLoads];
+  if constexpr (!STAGED) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row, chunk;
+      part(i, row, chunk);
+      // what lies beyond the matrix is loaded from within it, and its results are not stored
+      each[i] = WEIGHT ? row * (int)a.dy.stride + min(chunk * 8, a.rows - r0 - 8) * 2 : min(row, a.rows - 1 - r0) * (int)a.dy.stride + chunk * 16;
+    }
+  }
+  const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
+  auto fill = [&](int64_t s) {
+    const Ref g = ref(dy0 + (WEIGHT ? s * kStep * a.dy.stride : s * kStep * 2));
+    char* l = place_of(s) + wave * kWave * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, each[i], 0);
+  };
+  Quad held[kLoads];
+  auto read = [&](int64_t s) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      int row, chunk;
+      part(i, row, chunk);
+      if constexpr (WEIGHT) held[i] = load8<DT>(a.dy.row(s * kStep + row) + (int64_t)(r0 + chunk * 8) * 2, s * kStep + row < a.sum ? a.rows - r0 - chunk * 8 : 0);
+      else held[i] = load8<DT>(a.dy.row(min(r0 + row, a.rows - 1)) + (s * kStep + chunk * 8) * 2, a.sum - s * kStep - chunk * 8);
+    }
+  };
+  auto place = [&](int64_t s) {
+    char* l = place_of(s) + threadIdx.x * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) *reinterpret_cast<Quad*>(l + i * T * 16) = held[i];
+  };
+
+  Quad codes[kCodes];
+  float scale[kCodes];
+  const int8_t* cp = a.c.codes + c0;
+  auto read_codes = [&](int64_t s) {
+#pragma unroll
+    for (int i = 0; i < kCodes; ++i) {
+      const int id = i * T + (int)threadIdx.x, col = id % (BC / 16) * 16;
+      const int64_t row = s * kStep + id / (BC / 16);
+      codes[i] = Quad{0, 0, 0, 0};
+      scale[i] = 0.f;
+      if (row < a.sum && c0 + col < a.cols) {
+        codes[i] = load16(cp + row * a.c.stride + col, a.cols - c0 - col);
+        scale[i] = a.c.scale[row * a.c.groups + ((c0 + col) >> a.c.shift)];
+      }
+    }
+  };
+  auto place_codes = [&](int64_t s) {
+    char* l = place_of(s) + kDy;
+#pragma unroll
+    for (int i = 0; i < kCodes; ++i) {
+      const int id = i * T + (int)threadIdx.x, row = id / (BC / 16), block = id % (BC / 16);
+      Quad q[2];
+      widen16<DT>(codes[i], scale[i], q);
+      char* at = l + row * (BC * 2) + (block ^ bend(row)) * 32;
+      const bool upper = lane & 4;          // lanes 4 to 7 store their upper halves first: eight lanes then meet all banks
+      *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
+      *reinterpret_cast<Quad*>(at + (upper ? 0 : 16)) = upper ? q[0] : q[1];
+    }
+  };
+
+  v4f acc[FC][FR] = {};
+  const int wr = wave % WR, wc = wave / WR;
+  auto multiply = [&](int64_t s) {
+    const char* l = place_of(s);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      Quad c[FC], d[FR];
+#pragma unroll
+      for (int i = 0; i < FC; ++i) c[i] = across<BC>(l + kDy, k * 32, wc * FC + i, lane);
+#pragma unroll
+      for (int j = 0; j < FR; ++j) {
+        if constexpr (WEIGHT) d[j] = across<BR>(l, k * 32, wr * FR + j, lane);
+        else d[j] = *reinterpret_cast<const Quad*>(l + ((wr * FR + j) * 16 + lane % 16) * 128 + (((k * 4 + lane / 16) ^ (lane % 8)) * 16));
+      }
+#pragma unroll
+      for (int i = 0; i < FC; ++i)
+#pragma unroll
+        for (int j = 0; j < FR; ++j) acc[i][j] = mfma_of<DT>(c[i], d[j], acc[i][j]);
+    }
+  };
+
+  read_codes(first);
+  if constexpr (STAGED) {
+    read(first);
+    place(first);
+  } else if (first < whole) {
+    fill(first);
+  }
+  place_codes(first);
+  if (first + 1 < last) {
+    read_codes(first + 1);
+    if constexpr (STAGED) read(first + 1);
+  }
+  for (int64_t s = first; s < whole; ++s) {
+    barrier_but<0>();
+    if (s + 1 < last) {
+      if constexpr (STAGED) place(s + 1);
+      else if (s + 1 < whole) fill(s + 1);
+      place_codes(s + 1);
+      if (s + 2 < last) {
+        read_codes(s + 2);
+        if constexpr (STAGED) read(s + 2);
+      }
+    }
+    multiply(s);
+  }
+  if (whole < last) {                       // the sum's end, less than a step
+    read(whole);
+    __syncthreads();
+    place(whole);
+    __syncthreads();
+    multiply(whole);
+  }
+
+#pragma unroll
+  for (int j = 0; j < FR; ++j) {
+    const int r = r0 + (wr * FR + j) * 16 + lane % 16;
+    if (r >= a.rows) continue;
+    char* row = a.out.row((int64_t)split * a.rows + r);
+#pragma unroll
+    for (int i = 0; i < FC; ++i) {
+      const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
+      if (c < a.cols) store4<OT>(row, c, a.cols, acc[i][j]);
+    }
+  }
+}
+
+// ---- float32 dy, a scale for each row of codes -------------------------------------------------------------------------------------------
+
+// dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_pair); codes are exact in bf16.  Three products instead
+// of one, each 16 times as fast as the float32 matrix instructions'.
+constexpr int kStep32 = 32;
+
+template <int WR, int WC, int FR, int FC, bool WEIGHT>
+__global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
+  constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
+  constexpr int kPart = BR * kStep32 * 2, kBytes = 3 * kPart + BC * kStep32 * 2;
+  constexpr int kLoads = BR * kStep32 / 8 / T, kCodes = BC * kStep32 / 16 / T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int split = blockIdx.x / a.tiles;
+  const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
+  const int r0 = tile.x * BR, c0 = tile.y * BC;
+  const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep32 - 1) / kStep32);
+  auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
+
+  Eight<TGRAD_F32> held[kLoads];
+  Quad codes[kCodes];
+  float scale[kLoads][WEIGHT ? 1 : 8];
+  auto read = [&](int64_t s) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int id = i * T + (int)threadIdx.x;
+      held[i].clear();
+      if constexpr (WEIGHT) {
+        const int64_t row = s * kStep32 + id / (BR / 8);
+        const int n = a.rows - r0 - id % (BR / 8) * 8;
+        scale[i][0] = 0.f;
+        if (row < a.sum && n > 0) {
+          held[i].load(a.dy.row(row) + (int64_t)(a.rows - n) * 4, n);
+          scale[i][0] = a.c.scale[row];
+        }
+      } else {
+        const int64_t at = s * kStep32 + id % 4 * 8;
+        const int n = (int)min(a.sum - at, (int64_t)8);
+        if (n > 0) held[i].load(a.dy.row(min(r0 + id / 4, a.rows - 1)) + at * 4, n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) scale[i][k] = k < n ? a.c.scale[at + k] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kCodes; ++i) {
+      const int id = i * T + (int)threadIdx.x, col = id % (BC / 16) * 16;
+      const int64_t row = s * kStep32 + id / (BC / 16);
+      codes[i] = Quad{0, 0, 0, 0};
+      if (row < a.sum && c0 + col < a.cols) codes[i] = load16(a.c.codes + row * a.c.stride + c0 + col, a.cols - c0 - col);
+    }
+  };
+  auto place = [&](int64_t s) {
+    char* l = place_of(s);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int id = i * T + (int)threadIdx.x;
+      float f[8];
+      held[i].get(f);
+      u32v4 h, m, lo;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) {
+        uint32_t x, y, z;
+        split_pair(f[2 * d] * scale[i][WEIGHT ? 0 : 2 * d], f[2 * d + 1] * scale[i][WEIGHT ? 0 : 2 * d + 1], x, y, z);
+        h[d] = x;
+        m[d] = y;
+        lo[d] = z;
+      }
+      int at;
+      if constexpr (WEIGHT) {
+        const int row = id / (BR / 8), c = id % (BR / 8);
+        at = row * (BR * 2) + ((c / 2) ^ bend(row)) * 32 + c % 2 * 16;
+      } else {
+        const int row = id / 4;                                    // rows of 64 bytes, two to all banks
+        at = row * 64 + ((id % 4) ^ (row / 2 % 4)) * 16;
+      }
+      *reinterpret_cast<u32v4*>(l + at) = h;
+      *reinterpret_cast<u32v4*>(l + kPart + at) = m;
+      *reinterpret_cast<u32v4*>(l + 2 * kPart + at) = lo;
+    }
+#pragma unroll
+    for (int i = 0; i < kCodes; ++i) {
+      const int id = i * T + (int)threadIdx.x, row = id / (BC / 16), block = id % (BC / 16);
+      Quad q[2];
+      widen16<TGRAD_BF16>(codes[i], 1.f, q);
+      char* at = l + 3 * kPart + row * (BC * 2) + (block ^ bend(row)) * 32;
+      const bool upper = lane & 4;
+      *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
+      *reinterpret_cast<Quad*>(at + (upper ? 0 : 16)) = upper ? q[0] : q[1];
+    }
+  };
+
+  v4f acc[FC][FR] = {};
+  const int wr = wave % WR, wc = wave / WR;
+  auto multiply = [&](int64_t s) {
+    const char* l = place_of(s);
+    Quad c[FC];
+#pragma unroll
+    for (int i = 0; i < FC; ++i) c[i] = across<BC>(l + 3 * kPart, 0, wc * FC + i, lane);
+#pragma unroll
+    for (int p = 2; p >= 0; --p) {          // the smallest part first
+      Quad d[FR];
+#pragma unroll
+      for (int j = 0; j < FR; ++j) {
+        const int row = (wr * FR + j) * 16 + lane % 16;
+        if constexpr (WEIGHT) d[j] = across<BR>(l + p * kPart, 0, wr * FR + j, lane);
+        else d[j] = *reinterpret_cast<const Quad*>(l + p * kPart + row * 64 + ((lane / 16) ^ (row / 2 % 4)) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < FC; ++i)
+#pragma unroll
+        for (int j = 0; j < FR; ++j) acc[i][j] = mfma_of<TGRAD_BF16>(c[i], d[j], acc[i][j]);
+    }
+  };
+
+  read(first);
+  place(first);
+  if (first + 1 < last) read(first + 1);
+  for (int64_t s = first; s < last; ++s) {
+    __syncthreads();
+    if (s + 1 < last) place(s + 1);
+    if (s + 2 < last) read(s + 2);
+    multiply(s);
+  }
+#pragma unroll
+  for (int j = 0; j < FR; ++j) {
+    const int r = r0 + (wr * FR + j) * 16 + lane % 16;
+    if (r >= a.rows) continue;
+    char* row = a.out.row((int64_t)split * a.rows + r);
+#pragma unroll
+    for (int i = 0; i < FC; ++i) {
+      const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
+      if (c < a.cols) store4<TGRAD_F32>(row, c, a.cols, acc[i][j]);
+    }
+  }
+}
+
+// ---- float32 dy, a scale for groups of columns: 64 x 64 results a workgroup, 4 x 4 a thread, float32 ---------------------------------------
+
+template <bool WEIGHT>
+__global__ __launch_bounds__(256) void k_grad_groups(Grad a) {
+  __shared__ float as[16][65], bs[16][65];
+  const int r0 = blockIdx.x / a.tiles_c * 64, c0 = blockIdx.x % a.tiles_c * 64;
+  const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
+  float acc[4][4] = {};
+  for (int64_t s0 = 0; s0 < a.sum; s0 += 16) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x + 256 * i;
+      const int s = WEIGHT ? e / 64 : e % 16, r = WEIGHT ? e % 64 : e / 16, v = e / 64, k = e % 64;
+      float x = 0.f, y = 0.f;
+      if (s0 + s < a.sum && r0 + r < a.rows)
+        x = WEIGHT ? reinterpret_cast<const float*>(a.dy.row(s0 + s))[r0 + r] : reinterpret_cast<const float*>(a.dy.row(r0 + r))[s0 + s];
+      if (s0 + v < a.sum && c0 + k < a.cols)
+        y = (float)a.c.codes[(s0 + v) * a.c.stride + c0 + k] * a.c.scale[(s0 + v) * a.c.groups + ((c0 + k) >> a.c.shift)];
+      as[s][r] = x;
+      bs[v][k] = y;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 16; ++s)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] += as[s][tr + 16 * i] * bs[s][tc + 16 * j];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = r0 + tr + 16 * i, k = c0 + tc + 16 * j;
+      if (r < a.rows && k < a.cols) reinterpret_cast<float*>(a.out.row(r))[k] = acc[i][j];
+    }
+}
+
+// The splits' sums, added up in their order: four results a thread.
+template <int OT>
+__global__ __launch_bounds__(256) void k_add_splits(const float* __restrict__ part, int splits, int rows, int cols, Mat out) {
+  const int64_t per = (cols + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int r = (int)(id / per), c = (int)(id % per) * 4;
+  if (r >= rows) return;
+  v4f sum = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const float* from = part + ((int64_t)s * rows + r) * cols + c;
+    if (c + 4 <= cols) {
+      sum += __builtin_bit_cast(v4f, *reinterpret_cast<const QuadAny*>(from));
+    } else {
+      for (int k = 0; k < cols - c; ++k) sum[k] += from[k];
+    }
+  }
+  store4<OT>(out.row(r), c, cols, sum);
+}
+
+// ---- host -------------------------------------------------------------------------------------------------------------------------------
+
+struct Cut {
+  int tile, tiles_c, tiles, splits, steps;
+};
+// Tiles of 256 x 256 where they fill three quarters of the compute units (one workgroup each), else of 128 x 128 and the sum in splits where there are
+// fewer than two for every compute unit.
+Cut cut_of(int64_t rows, int64_t cols, int64_t sum, bool wide, int step) {
+  auto tiles = [&](int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
+  Cut c;
+  c.tile = wide && tiles(256) >= 192 ? 256 : 128;
+  c.tiles_c = (int)((cols + c.tile - 1) / c.tile);
+  c.tiles = (int)std::max<int64_t>(1, std::min<int64_t>(tiles(c.tile), kMostRows));
+  const int64_t steps = std::max<int64_t>(1, (sum + step - 1) / step);
+  const int64_t splits = c.tile == 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(512 / c.tiles, steps / 4));
+  c.steps = (int)((steps + splits - 1) / splits);
+  c.splits = (int)((steps + c.steps - 1) / c.steps);
+  return c;
+}
+
+template <typename Kern>
+void launch_cut(hipStream_t s, Kern k, int threads, size_t lds, const Cut& c, const Grad& g) {
+  allow_lds(k, lds);
+  k<<<dim3((uint32_t)(c.tiles * c.splits)), dim3(threads), lds, s>>>(g);
+}
+
+template <int DT, int OT, bool WEIGHT>
+void launch_tiles(hipStream_t s, const Cut& c, bool direct, const Grad& g) {
+  constexpr size_t big = 2 * (256 + 256) * kStep * 2, small = 2 * (128 + 128) * kStep * 2;
+  if constexpr (OT >= 0) {
+    if (c.tile == 256) return launch_cut(s, k_grad_tiles<4, 2, 4, 8, DT, OT, WEIGHT, false>, 512, big, c, g);
+  }
+  if (direct) launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, false>, 256, small, c, g);
+  else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, true>, 256, small, c, g);
+}
+
+void launch_add(hipStream_t s, const float* part, int splits, const tgrad_matrix* out) {
+  const int64_t threads = out->rows * ((out->cols + 3) / 4);
+  for_real(out->dtype, [&](auto t) {
+    k_add_splits<decltype(t)::value><<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, s>>>(part, splits, (int)out->rows, (int)out->cols, mat(out));
+  });
+}
+
+// dy that goes straight to LDS: 16-byte rows, whole chunks of eight across the sum, offsets of 32 bits within a tile.
+bool straight(const tgrad_matrix* dy, bool weight) {
+  return (uintptr_t)dy->data % 16 == 0 && dy->row_stride % 8 == 0 && (!weight || dy->cols % 8 == 0) && dy->row_stride <= ((int64_t)1 << 21);
+}
+
+template <bool WEIGHT>
+void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {
+  Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0};
+  if (dy->dtype == TGRAD_F32 && g.c.groups > 1) {
+    g.tiles_c = (g.cols + 63) / 64;
+    k_grad_groups<WEIGHT><<<dim3((uint32_t)((g.rows + 63) / 64 * (int64_t)g.tiles_c)), dim3(256), 0, s>>>(g);
+    return;
+  }
+  const bool direct = dy->dtype != TGRAD_F32 && straight(dy, WEIGHT);
+  const Cut cut = cut_of(out->rows, out->cols, g.sum, direct, dy->dtype == TGRAD_F32 ? kStep32 : kStep);
+  g.tiles_c = cut.tiles_c;
+  g.tiles = cut.tiles;
+  g.steps = cut.steps;
+  if (cut.splits > 1) g.out = Mat{static_cast<char*>(scratch), out->cols * 4};
+  constexpr size_t lds32 = 2 * (3 * 128 + 128) * kStep32 * 2;
+  if (dy->dtype == TGRAD_F32) {
+    launch_cut(s, k_grad_split<2, 2, 4, 4, WEIGHT>, 256, lds32, cut, g);
+  } else if (cut.splits > 1) {
+    if (dy->dtype == TGRAD_BF16) launch_tiles<TGRAD_BF16, -1, WEIGHT>(s, cut, direct, g);
+    else launch_tiles<TGRAD_F16, -1, WEIGHT>(s, cut, direct, g);
+  } else if (dy->dtype == TGRAD_BF16) {
+    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_BF16, TGRAD_F32, WEIGHT>(s, cut, direct, g);
+    else launch_tiles<TGRAD_BF16, TGRAD_BF16, WEIGHT>(s, cut, direct, g);
+  } else {
+    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_F16, TGRAD_F32, WEIGHT>(s, cut, direct, g);
+    else launch_tiles<TGRAD_F16, TGRAD_F16, WEIGHT>(s, cut, direct, g);
+  }
+  if (cut.splits > 1) launch_add(s, static_cast<const float*>(scratch), cut.splits, out);
+}
+
+template <bool WEIGHT>
+int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
+  if (!good(dy) || !good(c) || !good(out) || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
+  if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
+  if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
+  if (too_many(out)) return TGRAD_ERR_UNSUPPORTED;
+  if (pending()) return TGRAD_ERR_HIP;
+  if (out->rows == 0) return TGRAD_OK;
+  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, workspace_dev);
+  return launched();
+}
+
+}  // namespace
+
+namespace tgrad {
+
+// Splits' sums, for the type of dy and the alignment that need most.
+size_t gradient_scratch(bool weight, int64_t tokens, int64_t inner, int64_t outer) {
+  const int64_t rows = weight ? outer : tokens, sum = weight ? tokens : outer;
+  size_t most = 0;
+  for (bool wide : {false, true})
+    for (int step : {kStep, kStep32}) {
+      const Cut c = cut_of(rows, inner, sum, wide, step);
+      if (c.splits > 1) most = std::max(most, (size_t)c.splits * rows * inner * 4);
+    }
+  return aligned(most);
+}
+
+}  // namespace tgrad
+
+extern "C" {
+
+int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream) {
+  return gradient<false>(dy, w, dx, workspace_dev, hip_stream);
+}
+
+int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream) {
+  return gradient<true>(dy, x, dw, workspace_dev, hip_stream);
+}
+
+}  // extern "C"

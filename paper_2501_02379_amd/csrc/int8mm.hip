@@ -1,48 +1,18 @@
-// Products with 8-bit codes: tokens times a weight, both as codes, and that product's two gradients, of which one factor is codes.
-#include "block8.h"
+// Tokens times a weight, both as 8-bit codes with a scale a row.
+#include "tiles8.h"
 
 using namespace tgrad;
 
 namespace tgrad {
 void launch_quantize(hipStream_t s, const tgrad_matrix* x, const tgrad_codes* out);
+size_t gradient_scratch(bool weight, int64_t tokens, int64_t inner, int64_t outer);
 }
 
 namespace {
 
 // ---- codes times codes: tiles of results, v_mfma_i32_16x16x64_i8 ----------------------------------------------------------------------
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef __amdgpu_buffer_rsrc_t Ref;
-
-constexpr int kStep = 128;                // bytes of the sum in memory on the chip at a time: a row of it is 8 chunks of 16
-
-__device__ __forceinline__ Quad load16(const int8_t* p, int64_t n) {
-  Quad q = {0, 0, 0, 0};
-  if (n >= 16) {
-    q = *reinterpret_cast<const QuadByte*>(p);
-  } else if (n > 0) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < n) q[i / 4] |= (uint32_t)(uint8_t)p[i] << (8 * (i % 4));
-  }
-  return q;
-}
-
-// Memory from p on, for loads that go straight to LDS: 16 bytes a lane, the lanes' one behind the other.
-__device__ __forceinline__ Ref ref(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, 0x7FFFFFF8, 0x00020000); }
-__device__ __forceinline__ void to_lds(const Ref& g, char* l, int each, int all) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(g, (__attribute__((address_space(3))) void*)l, 16, each, all, 0, 0);
-}
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-
-// A launch's workgroups go round the 8 dies; here each die gets neighbouring tiles, in bands of 4 tiles of rows, so that those at work at a time
-// share what its L2 holds.  -> (tile of rows, tile of columns)
-__device__ __forceinline__ int2 tile_of(int id, int total, int tiles_c) {
-  const int q = total / 8, r = total % 8, die = id % 8;
-  id = die * q + min(die, r) + id / 8;
-  const int band = id / (4 * tiles_c), in = id % (4 * tiles_c), tall = min(4, total / tiles_c - band * 4);
-  return make_int2(band * 4 + in % tall, in / tall);
-}
+constexpr int kStep = 128;                // bytes of the sum in LDS at a time: a row of it is 8 chunks of 16
 
 // y[t][n] = sum_k x[t][k] w[n][k].  WT x WN wavefronts, each FT x FN results of 16 x 16.  A step's 128 bytes of every row lie in LDS, chunk c of row r
 // at chunk c ^ (r % 8), so that eight rows' loads of one chunk meet eight banks; `BUFS` steps are there or on their way.  One
@@ -130,9 +100,8 @@ __global__ __launch_bounds__(WT * WN * 64) void k_codes_tiles(Codes8 x, Codes8 w
     for (int i = 0; i < BUFS - 1; ++i)
       if (first + i < whole) fill(first + i);
     for (int s = first; s < whole; ++s) {
-      if (s + BUFS - 2 < whole) wait_loads<kLoads * (BUFS - 2)>();
-      else wait_loads<0>();
-      __builtin_amdgcn_s_barrier();
+      if (s + BUFS - 2 < whole) barrier_but<kLoads * (BUFS - 2)>();
+      else barrier_but<0>();
       if (s + BUFS - 1 < whole) fill(s + BUFS - 1);
       multiply(s);
     }
@@ -299,51 +268,7 @@ __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, boo
   }
 }
 
-// ---- gradients: 64 x 64 results a workgroup, 4 x 4 a thread, float32 ---------------------------------------------------------------
-
-template <int DT, int OT, bool WEIGHT>
-__global__ __launch_bounds__(256) void k_grad_tile(Mat dy, Codes8 c, int64_t rows, int64_t cols, int64_t sum, Mat out) {
-  __shared__ float as[16][65], bs[16][65];
-  const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
-  const int tr = threadIdx.x / 16, tc = threadIdx.x % 16;
-  typedef typename Elem<DT>::raw raw;
-  float acc[4][4] = {};
-  for (int64_t s0 = 0; s0 < sum; s0 += 16) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = threadIdx.x + 256 * i;
-      const int s = WEIGHT ? e / 64 : e % 16, r = WEIGHT ? e % 64 : e / 16;
-      float a = 0.f, b = 0.f;
-      if (s0 + s < sum && r0 + r < rows) a = Elem<DT>::widen(WEIGHT ? reinterpret_cast<const raw*>(dy.row(s0 + s))[r0 + r] : reinterpret_cast<const raw*>(dy.row(r0 + r))[s0 + s]);
-      const int bs_s = e / 64, k = e % 64;
-      if (s0 + bs_s < sum && c0 + k < cols) {
-        b = (float)c.codes[(s0 + bs_s) * c.stride + c0 + k] * c.scale[(s0 + bs_s) * c.groups + ((c0 + k) >> c.shift)];
-        b = Elem<DT>::widen(Elem<DT>::narrow(in_float32(b)));
-      }
-      as[s][r] = a;
-      bs[bs_s][k] = b;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < 16; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += as[s][tr + 16 * i] * bs[s][tc + 16 * j];
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = r0 + tr + 16 * i, k = c0 + tc + 16 * j;
-      if (r < rows && k < cols) reinterpret_cast<typename Elem<OT>::raw*>(out.row(r))[k] = Elem<OT>::narrow(acc[i][j]);
-    }
-}
-
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
-
-size_t aligned(size_t n) { return (n + kScratchAlign - 1) / kScratchAlign * kScratchAlign; }
 
 size_t few_lds(int64_t tokens, int64_t inner) {
   return sizeof(int) * kFewWaves * kWave * 4 + 16 * 4 + kFewWaves * 4 + (size_t)tokens * ((inner + 63) / 64 * 64);
@@ -368,7 +293,7 @@ Cut cut_of(int64_t tokens, int64_t outer, int64_t inner, bool direct) {
   Cut c;
   c.tile = tokens <= 64 ? 64 : direct && tiles(256) >= 192 ? 256 : 128;
   c.tiles_n = (int)((outer + c.tile - 1) / c.tile);
-  c.tiles = (int)std::min<int64_t>(tiles(c.tile), kMostRows);
+  c.tiles = (int)std::max<int64_t>(1, std::min<int64_t>(tiles(c.tile), kMostRows));
   const int64_t steps = (inner + kStep - 1) / kStep, want = c.tile == 256 ? 1 : c.tile == 128 ? 512 : 1024;
   int64_t splits = std::max<int64_t>(1, std::min<int64_t>(want / c.tiles, steps / 4));
   c.steps = (int)((steps + splits - 1) / splits);
@@ -428,33 +353,6 @@ void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, c
   }
 }
 
-template <bool WEIGHT>
-void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out) {
-  const int64_t sum = WEIGHT ? dy->rows : dy->cols;
-  for_real(dy->dtype, [&](auto t) {
-    constexpr int DT = decltype(t)::value;
-    const dim3 grid((uint32_t)((out->cols + 63) / 64), (uint32_t)((out->rows + 63) / 64));
-    if (out->dtype == DT) k_grad_tile<DT, DT, WEIGHT><<<grid, dim3(256), 0, s>>>(mat(dy), codes8(c), out->rows, out->cols, sum, mat(out));
-    else k_grad_tile<DT, TGRAD_F32, WEIGHT><<<grid, dim3(256), 0, s>>>(mat(dy), codes8(c), out->rows, out->cols, sum, mat(out));
-  });
-}
-
-// A launch has fewer than 2^32 threads.
-bool too_many(const tgrad_matrix* y) { return ((y->rows + 63) / 64) * ((y->cols + 63) / 64) >= ((int64_t)1 << 21); }
-
-bool scratch_ok(const void* p) { return p && (uintptr_t)p % kScratchAlign == 0; }
-
-template <bool WEIGHT>
-int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
-  if (!good(dy) || !good(c) || !good(out) || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
-  if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
-  if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
-  if (pending()) return TGRAD_ERR_HIP;
-  if (out->rows == 0) return TGRAD_OK;
-  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out);
-  return launched();
-}
-
 }  // namespace
 
 extern "C" {
@@ -466,6 +364,8 @@ int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer,
   if (op == TGRAD_CODES_MATMUL || op == TGRAD_CODES_LINEAR) {
     if (inner <= TGRAD_CODES_MAX_INNER && tokens > 0) n += part_bytes(tokens, outer, inner);
     if (op == TGRAD_CODES_LINEAR) n += scratch_codes(tokens, inner);
+  } else {
+    n += gradient_scratch(op == TGRAD_CODES_GRAD_WEIGHT, tokens, inner, outer);
   }
   *workspace_bytes = n;
   return TGRAD_OK;
@@ -505,14 +405,6 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
   launch_quantize(s, x, c);
   launch_product(s, c, w, y, workspace_dev);
   return launched();
-}
-
-int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream) {
-  return gradient<false>(dy, w, dx, workspace_dev, hip_stream);
-}
-
-int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream) {
-  return gradient<true>(dy, x, dw, workspace_dev, hip_stream);
 }
 
 }  // extern "C"

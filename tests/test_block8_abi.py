@@ -133,6 +133,8 @@ def test_sizes_of_scratch():
         got.append(n.value)
     assert got == sorted(got)
     for op in range(4):
+        for sizes in ((0, 33, 55), (77, 33, 0), (0, 33, 0), (1, 1, 1), (1, 1 << 20, 1 << 20)):
+            assert lib.tgrad_codes_query_size(op, *sizes, C.byref(n)) == T.TGRAD_OK and n.value >= 256
         assert lib.tgrad_codes_query_size(op, 77, 33, 55, C.byref(n)) == T.TGRAD_OK and n.value >= 256
     for args in ((-1, 1, 1, 1), (4, 1, 1, 1), (0, -1, 1, 1), (0, 1, 0, 1), (0, 1, 1, -1), (0, 1 << 31, 1, 1), (0, 1, 1 << 31, 1)):
         assert lib.tgrad_codes_query_size(*args, C.byref(n)) == BAD

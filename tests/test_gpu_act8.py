@@ -171,7 +171,7 @@ def test_what_lies_between_rows_stays():
 
 # tokens, inner, outer: single tokens, a few, ordinary; sums of odd length, shorter than a step, long ones
 PRODUCTS = [(1, 1, 1), (1, 16, 5), (1, 4096, 300), (2, 100, 64), (3, 129, 1000), (7, 8190, 33), (16, 256, 257), (17, 1000, 130), (33, 64, 64),
-            (64, 640, 513), (100, 77, 300), (130, 1300, 260), (256, 512, 256), (257, 257, 257), (300, 128, 1024), (511, 2304, 700),
+            (64, 640, 513), (100, 77, 300), (130, 1300, 260), (256, 512, 256), (257, 257, 257), (300, 128, 1024), (511, 2304, 700), (3600, 333, 3700),
             (1, 131072, 3), (40, 131072, 17)]
 
 
@@ -222,7 +222,8 @@ def test_a_token_with_a_nan_spoils_its_own_row_alone():
 
 
 GRADS = [(1, 1, 1), (1, 300, 77), (5, 64, 33), (31, 65, 130), (64, 128, 256), (100, 513, 66), (257, 255, 129), (640, 96, 300), (2051, 70, 40),
-         (300, 1030, 520), (5000, 64, 32), (20000, 33, 48)]
+         (300, 1030, 520), (5000, 64, 32), (20000, 33, 48), (3584, 96, 100),
+         (3700, 3588, 40), (40, 3700, 3592)]
 
 
 def close_gradient(got, a, b, dtype, out, terms):

@@ -244,6 +244,135 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
   }
 }
 
+// The same with 256 x 256 results of 8 wavefronts, 2 x 4 of 8 x 4, in steps of 32 of which four are there or on their way, in turns: wavefronts 0 to 3 read a
+// step's operands while 4 to 7, a turn behind, multiply the step before.  dy goes straight to LDS three steps ahead; codes are loaded four
+// steps ahead and widened into LDS two steps ahead.  All loads are unconditional, of memory that ends where the matrices do, so that they are
+// counted the same in every step and read 0 behind the sum's end.
+// dy: 16-byte rows, whole chunks of eight columns; codes: 16-byte rows, whole chunks of 16 columns.
+constexpr int kWide = 256, kWideStep = 32, kWideBufs = 4, kWideDy = kWide * kWideStep * 2, kWideBytes = 2 * kWideDy;
+
+template <int DT, int OT, bool WEIGHT>
+__global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
+  constexpr int T = 512, FR = 8, FC = 4, kLoads = kWideDy / 16 / T;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int2 tile = tile_of(blockIdx.x, a.tiles, a.tiles_c);
+  const int r0 = tile.x * kWide, c0 = tile.y * kWide;
+  const int steps = (int)((a.sum + kWideStep - 1) / kWideStep);
+
+  // dy: what lies beyond its rows or columns is loaded from within, and its results are not stored
+  int each[kLoads], ahead[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int id = i * T + (int)threadIdx.x;
+    if constexpr (WEIGHT) {
+      const int row = id / 32, c = id % 32, chunk = ((c / 2) ^ bend(row)) * 2 + c % 2;
+      each[i] = row * (int)a.dy.stride + min(chunk * 8, a.rows - r0 - 8) * 2;
+      ahead[i] = 0;
+    } else {
+      const int row = id / 4, chunk = (id % 4) ^ (row / 2 % 4);
+      each[i] = min(row, a.rows - 1 - r0) * (int)a.dy.stride + chunk * 16;
+      ahead[i] = chunk * 8;
+    }
+  }
+  const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
+  auto fill = [&](int s) {
+    const int left = (int)min(a.sum - (int64_t)s * kWideStep, (int64_t)kWideStep);
+    char* l = lds + s % kWideBufs * kWideBytes + wave * kWave * 16;
+    if constexpr (WEIGHT) {
+      const Ref g = ref(dy0 + (int64_t)s * kWideStep * a.dy.stride, left > 0 ? (left - 1) * (int)a.dy.stride + min(a.rows - r0, kWide) * 2 : 0);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, each[i], 0);
+    } else {
+      const Ref g = ref(dy0 + (int64_t)s * kWideStep * 2);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, ahead[i] < left ? each[i] : 0x7FFFFFFC, 0);
+    }
+  };
+
+  // codes: 16 of a row for each thread
+  const int row = threadIdx.x / 16, block = threadIdx.x % 16;
+  const int code_at = row * (int)a.c.stride + block * 16;
+  const int scale_at = (row * (int)a.c.groups + ((c0 + block * 16) >> a.c.shift)) * 4;
+  struct Held {
+    Quad codes;
+    float scale;
+  };
+  auto read_codes = [&](int s, Held& h) {
+    const int left = (int)max((int64_t)0, min(a.sum - (int64_t)s * kWideStep, (int64_t)kWideStep));
+    const int64_t from = left > 0 ? (int64_t)s * kWideStep : 0;
+    const Ref c = ref(a.c.codes + from * a.c.stride + c0, left > 0 ? (left - 1) * (int)a.c.stride + a.cols - c0 : 0);
+    const Ref g = ref(a.c.scale + from * a.c.groups, left * (int)a.c.groups * 4);
+    h.codes = __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(c, code_at, 0, 0));
+    h.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(g, scale_at, 0, 0));
+  };
+  const int place = kWideDy + row * (kWide * 2) + (block ^ bend(row)) * 32;
+  auto place_codes = [&](int s, const Held& h) {
+    Quad q[2];
+    widen16<DT>(h.codes, h.scale, q);
+    char* at = lds + s % kWideBufs * kWideBytes + place;
+    const bool upper = lane & 4;            // lanes 4 to 7 store their upper halves first: eight lanes then meet all banks
+    *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
+    *reinterpret_cast<Quad*>(at + (upper ? 0 : 16)) = upper ? q[0] : q[1];
+  };
+
+  v4f acc[FC][FR] = {};
+  const int wc = wave % 4, wr = wave / 4;
+  const bool late = wave >= 4;
+  auto step = [&](int s, Held& h) {
+    Quad c[FC], d[FR];
+    const char* l = lds + s % kWideBufs * kWideBytes;
+    fill(s + 3);                            // behind the sum's end it fills with zeros, which nobody reads
+    place_codes(s + 2, h);
+    read_codes(s + 4, h);
+#pragma unroll
+    for (int i = 0; i < FC; ++i) c[i] = across<kWide>(l + kWideDy, 0, wc * FC + i, lane);
+#pragma unroll
+    for (int j = 0; j < FR; ++j) {
+      if constexpr (WEIGHT) d[j] = across<kWide>(l, 0, wr * FR + j, lane);
+      else d[j] = *reinterpret_cast<const Quad*>(l + ((wr * FR + j) * 16 + lane % 16) * 64 + ((lane / 16) ^ (lane / 2 % 4)) * 16);
+    }
+    // still on their way: codes of s + 2 (placed, so there), dy of s + 2, codes of s + 3, dy of s + 3, codes of s + 4
+    turn_but<2 * (kLoads + 2)>();
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < FC; ++i)
+#pragma unroll
+      for (int j = 0; j < FR; ++j) acc[i][j] = mfma_of<DT>(c[i], d[j], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
+    turn();
+  };
+  Held h0, h1;
+  read_codes(0, h0);
+  read_codes(1, h1);
+  fill(0);
+  fill(1);
+  fill(2);
+  place_codes(0, h0);
+  place_codes(1, h1);
+  read_codes(2, h0);
+  read_codes(3, h1);
+  turn_but<0>();
+  if (late) turn();
+  for (int s = 0; s < steps; s += 2) {
+    step(s, h0);
+    step(s + 1, h1);                        // with an odd number of steps the last one adds zeros
+  }
+  if (!late) turn();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < FR; ++j) {
+    const int r = r0 + (wr * FR + j) * 16 + lane % 16;
+    if (r >= a.rows) continue;
+    char* out = a.out.row(r);
+#pragma unroll
+    for (int i = 0; i < FC; ++i) {
+      const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
+      if (c < a.cols) store4<OT>(out, c, a.cols, acc[i][j]);
+    }
+  }
+}
+
 // ---- float32 dy, a scale for each row of codes -------------------------------------------------------------------------------------------
 
 // dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_pair); codes are exact in bf16.  Three products instead
@@ -465,9 +594,9 @@ void launch_cut(hipStream_t s, Kern k, int threads, size_t lds, const Cut& c, co
 
 template <int DT, int OT, bool WEIGHT>
 void launch_tiles(hipStream_t s, const Cut& c, bool direct, const Grad& g) {
-  constexpr size_t big = 2 * (256 + 256) * kStep * 2, small = 2 * (128 + 128) * kStep * 2;
+  constexpr size_t small = 2 * (128 + 128) * kStep * 2;
   if constexpr (OT >= 0) {
-    if (c.tile == 256) return launch_cut(s, k_grad_tiles<4, 2, 4, 8, DT, OT, WEIGHT, false>, 512, big, c, g);
+    if (c.tile == kWide) return launch_cut(s, k_grad_wide<DT, OT, WEIGHT>, 512, kWideBufs * kWideBytes, c, g);
   }
   if (direct) launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, false>, 256, small, c, g);
   else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, true>, 256, small, c, g);
@@ -485,6 +614,8 @@ bool straight(const tgrad_matrix* dy, bool weight) {
   return (uintptr_t)dy->data % 16 == 0 && dy->row_stride % 8 == 0 && (!weight || dy->cols % 8 == 0) && dy->row_stride <= ((int64_t)1 << 21);
 }
 
+bool straight(const tgrad_codes* c) { return (uintptr_t)c->codes % 16 == 0 && c->row_stride % 16 == 0 && c->row_stride <= ((int64_t)1 << 22); }
+
 template <bool WEIGHT>
 void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {
   Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0};
@@ -494,7 +625,8 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
     return;
   }
   const bool direct = dy->dtype != TGRAD_F32 && straight(dy, WEIGHT);
-  const Cut cut = cut_of(out->rows, out->cols, g.sum, direct, dy->dtype == TGRAD_F32 ? kStep32 : kStep);
+  const bool wide = direct && dy->cols % 8 == 0 && c->cols % 16 == 0 && straight(c);
+  const Cut cut = cut_of(out->rows, out->cols, g.sum, wide, dy->dtype == TGRAD_F32 ? kStep32 : kStep);
   g.tiles_c = cut.tiles_c;
   g.tiles = cut.tiles;
   g.steps = cut.steps;

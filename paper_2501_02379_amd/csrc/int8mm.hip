@@ -14,13 +14,29 @@ namespace {
 
 constexpr int kStep = 128;                // bytes of the sum in LDS at a time: a row of it is 8 chunks of 16
 
+// Four neighbours of a row of results.
+template <int OT>
+__device__ __forceinline__ void store_scaled(char* row, int n, int outer, i32x4 sum, float sx, const float* sw) {
+  typedef typename Elem<OT>::raw raw;
+  raw* to = reinterpret_cast<raw*>(row) + n;
+  if (n + 4 <= outer) {
+    float f[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) f[r] = scaled(sum[r], sx, sw[n + r]);
+    *reinterpret_cast<typename Four<OT>::any*>(to) = Four<OT>::narrow(f);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < outer) to[r] = Elem<OT>::narrow(scaled(sum[r], sx, sw[n + r]));
+  }
+}
+
 // y[t][n] = sum_k x[t][k] w[n][k].  WT x WN wavefronts, each FT x FN results of 16 x 16.  A step's 128 bytes of every row lie in LDS, chunk c of row r
 // at chunk c ^ (r % 8), so that eight rows' loads of one chunk meet eight banks; `BUFS` steps are there or on their way.  One
 // barrier a step: it says that everyone's part of this step has arrived and that everyone is done with the step before, whose place is filled
 // next.  OT < 0: sums go to `part`, [split][tokens][outer], and are added up by k_add_parts.
 // STAGED: rows that do not start at multiples of 16 bytes go through registers.
-// 8192^3: 457 us, 2400 TOP/s with 4 x 2 wavefronts of 4 x 8 results (2 x 4 of 8 x 4: 519; four wavefronts of 8 x 8: 582; 128 x 128 tiles, two
-// workgroups a compute unit: 546).
+// (8192^3 in tiles of 128 x 128, two workgroups a compute unit: 546 us; four wavefronts of 8 x 8 results: 582.)
 template <int WT, int WN, int FT, int FN, int BUFS, bool STAGED, int OT>
 __global__ __launch_bounds__(WT * WN * 64) void k_codes_tiles(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int* part, int tiles_n, int tiles,
                                                               int steps_a_split) {
@@ -133,20 +149,94 @@ __global__ __launch_bounds__(WT * WN * 64) void k_codes_tiles(Codes8 x, Codes8 w
             if (n + r < outer) to[r] = acc[i][j][r];
         }
       } else {
-        typedef typename Elem<OT>::raw raw;
-        raw* to = reinterpret_cast<raw*>(y.row(t)) + n;
-        if (n + 4 <= outer) {
-          float f[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) f[r] = scaled(acc[i][j][r], sx, w.scale[n + r]);
-          *reinterpret_cast<typename Four<OT>::any*>(to) = Four<OT>::narrow(f);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (n + r < outer) to[r] = Elem<OT>::narrow(scaled(acc[i][j][r], sx, w.scale[n + r]));
-        }
+        store_scaled<OT>(y.row(t), n, outer, acc[i][j], sx, w.scale);
       }
     }
+  }
+}
+
+// The same with 256 x 256 results of 8 wavefronts, 2 x 4 of 8 x 4, in steps of 64 bytes of which four are there or on their way (rows of 64 bytes, chunk c of row
+// r at chunk c ^ (r / 2 % 4)).  A step is two turns: wavefronts 0 to 3 read the step's operands while 4 to 7, a turn behind, multiply the
+// step before.  What is filled in a step was last read three turns ago at least, and is read five or six turns later.
+// 8192^3: 445 us, 2470 TOP/s, where k_codes_tiles of this size takes 510 (4 x 2 of 4 x 8: 488).  Registers alone, with no memory, reach 3260 to 4020 on random codes: the
+// card's power is the limit then (4800 on zeros).
+constexpr int kWide = 256, kWideStep = 64, kWideBufs = 4, kWideBytes = 2 * kWide * kWideStep;
+
+template <int OT>
+__global__ __launch_bounds__(512) void k_codes_wide(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int tiles_n, int tiles) {
+  constexpr int T = 512, FT = 8, FN = 4, kLoads = kWideBytes / 16 / T, kLoadsN = kLoads / 2;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
+  const int2 tile = tile_of(blockIdx.x, tiles, tiles_n);
+  const int t0 = tile.x * kWide, n0 = tile.y * kWide;
+  const int8_t* xp = x.codes + (int64_t)t0 * x.stride;
+  const int8_t* wp = w.codes + (int64_t)n0 * w.stride;
+  auto row_of = [&](int i) {
+    const int r = (i * T + (int)threadIdx.x) / 4;
+    return i < kLoadsN ? min(r, outer - 1 - n0) : min(r - kWide, tokens - 1 - t0);
+  };
+  const int chunk = ((int)threadIdx.x % 4 ^ (int)threadIdx.x / 8 % 4) * 16;
+  int each[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) each[i] = row_of(i) * (int)(i < kLoadsN ? w.stride : x.stride) + chunk;
+  const Ref xr = ref(xp), wr = ref(wp);
+  auto fill = [&](int s) {
+    char* l = lds + s % kWideBufs * kWideBytes + wave * kWave * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) to_lds(i < kLoadsN ? wr : xr, l + i * T * 16, each[i], s * kWideStep);
+  };
+  i32x4 acc[FN][FT] = {};
+  const int wn = wave % 4, wt = wave / 4;
+  const int at = lane % 16 * kWideStep + ((lane / 16) ^ (lane / 2 % 4)) * 16;
+  i32x4 a[FN], b[FT];
+  auto operands = [&](int s) {
+    const char* l = lds + s % kWideBufs * kWideBytes + at;
+#pragma unroll
+    for (int i = 0; i < FN; ++i) a[i] = *reinterpret_cast<const i32x4*>(l + (wn * FN + i) * 16 * kWideStep);
+#pragma unroll
+    for (int j = 0; j < FT; ++j) b[j] = *reinterpret_cast<const i32x4*>(l + (kWide + (wt * FT + j) * 16) * kWideStep);
+  };
+  auto multiply = [&]() {
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int j = 0; j < FT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[j], acc[i][j], 0, 0, 0);
+  };
+  const int whole = inner / kWideStep;
+  const bool late = wave >= 4;
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (i < whole) fill(i);
+  turn_but<0>();
+  if (late) turn();
+  for (int s = 0; s < whole; ++s) {
+    if (s + 3 < whole) fill(s + 3);
+    operands(s);
+    if (s + 3 < whole) turn_but<2 * kLoads>();
+    else turn_but<0>();
+    __builtin_amdgcn_s_setprio(1);
+    multiply();
+    __builtin_amdgcn_s_setprio(0);
+    turn();
+  }
+  if (!late) turn();
+  if (whole * kWideStep < inner) {        // the sum's end, less than a step, through registers; everyone is done with the first place
+    char* l = lds + whole % kWideBufs * kWideBytes + threadIdx.x * 16;
+    const int from = whole * kWideStep + chunk;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      *reinterpret_cast<Quad*>(l + i * T * 16) = load16((i < kLoadsN ? wp + row_of(i) * w.stride : xp + row_of(i) * x.stride) + from, inner - from);
+    __syncthreads();
+    operands(whole);
+    multiply();
+  }
+#pragma unroll
+  for (int j = 0; j < FT; ++j) {
+    const int t = t0 + (wt * FT + j) * 16 + lane % 16;
+    if (t >= tokens) continue;
+    const float sx = x.scale[t];
+#pragma unroll
+    for (int i = 0; i < FN; ++i) store_scaled<OT>(y.row(t), n0 + (wn * FN + i) * 16 + lane / 16 * 4, outer, acc[i][j], sx, w.scale);
   }
 }
 
@@ -322,7 +412,11 @@ template <bool STAGED, int OT>
 void launch_tiles(hipStream_t s, const Cut& c, const Codes8& x, const Codes8& w, const tgrad_matrix* y, int inner, int* part) {
   if (c.tile == 64) launch_tiles_as<2, 2, 2, 2, STAGED ? 2 : 3, STAGED, OT>(s, c, x, w, y, inner, part);
   else if (STAGED || c.tile == 128) launch_tiles_as<2, 2, 4, 4, 2, STAGED, OT>(s, c, x, w, y, inner, part);
-  else if constexpr (OT >= 0) launch_tiles_as<4, 2, 4, 8, 2, false, OT>(s, c, x, w, y, inner, part);
+  else if constexpr (OT >= 0) {
+    auto k = k_codes_wide<OT>;
+    allow_lds(k, kWideBufs * kWideBytes);
+    k<<<dim3((uint32_t)c.tiles), dim3(512), kWideBufs * kWideBytes, s>>>(x, w, (int)y->rows, (int)y->cols, inner, mat(y), c.tiles_n, c.tiles);
+  }
 }
 
 void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* parts) {

@@ -21,7 +21,9 @@ __device__ __forceinline__ Quad load16(const int8_t* p, int64_t n) {
 }
 
 // Memory from p on, for loads that go straight to LDS: 16 bytes a lane, the lanes' one behind the other.
-__device__ __forceinline__ Ref ref(const void* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, 0x7FFFFFF8, 0x00020000); }
+__device__ __forceinline__ Ref ref(const void* p, int bytes = 0x7FFFFFF8) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, bytes, 0x00020000);       // what lies behind `bytes` reads as 0
+}
 __device__ __forceinline__ void to_lds(const Ref& g, char* l, int each, int all) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(g, (__attribute__((address_space(3))) void*)l, 16, each, all, 0, 0);
 }
@@ -31,6 +33,22 @@ __device__ __forceinline__ void barrier_but() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// The same for the wide tiles, whose two halves of a workgroup take turns: while four wavefronts, one on each SIMD, read operands, the other four
+// multiply.  Nothing moves across.
+template <int N>
+__device__ __forceinline__ void turn_but() {
+  __builtin_amdgcn_sched_barrier(0);
+  barrier_but<N>();
+  __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void turn() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // A launch's workgroups go round the 8 dies; here each die gets neighbouring tiles, in bands of 4 tiles of rows, so that those at work at a time

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
     const Ref g = ref(dy0 + (WEIGHT ? s * kStep * a.dy.stride : s * kStep * 2));
     char* l = place_of(s) + wave * kWave * 16;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, each[i], 0);
+    for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, each[i]);
   };
   Quad held[kLoads];
   auto read = [&](int64_t s) {
@@ -276,17 +276,19 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     }
   }
   const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
+  const int sum = (int)a.sum, across_bytes = min(a.rows - r0, kWide) * 2;
   auto fill = [&](int s) {
-    const int left = (int)min(a.sum - (int64_t)s * kWideStep, (int64_t)kWideStep);
+    const int left = min(sum - s * kWideStep, kWideStep);
     char* l = lds + s % kWideBufs * kWideBytes + wave * kWave * 16;
     if constexpr (WEIGHT) {
-      const Ref g = ref(dy0 + (int64_t)s * kWideStep * a.dy.stride, left > 0 ? (left - 1) * (int)a.dy.stride + min(a.rows - r0, kWide) * 2 : 0);
+      const int bytes = (left - 1) * (int)a.dy.stride + across_bytes;
+      const Ref g = ref(dy0 + (int64_t)s * kWideStep * a.dy.stride, left > 0 ? bytes : 0);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, each[i], 0);
+      for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, each[i]);
     } else {
       const Ref g = ref(dy0 + (int64_t)s * kWideStep * 2);
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) to_lds(g, l + i * T * 16, ahead[i] < left ? each[i] : 0x7FFFFFFC, 0);
+      for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, ahead[i] < left ? each[i] : 0x7FFFFFFC);
     }
   };
 
@@ -299,10 +301,10 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     float scale;
   };
   auto read_codes = [&](int s, Held& h) {
-    const int left = (int)max((int64_t)0, min(a.sum - (int64_t)s * kWideStep, (int64_t)kWideStep));
-    const int64_t from = left > 0 ? (int64_t)s * kWideStep : 0;
-    const Ref c = ref(a.c.codes + from * a.c.stride + c0, left > 0 ? (left - 1) * (int)a.c.stride + a.cols - c0 : 0);
-    const Ref g = ref(a.c.scale + from * a.c.groups, left * (int)a.c.groups * 4);
+    const int left = min(sum - s * kWideStep, kWideStep);
+    const int bytes = (left - 1) * (int)a.c.stride + a.cols - c0;
+    const Ref c = ref(a.c.codes + (int64_t)s * kWideStep * a.c.stride + c0, left > 0 ? bytes : 0);
+    const Ref g = ref(a.c.scale + (int64_t)s * kWideStep * a.c.groups, max(left, 0) * (int)a.c.groups * 4);
     h.codes = __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(c, code_at, 0, 0));
     h.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(g, scale_at, 0, 0));
   };
@@ -322,9 +324,6 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   auto step = [&](int s, Held& h) {
     Quad c[FC], d[FR];
     const char* l = lds + s % kWideBufs * kWideBytes;
-    fill(s + 3);                            // behind the sum's end it fills with zeros, which nobody reads
-    place_codes(s + 2, h);
-    read_codes(s + 4, h);
 #pragma unroll
     for (int i = 0; i < FC; ++i) c[i] = across<kWide>(l + kWideDy, 0, wc * FC + i, lane);
 #pragma unroll
@@ -332,13 +331,21 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
       if constexpr (WEIGHT) d[j] = across<kWide>(l, 0, wr * FR + j, lane);
       else d[j] = *reinterpret_cast<const Quad*>(l + ((wr * FR + j) * 16 + lane % 16) * 64 + ((lane / 16) ^ (lane / 2 % 4)) * 16);
     }
-    // still on their way: codes of s + 2 (placed, so there), dy of s + 2, codes of s + 3, dy of s + 3, codes of s + 4
-    turn_but<2 * (kLoads + 2)>();
+    // dy of s + 1 has to be there; behind it came codes of s + 2, dy of s + 2, codes of s + 3
+    turn_but<kLoads + 4>();
     __builtin_amdgcn_s_setprio(1);
+    place_codes(s + 2, h);
+    fill(s + 3);                            // behind the sum's end both read zeros
+    read_codes(s + 4, h);
 #pragma unroll
     for (int i = 0; i < FC; ++i)
 #pragma unroll
       for (int j = 0; j < FR; ++j) acc[i][j] = mfma_of<DT>(c[i], d[j], acc[i][j]);
+#pragma unroll
+    for (int i = 0; i < FC * FR; ++i) {     // a product, and what vector instructions fit beside it
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+    }
     __builtin_amdgcn_s_setprio(0);
     turn();
   };

@@ -27,6 +27,16 @@ __device__ __forceinline__ Ref ref(const void* p, int bytes = 0x7FFFFFF8) {
 __device__ __forceinline__ void to_lds(const Ref& g, char* l, int each, int all) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(g, (__attribute__((address_space(3))) void*)l, 16, each, all, 0, 0);
 }
+// The same as an instruction that the compiler does not know for a load: it waits for all loads to LDS in front of a transposing read of LDS, whichever
+// part they go to.  The caller counts them (barrier_but); the compiler's own waits for other loads only become stricter.  `l`: the same for the wavefront.
+__device__ __forceinline__ void to_lds_uncounted(const Ref& g, const char* l, int each) {
+  const int at = __builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) const char*)l);
+  int m0;                                  // left as it was found
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(at), "v"(each), "s"(g)
+               : "memory");
+}
 // A barrier behind which everyone's LDS stores are there, and everyone's loads to LDS but the last N of each wavefront.
 template <int N>
 __device__ __forceinline__ void barrier_but() {

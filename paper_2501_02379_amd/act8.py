@@ -200,6 +200,8 @@ def _gradient(name, op, dy, codes, dtype, out):
         c = describe_codes(codes, "x", dy, rows=d.rows)
         tokens, outer, rows = d.rows, d.cols, d.cols
     out, e = _result(out, "out", dy, rows, c.cols, dtype)
+    if (d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8:
+        op += T.TGRAD_CODES_UNALIGNED
     ws = _scratch(op, tokens, c.cols, outer, dev)
     call(dev, getattr(T.load(), name), name, C.byref(d), C.byref(c), C.byref(e), ws.data_ptr(), stream_of(dev))
     return out

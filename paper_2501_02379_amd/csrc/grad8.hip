@@ -79,6 +79,7 @@ struct Grad {
   int64_t sum;
   int rows, cols;                         // of the result
   int tiles_c, tiles, steps;              // steps of a split
+  int dy_rows;                            // rows, or more of them: what of dy can be read for dw, a multiple of 8
 };
 
 // ---- two-byte dy ----------------------------------------------------------------------------------------------------------------------
@@ -86,9 +87,8 @@ struct Grad {
 constexpr int kStep = 64;                 // of the sum in LDS at a time
 
 // WR x WC wavefronts, each FR x FC results of 16 x 16; two steps in LDS, one barrier a step.  WEIGHT: dy lies across the sum, else along it (rows of
-// 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end and where STAGED (rows that do not start at
-// multiples of 16 bytes); codes go through registers, a step ahead.
-template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT, bool STAGED>
+// 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end; codes go through registers, a step ahead.
+template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
 __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
   constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
   constexpr int kDy = BR * kStep * 2, kBytes = kDy + BC * kStep * 2;
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
   const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
   const int r0 = tile.x * BR, c0 = tile.y * BC;
   const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep - 1) / kStep);
-  const int64_t whole = STAGED ? last : min(last, a.sum / kStep);
+  const int64_t whole = min(last, a.sum / kStep);
   auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
 
   // this thread's chunks of dy: row of the tile and chunk of eight numbers
@@ -115,14 +115,12 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
     }
   };
   int each[kLoads];
-  if constexpr (!STAGED) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      int row, chunk;
-      part(i, row, chunk);
-      // what lies beyond the matrix is loaded from within it, and its results are not stored
-      each[i] = WEIGHT ? row * (int)a.dy.stride + min(chunk * 8, a.rows - r0 - 8) * 2 : min(row, a.rows - 1 - r0) * (int)a.dy.stride + chunk * 16;
-    }
+  for (int i = 0; i < kLoads; ++i) {
+    int row, chunk;
+    part(i, row, chunk);
+    // what lies beyond the matrix is loaded from within it, and its results are not stored
+    each[i] = WEIGHT ? row * (int)a.dy.stride + min(chunk * 8, a.dy_rows - r0 - 8) * 2 : min(row, a.rows - 1 - r0) * (int)a.dy.stride + chunk * 16;
   }
   const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
   auto fill = [&](int64_t s) {
@@ -199,27 +197,15 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
   };
 
   read_codes(first);
-  if constexpr (STAGED) {
-    read(first);
-    place(first);
-  } else if (first < whole) {
-    fill(first);
-  }
+  if (first < whole) fill(first);
   place_codes(first);
-  if (first + 1 < last) {
-    read_codes(first + 1);
-    if constexpr (STAGED) read(first + 1);
-  }
+  if (first + 1 < last) read_codes(first + 1);
   for (int64_t s = first; s < whole; ++s) {
     barrier_but<0>();
     if (s + 1 < last) {
-      if constexpr (STAGED) place(s + 1);
-      else if (s + 1 < whole) fill(s + 1);
+      if (s + 1 < whole) fill(s + 1);
       place_codes(s + 1);
-      if (s + 2 < last) {
-        read_codes(s + 2);
-        if constexpr (STAGED) read(s + 2);
-      }
+      if (s + 2 < last) read_codes(s + 2);
     }
     multiply(s);
   }
@@ -248,17 +234,21 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
 // step's operands while 4 to 7, a turn behind, multiply the step before.  dy goes straight to LDS three steps ahead; codes are loaded four
 // steps ahead and widened into LDS two steps ahead.  All loads are unconditional, of memory that ends where the matrices do, so that they are
 // counted the same in every step and read 0 behind the sum's end.
-// dy: 16-byte rows, whole chunks of eight columns; codes: 16-byte rows, whole chunks of 16 columns.
+// dy: 16-byte rows, whole chunks of eight columns; codes: 16-byte rows.
 constexpr int kWide = 256, kWideStep = 32, kWideBufs = 4, kWideDy = kWide * kWideStep * 2, kWideBytes = 2 * kWideDy;
 
-template <int DT, int OT, bool WEIGHT>
+// 8192^3 bf16: dw 921 us, dx 983 (1190 and 1120 TFLOP/s; with loads to LDS that the compiler waits for 1130 and 1143, in tiles of 128 x 128 1200).
+// RAGGED: the codes' last row ends within a chunk (its branch costs the others 12 percent).
+template <int DT, int OT, bool WEIGHT, bool RAGGED>
 __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   constexpr int T = 512, FR = 8, FC = 4, kLoads = kWideDy / 16 / T;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
-  const int2 tile = tile_of(blockIdx.x, a.tiles, a.tiles_c);
+  const int split = blockIdx.x / a.tiles;
+  const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
   const int r0 = tile.x * kWide, c0 = tile.y * kWide;
-  const int steps = (int)((a.sum + kWideStep - 1) / kWideStep);
+  const int64_t from = (int64_t)split * a.steps * kWideStep;           // this split's part of the sum
+  const int sum = (int)min(a.sum - from, (int64_t)a.steps * kWideStep), steps = (sum + kWideStep - 1) / kWideStep;
 
   // dy: what lies beyond its rows or columns is loaded from within, and its results are not stored
   int each[kLoads], ahead[kLoads];
@@ -267,7 +257,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     const int id = i * T + (int)threadIdx.x;
     if constexpr (WEIGHT) {
       const int row = id / 32, c = id % 32, chunk = ((c / 2) ^ bend(row)) * 2 + c % 2;
-      each[i] = row * (int)a.dy.stride + min(chunk * 8, a.rows - r0 - 8) * 2;
+      each[i] = row * (int)a.dy.stride + min(chunk * 8, a.dy_rows - r0 - 8) * 2;
       ahead[i] = 0;
     } else {
       const int row = id / 4, chunk = (id % 4) ^ (row / 2 % 4);
@@ -275,8 +265,8 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
       ahead[i] = chunk * 8;
     }
   }
-  const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
-  const int sum = (int)a.sum, across_bytes = min(a.rows - r0, kWide) * 2;
+  const char* dy0 = WEIGHT ? a.dy.row(from) + (int64_t)r0 * 2 : a.dy.row(r0) + from * 2;
+  const int across_bytes = min(a.dy_rows - r0, kWide) * 2;
   auto fill = [&](int s) {
     const int left = min(sum - s * kWideStep, kWideStep);
     char* l = lds + s % kWideBufs * kWideBytes + wave * kWave * 16;
@@ -300,13 +290,21 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     Quad codes;
     float scale;
   };
+  const int8_t* codes0 = a.c.codes + from * a.c.stride + c0;
+  const float* scale0 = a.c.scale + from * a.c.groups;
   auto read_codes = [&](int s, Held& h) {
     const int left = min(sum - s * kWideStep, kWideStep);
-    const int bytes = (left - 1) * (int)a.c.stride + a.cols - c0;
-    const Ref c = ref(a.c.codes + (int64_t)s * kWideStep * a.c.stride + c0, left > 0 ? bytes : 0);
-    const Ref g = ref(a.c.scale + (int64_t)s * kWideStep * a.c.groups, max(left, 0) * (int)a.c.groups * 4);
-    h.codes = __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(c, code_at, 0, 0));
+    const bool end = from + s * kWideStep + left >= a.sum;             // this step has the last row, or nothing
+    const int bytes = left * (int)a.c.stride - (end ? (int)a.c.stride - (a.cols - c0) : 0);
+    const int8_t* at = codes0 + (int64_t)s * kWideStep * a.c.stride;
+    const Ref g = ref(scale0 + (int64_t)s * kWideStep * a.c.groups, max(left, 0) * (int)a.c.groups * 4);
+    h.codes = __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(ref(at, left > 0 ? bytes : 0), code_at, 0, 0));
     h.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(g, scale_at, 0, 0));
+    if (RAGGED && end && left > 0) {        // buffers end at whole dwords: the last row's end byte by byte.  All loads are then waited for
+      const int n = a.cols - c0 - block * 16;
+      if (row == left - 1 && n > 0 && n < 16) h.codes = load16(at + code_at, n);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
   };
   const int place = kWideDy + row * (kWide * 2) + (block ^ bend(row)) * 32;
   auto place_codes = [&](int s, const Held& h) {
@@ -371,7 +369,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   for (int j = 0; j < FR; ++j) {
     const int r = r0 + (wr * FR + j) * 16 + lane % 16;
     if (r >= a.rows) continue;
-    char* out = a.out.row(r);
+    char* out = a.out.row((int64_t)split * a.rows + r);
 #pragma unroll
     for (int i = 0; i < FC; ++i) {
       const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
@@ -419,8 +417,10 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
         const int64_t at = s * kStep32 + id % 4 * 8;
         const int n = (int)min(a.sum - at, (int64_t)8);
         if (n > 0) held[i].load(a.dy.row(min(r0 + id / 4, a.rows - 1)) + at * 4, n);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) scale[i][k] = k < n ? a.c.scale[at + k] : 0.f;
+        Eight<TGRAD_F32> e;
+        e.clear();
+        if (n > 0) e.load(reinterpret_cast<const char*>(a.c.scale + at), n);
+        e.get(scale[i]);
       }
     }
 #pragma unroll
@@ -555,6 +555,13 @@ __global__ __launch_bounds__(256) void k_grad_groups(Grad a) {
     }
 }
 
+// dy in rows that start at multiples of 16 bytes and end at multiples of eight numbers, with zeros there: eight numbers a thread.
+template <int DT>
+__global__ __launch_bounds__(256) void k_align(Mat dy, int64_t rows, int64_t cols, char* out) {
+  const int64_t per = (cols + 7) / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x, r = id / per, at = id % per * 8;
+  if (r < rows) *reinterpret_cast<Quad*>(out + id * 16) = load8<DT>(dy.row(r) + at * 2, cols - at);
+}
+
 // The splits' sums, added up in their order: four results a thread.
 template <int OT>
 __global__ __launch_bounds__(256) void k_add_splits(const float* __restrict__ part, int splits, int rows, int cols, Mat out) {
@@ -578,16 +585,23 @@ __global__ __launch_bounds__(256) void k_add_splits(const float* __restrict__ pa
 struct Cut {
   int tile, tiles_c, tiles, splits, steps;
 };
-// Tiles of 256 x 256 where they fill three quarters of the compute units (one workgroup each), else of 128 x 128 and the sum in splits where there are
-// fewer than two for every compute unit.
+// Tiles of 256 x 256, one workgroup a compute unit, where they fill three quarters of the units, by themselves or with the sum in splits of 1024 at
+// least that waste no more than a quarter of their results; else tiles of 128 x 128, with splits up to two for every unit.
+// (dw of 131072 x 512 x 768 float16: 187 us in tiles of 128, 42 splits of 6 wide ones 142; dx of 2048 x 2048 x 8192 bf16: 104, 4 splits of 64 wide ones 86.)
 Cut cut_of(int64_t rows, int64_t cols, int64_t sum, bool wide, int step) {
   auto tiles = [&](int64_t b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
+  const int64_t big = std::max<int64_t>(1, tiles(kWide)), all = std::max<int64_t>(1, (sum + kWideStep - 1) / kWideStep);
+  int64_t splits = 1;
+  if (wide && big < 192) {
+    if (rows * cols * 4 >= big * kWide * kWide * 3) splits = std::max<int64_t>(1, std::min<int64_t>(256 / big, all / 32));
+    wide = big * splits >= 192;
+  }
   Cut c;
-  c.tile = wide && tiles(256) >= 192 ? 256 : 128;
+  c.tile = wide ? kWide : 128;
   c.tiles_c = (int)((cols + c.tile - 1) / c.tile);
   c.tiles = (int)std::max<int64_t>(1, std::min<int64_t>(tiles(c.tile), kMostRows));
-  const int64_t steps = std::max<int64_t>(1, (sum + step - 1) / step);
-  const int64_t splits = c.tile == 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(512 / c.tiles, steps / 4));
+  const int64_t steps = wide ? all : std::max<int64_t>(1, (sum + step - 1) / step);
+  if (!wide) splits = std::max<int64_t>(1, std::min<int64_t>(512 / c.tiles, steps / 4));
   c.steps = (int)((steps + splits - 1) / splits);
   c.splits = (int)((steps + c.steps - 1) / c.steps);
   return c;
@@ -600,13 +614,10 @@ void launch_cut(hipStream_t s, Kern k, int threads, size_t lds, const Cut& c, co
 }
 
 template <int DT, int OT, bool WEIGHT>
-void launch_tiles(hipStream_t s, const Cut& c, bool direct, const Grad& g) {
-  constexpr size_t small = 2 * (128 + 128) * kStep * 2;
-  if constexpr (OT >= 0) {
-    if (c.tile == kWide) return launch_cut(s, k_grad_wide<DT, OT, WEIGHT>, 512, kWideBufs * kWideBytes, c, g);
-  }
-  if (direct) launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, false>, 256, small, c, g);
-  else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, true>, 256, small, c, g);
+void launch_tiles(hipStream_t s, const Cut& c, const Grad& g) {
+  if (c.tile == kWide && g.cols % 16) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, true>, 512, kWideBufs * kWideBytes, c, g);
+  else if (c.tile == kWide) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, false>, 512, kWideBufs * kWideBytes, c, g);
+  else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT>, 256, 2 * (128 + 128) * kStep * 2, c, g);
 }
 
 void launch_add(hipStream_t s, const float* part, int splits, const tgrad_matrix* out) {
@@ -616,50 +627,64 @@ void launch_add(hipStream_t s, const float* part, int splits, const tgrad_matrix
   });
 }
 
-// dy that goes straight to LDS: 16-byte rows, whole chunks of eight across the sum, offsets of 32 bits within a tile.
-bool straight(const tgrad_matrix* dy, bool weight) {
-  return (uintptr_t)dy->data % 16 == 0 && dy->row_stride % 8 == 0 && (!weight || dy->cols % 8 == 0) && dy->row_stride <= ((int64_t)1 << 21);
+// What goes straight to LDS: rows at multiples of 16 bytes, whole chunks of eight numbers, offsets of 32 bits within a tile.
+bool straight(const tgrad_matrix* dy) {
+  return (uintptr_t)dy->data % 16 == 0 && dy->row_stride % 8 == 0 && dy->cols % 8 == 0 && dy->row_stride <= ((int64_t)1 << 21);
 }
-
 bool straight(const tgrad_codes* c) { return (uintptr_t)c->codes % 16 == 0 && c->row_stride % 16 == 0 && c->row_stride <= ((int64_t)1 << 22); }
+size_t copy_bytes(int64_t tokens, int64_t outer) { return aligned((size_t)tokens * ((outer + 7) / 8 * 16)); }
 
 template <bool WEIGHT>
 void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {
-  Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0};
+  Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0, (int)out->rows};
   if (dy->dtype == TGRAD_F32 && g.c.groups > 1) {
     g.tiles_c = (g.cols + 63) / 64;
     k_grad_groups<WEIGHT><<<dim3((uint32_t)((g.rows + 63) / 64 * (int64_t)g.tiles_c)), dim3(256), 0, s>>>(g);
     return;
   }
-  const bool direct = dy->dtype != TGRAD_F32 && straight(dy, WEIGHT);
-  const bool wide = direct && dy->cols % 8 == 0 && c->cols % 16 == 0 && straight(c);
-  const Cut cut = cut_of(out->rows, out->cols, g.sum, wide, dy->dtype == TGRAD_F32 ? kStep32 : kStep);
+  char* parts = static_cast<char*>(scratch);
+  if (dy->dtype != TGRAD_F32 && !straight(dy) && dy->rows > 0) {
+    const int64_t per = (dy->cols + 7) / 8;
+    rows_in_launches(dy->rows, 256, (per + 255) / 256, [&](int64_t first, int64_t rows) {
+      for_real(dy->dtype, [&](auto t) {
+        k_align<decltype(t)::value><<<dim3((uint32_t)((rows * per + 255) / 256)), dim3(256), 0, s>>>(
+            Mat{g.dy.data + first * g.dy.stride, g.dy.stride}, rows, dy->cols, parts + first * per * 16);
+      });
+    });
+    g.dy = Mat{parts, per * 16};
+    if (WEIGHT) g.dy_rows = (int)(per * 8);
+    parts += copy_bytes(dy->rows, dy->cols);
+  }
+  const Cut cut = cut_of(out->rows, out->cols, g.sum, dy->dtype != TGRAD_F32 && straight(c) && g.dy.stride <= ((int64_t)1 << 22),
+                         dy->dtype == TGRAD_F32 ? kStep32 : kStep);
   g.tiles_c = cut.tiles_c;
   g.tiles = cut.tiles;
   g.steps = cut.steps;
-  if (cut.splits > 1) g.out = Mat{static_cast<char*>(scratch), out->cols * 4};
-  constexpr size_t lds32 = 2 * (3 * 128 + 128) * kStep32 * 2;
+  if (cut.splits > 1) g.out = Mat{parts, out->cols * 4};
   if (dy->dtype == TGRAD_F32) {
-    launch_cut(s, k_grad_split<2, 2, 4, 4, WEIGHT>, 256, lds32, cut, g);
+    launch_cut(s, k_grad_split<2, 2, 4, 4, WEIGHT>, 256, 2 * (3 * 128 + 128) * kStep32 * 2, cut, g);
   } else if (cut.splits > 1) {
-    if (dy->dtype == TGRAD_BF16) launch_tiles<TGRAD_BF16, -1, WEIGHT>(s, cut, direct, g);
-    else launch_tiles<TGRAD_F16, -1, WEIGHT>(s, cut, direct, g);
+    if (dy->dtype == TGRAD_BF16) launch_tiles<TGRAD_BF16, -1, WEIGHT>(s, cut, g);
+    else launch_tiles<TGRAD_F16, -1, WEIGHT>(s, cut, g);
   } else if (dy->dtype == TGRAD_BF16) {
-    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_BF16, TGRAD_F32, WEIGHT>(s, cut, direct, g);
-    else launch_tiles<TGRAD_BF16, TGRAD_BF16, WEIGHT>(s, cut, direct, g);
+    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_BF16, TGRAD_F32, WEIGHT>(s, cut, g);
+    else launch_tiles<TGRAD_BF16, TGRAD_BF16, WEIGHT>(s, cut, g);
   } else {
-    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_F16, TGRAD_F32, WEIGHT>(s, cut, direct, g);
-    else launch_tiles<TGRAD_F16, TGRAD_F16, WEIGHT>(s, cut, direct, g);
+    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_F16, TGRAD_F32, WEIGHT>(s, cut, g);
+    else launch_tiles<TGRAD_F16, TGRAD_F16, WEIGHT>(s, cut, g);
   }
-  if (cut.splits > 1) launch_add(s, static_cast<const float*>(scratch), cut.splits, out);
+  if (cut.splits > 1) launch_add(s, reinterpret_cast<const float*>(parts), cut.splits, out);
 }
+
+// Two-byte rows of 2^21 numbers and more, whose tiles 32-bit offsets do not reach, are refused.
+bool reachable(const tgrad_matrix* dy) { return dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21); }
 
 template <bool WEIGHT>
 int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
   if (!good(dy) || !good(c) || !good(out) || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
   if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
   if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
-  if (too_many(out)) return TGRAD_ERR_UNSUPPORTED;
+  if (too_many(out) || !reachable(dy)) return TGRAD_ERR_UNSUPPORTED;
   if (pending()) return TGRAD_ERR_HIP;
   if (out->rows == 0) return TGRAD_OK;
   launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, workspace_dev);
@@ -671,7 +696,7 @@ int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* o
 namespace tgrad {
 
 // Splits' sums, for the type of dy and the alignment that need most.
-size_t gradient_scratch(bool weight, int64_t tokens, int64_t inner, int64_t outer) {
+size_t gradient_scratch(bool weight, bool copy, int64_t tokens, int64_t inner, int64_t outer) {
   const int64_t rows = weight ? outer : tokens, sum = weight ? tokens : outer;
   size_t most = 0;
   for (bool wide : {false, true})
@@ -679,7 +704,7 @@ size_t gradient_scratch(bool weight, int64_t tokens, int64_t inner, int64_t oute
       const Cut c = cut_of(rows, inner, sum, wide, step);
       if (c.splits > 1) most = std::max(most, (size_t)c.splits * rows * inner * 4);
     }
-  return aligned(most);
+  return aligned(most) + (copy ? copy_bytes(tokens, outer) : 0);
 }
 
 }  // namespace tgrad

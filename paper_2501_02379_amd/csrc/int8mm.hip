@@ -5,7 +5,7 @@ using namespace tgrad;
 
 namespace tgrad {
 void launch_quantize(hipStream_t s, const tgrad_matrix* x, const tgrad_codes* out);
-size_t gradient_scratch(bool weight, int64_t tokens, int64_t inner, int64_t outer);
+size_t gradient_scratch(bool weight, bool copy, int64_t tokens, int64_t inner, int64_t outer);
 }
 
 namespace {
@@ -452,14 +452,16 @@ void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, c
 extern "C" {
 
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes) {
-  if (!workspace_bytes || op < TGRAD_CODES_MATMUL || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
+  const bool copy = op & TGRAD_CODES_UNALIGNED;
+  if (copy) op -= TGRAD_CODES_UNALIGNED;
+  if (!workspace_bytes || op < (copy ? TGRAD_CODES_GRAD_INPUT : TGRAD_CODES_MATMUL) || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
   if (!extents_ok(tokens, inner, inner) || !extents_ok(outer, inner, inner)) return TGRAD_ERR_INVALID_ARG;
   size_t n = kScratchAlign;
   if (op == TGRAD_CODES_MATMUL || op == TGRAD_CODES_LINEAR) {
     if (inner <= TGRAD_CODES_MAX_INNER && tokens > 0) n += part_bytes(tokens, outer, inner);
     if (op == TGRAD_CODES_LINEAR) n += scratch_codes(tokens, inner);
   } else {
-    n += gradient_scratch(op == TGRAD_CODES_GRAD_WEIGHT, tokens, inner, outer);
+    n += gradient_scratch(op == TGRAD_CODES_GRAD_WEIGHT, copy, tokens, inner, outer);
   }
   *workspace_bytes = n;
   return TGRAD_OK;

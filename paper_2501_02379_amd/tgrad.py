@@ -21,6 +21,7 @@ TGRAD_SELECT_RANDOM = 1
 TGRAD_ORDER_US_LR, TGRAD_ORDER_LR_US, TGRAD_ORDER_SUM = 0, 1, 2
 
 TGRAD_CODES_MATMUL, TGRAD_CODES_LINEAR, TGRAD_CODES_GRAD_INPUT, TGRAD_CODES_GRAD_WEIGHT = 0, 1, 2, 3
+TGRAD_CODES_UNALIGNED = 4
 TGRAD_ACT_SILU, TGRAD_ACT_GELU = 0, 1
 
 TGRAD_OK = 0

@@ -223,7 +223,8 @@ def test_a_token_with_a_nan_spoils_its_own_row_alone():
 
 GRADS = [(1, 1, 1), (1, 300, 77), (5, 64, 33), (31, 65, 130), (64, 128, 256), (100, 513, 66), (257, 255, 129), (640, 96, 300), (2051, 70, 40),
          (300, 1030, 520), (5000, 64, 32), (20000, 33, 48), (3584, 96, 100),
-         (3700, 3588, 40), (40, 3700, 3592)]
+         (3700, 3588, 40), (40, 3700, 3592),
+         (70000, 264, 250), (257, 2090, 2050)]
 
 
 def close_gradient(got, a, b, dtype, out, terms):

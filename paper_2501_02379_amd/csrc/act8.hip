@@ -11,20 +11,44 @@ namespace {
 // Activations and their derivatives.
 template <int ACT> struct Act;
 template <> struct Act<TGRAD_ACT_SILU> {
-  static __device__ __forceinline__ float value(float v) { return v / (1.f + __expf(-v)); }
+  static __device__ __forceinline__ float value(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
   static __device__ __forceinline__ void both(float v, float& y, float& slope) {
-    const float p = 1.f / (1.f + __expf(-v));
+    const float p = __builtin_amdgcn_rcpf(1.f + __expf(-v));
     y = v * p;
     slope = p * (1.f + v * (1.f - p));
   }
 };
-// erfc keeps its digits where 1 + erf loses them, below -2
+// The normal distribution function from its tail, Phi(-z) = exp(-z^2 / 2) P(t) with t = 1 / (1 + c z), z = |v|: P(t) = exp(z^2 / 2) Phi(-z) is smooth on 0..1,
+// and a polynomial fitted to it by least squares in 64 bits, weighted by 1 / P, is off by 1e-07 of it.  Tails keep their digits that way, which
+// (1 + erf) / 2 loses below -2.  (With erfc of the device library: 519 us where silu takes 409.)
 template <> struct Act<TGRAD_ACT_GELU> {
-  static __device__ __forceinline__ float value(float v) { return 0.5f * v * erfcf(v * -0.70710678f); }
+  static __device__ __forceinline__ void tail(float v, float& bell, float& q) {
+    const float z = fabsf(v);
+    bell = __builtin_amdgcn_exp2f(v * v * -0.72134752f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.40f, z, 1.f));
+    float p = 3.219981867e-02f;
+    p = fmaf(p, t, -1.766817470e-01f);
+    p = fmaf(p, t, 3.818516465e-01f);
+    p = fmaf(p, t, -3.732105289e-01f);
+    p = fmaf(p, t, 1.186081176e-01f);
+    p = fmaf(p, t, -2.625735117e-02f);
+    p = fmaf(p, t, 9.109580981e-02f);
+    p = fmaf(p, t, 1.331981479e-01f);
+    p = fmaf(p, t, 1.596197832e-01f);
+    p = fmaf(p, t, 1.595763111e-01f);
+    q = bell * p * t;
+  }
+  static __device__ __forceinline__ float value(float v) {
+    float bell, q;
+    tail(v, bell, q);
+    return v * (v > 0.f ? 1.f - q : q);
+  }
   static __device__ __forceinline__ void both(float v, float& y, float& slope) {
-    const float p = 0.5f * erfcf(v * -0.70710678f);
+    float bell, q;
+    tail(v, bell, q);
+    const float p = v > 0.f ? 1.f - q : q;
     y = v * p;
-    slope = p + v * 0.39894228f * __expf(-0.5f * v * v);
+    slope = p + v * 0.39894228f * bell;
   }
 };
 

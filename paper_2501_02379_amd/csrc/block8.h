@@ -114,10 +114,35 @@ __device__ __forceinline__ uint32_t largest(const float* f) {
   for (int i = 0; i < 8; ++i) m = max(m, magnitude(f[i]));
   return m;
 }
-// ... over neighbouring lanes, `lanes` a power of two up to 64
+// A lane's value from a neighbour in the same 16 lanes, with no trip through LDS: STEP 1 and 2: lane ^ STEP; 4 and 8: the lane that mirrors it in 8 and 16
+// (another half's value, which is all that a running maximum or sum of halves needs).
+template <int STEP>
+__device__ __forceinline__ uint32_t neighbour(uint32_t v) {
+  constexpr int kCtrl = STEP == 1 ? 0xB1 : STEP == 2 ? 0x4E : STEP == 4 ? 0x141 : 0x140;
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, kCtrl, 0xF, 0xF, true);
+}
+template <int STEP>
+__device__ __forceinline__ float neighbour(float v) { return __uint_as_float(neighbour<STEP>(__float_as_uint(v))); }
+
+// The largest over neighbouring lanes, `lanes` 1 or a power of two from 4 to 64
 __device__ __forceinline__ uint32_t largest_of_lanes(uint32_t m, int lanes) {
-  for (int d = 1; d < lanes; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
+  if (lanes < 4) return m;
+  m = max(m, neighbour<1>(m));
+  m = max(m, neighbour<2>(m));
+  if (lanes >= 8) m = max(m, neighbour<4>(m));
+  if (lanes >= 16) m = max(m, neighbour<8>(m));
+  if (lanes >= 32) m = max(m, (uint32_t)__shfl_xor((int)m, 16));
+  if (lanes >= 64) m = max(m, (uint32_t)__shfl_xor((int)m, 32));
   return m;
+}
+// The sum over a wavefront, the same in every lane
+__device__ __forceinline__ float sum_of_lanes(float v) {
+  v += neighbour<1>(v);
+  v += neighbour<2>(v);
+  v += neighbour<4>(v);
+  v += neighbour<8>(v);
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
 }
 // ... over a workgroup of WAVES wavefronts
 template <int WAVES>

@@ -10,16 +10,12 @@ using namespace tgrad;
 
 namespace {
 
-// Two sums over a workgroup, as block_sum.
+// Sums over a workgroup, the same in every thread; each call has its own `lds`, so that one barrier does.
 template <int WAVES>
-__device__ __forceinline__ float2 block_sum2(float2 v, float2* lds) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    v.x += __shfl_xor(v.x, d);
-    v.y += __shfl_xor(v.y, d);
-  }
+__device__ __forceinline__ float2 sums_of_block(float2 v, float2* lds) {
+  v.x = sum_of_lanes(v.x);
+  v.y = sum_of_lanes(v.y);
   if constexpr (WAVES == 1) return v;
-  __syncthreads();
   if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
   __syncthreads();
   v = lds[0];
@@ -28,6 +24,17 @@ __device__ __forceinline__ float2 block_sum2(float2 v, float2* lds) {
     v.x += lds[w].x;
     v.y += lds[w].y;
   }
+  return v;
+}
+template <int WAVES>
+__device__ __forceinline__ float sum_of_block(float v, float* lds) {
+  v = sum_of_lanes(v);
+  if constexpr (WAVES == 1) return v;
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int w = 1; w < WAVES; ++w) v += lds[w];
   return v;
 }
 
@@ -42,7 +49,7 @@ struct Desc {
 
 // Mean and factor of a row held in registers (numbers beyond its end are 0 there).  The mean is taken off before squares are summed.
 template <int T, int NV>
-__device__ __forceinline__ float2 stats_of(float (*v)[8], const Desc& d, float* lds) {
+__device__ __forceinline__ float2 stats_of(float (*v)[8], const Desc& d, float (*lds)[T / kWave]) {
   float mean = 0.f;
   if (d.centered) {
     float s = 0.f;
@@ -50,7 +57,7 @@ __device__ __forceinline__ float2 stats_of(float (*v)[8], const Desc& d, float* 
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int k = 0; k < 8; ++k) s += v[i][k];
-    mean = block_sum<T / kWave>(s, lds) / (float)d.cols;
+    mean = sum_of_block<T / kWave>(s, lds[0]) / (float)d.cols;
   }
   float s = 0.f;
 #pragma unroll
@@ -62,13 +69,13 @@ __device__ __forceinline__ float2 stats_of(float (*v)[8], const Desc& d, float* 
       s += c * c;
     }
   }
-  s = block_sum<T / kWave>(s, lds);
+  s = sum_of_block<T / kWave>(s, lds[1]);
   return make_float2(mean, 1.f / sqrtf(s / (float)d.cols + d.eps));
 }
 
 template <int XT, int BT, bool BLOCK, int T, int NV>
 __global__ __launch_bounds__(T) void k_block_norm(Desc d, int64_t first, Mat x, Mat block, Mat x_out, Mat h, Codes8 h8, float4* stats) {
-  __shared__ float lds[T / kWave];
+  __shared__ float lds[4][T / kWave];
   __shared__ uint32_t lds_top[T / kWave];
   const int64_t row = first + blockIdx.x;
   constexpr int xs = sizeof(typename Elem<XT>::raw), bs = sizeof(typename Elem<BT>::raw);
@@ -129,7 +136,7 @@ __global__ __launch_bounds__(T) void k_block_norm(Desc d, int64_t first, Mat x, 
       for (int k = 0; k < 8; ++k)
         if (col + k >= d.cols) v[i][k] = 0.f;
     }
-    const float2 m = stats_of<T, NV>(v, d, lds);
+    const float2 m = stats_of<T, NV>(v, d, lds + 2);
     st.z = m.x;
     st.w = m.y;
     uint32_t top = 0;
@@ -168,8 +175,10 @@ struct Chunks {
   int64_t count, rows, per_gate, span;    // span: rows of the matrix to `per_gate` chunks
 };
 
+constexpr int kHeldCols = 8192;           // a row that one workgroup holds
+
 Chunks chunks_of(int64_t rows, int64_t cols, int64_t shared) {
-  const int64_t most = cols > 4096 ? 256 : cols > 512 ? 512 : 2048;
+  const int64_t most = cols > kHeldCols ? 128 : cols > 4096 ? 256 : cols > 2048 ? 512 : cols > 512 ? 1024 : 4096;
   const int64_t want = std::max<int64_t>(1, (rows + most - 1) / most);
   Chunks c;
   shared = std::min(shared, std::max<int64_t>(rows, 1));
@@ -190,24 +199,73 @@ Chunks chunks_of(int64_t rows, int64_t cols, int64_t shared) {
 struct Back {
   Mat dx_out, dh, x_out, block, dx, dblock;
   const float4* stats;
+  float4* sums;                           // of every row, where it is longer than kHeldCols: along and off of both norms
   char* dgate;                            // rows of cols elements of the block's type
   float *dpost, *dpre, *gate_sums;        // [chunks][cols]; gate_sums where a row of the gate has several chunks
   Chunks chunks;
   int64_t rows;
 };
 
+// The gradient u = dh w_pre goes on as inv (u - n along - off); see the top.
+struct Through {
+  float mean, inv, along, off;
+  __device__ __forceinline__ float normed(float v) const { return (v - mean) * inv; }
+  __device__ __forceinline__ float of(float u, float n) const { return inv * (u - n * along - off); }
+};
+
+// A row's units in flight: what one thread has of it.
 template <int XT, int BT, bool BLOCK, int T, int NV>
+struct RowParts {
+  Eight<XT> d[NV], x[NV];
+  Eight<BT> h[NV], b[NV], g[NV];
+  float4 st;
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      d[i].clear();
+      x[i].clear();
+      h[i].clear();
+      b[i].clear();
+      g[i].clear();
+    }
+    st = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  __device__ __forceinline__ void load(const Desc& q, const Back& a, int64_t row, int col0, bool gate) {
+    constexpr int xs = sizeof(typename Elem<XT>::raw), bs = sizeof(typename Elem<BT>::raw);
+    st = a.stats[row];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int col = col0 + (threadIdx.x + i * T) * 8, n = q.cols - col;
+      if (n <= 0) continue;
+      if (a.dx_out.data) d[i].load(a.dx_out.row(row) + (int64_t)col * xs, n);
+      if (q.pre) {
+        h[i].load(a.dh.row(row) + (int64_t)col * bs, n);
+        x[i].load(a.x_out.row(row) + (int64_t)col * xs, n);
+      }
+      if constexpr (BLOCK) {
+        b[i].load(a.block.row(row) + (int64_t)col * bs, n);
+        if (gate) g[i].load(q.gate.row(row / q.shared) + (int64_t)col * bs, n);
+      }
+    }
+  }
+};
+
+// One row after another, the next one's loads ahead of this one's sums.  GIVEN: a row's sums are there already, and a workgroup has T * NV * 8 of its columns,
+// blockIdx.y says which.
+template <int XT, int BT, bool BLOCK, int T, int NV, bool GIVEN>
 __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
-  __shared__ float2 lds[T / kWave];
+  __shared__ float2 lds[2][2][T / kWave];
   constexpr int xs = sizeof(typename Elem<XT>::raw), bs = sizeof(typename Elem<BT>::raw);
   const int64_t chunk = blockIdx.x, part = chunk % a.chunks.per_gate, base = chunk / a.chunks.per_gate * a.chunks.span;
   const int64_t begin = base + part * a.chunks.rows;
   const int64_t end = min(min(begin + a.chunks.rows, base + a.chunks.span), a.rows);
+  const int col0 = GIVEN ? blockIdx.y * (T * NV * 8) : 0;
   const float per = 1.f / (float)d.cols;
   float pre_sum[NV][8], post_sum[NV][8], gate_sum[NV][8], w_pre[NV][8], w_post[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (threadIdx.x + i * T) * 8;
+    const int col = col0 + (threadIdx.x + i * T) * 8;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       pre_sum[i][k] = post_sum[i][k] = gate_sum[i][k] = w_pre[i][k] = 0.f;
@@ -216,60 +274,51 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
     if (d.pre && col < d.cols) load_weights(d.pre, d.weight_dtype, col, d.cols - col, w_pre[i]);
     if (d.post && col < d.cols) load_weights(d.post, d.weight_dtype, col, d.cols - col, w_post[i]);
   }
-  for (int64_t row = begin; row < end; ++row) {
-    const float4 st = a.stats[row];
-    Eight<XT> ed[NV], ex[NV];
-    Eight<BT> eh[NV], eb[NV], eg[NV];
+  RowParts<XT, BT, BLOCK, T, NV> now, next;
+  now.clear();
+  next.clear();
+  if (begin < end) next.load(d, a, begin, col0, d.gate.data != nullptr);
+  int which = 0;
+  for (int64_t row = begin; row < end; ++row, which ^= 1) {
+    now = next;
+    const bool gate_ends = row + 1 == end || (row + 1) % d.shared == 0;
+    if (row + 1 < end) next.load(d, a, row + 1, col0, d.gate.data && gate_ends);
+    float4 given = make_float4(0.f, 0.f, 0.f, 0.f);
+    if constexpr (GIVEN) given = a.sums[row];
+    Through px = {now.st.z, now.st.w, given.x, given.y}, pb = {now.st.x, now.st.y, given.z, given.w};
     float dx[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int col = (threadIdx.x + i * T) * 8, n = d.cols - col;
-      ed[i].clear();
-      ex[i].clear();
-      eh[i].clear();
-      eb[i].clear();
-      eg[i].clear();
-      if (n > 0) {
-        if (a.dx_out.data) ed[i].load(a.dx_out.row(row) + (int64_t)col * xs, n);
-        if (d.pre) {
-          eh[i].load(a.dh.row(row) + (int64_t)col * bs, n);
-          ex[i].load(a.x_out.row(row) + (int64_t)col * xs, n);
-        }
-        if constexpr (BLOCK) {
-          eb[i].load(a.block.row(row) + (int64_t)col * bs, n);
-          if (d.gate.data) eg[i].load(d.gate.row(row / d.shared) + (int64_t)col * bs, n);
-        }
-      }
-    }
-    float2 s = make_float2(0.f, 0.f);
     if (d.pre) {
+      float2 s = make_float2(0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         float x[8], u[8];
-        ex[i].get(x);
-        eh[i].get(u);
+        now.x[i].get(x);
+        now.h[i].get(u);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float n = (x[k] - st.z) * st.w, g = u[k] * w_pre[i][k];
+          const float n = px.normed(x[k]), g = u[k] * w_pre[i][k];
           s.x += g * n;
           s.y += g;
           pre_sum[i][k] += u[k] * n;
         }
       }
-      s = block_sum2<T / kWave>(s, lds);
+      if constexpr (!GIVEN) {
+        s = sums_of_block<T / kWave>(s, lds[which][0]);
+        px.along = s.x * per;
+        px.off = d.centered ? s.y * per : 0.f;
+      }
     }
-    const float along = s.x * per, off = d.centered ? s.y * per : 0.f;
-    s = make_float2(0.f, 0.f);
+    float2 s = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int col = (threadIdx.x + i * T) * 8;
+      const int col = col0 + (threadIdx.x + i * T) * 8;
       float x[8], u[8], b[8], g[8];
-      ed[i].get(dx[i]);
+      now.d[i].get(dx[i]);
       if (d.pre) {
-        ex[i].get(x);
-        eh[i].get(u);
+        now.x[i].get(x);
+        now.h[i].get(u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dx[i][k] += st.w * (u[k] * w_pre[i][k] - (x[k] - st.z) * st.w * along - off);
+        for (int k = 0; k < 8; ++k) dx[i][k] += px.of(u[k] * w_pre[i][k], px.normed(x[k]));
       }
       if (col < d.cols) {
         Eight<XT> o;
@@ -277,12 +326,12 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
         o.store(a.dx.row(row) + (int64_t)col * xs, d.cols - col);
       }
       if constexpr (BLOCK) {
-        eb[i].get(b);
-        eg[i].get(g);
+        now.b[i].get(b);
+        now.g[i].get(g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float q = col + k < d.cols ? d.scale * dx[i][k] : 0.f;
-          const float n = d.post ? (b[k] - st.x) * st.y : b[k];
+          const float n = d.post ? pb.normed(b[k]) : b[k];
           const float w = d.gate.data ? g[k] : 1.f;
           gate_sum[i][k] += q * n * w_post[i][k];
           post_sum[i][k] += q * w * n;
@@ -293,18 +342,21 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
       }
     }
     if constexpr (BLOCK) {
-      if (d.post) s = block_sum2<T / kWave>(s, lds);
-      const float along2 = s.x * per, off2 = d.centered ? s.y * per : 0.f;
+      if constexpr (!GIVEN) {
+        if (d.post) s = sums_of_block<T / kWave>(s, lds[which][1]);
+        pb.along = s.x * per;
+        pb.off = d.centered ? s.y * per : 0.f;
+      }
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int col = (threadIdx.x + i * T) * 8;
+        const int col = col0 + (threadIdx.x + i * T) * 8;
         float b[8], g[8];
-        eb[i].get(b);
-        eg[i].get(g);
+        now.b[i].get(b);
+        now.g[i].get(g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float up = d.scale * dx[i][k] * (d.gate.data ? g[k] : 1.f) * w_post[i][k];
-          b[k] = d.post ? st.y * (up - (b[k] - st.x) * st.y * along2 - off2) : up;
+          b[k] = d.post ? pb.of(up, pb.normed(b[k])) : up;
         }
         if (col < d.cols) {
           Eight<BT> o;
@@ -313,10 +365,10 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
         }
       }
       // the last of a gate's rows here: all of them, or this chunk's share
-      if (d.gate.data && (row + 1 == end || (row + 1) % d.shared == 0)) {
+      if (d.gate.data && gate_ends) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          const int col = (threadIdx.x + i * T) * 8;
+          const int col = col0 + (threadIdx.x + i * T) * 8;
           if (col < d.cols) {
             if (a.chunks.per_gate > 1) {
               Eight<TGRAD_F32> o;
@@ -336,7 +388,7 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int col = (threadIdx.x + i * T) * 8;
+    const int col = col0 + (threadIdx.x + i * T) * 8;
     if (col >= d.cols) continue;
     Eight<TGRAD_F32> o;
     if (a.dpre) {
@@ -354,34 +406,113 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
   }
 }
 
-// out[g][col] = sum over the `per` chunks of g.  64 columns and 16 shares of the chunks to a workgroup; shares, then their sums in order.
-template <int DT>
-__global__ __launch_bounds__(1024) void k_chunk_sums(const float* __restrict__ part, int64_t per, int cols, char* out) {
-  __shared__ float lds[16][64];
-  const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane;
-  const int64_t g = blockIdx.y;
+// The sums of a row that is longer than kHeldCols, read twice (the second time from L2: 320 KB a row at most, one row a compute unit): a workgroup a row.
+template <int XT, int BT, bool BLOCK>
+__global__ __launch_bounds__(1024) void k_block_norm_sums(Desc d, Back a, int64_t first) {
+  constexpr int T = 1024;
+  __shared__ float2 lds[2][T / kWave];
+  const int64_t row = first + blockIdx.x;
+  const float per = 1.f / (float)d.cols;
+  const float4 st = a.stats[row];
+  Through px = {st.z, st.w, 0.f, 0.f}, pb = {st.x, st.y, 0.f, 0.f};
+  RowParts<XT, BT, BLOCK, T, 1> r;
+  float2 s = make_float2(0.f, 0.f);
+  if (d.pre) {
+    for (int col0 = 0; col0 < d.cols; col0 += T * 8) {
+      const int col = col0 + threadIdx.x * 8;
+      if (col >= d.cols) break;
+      float w[8], x[8], u[8];
+      r.clear();
+      r.load(d, Back{Mat{nullptr, 0}, a.dh, a.x_out, a.block, a.dx, a.dblock, a.stats}, row, col0, false);
+      load_weights(d.pre, d.weight_dtype, col, d.cols - col, w);
+      r.x[0].get(x);
+      r.h[0].get(u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float g = col + k < d.cols ? u[k] * w[k] : 0.f;
+        s.x += g * px.normed(x[k]);
+        s.y += g;
+      }
+    }
+    s = sums_of_block<T / kWave>(s, lds[0]);
+    px.along = s.x * per;
+    px.off = d.centered ? s.y * per : 0.f;
+  }
+  if constexpr (BLOCK) {
+    if (d.post) {
+      s = make_float2(0.f, 0.f);
+      for (int col0 = 0; col0 < d.cols; col0 += T * 8) {
+        const int col = col0 + threadIdx.x * 8;
+        if (col >= d.cols) break;
+        float w[8], x[8], u[8], dx[8], b[8], g[8];
+        r.clear();
+        r.load(d, a, row, col0, d.gate.data != nullptr);
+        r.d[0].get(dx);
+        r.b[0].get(b);
+        r.g[0].get(g);
+        if (d.pre) {
+          load_weights(d.pre, d.weight_dtype, col, d.cols - col, w);
+          r.x[0].get(x);
+          r.h[0].get(u);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dx[k] += px.of(u[k] * w[k], px.normed(x[k]));
+        }
+        load_weights(d.post, d.weight_dtype, col, d.cols - col, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float up = col + k < d.cols ? d.scale * dx[k] * (d.gate.data ? g[k] : 1.f) * w[k] : 0.f;
+          s.x += up * pb.normed(b[k]);
+          s.y += up;
+        }
+      }
+      s = sums_of_block<T / kWave>(s, lds[1]);
+      pb.along = s.x * per;
+      pb.off = d.centered ? s.y * per : 0.f;
+    }
+  }
+  if (threadIdx.x == 0) a.sums[row] = make_float4(px.along, px.off, pb.along, pb.off);
+}
+
+// out[g][col] = sum over the `per` chunks of g, for up to three results at once.  16 columns and 64 shares of the chunks to a workgroup; shares, then their
+// sums in order.
+struct SumJob {
+  const float* part;
+  int64_t per, gates;
+  char* out;
+  int dt;
+};
+struct SumJobs {
+  SumJob job[3];
+};
+__global__ __launch_bounds__(1024) void k_chunk_sums(SumJobs jobs, int64_t first, int cols) {
+  __shared__ float lds[64][17];
+  const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
+  const int col = blockIdx.x * 16 + lane;
+  int64_t g = first + blockIdx.y;
+  int j = 0;
+  while (j < 2 && g >= jobs.job[j].gates) g -= jobs.job[j++].gates;
+  const SumJob job = jobs.job[j];
   float s = 0.f;
-  if (col < cols)
-    for (int64_t c = share; c < per; c += 16) s += part[(g * per + c) * cols + col];
+  if (col < cols) {
+    const float* at = job.part + g * job.per * cols + col;
+#pragma unroll 8
+    for (int64_t c = share; c < job.per; c += 64) s += at[c * cols];
+  }
   lds[share][lane] = s;
   __syncthreads();
   if (share == 0 && col < cols) {
-#pragma unroll
-    for (int w = 1; w < 16; ++w) s += lds[w][lane];
-    reinterpret_cast<typename Elem<DT>::raw*>(out)[g * cols + col] = Elem<DT>::narrow(s);
+    for (int w = 1; w < 64; ++w) s += lds[w][lane];
+    const int64_t to = g * cols + col;
+    if (job.dt == TGRAD_F32) reinterpret_cast<float*>(job.out)[to] = s;
+    else if (job.dt == TGRAD_BF16) reinterpret_cast<uint16_t*>(job.out)[to] = Elem<TGRAD_BF16>::narrow(s);
+    else reinterpret_cast<_Float16*>(job.out)[to] = Elem<TGRAD_F16>::narrow(s);
   }
 }
 
-void launch_chunk_sums(hipStream_t s, int dt, const float* part, int64_t gates, int64_t per, int cols, void* out) {
-  const size_t es = real_bytes(dt);
-  for (int64_t at = 0; at < gates; at += 32768) {
-    const int64_t n = std::min<int64_t>(gates - at, 32768);
-    for_real(dt, [&](auto t) {
-      k_chunk_sums<decltype(t)::value><<<dim3((cols + 63) / 64, (uint32_t)n), dim3(1024), 0, s>>>(
-          part + at * per * cols, per, cols, static_cast<char*>(out) + at * cols * es);
-    });
-  }
+void launch_chunk_sums(hipStream_t s, const SumJobs& jobs, int cols) {
+  const int64_t all = jobs.job[0].gates + jobs.job[1].gates + jobs.job[2].gates;
+  for (int64_t at = 0; at < all; at += 32768)
+    k_chunk_sums<<<dim3((cols + 15) / 16, (uint32_t)std::min<int64_t>(all - at, 32768)), dim3(1024), 0, s>>>(jobs, at, cols);
 }
 
 // Threads and units of a row, all of them held in registers.
@@ -400,6 +531,20 @@ void for_width(int64_t rows, int cols, F&& f) {
   else if (units <= 1024) f(t1024(), n1());
   else if (units <= 2048) f(t1024(), n2());
   else f(t1024(), n4());
+}
+
+template <typename F>
+void for_width_back(int cols, F&& f) {
+  const int units = (cols + 7) / 8;
+  typedef std::integral_constant<int, 64> t64;
+  typedef std::integral_constant<int, 256> t256;
+  typedef std::integral_constant<int, 512> t512;
+  typedef std::integral_constant<int, 1> n1;
+  typedef std::integral_constant<int, 2> n2;
+  if (units <= 64) f(t64(), n1());
+  else if (units <= 256) f(t256(), n1());
+  else if (units <= 512) f(t512(), n1());
+  else f(t512(), n2());
 }
 
 // f(type of the stream, type of the block): the same, or a stream in float32.
@@ -427,16 +572,19 @@ Desc describe(const tgrad_block* d, int cols, int bt) {
 bool types_ok(int xt, int bt) { return xt == bt || xt == TGRAD_F32; }
 
 // Scratch of the backward pass.
-struct Sums {
-  size_t dpost, dpre, gate, bytes;
+struct Scratch {
+  size_t dpost, dpre, gate, sums, bytes;
 };
-Sums sums_of(const Chunks& c, int64_t cols) {
-  Sums s;
-  const size_t each = ((size_t)c.count * (size_t)cols * 4 + kScratchAlign - 1) / kScratchAlign * kScratchAlign;
+Scratch scratch_of(const Chunks& c, int64_t rows, int64_t cols) {
+  auto aligned = [](size_t n) { return (n + kScratchAlign - 1) / kScratchAlign * kScratchAlign; };
+  const size_t each = aligned((size_t)c.count * (size_t)cols * 4);
+  Scratch s;
   s.dpost = 0;
   s.dpre = each;
   s.gate = 2 * each;
-  s.bytes = std::max<size_t>((c.per_gate > 1 ? 3 : 2) * each, kScratchAlign);
+  s.sums = (c.per_gate > 1 ? 3 : 2) * each;
+  s.bytes = s.sums + (cols > kHeldCols ? aligned((size_t)rows * 16) : 0);
+  s.bytes = std::max<size_t>(s.bytes, kScratchAlign);
   return s;
 }
 
@@ -483,7 +631,7 @@ int tgrad_block_norm(const tgrad_block* desc, const tgrad_matrix* x, const tgrad
 int tgrad_block_norm_query_size(int64_t rows, int64_t cols, int64_t rows_per_gate, size_t* workspace_bytes) {
   if (!workspace_bytes || !extents_ok(rows, cols, cols) || rows_per_gate < 1) return TGRAD_ERR_INVALID_ARG;
   if (cols > TGRAD_NORM_MAX_COLS) return TGRAD_ERR_UNSUPPORTED;
-  *workspace_bytes = sums_of(chunks_of(rows, cols, rows_per_gate), cols).bytes;
+  *workspace_bytes = scratch_of(chunks_of(rows, cols, rows_per_gate), rows, cols).bytes;
   return TGRAD_OK;
 }
 
@@ -510,8 +658,9 @@ int tgrad_block_norm_backward(const tgrad_block* desc, const tgrad_matrix* dx_ou
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const Desc d = describe(desc, (int)cols, bt);
   const Chunks c = chunks_of(rows, cols, desc->gate ? desc->rows_per_gate : 1);
-  const Sums sums = sums_of(c, cols);
+  const Scratch sc = scratch_of(c, rows, cols);
   char* ws = static_cast<char*>(workspace_dev);
+  const bool one = c.count == 1 && rows > 0;            // then the chunk's sums are the results
   Back a;
   a.dx_out = mat(dx_out);
   a.dh = mat(dh);
@@ -520,25 +669,40 @@ int tgrad_block_norm_backward(const tgrad_block* desc, const tgrad_matrix* dx_ou
   a.dx = mat(dx);
   a.dblock = mat(dblock);
   a.stats = reinterpret_cast<const float4*>(stats);
+  a.sums = reinterpret_cast<float4*>(ws + sc.sums);
   a.dgate = static_cast<char*>(dgate);
-  a.dpost = dpost ? reinterpret_cast<float*>(ws + sums.dpost) : nullptr;
-  a.dpre = dpre ? reinterpret_cast<float*>(ws + sums.dpre) : nullptr;
-  a.gate_sums = reinterpret_cast<float*>(ws + sums.gate);
+  a.dpost = !dpost ? nullptr : one ? dpost : reinterpret_cast<float*>(ws + sc.dpost);
+  a.dpre = !dpre ? nullptr : one ? dpre : reinterpret_cast<float*>(ws + sc.dpre);
+  a.gate_sums = reinterpret_cast<float*>(ws + sc.gate);
   a.chunks = c;
   a.rows = rows;
   if (rows > 0) {
     for_types(xt, bt, [&](auto x, auto b) {
-      for_width(rows, (int)cols, [&](auto t, auto n) {
-        constexpr int XT = decltype(x)::value, BT = decltype(b)::value, T = decltype(t)::value, NV = decltype(n)::value;
-        if (block) k_block_norm_back<XT, BT, true, T, NV><<<dim3((uint32_t)c.count), dim3(T), 0, s>>>(d, a);
-        else k_block_norm_back<XT, BT, false, T, NV><<<dim3((uint32_t)c.count), dim3(T), 0, s>>>(d, a);
-      });
+      constexpr int XT = decltype(x)::value, BT = decltype(b)::value;
+      auto run = [&](auto with) {
+        constexpr bool BLOCK = decltype(with)::value;
+        if (cols > kHeldCols) {
+          rows_in_launches(rows, 1024, 1, [&](int64_t first, int64_t some) {
+            k_block_norm_sums<XT, BT, BLOCK><<<dim3((uint32_t)some), dim3(1024), 0, s>>>(d, a, first);
+          });
+          k_block_norm_back<XT, BT, BLOCK, 256, 1, true><<<dim3((uint32_t)c.count, (uint32_t)((cols + 2047) / 2048)), dim3(256), 0, s>>>(d, a);
+        } else {
+          for_width_back((int)cols, [&](auto t, auto n) {
+            constexpr int T = decltype(t)::value, NV = decltype(n)::value;
+            k_block_norm_back<XT, BT, BLOCK, T, NV, false><<<dim3((uint32_t)c.count), dim3(T), 0, s>>>(d, a);
+          });
+        }
+      };
+      if (block) run(std::true_type());
+      else run(std::false_type());
     });
   }
   const int64_t chunks = rows > 0 ? c.count : 0;
-  if (dpost) launch_chunk_sums(s, TGRAD_F32, a.dpost, 1, chunks, (int)cols, dpost);
-  if (dpre) launch_chunk_sums(s, TGRAD_F32, a.dpre, 1, chunks, (int)cols, dpre);
-  if (rows > 0 && desc->gate && c.per_gate > 1) launch_chunk_sums(s, bt, a.gate_sums, c.count / c.per_gate, c.per_gate, (int)cols, dgate);
+  SumJobs jobs = {};
+  if (dpost && !one) jobs.job[0] = SumJob{a.dpost, chunks, 1, reinterpret_cast<char*>(dpost), TGRAD_F32};
+  if (dpre && !one) jobs.job[1] = SumJob{a.dpre, chunks, 1, reinterpret_cast<char*>(dpre), TGRAD_F32};
+  if (rows > 0 && desc->gate && c.per_gate > 1) jobs.job[2] = SumJob{a.gate_sums, c.per_gate, c.count / c.per_gate, a.dgate, bt};
+  launch_chunk_sums(s, jobs, (int)cols);
   return launched();
 }
 

@@ -541,12 +541,13 @@ int tgrad_quantize(const tgrad_matrix* x, const tgrad_codes* out, void* hip_stre
 int tgrad_dequantize(const tgrad_codes* codes, const tgrad_matrix* out, void* hip_stream);
 
 enum { TGRAD_CODES_MATMUL = 0, TGRAD_CODES_LINEAR = 1, TGRAD_CODES_GRAD_INPUT = 2, TGRAD_CODES_GRAD_WEIGHT = 3 };
-#define TGRAD_CODES_UNALIGNED 4       /* added to a gradient's op: dy's rows do not start at multiples of 16 bytes, or its cols are no multiple of 8 */
+/* added to a gradient's op: dy's rows do not start at multiples of 16 bytes, are no multiple of 8 long, or lie more than 2^21 elements apart */
+#define TGRAD_CODES_UNALIGNED 4
 #define TGRAD_CODES_MAX_INNER 131072   /* longest sum of products of codes that int32 holds: 127^2 2^17 < 2^31 */
 
 /*
  * Bytes of scratch of the four calls below, for tokens x inner times inner x outer.  Two-byte dy that is not aligned is copied there first, which
- * needs TGRAD_CODES_UNALIGNED.  Host-only.  Errors: INVALID_ARG.
+ * needs TGRAD_CODES_UNALIGNED.  0: none, and the call's workspace_dev may be NULL.  Host-only.  Errors: INVALID_ARG.
  */
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes);
 

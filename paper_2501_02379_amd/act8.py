@@ -46,47 +46,63 @@ class Activation(NamedTuple):
 
 def describe(x, what, like=None, rows=None, cols=None, dtype=None):
     """A matrix as the library takes it; anything it does not take is refused."""
-    if not isinstance(x, torch.Tensor) or x.dim() != 2 or x.dtype not in REAL_TYPES or not x.is_cuda:
+    if not isinstance(x, torch.Tensor):
         refuse(what + ": a 2-D float32, bfloat16 or float16 tensor on the GPU")
-    n, m = x.shape
-    if (m > 1 and x.stride(1) != 1 and n > 0) or x.is_neg():               # memory holds other numbers than a tensor with that pending
+    shape, t = x.shape, x.dtype
+    code = REAL_TYPES.get(t)
+    if len(shape) != 2 or code is None or not x.is_cuda:
+        refuse(what + ": a 2-D float32, bfloat16 or float16 tensor on the GPU")
+    n, m = shape
+    stride, step = x.stride()
+    if (step != 1 and m > 1 and n > 0) or x.is_neg():                      # memory holds other numbers than a tensor with that pending
         refuse(what + ": dense rows, no pending negation")
-    if like is not None and x.device != like.device:
+    if like is not None and x.get_device() != like.get_device():
         refuse(what + ": on the other tensors' device")
-    if (rows is not None and n != rows) or (cols is not None and m != cols) or (dtype is not None and x.dtype is not dtype):
+    if (rows is not None and n != rows) or (cols is not None and m != cols) or (dtype is not None and t is not dtype):
         refuse("%s: %s x %s%s" % (what, "rows" if rows is None else rows, "cols" if cols is None else cols, "" if dtype is None else " of %s" % dtype))
-    return T.tgrad_matrix(x.data_ptr(), n, m, x.stride(0) if n > 1 else m, REAL_TYPES[x.dtype])
+    return T.tgrad_matrix(x.data_ptr(), n, m, stride if n > 1 else m, code)
 
 
 def describe_codes(c, what, like=None, rows=None, cols=None):
     if not isinstance(c, Codes) or not isinstance(c.codes, torch.Tensor) or not isinstance(c.scale, torch.Tensor):
         refuse(what + ": Codes")
     q, s, g = c
-    if q.dim() != 2 or q.dtype is not torch.int8 or not q.is_cuda or (q.shape[1] > 1 and q.stride(1) != 1 and q.shape[0] > 0):
+    shape = q.shape
+    if len(shape) != 2 or q.dtype is not torch.int8 or not q.is_cuda:
         refuse(what + ": int8 codes on the GPU, 2-D, dense rows")
-    n, m = q.shape
-    if s.dtype is not torch.float32 or s.device != q.device or not s.is_contiguous() or s.is_neg() or \
+    n, m = shape
+    stride, step = q.stride()
+    device = q.get_device()
+    if step != 1 and m > 1 and n > 0:
+        refuse(what + ": int8 codes on the GPU, 2-D, dense rows")
+    if s.dtype is not torch.float32 or s.get_device() != device or not s.is_contiguous() or s.is_neg() or \
             s.numel() != n * (1 if not g else -(-m // g) if g > 0 else -1):
         refuse(what + ": float32 scales, dense, one for each group of columns of each row, on the codes' device, no pending negation")
-    if like is not None and q.device != like.device:
+    if like is not None and device != like.get_device():
         refuse(what + ": on the other tensors' device")
     if (rows is not None and n != rows) or (cols is not None and m != cols):
         refuse("%s: %s x %s" % (what, "rows" if rows is None else rows, "cols" if cols is None else cols))
-    return T.tgrad_codes(q.data_ptr(), s.data_ptr(), n, m, q.stride(0) if n > 1 else m, g)
+    return T.tgrad_codes(q.data_ptr(), s.data_ptr(), n, m, stride if n > 1 else m, g)
 
 
 def new_codes(rows, cols, group, device) -> Codes:
     """Memory for codes, rows at multiples of 16 bytes."""
     pitch = -(-cols // 16) * 16
-    codes = torch.empty(rows, pitch, dtype=torch.int8, device=device)
+    codes = torch.empty((rows, pitch), dtype=torch.int8, device=device)
     return Codes(codes[:, :cols] if pitch != cols else codes,
-                 torch.empty(rows, -(-cols // group) if group else 1, dtype=torch.float32, device=device), group)
+                 torch.empty((rows, -(-cols // group) if group else 1), dtype=torch.float32, device=device), group)
+
+
+def new_matrix(rows, cols, dtype, device):
+    """A new tensor and its description."""
+    x = torch.empty((rows, cols), dtype=dtype, device=device)
+    return x, T.tgrad_matrix(x.data_ptr(), rows, cols, cols, REAL_TYPES[dtype])
 
 
 def _result(out, what, like, rows, cols, dtype):
     """`out`, checked, or a new tensor, and its description."""
     if out is None:
-        out = torch.empty(rows, cols, dtype=dtype, device=like.device)
+        return new_matrix(rows, cols, dtype, like.device)
     return out, describe(out, what, like, rows, cols, dtype)
 
 
@@ -99,8 +115,12 @@ def _scratch_bytes(op, tokens, inner, outer):
     return n.value
 
 
-def _scratch(op, tokens, inner, outer, device):
-    return torch.empty(_scratch_bytes(op, tokens, inner, outer), dtype=torch.uint8, device=device)
+def scratch(n, device):
+    """n bytes and their address; no memory where n is 0."""
+    if n == 0:
+        return None, None
+    t = torch.empty(n, dtype=torch.uint8, device=device)
+    return t, t.data_ptr()
 
 
 def _group(group):
@@ -151,8 +171,8 @@ def tgrad_codes_matmul(x: Codes, weight: Codes, *, dtype=torch.bfloat16, out=Non
         refuse("dtype: float32, bfloat16 or float16")
     dev = x.codes.device
     y, d = _result(out, "out", x.codes, c.rows, w.rows, dtype)
-    ws = _scratch(T.TGRAD_CODES_MATMUL, c.rows, c.cols, w.rows, dev)
-    call(dev, T.load().tgrad_codes_matmul, "tgrad_codes_matmul", C.byref(c), C.byref(w), C.byref(d), ws.data_ptr(), stream_of(dev))
+    ws, at = scratch(_scratch_bytes(T.TGRAD_CODES_MATMUL, c.rows, c.cols, w.rows), dev)
+    call(dev, T.load().tgrad_codes_matmul, "tgrad_codes_matmul", C.byref(c), C.byref(w), C.byref(d), at, stream_of(dev))
     return y
 
 
@@ -168,9 +188,9 @@ def tgrad_codes_linear(x, weight: Codes, *, keep: bool = False, dtype=None, out=
         refuse("dtype: float32, bfloat16 or float16")
     y, e = _result(out, "out", x, d.rows, w.rows, dtype)
     x8 = new_codes(d.rows, d.cols, 0, dev) if keep else None
-    ws = _scratch(T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows, dev)
+    ws, at = scratch(_scratch_bytes(T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows), dev)
     call(dev, T.load().tgrad_codes_linear, "tgrad_codes_linear", C.byref(d), C.byref(w), C.byref(describe_codes(x8, "keep")) if keep else None,
-         C.byref(e), ws.data_ptr(), stream_of(dev))
+         C.byref(e), at, stream_of(dev))
     return Linear(y, x8)
 
 
@@ -200,10 +220,10 @@ def _gradient(name, op, dy, codes, dtype, out):
         c = describe_codes(codes, "x", dy, rows=d.rows)
         tokens, outer, rows = d.rows, d.cols, d.cols
     out, e = _result(out, "out", dy, rows, c.cols, dtype)
-    if (d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8:
+    if (d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8 or d.row_stride > 1 << 21:
         op += T.TGRAD_CODES_UNALIGNED
-    ws = _scratch(op, tokens, c.cols, outer, dev)
-    call(dev, getattr(T.load(), name), name, C.byref(d), C.byref(c), C.byref(e), ws.data_ptr(), stream_of(dev))
+    ws, at = scratch(_scratch_bytes(op, tokens, c.cols, outer), dev)
+    call(dev, getattr(T.load(), name), name, C.byref(d), C.byref(c), C.byref(e), at, stream_of(dev))
     return out
 
 

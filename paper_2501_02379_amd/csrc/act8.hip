@@ -194,16 +194,17 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
   const int units = (cols + 7) / 8, es = sizeof(typename Elem<DT>::raw);
   float held[NV][8];
   uint32_t top = 0;
-  auto unit = [&](int u, float* r, bool keep) {
-    Eight<DT> e, h;
-    float v[8], g[8];
-    Place p{row, u * 8, u < units};
+  auto load = [&](int u, Eight<DT>& e, Eight<DT>& h) {
     e.clear();
     h.clear();
-    if (p.in) {
+    if (u < units) {
       e.load(src + (int64_t)u * 8 * es, cols - u * 8);
       if constexpr (GATED) h.load(gsrc + (int64_t)u * 8 * es, cols - u * 8);
     }
+  };
+  auto unit = [&](int u, const Eight<DT>& e, const Eight<DT>& h, float* r, bool keep) {
+    float v[8], g[8];
+    const Place p{row, u * 8, u < units};
     e.get(v);
     h.get(g);
     activate<DT, ACT, GATED>(v, g, r);
@@ -212,14 +213,17 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
       if constexpr (GATED) keep_group(g, p, cols, gate8);
     }
   };
+  Eight<DT> e, h;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    unit(threadIdx.x + i * T, held[i], true);
+    load(threadIdx.x + i * T, e, h);
+    unit(threadIdx.x + i * T, e, h, held[i], true);
     top = max(top, largest(held[i]));
   }
   for (int u0 = NV * T; u0 < units; u0 += T) {      // whole wavefronts: groups are formed across lanes
     float r[8];
-    unit(u0 + threadIdx.x, r, true);
+    load(u0 + threadIdx.x, e, h);
+    unit(u0 + threadIdx.x, e, h, r, true);
     top = max(top, largest(r));
   }
   const Rounding r8 = rounding_of(largest_of_block<T / kWave>(top, lds));
@@ -232,7 +236,8 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
   }
   for (int u = threadIdx.x + NV * T; u < units; u += T) {
     float r[8];
-    unit(u, r, false);
+    load(u, e, h);
+    unit(u, e, h, r, false);
     store_codes(dst + (int64_t)u * 8, codes_of(r, r8), cols - u * 8);
   }
 }
@@ -271,22 +276,26 @@ __global__ __launch_bounds__(256) void k_activation_back(Mat dy, Codes8 x8, Code
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
-// Threads and held units of a workgroup that has a row to itself.
+// Threads and held units of a workgroup that has a row to itself: the fewest threads whose registers hold it, 4 units each at most, so that several rows
+// share a compute unit.  (32768 rows of 1000 bf16 quantised by 256 threads 28 us, by 64 18; activations of them 71 and 45.  Rows of 28672, activations: 1024
+// threads 408 us, 512 of 8 units 560; 1024 with their registers halved for two rows a unit spill: 1110.)
 template <typename F>
 void for_row(int64_t rows, int cols, F&& f) {
   const int units = (cols + 7) / 8;
   typedef std::integral_constant<int, 64> t64;
   typedef std::integral_constant<int, 256> t256;
+  typedef std::integral_constant<int, 512> t512;
   typedef std::integral_constant<int, 1024> t1024;
   typedef std::integral_constant<int, 1> n1;
   typedef std::integral_constant<int, 2> n2;
   typedef std::integral_constant<int, 4> n4;
   if (units <= 64) f(t64(), n1());
+  else if (units <= 128) f(t64(), n2());
   else if (units <= 256) f(t256(), n1());
   else if (units <= 512) f(t256(), n2());
   else if (units <= 1024 && rows > compute_units()) f(t256(), n4());
   else if (units <= 1024) f(t1024(), n1());
-  else if (units <= 2048) f(t1024(), n2());
+  else if (units <= 2048) f(t512(), n4());
   else f(t1024(), n4());
 }
 

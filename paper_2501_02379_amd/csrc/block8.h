@@ -60,7 +60,12 @@ template <int DT> struct Eight {
     raw* p = reinterpret_cast<raw*>(at);
     if (n >= 8) {
 #pragma unroll
-      for (int i = 0; i < kQuads; ++i) reinterpret_cast<QuadAny*>(p)[i] = q[i];
+      for (int i = 0; i < kQuads; ++i) {
+        // results go past the caches, but for float32, whose lanes have half a line at a time (dequantising 8192^2: bf16 31 -> 31 us, 8192 x 28672
+        // 122 -> 101, float32 65 -> 101; a norm of 8192 x 16384 bf16 99 -> 88)
+        if constexpr (kQuads == 1) __builtin_nontemporal_store(q[i], reinterpret_cast<QuadAny*>(p) + i);
+        else reinterpret_cast<QuadAny*>(p)[i] = q[i];
+      }
     } else {
       float f[8];
       get(f);
@@ -214,7 +219,7 @@ __device__ __forceinline__ Duo codes_of(const float* f, const Rounding& r) {
 }
 __device__ __forceinline__ void store_codes(int8_t* p, Duo d, int n) {
   if (n >= 8) {
-    *reinterpret_cast<DuoByte*>(p) = d;
+    __builtin_nontemporal_store(d, reinterpret_cast<DuoByte*>(p));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

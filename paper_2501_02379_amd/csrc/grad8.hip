@@ -676,21 +676,6 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
   if (cut.splits > 1) launch_add(s, reinterpret_cast<const float*>(parts), cut.splits, out);
 }
 
-// Two-byte rows of 2^21 numbers and more, whose tiles 32-bit offsets do not reach, are refused.
-bool reachable(const tgrad_matrix* dy) { return dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21); }
-
-template <bool WEIGHT>
-int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
-  if (!good(dy) || !good(c) || !good(out) || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
-  if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
-  if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
-  if (too_many(out) || !reachable(dy)) return TGRAD_ERR_UNSUPPORTED;
-  if (pending()) return TGRAD_ERR_HIP;
-  if (out->rows == 0) return TGRAD_OK;
-  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, workspace_dev);
-  return launched();
-}
-
 }  // namespace
 
 namespace tgrad {
@@ -708,6 +693,27 @@ size_t gradient_scratch(bool weight, bool copy, int64_t tokens, int64_t inner, i
 }
 
 }  // namespace tgrad
+
+namespace {
+
+// Two-byte rows of 2^21 numbers and more, whose tiles 32-bit offsets do not reach, are refused.
+bool reachable(const tgrad_matrix* dy) { return dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21); }
+
+template <bool WEIGHT>
+int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
+  if (!good(dy) || !good(c) || !good(out)) return TGRAD_ERR_INVALID_ARG;
+  if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
+  if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
+  if (too_many(out) || !reachable(dy)) return TGRAD_ERR_UNSUPPORTED;
+  const bool copy = dy->dtype != TGRAD_F32 && !straight(dy);
+  if (!scratch_ok(workspace_dev, gradient_scratch(WEIGHT, copy, dy->rows, c->cols, dy->cols))) return TGRAD_ERR_INVALID_ARG;
+  if (pending()) return TGRAD_ERR_HIP;
+  if (out->rows == 0) return TGRAD_OK;
+  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, workspace_dev);
+  return launched();
+}
+
+}  // namespace
 
 extern "C" {
 

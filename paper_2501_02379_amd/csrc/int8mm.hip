@@ -447,6 +447,14 @@ void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, c
   }
 }
 
+// A few tokens are quantised by the product's own launch.
+bool fused(int64_t tokens, int64_t inner) { return tokens <= kFusedTokens && tokens * inner <= kFusedCodes && inner <= kFewThreads * 8 * kFusedUnits; }
+
+size_t product_scratch(int64_t tokens, int64_t outer, int64_t inner) { return inner <= TGRAD_CODES_MAX_INNER ? part_bytes(tokens, outer, inner) : 0; }
+size_t linear_scratch(int64_t tokens, int64_t outer, int64_t inner) {
+  return fused(tokens, inner) ? 0 : product_scratch(tokens, outer, inner) + scratch_codes(tokens, inner);
+}
+
 }  // namespace
 
 extern "C" {
@@ -456,21 +464,17 @@ int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer,
   if (copy) op -= TGRAD_CODES_UNALIGNED;
   if (!workspace_bytes || op < (copy ? TGRAD_CODES_GRAD_INPUT : TGRAD_CODES_MATMUL) || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
   if (!extents_ok(tokens, inner, inner) || !extents_ok(outer, inner, inner)) return TGRAD_ERR_INVALID_ARG;
-  size_t n = kScratchAlign;
-  if (op == TGRAD_CODES_MATMUL || op == TGRAD_CODES_LINEAR) {
-    if (inner <= TGRAD_CODES_MAX_INNER && tokens > 0) n += part_bytes(tokens, outer, inner);
-    if (op == TGRAD_CODES_LINEAR) n += scratch_codes(tokens, inner);
-  } else {
-    n += gradient_scratch(op == TGRAD_CODES_GRAD_WEIGHT, copy, tokens, inner, outer);
-  }
-  *workspace_bytes = n;
+  *workspace_bytes = op == TGRAD_CODES_MATMUL ? product_scratch(tokens, outer, inner)
+                   : op == TGRAD_CODES_LINEAR ? linear_scratch(tokens, outer, inner)
+                                              : gradient_scratch(op == TGRAD_CODES_GRAD_WEIGHT, copy, tokens, inner, outer);
   return TGRAD_OK;
 }
 
 int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* workspace_dev, void* hip_stream) {
-  if (!good(x) || !good(w) || !good(y) || x->group || w->group || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
+  if (!good(x) || !good(w) || !good(y) || x->group || w->group) return TGRAD_ERR_INVALID_ARG;
   if (x->cols != w->cols || !same_size(y, x->rows, w->rows)) return TGRAD_ERR_INVALID_ARG;
   if (too_many(y) || x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
+  if (!scratch_ok(workspace_dev, product_scratch(y->rows, y->cols, x->cols))) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
   if (y->rows == 0) return TGRAD_OK;
   launch_product(static_cast<hipStream_t>(hip_stream), x, w, y, workspace_dev);
@@ -479,14 +483,15 @@ int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_m
 
 int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_codes* keep, const tgrad_matrix* y, void* workspace_dev,
                       void* hip_stream) {
-  if (!good(x) || !good(w) || !good(y) || w->group || !scratch_ok(workspace_dev)) return TGRAD_ERR_INVALID_ARG;
+  if (!good(x) || !good(w) || !good(y) || w->group) return TGRAD_ERR_INVALID_ARG;
   if (x->cols != w->cols || !same_size(y, x->rows, w->rows)) return TGRAD_ERR_INVALID_ARG;
   if (keep && (!good(keep) || keep->group || !same_size(keep, x->rows, x->cols))) return TGRAD_ERR_INVALID_ARG;
   if (too_many(y) || x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
+  if (!scratch_ok(workspace_dev, linear_scratch(y->rows, y->cols, x->cols))) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
   if (y->rows == 0) return TGRAD_OK;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (x->rows <= kFusedTokens && x->rows * x->cols <= kFusedCodes && x->cols <= kFewThreads * 8 * kFusedUnits) {
+  if (fused(x->rows, x->cols)) {
     for_real(x->dtype, [&](auto xt) {
       for_real(y->dtype, [&](auto yt) {
         k_codes_few<decltype(xt)::value, decltype(yt)::value><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(x->rows, x->cols), s>>>(

@@ -521,6 +521,7 @@ void for_width(int64_t rows, int cols, F&& f) {
   const int units = (cols + 7) / 8;
   typedef std::integral_constant<int, 64> t64;
   typedef std::integral_constant<int, 256> t256;
+  typedef std::integral_constant<int, 512> t512;
   typedef std::integral_constant<int, 1024> t1024;
   typedef std::integral_constant<int, 1> n1;
   typedef std::integral_constant<int, 2> n2;
@@ -528,8 +529,8 @@ void for_width(int64_t rows, int cols, F&& f) {
   if (units <= 64) f(t64(), n1());
   else if (units <= 256) f(t256(), n1());
   else if (units <= 512) f(t256(), n2());
-  else if (units <= 1024) f(t1024(), n1());
-  else if (units <= 2048) f(t1024(), n2());
+  else if (units <= 1024) f(t512(), n2());
+  else if (units <= 2048) f(t512(), n4());
   else f(t1024(), n4());
 }
 

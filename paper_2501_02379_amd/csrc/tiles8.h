@@ -73,7 +73,7 @@ __device__ __forceinline__ int2 tile_of(int id, int total, int tiles_c) {
 // ---- host ---------------------------------------------------------------------------------------------------------------
 
 inline size_t aligned(size_t n) { return (n + kScratchAlign - 1) / kScratchAlign * kScratchAlign; }
-inline bool scratch_ok(const void* p) { return p && (uintptr_t)p % kScratchAlign == 0; }
+inline bool scratch_ok(const void* p, size_t needed) { return needed == 0 || (p && (uintptr_t)p % kScratchAlign == 0); }
 // A launch has fewer than 2^32 threads.
 inline bool too_many(const tgrad_matrix* y) { return ((y->rows + 63) / 64) * ((y->cols + 63) / 64) >= ((int64_t)1 << 21); }
 

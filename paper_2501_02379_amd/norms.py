@@ -33,24 +33,31 @@ class BlockNormGrads(NamedTuple):
     dpre: Optional[torch.Tensor]
 
 
-def _describe(x, block, dtype, post, pre, gate, rows_per_gate, scale, eps, centered):
-    rows, cols = x.shape
-    weights = [w for w in (post, pre) if w is not None]
-    for w in weights:
-        if w.dim() != 1 or w.shape[0] != cols or w.dtype not in REAL_TYPES or w.device != x.device or not w.is_contiguous() or w.is_neg() or \
-                w.dtype is not weights[0].dtype:
-            refuse("post_weight, pre_weight: [cols], dense, float32, bfloat16 or float16, both of one type, on x's device")
+def _weight(w, cols, x):
+    code = REAL_TYPES.get(w.dtype)
+    if code is None or w.dim() != 1 or w.shape[0] != cols or w.get_device() != x.get_device() or not w.is_contiguous() or w.is_neg():
+        refuse("post_weight, pre_weight: [cols], dense, float32, bfloat16 or float16, on x's device")
+    return w.data_ptr(), code
+
+
+def _describe(x, rows, cols, block, dtype, post, pre, gate, rows_per_gate, scale, eps, centered):
     if block is None and (post is not None or gate is not None or pre is None):
         refuse("without a block there is a pre_weight, and neither post_weight nor gate")
+    post_at, code = _weight(post, cols, x) if post is not None else (None, T.TGRAD_F32)
+    pre_at, pre_code = _weight(pre, cols, x) if pre is not None else (None, code)
+    if post is None:
+        code = pre_code
+    if code != pre_code:
+        refuse("post_weight, pre_weight: of one type")
     if rows_per_gate < 1:
         refuse("rows_per_gate: at least 1")
+    gate_at, gate_stride = None, 0
     if gate is not None:
         g = act8.describe(gate, "gate", x, -(-rows // rows_per_gate), cols, dtype)
+        gate_at, gate_stride = g.data, g.row_stride
     if not (math.isfinite(scale) and math.isfinite(eps) and eps > 0):
         refuse("scale: finite; eps: above 0, finite")
-    return T.tgrad_block(post.data_ptr() if post is not None else None, pre.data_ptr() if pre is not None else None,
-                         gate.data_ptr() if gate is not None else None, g.row_stride if gate is not None else 0, rows_per_gate,
-                         REAL_TYPES[weights[0].dtype] if weights else T.TGRAD_F32, scale, eps, 1 if centered else 0)
+    return T.tgrad_block(post_at, pre_at, gate_at, gate_stride, rows_per_gate, code, scale, eps, 1 if centered else 0)
 
 
 @functools.lru_cache(maxsize=1024)
@@ -86,17 +93,17 @@ def tgrad_block_norm(x, block=None, *, post_weight=None, gate=None, rows_per_gat
     if dtype not in REAL_TYPES:
         refuse("dtype: float32, bfloat16 or float16")
     _types(x, dtype)
-    desc = _describe(x, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, eps, centered)
-    out, o = act8._result(None, "x", x, d.rows, d.cols, x.dtype) if block is not None else (x, None)
+    desc = _describe(x, d.rows, d.cols, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, eps, centered)
+    out, o = act8.new_matrix(d.rows, d.cols, x.dtype, dev) if block is not None else (x, None)
     h = e = c = None
     if pre_weight is not None and quantize:
         h = act8.new_codes(d.rows, d.cols, 0, dev)
         c = act8.describe_codes(h, "h")
     elif pre_weight is not None:
-        h, e = act8._result(None, "h", x, d.rows, d.cols, dtype)
+        h, e = act8.new_matrix(d.rows, d.cols, dtype, dev)
     elif quantize:
         refuse("quantize: with a pre_weight")
-    stats = torch.empty(d.rows, 4, dtype=torch.float32, device=dev) if keep else None
+    stats = torch.empty((d.rows, 4), dtype=torch.float32, device=dev) if keep else None
     call(dev, T.load().tgrad_block_norm, "tgrad_block_norm", C.byref(desc), C.byref(d), _ref(b), _ref(o), _ref(e), _ref(c),
          stats.data_ptr() if keep else None, stream_of(dev))
     return BlockNorm(out, h, stats)
@@ -117,21 +124,19 @@ def tgrad_block_norm_backward(dx, dh, x, block=None, *, stats, post_weight=None,
     if dtype not in REAL_TYPES:
         refuse("dh: float32, bfloat16 or float16")
     _types(x, dtype)
-    desc = _describe(x, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, 1.0, centered)
+    desc = _describe(x, rows, cols, block, dtype, post_weight, pre_weight, gate, rows_per_gate, scale, 1.0, centered)
     a = act8.describe(dx, "dx", x, rows, cols, x.dtype) if dx is not None else None
     u = act8.describe(dh, "dh", x, rows, cols, dtype) if dh is not None else None
     if stats is None or stats.dtype is not torch.float32 or tuple(stats.shape) != (rows, 4) or stats.device != dev or not stats.is_contiguous() or \
             stats.is_neg() or stats.data_ptr() % 16:
         refuse("stats: float32[rows, 4] of the forward call")
-    new = lambda *shape, t: torch.empty(*shape, dtype=t, device=dev)  # noqa: E731
-    gx = new(rows, cols, t=x.dtype)
-    gb = new(rows, cols, t=dtype) if block is not None else None
-    gg = new(*gate.shape, t=dtype) if gate is not None else None
-    gpost = new(cols, t=torch.float32) if post_weight is not None else None
-    gpre = new(cols, t=torch.float32) if pre_weight is not None else None
-    ws = new(_scratch_bytes(rows, cols, rows_per_gate if gate is not None else 1), t=torch.uint8)
+    gx, ex = act8.new_matrix(rows, cols, x.dtype, dev)
+    gb, eb = act8.new_matrix(rows, cols, dtype, dev) if block is not None else (None, None)
+    gg = torch.empty(gate.shape, dtype=dtype, device=dev) if gate is not None else None
+    gpost = torch.empty(cols, dtype=torch.float32, device=dev) if post_weight is not None else None
+    gpre = torch.empty(cols, dtype=torch.float32, device=dev) if pre_weight is not None else None
+    ws, ws_at = act8.scratch(_scratch_bytes(rows, cols, rows_per_gate if gate is not None else 1), dev)
     at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     call(dev, T.load().tgrad_block_norm_backward, "tgrad_block_norm_backward", C.byref(desc), _ref(a), _ref(u), C.byref(o), _ref(b),
-         stats.data_ptr(), C.byref(act8.describe(gx, "dx")), C.byref(act8.describe(gb, "dblock")) if gb is not None else None, at(gg),
-         at(gpost), at(gpre), ws.data_ptr(), stream_of(dev))
+         stats.data_ptr(), C.byref(ex), _ref(eb), at(gg), at(gpost), at(gpre), ws_at, stream_of(dev))
     return BlockNormGrads(gx, gb, gg, gpost, gpre)

@@ -65,8 +65,10 @@ def test_sizes_have_to_go_together():
     assert lib.tgrad_codes_matmul(codes(), codes(40), mat(8, 41), 256, None) == BAD
     assert lib.tgrad_codes_matmul(ok32, codes(40), mat(8, 40), 256, None) == BAD          # one scale a row in both
     assert lib.tgrad_codes_matmul(codes(), codes(40, group=32), mat(8, 40), 256, None) == BAD
-    assert lib.tgrad_codes_matmul(codes(), codes(40), mat(8, 40), 264, None) == BAD
-    assert lib.tgrad_codes_matmul(codes(), codes(40), mat(8, 40), None, None) == BAD
+    for ws in (264, None):                                                                # 20 tokens need scratch
+        assert lib.tgrad_codes_matmul(codes(20, 4096), codes(40, 4096), mat(20, 40), ws, None) == BAD
+        assert lib.tgrad_codes_linear(mat(20), codes(40), None, mat(20, 40), ws, None) == BAD
+        assert lib.tgrad_codes_grad_weight(mat(8, 99), codes(8, 50), mat(99, 50), ws, None) == BAD      # and so does dy with odd rows
     long = 131073
     assert lib.tgrad_codes_matmul(codes(1, long), codes(1, long), mat(1, 1), 256, None) == T.TGRAD_ERR_UNSUPPORTED
     assert lib.tgrad_codes_linear(mat(1, long), codes(1, long), None, mat(1, 1), 256, None) == T.TGRAD_ERR_UNSUPPORTED
@@ -76,7 +78,6 @@ def test_sizes_have_to_go_together():
     assert lib.tgrad_codes_grad_input(mat(), codes(100, 50), mat(8, 50, dtype=T.TGRAD_F16), 256, None) == BAD
     assert lib.tgrad_codes_grad_input(mat(dtype=f32, data=4096), codes(100, 50), mat(8, 50), 256, None) == BAD
     assert lib.tgrad_codes_grad_weight(mat(), codes(9, 50), mat(100, 50), 256, None) == BAD
-    assert lib.tgrad_codes_grad_weight(mat(), codes(8, 50), mat(100, 50), 8, None) == BAD
     assert lib.tgrad_activation(mat(), mat(dtype=f32), 0, mat(), None, None, None, None) == BAD
     assert lib.tgrad_activation(mat(), None, 2, mat(), None, None, None, None) == BAD
     assert lib.tgrad_activation(mat(), None, 0, None, None, ok32, None, None) == BAD       # no result
@@ -129,13 +130,13 @@ def test_sizes_of_scratch():
     got = []
     for tokens in (0, 1, 1000, 100000):
         assert lib.tgrad_codes_query_size(T.TGRAD_CODES_LINEAR, tokens, 4096, 4096, C.byref(n)) == T.TGRAD_OK
-        assert n.value % 256 == 0 and n.value >= tokens * 4096 + 256
+        assert n.value % 256 == 0 and n.value >= (tokens * 4096 if tokens > 4 else 0)
         got.append(n.value)
     assert got == sorted(got)
     for op in range(4):
         for sizes in ((0, 33, 55), (77, 33, 0), (0, 33, 0), (1, 1, 1), (1, 1 << 20, 1 << 20)):
-            assert lib.tgrad_codes_query_size(op, *sizes, C.byref(n)) == T.TGRAD_OK and n.value >= 256
-        assert lib.tgrad_codes_query_size(op, 77, 33, 55, C.byref(n)) == T.TGRAD_OK and n.value >= 256
+            assert lib.tgrad_codes_query_size(op, *sizes, C.byref(n)) == T.TGRAD_OK and n.value % 256 == 0
+        assert lib.tgrad_codes_query_size(op, 77, 33, 55, C.byref(n)) == T.TGRAD_OK and n.value % 256 == 0
     for args in ((-1, 1, 1, 1), (4, 1, 1, 1), (0, -1, 1, 1), (0, 1, 0, 1), (0, 1, 1, -1), (0, 1 << 31, 1, 1), (0, 1, 1 << 31, 1)):
         assert lib.tgrad_codes_query_size(*args, C.byref(n)) == BAD
     assert lib.tgrad_codes_query_size(0, 1, 1, 1, None) == BAD

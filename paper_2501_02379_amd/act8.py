@@ -85,12 +85,13 @@ def describe_codes(c, what, like=None, rows=None, cols=None):
     return T.tgrad_codes(q.data_ptr(), s.data_ptr(), n, m, stride if n > 1 else m, g)
 
 
-def new_codes(rows, cols, group, device) -> Codes:
-    """Memory for codes, rows at multiples of 16 bytes."""
+def new_codes(rows, cols, group, device):
+    """Memory for codes, rows at multiples of 16 bytes, and its description."""
     pitch = -(-cols // 16) * 16
     codes = torch.empty((rows, pitch), dtype=torch.int8, device=device)
-    return Codes(codes[:, :cols] if pitch != cols else codes,
-                 torch.empty((rows, -(-cols // group) if group else 1), dtype=torch.float32, device=device), group)
+    scale = torch.empty((rows, -(-cols // group) if group else 1), dtype=torch.float32, device=device)
+    return Codes(codes[:, :cols] if pitch != cols else codes, scale, group), \
+        T.tgrad_codes(codes.data_ptr(), scale.data_ptr(), rows, cols, pitch, group)
 
 
 def new_matrix(rows, cols, dtype, device):
@@ -123,6 +124,10 @@ def scratch(n, device):
     return t, t.data_ptr()
 
 
+def _ref(d):
+    return None if d is None else C.byref(d)
+
+
 def _group(group):
     if group not in (0, 32, 64, 128, 256, 512):
         refuse("group: 0 (the whole row), 32, 64, 128, 256 or 512 columns")
@@ -142,12 +147,14 @@ _on_stream = on_stream_with(lambda a: [t for t in a if isinstance(t, torch.Tenso
 def tgrad_quantize(x, *, group: int = 0, out: Optional[Codes] = None) -> Codes:
     """x in 8 bits, a scale for `group` columns (0: the whole row).  `out`: where the codes go."""
     d = describe(x, "x")
+    dev = x.device
     if out is None:
-        out = new_codes(d.rows, d.cols, _group(group), x.device)
-    elif isinstance(out, Codes) and out.group != group:
-        refuse("out: codes in groups of `group` columns")
-    call(x.device, T.load().tgrad_quantize, "tgrad_quantize", C.byref(d), C.byref(describe_codes(out, "out", x, d.rows, d.cols)),
-         stream_of(x.device))
+        out, c = new_codes(d.rows, d.cols, _group(group), dev)
+    else:
+        c = describe_codes(out, "out", x, d.rows, d.cols)
+        if c.group != group:
+            refuse("out: codes in groups of `group` columns")
+    call(dev, T.load().tgrad_quantize, "tgrad_quantize", C.byref(d), C.byref(c), stream_of(dev))
     return out
 
 
@@ -187,10 +194,9 @@ def tgrad_codes_linear(x, weight: Codes, *, keep: bool = False, dtype=None, out=
     if dtype not in REAL_TYPES:
         refuse("dtype: float32, bfloat16 or float16")
     y, e = _result(out, "out", x, d.rows, w.rows, dtype)
-    x8 = new_codes(d.rows, d.cols, 0, dev) if keep else None
+    x8, c = new_codes(d.rows, d.cols, 0, dev) if keep else (None, None)
     ws, at = scratch(_scratch_bytes(T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows), dev)
-    call(dev, T.load().tgrad_codes_linear, "tgrad_codes_linear", C.byref(d), C.byref(w), C.byref(describe_codes(x8, "keep")) if keep else None,
-         C.byref(e), at, stream_of(dev))
+    call(dev, T.load().tgrad_codes_linear, "tgrad_codes_linear", C.byref(d), C.byref(w), _ref(c), C.byref(e), at, stream_of(dev))
     return Linear(y, x8)
 
 
@@ -237,16 +243,16 @@ def tgrad_activation(x, gate=None, *, act: str = "silu", group: int = 128, keep:
     g = describe(gate, "gate", x, d.rows, d.cols, x.dtype) if gate is not None else None
     if keep and not _group(group):
         refuse("group: 32, 64, 128, 256 or 512 columns")
-    if quantize:
-        y = new_codes(d.rows, d.cols, 0, dev) if out is None else out
-        e = describe_codes(y, "out", x, d.rows, d.cols)
+    if quantize and out is None:
+        y, e = new_codes(d.rows, d.cols, 0, dev)
+    elif quantize:
+        y, e = out, describe_codes(out, "out", x, d.rows, d.cols)
     else:
         y, e = _result(out, "out", x, d.rows, d.cols, x.dtype)
-    x8 = new_codes(d.rows, d.cols, group, dev) if keep else None
-    gate8 = new_codes(d.rows, d.cols, group, dev) if keep and g is not None else None
-    ref = lambda c: C.byref(describe_codes(c, "checkpoint")) if c is not None else None  # noqa: E731
-    call(dev, T.load().tgrad_activation, "tgrad_activation", C.byref(d), C.byref(g) if g is not None else None, code,
-         None if quantize else C.byref(e), C.byref(e) if quantize else None, ref(x8), ref(gate8), stream_of(dev))
+    x8, cx = new_codes(d.rows, d.cols, group, dev) if keep else (None, None)
+    gate8, cg = new_codes(d.rows, d.cols, group, dev) if keep and g is not None else (None, None)
+    call(dev, T.load().tgrad_activation, "tgrad_activation", C.byref(d), _ref(g), code, None if quantize else C.byref(e),
+         C.byref(e) if quantize else None, _ref(cx), _ref(cg), stream_of(dev))
     return Activation(y, x8, gate8)
 
 

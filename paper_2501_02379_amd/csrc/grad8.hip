@@ -378,13 +378,14 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   }
 }
 
-// ---- float32 dy, a scale for each row of codes -------------------------------------------------------------------------------------------
+// ---- float32 dy, and two-byte dy of a few tokens: a scale for each row of codes -------------------------------------------------------------------------------------------
 
 // dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_pair); codes are exact in bf16.  Three products instead
-// of one, each 16 times as fast as the float32 matrix instructions'.
+// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 397 us for dw, 419 for dx, 340 TFLOP/s.)  Two-byte dy of up to 64
+// tokens takes this way too: memory bounds such products, so that no value need be rounded.
 constexpr int kStep32 = 32;
 
-template <int WR, int WC, int FR, int FC, bool WEIGHT>
+template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
 __global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
   constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
   constexpr int kPart = BR * kStep32 * 2, kBytes = 3 * kPart + BC * kStep32 * 2;
@@ -397,7 +398,8 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
   const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep32 - 1) / kStep32);
   auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
 
-  Eight<TGRAD_F32> held[kLoads];
+  constexpr int es = sizeof(typename Elem<DT>::raw);
+  Eight<DT> held[kLoads];
   Quad codes[kCodes];
   float scale[kLoads][WEIGHT ? 1 : 8];
   auto read = [&](int64_t s) {
@@ -410,13 +412,13 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
         const int n = a.rows - r0 - id % (BR / 8) * 8;
         scale[i][0] = 0.f;
         if (row < a.sum && n > 0) {
-          held[i].load(a.dy.row(row) + (int64_t)(a.rows - n) * 4, n);
+          held[i].load(a.dy.row(row) + (int64_t)(a.rows - n) * es, n);
           scale[i][0] = a.c.scale[row];
         }
       } else {
         const int64_t at = s * kStep32 + id % 4 * 8;
         const int n = (int)min(a.sum - at, (int64_t)8);
-        if (n > 0) held[i].load(a.dy.row(min(r0 + id / 4, a.rows - 1)) + at * 4, n);
+        if (n > 0) held[i].load(a.dy.row(min(r0 + id / 4, a.rows - 1)) + at * es, n);
         Eight<TGRAD_F32> e;
         e.clear();
         if (n > 0) e.load(reinterpret_cast<const char*>(a.c.scale + at), n);
@@ -511,7 +513,7 @@ __global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
 #pragma unroll
     for (int i = 0; i < FC; ++i) {
       const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
-      if (c < a.cols) store4<TGRAD_F32>(row, c, a.cols, acc[i][j]);
+      if (c < a.cols) store4<OT>(row, c, a.cols, acc[i][j]);
     }
   }
 }
@@ -634,6 +636,8 @@ bool straight(const tgrad_matrix* dy) {
 bool straight(const tgrad_codes* c) { return (uintptr_t)c->codes % 16 == 0 && c->row_stride % 16 == 0 && c->row_stride <= ((int64_t)1 << 22); }
 size_t copy_bytes(int64_t tokens, int64_t outer) { return aligned((size_t)tokens * ((outer + 7) / 8 * 16)); }
 
+bool in_parts(const tgrad_matrix* dy, const tgrad_codes* c) { return dy->dtype == TGRAD_F32 || (dy->rows <= 64 && (c->group == 0 || c->cols <= c->group)); }
+
 template <bool WEIGHT>
 void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {
   Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0, (int)out->rows};
@@ -643,7 +647,8 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
     return;
   }
   char* parts = static_cast<char*>(scratch);
-  if (dy->dtype != TGRAD_F32 && !straight(dy) && dy->rows > 0) {
+  const bool split = in_parts(dy, c);
+  if (!split && !straight(dy) && dy->rows > 0) {
     const int64_t per = (dy->cols + 7) / 8;
     rows_in_launches(dy->rows, 256, (per + 255) / 256, [&](int64_t first, int64_t rows) {
       for_real(dy->dtype, [&](auto t) {
@@ -655,24 +660,22 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
     if (WEIGHT) g.dy_rows = (int)(per * 8);
     parts += copy_bytes(dy->rows, dy->cols);
   }
-  const Cut cut = cut_of(out->rows, out->cols, g.sum, dy->dtype != TGRAD_F32 && straight(c) && g.dy.stride <= ((int64_t)1 << 22),
-                         dy->dtype == TGRAD_F32 ? kStep32 : kStep);
+  const Cut cut = cut_of(out->rows, out->cols, g.sum, !split && straight(c) && g.dy.stride <= ((int64_t)1 << 22), split ? kStep32 : kStep);
   g.tiles_c = cut.tiles_c;
   g.tiles = cut.tiles;
   g.steps = cut.steps;
   if (cut.splits > 1) g.out = Mat{parts, out->cols * 4};
-  if (dy->dtype == TGRAD_F32) {
-    launch_cut(s, k_grad_split<2, 2, 4, 4, WEIGHT>, 256, 2 * (3 * 128 + 128) * kStep32 * 2, cut, g);
-  } else if (cut.splits > 1) {
-    if (dy->dtype == TGRAD_BF16) launch_tiles<TGRAD_BF16, -1, WEIGHT>(s, cut, g);
-    else launch_tiles<TGRAD_F16, -1, WEIGHT>(s, cut, g);
-  } else if (dy->dtype == TGRAD_BF16) {
-    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_BF16, TGRAD_F32, WEIGHT>(s, cut, g);
-    else launch_tiles<TGRAD_BF16, TGRAD_BF16, WEIGHT>(s, cut, g);
-  } else {
-    if (out->dtype == TGRAD_F32) launch_tiles<TGRAD_F16, TGRAD_F32, WEIGHT>(s, cut, g);
-    else launch_tiles<TGRAD_F16, TGRAD_F16, WEIGHT>(s, cut, g);
-  }
+  for_real(dy->dtype, [&](auto t) {
+    constexpr int DT = decltype(t)::value;
+    auto run = [&](auto o) {
+      constexpr int OT = decltype(o)::value;
+      if (split) launch_cut(s, k_grad_split<2, 2, 4, 4, DT, OT, WEIGHT>, 256, 2 * (3 * 128 + 128) * kStep32 * 2, cut, g);
+      else if constexpr (DT != TGRAD_F32) launch_tiles<DT, OT, WEIGHT>(s, cut, g);
+    };
+    if (cut.splits > 1) run(std::integral_constant<int, -1>());
+    else if (out->dtype == DT) run(t);
+    else run(std::integral_constant<int, TGRAD_F32>());
+  });
   if (cut.splits > 1) launch_add(s, reinterpret_cast<const float*>(parts), cut.splits, out);
 }
 
@@ -705,7 +708,7 @@ int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* o
   if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
   if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
   if (too_many(out) || !reachable(dy)) return TGRAD_ERR_UNSUPPORTED;
-  const bool copy = dy->dtype != TGRAD_F32 && !straight(dy);
+  const bool copy = !in_parts(dy, c) && !straight(dy);
   if (!scratch_ok(workspace_dev, gradient_scratch(WEIGHT, copy, dy->rows, c->cols, dy->cols))) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
   if (out->rows == 0) return TGRAD_OK;

@@ -16,6 +16,7 @@ import torch
 
 from . import act8
 from . import tgrad as T
+from .act8 import _ref
 from ._marshal import REAL_TYPES, call, refuse, stream_of
 
 
@@ -69,10 +70,6 @@ def _scratch_bytes(rows, cols, rows_per_gate):
     return n.value
 
 
-def _ref(d):
-    return None if d is None else C.byref(d)
-
-
 def _types(x, dtype):
     if x.dtype not in (dtype, torch.float32):
         refuse("x: float32, or the block's type")
@@ -97,8 +94,7 @@ def tgrad_block_norm(x, block=None, *, post_weight=None, gate=None, rows_per_gat
     out, o = act8.new_matrix(d.rows, d.cols, x.dtype, dev) if block is not None else (x, None)
     h = e = c = None
     if pre_weight is not None and quantize:
-        h = act8.new_codes(d.rows, d.cols, 0, dev)
-        c = act8.describe_codes(h, "h")
+        h, c = act8.new_codes(d.rows, d.cols, 0, dev)
     elif pre_weight is not None:
         h, e = act8.new_matrix(d.rows, d.cols, dtype, dev)
     elif quantize:

@@ -68,7 +68,7 @@ def test_sizes_have_to_go_together():
     for ws in (264, None):                                                                # 20 tokens need scratch
         assert lib.tgrad_codes_matmul(codes(20, 4096), codes(40, 4096), mat(20, 40), ws, None) == BAD
         assert lib.tgrad_codes_linear(mat(20), codes(40), None, mat(20, 40), ws, None) == BAD
-        assert lib.tgrad_codes_grad_weight(mat(8, 99), codes(8, 50), mat(99, 50), ws, None) == BAD      # and so does dy with odd rows
+        assert lib.tgrad_codes_grad_weight(mat(80, 99), codes(80, 50), mat(99, 50), ws, None) == BAD      # and so does dy with odd rows
     long = 131073
     assert lib.tgrad_codes_matmul(codes(1, long), codes(1, long), mat(1, 1), 256, None) == T.TGRAD_ERR_UNSUPPORTED
     assert lib.tgrad_codes_linear(mat(1, long), codes(1, long), None, mat(1, 1), 256, None) == T.TGRAD_ERR_UNSUPPORTED

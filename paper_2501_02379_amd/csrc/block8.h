@@ -163,29 +163,33 @@ __device__ __forceinline__ uint32_t largest_of_block(uint32_t m, uint32_t* lds) 
   return m;
 }
 
-// How a group is rounded, from the bits of its largest magnitude a.  The factor 127 / a is finite and normal where a is 2^-119 at least.
+// How a group is rounded, from the bits of its largest magnitude a.  The factor 127 / a is finite and normal where a is 2^-119 at least.  Both quotients
+// without a division (25 operations, as much as eight codes): q = a y with y the rounded 1 / 127 is next to a / 127, the rest a - 127 q is exact, and
+// q + rest y rounds to the right scale (Markstein); the factor, off by 2^-23 of itself at most, needs no more.
 struct Rounding {
   float scale, factor, top;
 };
 __device__ __forceinline__ Rounding rounding_of(uint32_t top_bits) {
   const float a = __uint_as_float(top_bits);
+  constexpr float kInverse = 1.f / 127.f;
   Rounding r;
   r.top = a;
+  const float q = a * kInverse;
+  r.scale = fmaf(fmaf(-q, 127.f, a), kInverse, q);
+  if (a < 0x1p-90f) r.scale = a / 127.f;                             // where the rest has too few bits
+  r.scale = fminf(r.scale, 0x1.0204060000000p+121f);                 // the largest scale with a finite 127 * scale: a / 127 rounds up at float32's end
+  const float s = a * 0x1p-6f, i = __builtin_amdgcn_rcpf(s);         // neither is subnormal
+  r.factor = fmaf(fmaf(-s, i, 1.f), i, i) * (127.f / 64.f);
+  if (a < 0x1p-119f) r.scale = r.factor = 0.f;
   if (top_bits >= 0x7F800000u) {          // an infinity or NaN
     r.scale = __uint_as_float(0x7FC00000u);
     r.factor = 0.f;
-  } else if (a < 0x1p-119f) {
-    r.scale = 0.f;
-    r.factor = 0.f;
-  } else {
-    r.scale = fminf(a / 127.f, 0x1.0204060000000p+121f);      // the largest scale with a finite 127 * scale: a / 127 rounds up at float32's end
-    r.factor = 127.f / a;
   }
   return r;
 }
 
 // Codes of eight numbers: 127 v / a, rounded to nearest even as the exact quotient is.  v * factor + 1.5 * 2^23 is one rounding, to a whole number in its low
-// byte; the factor is off by 2^-24 of itself, so 127 * 2^-24 = 7.6e-6 of a code at most, and quotients further than 1e-5 from a border are decided by that.
+// byte; the factor's error is 127 * 2^-23 = 1.5e-5 of a code at most, and quotients further than 2e-5 from a border are decided by that.
 // Next to a border 254 |v| is compared with an odd multiple of a, both exact in float64 (32 bits each).  Halves are no rare case: v = a / 2 is one, a common
 // one in two-byte types.  (Decided number by number it was 12 operations each instead of 5: an activation of 8192 x 2 x 28672 bf16 409 us.)
 __device__ __forceinline__ float exact_code(float v, const Rounding& r) {
@@ -203,10 +207,10 @@ __device__ __forceinline__ Duo codes_of(const float* f, const Rounding& r) {
     off[i] = fabsf(fmaf(f[i], r.factor, kWhole - t[i]));
     worst = fmaxf(worst, off[i]);
   }
-  if (worst > 0.49999f) {
+  if (worst > 0.49998f) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (off[i] > 0.49999f) t[i] = kWhole + exact_code(f[i], r);
+      if (off[i] > 0.49998f) t[i] = kWhole + exact_code(f[i], r);
   }
   Duo d;
 #pragma unroll

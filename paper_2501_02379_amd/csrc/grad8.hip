@@ -89,7 +89,7 @@ constexpr int kStep = 64;                 // of the sum in LDS at a time
 // WR x WC wavefronts, each FR x FC results of 16 x 16; two steps in LDS, one barrier a step.  WEIGHT: dy lies across the sum, else along it (rows of
 // 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end; codes go through registers, a step ahead.
 template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
-__global__ __launch_bounds__(WR * WC * 64) void k_grad_tiles(Grad a) {
+__global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
   constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
   constexpr int kDy = BR * kStep * 2, kBytes = kDy + BC * kStep * 2;
   constexpr int kLoads = kDy / 16 / T, kCodes = BC * kStep / 16 / T;
@@ -381,12 +381,12 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
 // ---- float32 dy, and two-byte dy of a few tokens: a scale for each row of codes -------------------------------------------------------------------------------------------
 
 // dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_pair); codes are exact in bf16.  Three products instead
-// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 397 us for dw, 419 for dx, 340 TFLOP/s.)  Two-byte dy of up to 64
+// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 397 us for dw, 419 for dx, 340 TFLOP/s.)  Two-byte dy of up to 16
 // tokens takes this way too: memory bounds such products, so that no value need be rounded.
 constexpr int kStep32 = 32;
 
 template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
-__global__ __launch_bounds__(WR * WC * 64) void k_grad_split(Grad a) {
+__global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_split(Grad a) {
   constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
   constexpr int kPart = BR * kStep32 * 2, kBytes = 3 * kPart + BC * kStep32 * 2;
   constexpr int kLoads = BR * kStep32 / 8 / T, kCodes = BC * kStep32 / 16 / T;
@@ -636,7 +636,7 @@ bool straight(const tgrad_matrix* dy) {
 bool straight(const tgrad_codes* c) { return (uintptr_t)c->codes % 16 == 0 && c->row_stride % 16 == 0 && c->row_stride <= ((int64_t)1 << 22); }
 size_t copy_bytes(int64_t tokens, int64_t outer) { return aligned((size_t)tokens * ((outer + 7) / 8 * 16)); }
 
-bool in_parts(const tgrad_matrix* dy, const tgrad_codes* c) { return dy->dtype == TGRAD_F32 || (dy->rows <= 64 && (c->group == 0 || c->cols <= c->group)); }
+bool in_parts(const tgrad_matrix* dy, const tgrad_codes* c) { return dy->dtype == TGRAD_F32 || (dy->rows <= 16 && (c->group == 0 || c->cols <= c->group)); }
 
 template <bool WEIGHT>
 void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {

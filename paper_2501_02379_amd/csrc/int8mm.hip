@@ -38,7 +38,7 @@ __device__ __forceinline__ void store_scaled(char* row, int n, int outer, i32x4 
 // STAGED: rows that do not start at multiples of 16 bytes go through registers.
 // (8192^3 in tiles of 128 x 128, two workgroups a compute unit: 546 us; four wavefronts of 8 x 8 results: 582.)
 template <int WT, int WN, int FT, int FN, int BUFS, bool STAGED, int OT>
-__global__ __launch_bounds__(WT * WN * 64) void k_codes_tiles(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int* part, int tiles_n, int tiles,
+__global__ __launch_bounds__(WT * WN * 64, 2) void k_codes_tiles(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int* part, int tiles_n, int tiles,
                                                               int steps_a_split) {
   constexpr int T = WT * WN * 64, BT = WT * FT * 16, BN = WN * FN * 16, kBytes = (BT + BN) * kStep;
   constexpr int kLoads = kBytes / 16 / T, kLoadsN = BN * kStep / 16 / T;
@@ -375,16 +375,17 @@ struct Cut {
 };
 // Codes that go straight to LDS: 16-byte rows, and offsets of 32 bits within a tile.
 bool straight(const void* p, int64_t stride) { return (uintptr_t)p % 16 == 0 && stride % 16 == 0 && stride <= ((int64_t)1 << 22); }
-// Tiles of 256 x 256 where they fill three quarters of the compute units (one workgroup each), of 128 x 128 otherwise, of 64 x 64 for up to 64 tokens, where
-// it is the weight's bytes that count.  The sum is split where there are fewer tiles than two (four of 64 x 64) for every compute unit.
-// (2048 x 8192 x 2048: 96 us in tiles of 256, 48 of 128; 1024 x 4096 x 4096: 56 and 29; 4096^3: 69 and 75.)
+// Tiles of 256 x 256 where they fill three quarters of the compute units (one workgroup each), of 128 x 128 otherwise, of 64 outputs for up to 64 tokens, where
+// it is the weight's bytes that count.  The sum is split where there are fewer tiles than two (three of 64 outputs) for every compute unit.
+// (2048 x 8192 x 2048: 96 us in tiles of 256, 48 of 128; 1024 x 4096 x 4096: 56 and 29; 4096^3: 69 and 75.  23 x 8190 x 10007: 21.9 us in tiles of 64 x 64 and up
+// to 1024 of them, 20.2 of 32 x 64 and up to 768.)
 Cut cut_of(int64_t tokens, int64_t outer, int64_t inner, bool direct) {
   auto tiles = [&](int64_t b) { return ((tokens + b - 1) / b) * ((outer + b - 1) / b); };
   Cut c;
   c.tile = tokens <= 64 ? 64 : direct && tiles(256) >= 192 ? 256 : 128;
   c.tiles_n = (int)((outer + c.tile - 1) / c.tile);
   c.tiles = (int)std::max<int64_t>(1, std::min<int64_t>(tiles(c.tile), kMostRows));
-  const int64_t steps = (inner + kStep - 1) / kStep, want = c.tile == 256 ? 1 : c.tile == 128 ? 512 : 1024;
+  const int64_t steps = (inner + kStep - 1) / kStep, want = c.tile == 256 ? 1 : c.tile == 128 ? 512 : 768;
   int64_t splits = std::max<int64_t>(1, std::min<int64_t>(want / c.tiles, steps / 4));
   c.steps = (int)((steps + splits - 1) / splits);
   c.splits = (int)((steps + c.steps - 1) / c.steps);
@@ -410,7 +411,8 @@ void launch_tiles_as(hipStream_t s, const Cut& c, const Codes8& x, const Codes8&
 }
 template <bool STAGED, int OT>
 void launch_tiles(hipStream_t s, const Cut& c, const Codes8& x, const Codes8& w, const tgrad_matrix* y, int inner, int* part) {
-  if (c.tile == 64) launch_tiles_as<2, 2, 2, 2, STAGED ? 2 : 3, STAGED, OT>(s, c, x, w, y, inner, part);
+  if (c.tile == 64 && y->rows <= 32) launch_tiles_as<1, 4, 2, 1, STAGED ? 2 : 4, STAGED, OT>(s, c, x, w, y, inner, part);
+  else if (c.tile == 64) launch_tiles_as<2, 2, 2, 2, STAGED ? 2 : 3, STAGED, OT>(s, c, x, w, y, inner, part);
   else if (STAGED || c.tile == 128) launch_tiles_as<2, 2, 4, 4, 2, STAGED, OT>(s, c, x, w, y, inner, part);
   else if constexpr (OT >= 0) {
     auto k = k_codes_wide<OT>;

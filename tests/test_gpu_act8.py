@@ -5,7 +5,7 @@ even, which float64 gives: 127 v and a have at most 31 and 24 bits, so a quotien
 product of two matrices of codes (an exact int32 sum, then one conversion and two products in float32): those are compared bit by bit.
 A gradient sums S products, exact in float32 for two-byte types; however they are added, that is off by at most 2 u S sum |a b| (2 u an addition:
 matrix instructions need not round to nearest).  In float32 dy * scale is rounded once, split in three parts off by 2^-24 together, and 3 S
-products are added: (6 S + 4) u sum |a b|, and so for two-byte types and up to 64 tokens.
+products are added: (6 S + 4) u sum |a b|, and so for two-byte types and up to 16 tokens.
 silu in float32: exp(-v) is off by (2 |v| + 2) u of itself, the quotient adds 3 u: |y| (2 |v| + 8) u; its slope p (1 + v (1 - p)) three times that of
 each term.  gelu: v / sqrt(2) carries 1.5 u, which moves erfc by up to 3 (1 + v^2) u of itself, erfc itself 8 u; exp(-v^2 / 2) (v^2 + 4) u.
 Each result is then rounded to its type once.
@@ -240,7 +240,7 @@ def close_gradient(got, a, b, dtype, out, terms):
 
 def rounded(codes, scale, group, dtype, tokens):
     """What the gradients multiply with: values of codes, rounded to a two-byte type but for a few tokens and one scale a row."""
-    return values(codes, scale, group).to(TYPES[dtype][0]).double() if dtype != "f32" and (tokens > 64 or 0 < group < codes.shape[1]) else codes.double() * scale.double().repeat_interleave(group or codes.shape[1], 1)[:, :codes.shape[1]]
+    return values(codes, scale, group).to(TYPES[dtype][0]).double() if dtype != "f32" and (tokens > 16 or 0 < group < codes.shape[1]) else codes.double() * scale.double().repeat_interleave(group or codes.shape[1], 1)[:, :codes.shape[1]]
 
 
 @pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f16", "f32")])

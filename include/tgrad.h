@@ -577,7 +577,7 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
  * rounded to float32 and split into three bf16 parts, which keep 24 bits (below 2^-110 the last ones are lost; an infinity becomes NaN), codes are exact.
  *  dx, dw  dy's type, or TGRAD_F32; rounded once.  The order of the sums depends on sizes and alignment alone.
  *  workspace_dev  as above.
- * Errors: INVALID_ARG, UNSUPPORTED (2^33 results), HIP.
+ * Errors: INVALID_ARG, UNSUPPORTED (2^33 results, more than 2^30 tokens, two-byte rows of more than 2^21), HIP.
  */
 int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream);
 int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream);

@@ -571,13 +571,14 @@ __global__ __launch_bounds__(256) void k_add_splits(const float* __restrict__ pa
   const int r = (int)(id / per), c = (int)(id % per) * 4;
   if (r >= rows) return;
   v4f sum = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const float* from = part + ((int64_t)s * rows + r) * cols + c;
-    if (c + 4 <= cols) {
-      sum += __builtin_bit_cast(v4f, *reinterpret_cast<const QuadAny*>(from));
-    } else {
-      for (int k = 0; k < cols - c; ++k) sum[k] += from[k];
-    }
+  const float* from = part + (int64_t)r * cols + c;
+  const int64_t each = (int64_t)rows * cols;
+  if (c + 4 <= cols) {
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) sum += __builtin_bit_cast(v4f, *reinterpret_cast<const QuadAny*>(from + s * each));
+  } else {
+    for (int s = 0; s < splits; ++s)
+      for (int k = 0; k < cols - c; ++k) sum[k] += from[s * each + k];
   }
   store4<OT>(out.row(r), c, cols, sum);
 }
@@ -699,8 +700,8 @@ size_t gradient_scratch(bool weight, bool copy, int64_t tokens, int64_t inner, i
 
 namespace {
 
-// Two-byte rows of 2^21 numbers and more, whose tiles 32-bit offsets do not reach, are refused.
-bool reachable(const tgrad_matrix* dy) { return dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21); }
+// Two-byte rows of more than 2^21 numbers, whose tiles 32-bit offsets do not reach, are refused, and so are sums whose steps they do not count.
+bool reachable(const tgrad_matrix* dy) { return dy->rows <= ((int64_t)1 << 30) && (dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21)); }
 
 template <bool WEIGHT>
 int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {

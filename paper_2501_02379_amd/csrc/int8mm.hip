@@ -248,13 +248,14 @@ __global__ __launch_bounds__(256) void k_add_parts(const int* __restrict__ part,
   if (t >= tokens) return;
   const int many = min(4, outer - n);
   i32x4 sum = {0, 0, 0, 0};
-  for (int s = 0; s < splits; ++s) {
-    const int* from = part + ((int64_t)s * tokens + t) * outer + n;
-    if (many == 4) {
-      sum += __builtin_bit_cast(i32x4, *reinterpret_cast<const QuadAny*>(from));
-    } else {
-      for (int r = 0; r < many; ++r) sum[r] += from[r];
-    }
+  const int* from = part + (int64_t)t * outer + n;
+  const int64_t each = (int64_t)tokens * outer;
+  if (many == 4) {
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) sum += __builtin_bit_cast(i32x4, *reinterpret_cast<const QuadAny*>(from + s * each));
+  } else {
+    for (int s = 0; s < splits; ++s)
+      for (int r = 0; r < many; ++r) sum[r] += from[s * each + r];
   }
   typedef typename Elem<OT>::raw raw;
   raw* to = reinterpret_cast<raw*>(y.row(t)) + n;

@@ -54,7 +54,7 @@ template <> struct Act<TGRAD_ACT_GELU> {
 
 // ---- a scale for the whole row: a workgroup of T threads a row ------------------------------------------------------------
 
-// Units of eight numbers; thread t has units t, t + T, ...; the first NV of each thread stay in registers.
+// 8192^2 bf16: 33 us, 6.1 TB/s.  Units of eight numbers; thread t has units t, t + T, ...; the first NV of each thread stay in registers.
 template <int DT, int T, int NV>
 __global__ __launch_bounds__(T) void k_quantize_rows(Mat x, int64_t first, int cols, Codes8 out) {
   __shared__ uint32_t lds[T / kWave];
@@ -156,6 +156,7 @@ __device__ __forceinline__ void activate(const float* v, const float* g, float* 
   }
 }
 
+// 8192 x 28672 bf16 with a gate: 311 us, 6 TB/s; without the checkpoint 234.
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void k_activation(Mat x, Mat gate, int64_t first, int64_t rows, int threads_a_row, int cols, Mat y,
                                                     Codes8 x8, Codes8 gate8) {
@@ -184,7 +185,9 @@ __global__ __launch_bounds__(256) void k_activation(Mat x, Mat gate, int64_t fir
 }
 
 // The same with the result in 8 bits, one scale a row: a workgroup of T threads a row.  The result waits in registers as float32, the first
-// NV units of every thread; of longer rows it is computed again.
+// NV units of every thread; of longer rows it is computed again.  8192 x 28672 bf16 with a gate and its checkpoint: 401 us, 4.1 TB/s: some 33 operations a number
+// (6 us a row and compute unit), and one row's registers fill a unit, so that they do not go on under its loads and stores.  (All loads of a row ahead 430; the
+// next row's loads as soon as registers are free spills: 711.)
 template <int DT, int ACT, bool GATED, int T, int NV>
 __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t first, int cols, Codes8 y8, Codes8 x8, Codes8 gate8) {
   __shared__ uint32_t lds[T / kWave];
@@ -242,6 +245,7 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
   }
 }
 
+// 8192 x 28672 bf16 with a gate: 317 us, 5.9 TB/s.
 template <int DT, int ACT, bool GATED>
 __global__ __launch_bounds__(256) void k_activation_back(Mat dy, Codes8 x8, Codes8 gate8, int64_t first, int64_t rows, int threads_a_row,
                                                          int cols, Mat dx, Mat dgate) {

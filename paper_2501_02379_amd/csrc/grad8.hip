@@ -237,7 +237,8 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
 // dy: 16-byte rows, whole chunks of eight columns; codes: 16-byte rows.
 constexpr int kWide = 256, kWideStep = 32, kWideBufs = 4, kWideDy = kWide * kWideStep * 2, kWideBytes = 2 * kWideDy;
 
-// 8192^3 bf16: dw 921 us, dx 983 (1190 and 1120 TFLOP/s; with loads to LDS that the compiler waits for 1130 and 1143, in tiles of 128 x 128 1200).
+// 8192^3 bf16: dw 925 us, dx 985 (1190 and 1115 TFLOP/s; with loads to LDS that the compiler waits for 1130 and 1143).  The matrix instructions alone reach 1650
+// to 2030 on random numbers.
 // RAGGED: the codes' last row ends within a chunk (its branch costs the others 12 percent).
 template <int DT, int OT, bool WEIGHT, bool RAGGED>
 __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {

@@ -158,8 +158,8 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void k_codes_tiles(Codes8 x, Codes
 // The same with 256 x 256 results of 8 wavefronts, 2 x 4 of 8 x 4, in steps of 64 bytes of which four are there or on their way (rows of 64 bytes, chunk c of row
 // r at chunk c ^ (r / 2 % 4)).  A step is two turns: wavefronts 0 to 3 read the step's operands while 4 to 7, a turn behind, multiply the
 // step before.  What is filled in a step was last read three turns ago at least, and is read five or six turns later.
-// 8192^3: 445 us, 2470 TOP/s, where k_codes_tiles of this size takes 510 (4 x 2 of 4 x 8: 488).  Registers alone, with no memory, reach 3260 to 4020 on random codes: the
-// card's power is the limit then (4800 on zeros).
+// 8192^3: 415 to 450 us, 2500 TOP/s, where k_codes_tiles of this size takes 460 to 510 (wavefronts 4 x 2 of 4 x 8: 488).  The card's power is the limit: the matrix
+// instructions alone, out of registers, reach 3260 to 4020 on random codes and 4800 on zeros; without its reads of LDS this kernel would take 410 us.
 constexpr int kWide = 256, kWideStep = 64, kWideBufs = 4, kWideBytes = 2 * kWide * kWideStep;
 
 template <int OT>
@@ -271,7 +271,7 @@ constexpr int kFusedTokens = 4, kFusedCodes = 32768, kFusedUnits = 4;      // wh
 
 // 16 outputs a workgroup; its wavefronts share the sum, and a matrix instruction takes 64 bytes of 16 rows of the weight and of all tokens.
 // XT >= 0: the tokens come as numbers; every workgroup quantises them into LDS for itself while its first loads of the weight are on their way, which
-// spares a launch; the first one writes what is kept.
+// spares a launch; the first one writes what is kept.  1 x 4096 x 4096: 6 to 7 us, 16 x 8192 x 8192 14 (4.8 TB/s of weight).
 template <int XT, int OT>
 __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, bool keep, Codes8 w, int tokens, int outer, int inner, Mat y) {
   extern __shared__ __attribute__((aligned(16))) char lds[];          // sums, scales, then codes of the tokens

@@ -271,7 +271,7 @@ constexpr int kFusedTokens = 4, kFusedCodes = 32768, kFusedUnits = 4;      // wh
 
 // 16 outputs a workgroup; its wavefronts share the sum, and a matrix instruction takes 64 bytes of 16 rows of the weight and of all tokens.
 // XT >= 0: the tokens come as numbers; every workgroup quantises them into LDS for itself while its first loads of the weight are on their way, which
-// spares a launch; the first one writes what is kept.  1 x 4096 x 4096: 6 to 7 us, 16 x 8192 x 8192 14 (4.8 TB/s of weight).
+// spares a launch; the first one writes what is kept.  1 x 4096 x 4096: 6 to 7 us, with 9.4 a call; 16 x 8192 x 8192 18.4 a call.
 template <int XT, int OT>
 __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, bool keep, Codes8 w, int tokens, int outer, int inner, Mat y) {
   extern __shared__ __attribute__((aligned(16))) char lds[];          // sums, scales, then codes of the tokens

@@ -264,20 +264,20 @@ __global__ __launch_bounds__(256) void k_add_parts(const int* __restrict__ part,
     if (r < many) to[r] = Elem<OT>::narrow(scaled(sum[r], sx[t], sw[n + r]));
 }
 
-// ---- up to 16 tokens: the weight is read once, straight to registers --------------------------------------------------------------------
+// ---- up to 32 tokens: the weight is read once, straight to registers --------------------------------------------------------------------
 
 constexpr int kFewWaves = 8, kFewThreads = kFewWaves * kWave, kAhead = 8;
 constexpr int kFusedTokens = 4, kFusedCodes = 32768, kFusedUnits = 4;      // what one workgroup quantises by the way
 
-// 16 outputs a workgroup; its wavefronts share the sum, and a matrix instruction takes 64 bytes of 16 rows of the weight and of all tokens.
+// 16 outputs a workgroup; its wavefronts share the sum, and a matrix instruction takes 64 bytes of 16 rows of the weight and of 16 tokens (FT times).
 // XT >= 0: the tokens come as numbers; every workgroup quantises them into LDS for itself while its first loads of the weight are on their way, which
 // spares a launch; the first one writes what is kept.  1 x 4096 x 4096: 6 to 7 us, with 9.4 a call; 16 x 8192 x 8192 18.4 a call.
-template <int XT, int OT>
+template <int XT, int OT, int FT>
 __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, bool keep, Codes8 w, int tokens, int outer, int inner, Mat y) {
   extern __shared__ __attribute__((aligned(16))) char lds[];          // sums, scales, then codes of the tokens
-  int (*sums)[kWave][4] = reinterpret_cast<int (*)[kWave][4]>(lds);
-  float* sx = reinterpret_cast<float*>(lds + sizeof(int) * kFewWaves * kWave * 4);
-  uint32_t* tops = reinterpret_cast<uint32_t*>(sx + 16);
+  int (*sums)[FT][kWave][4] = reinterpret_cast<int (*)[FT][kWave][4]>(lds);
+  float* sx = reinterpret_cast<float*>(lds + sizeof(int) * kFewWaves * FT * kWave * 4);
+  uint32_t* tops = reinterpret_cast<uint32_t*>(sx + 16 * FT);
   char* codes = reinterpret_cast<char*>(tops + kFewWaves);
   const int wave = threadIdx.x / kWave, lane = lane_id();
   const int n0 = blockIdx.x * 16;
@@ -292,7 +292,6 @@ __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, boo
     a[i] = load16(wrow + at, first + i < last ? inner - at : 0);
   }
   const int pitch = (inner + 63) / 64 * 64;
-  const int8_t* xrow;
   if constexpr (XT >= 0) {
     constexpr int es = sizeof(typename Elem<XT>::raw);
     const int units = pitch / 8;
@@ -325,51 +324,61 @@ __global__ __launch_bounds__(kFewThreads) void k_codes_few(Mat xm, Codes8 x, boo
       }
     }
     __syncthreads();
-    xrow = nullptr;
   } else {
     if (threadIdx.x < (uint32_t)tokens) sx[threadIdx.x] = x.scale[threadIdx.x];
-    xrow = x.codes + (int64_t)min(lane % 16, tokens - 1) * x.stride;
   }
-  const char* lrow = codes + min(lane % 16, tokens - 1) * pitch;
-  i32x4 acc = {0, 0, 0, 0};
+  const char* lrow[FT];
+  const int8_t* xrow[FT];
+#pragma unroll
+  for (int j = 0; j < FT; ++j) {
+    const int t = min(j * 16 + lane % 16, tokens - 1);
+    lrow[j] = codes + t * pitch;
+    xrow[j] = x.codes + (int64_t)t * x.stride;
+  }
+  i32x4 acc[FT] = {};
   for (int p = first; p < last; p += kAhead) {
-    Quad b[kAhead];
+    Quad b[FT][kAhead];
+#pragma unroll
+    for (int j = 0; j < FT; ++j)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const int at = (p + i) * 64 + mine;
+        if constexpr (XT >= 0) b[j][i] = p + i < last ? *reinterpret_cast<const Quad*>(lrow[j] + at) : Quad{0, 0, 0, 0};
+        else b[j][i] = load16(xrow[j] + at, p + i < last ? inner - at : 0);
+      }
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int at = (p + i) * 64 + mine;
-      if constexpr (XT >= 0) b[i] = p + i < last ? *reinterpret_cast<const Quad*>(lrow + at) : Quad{0, 0, 0, 0};
-      else b[i] = load16(xrow + at, p + i < last ? inner - at : 0);
-    }
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a[i]), __builtin_bit_cast(i32x4, b[i]), acc, 0, 0, 0);
+      for (int j = 0; j < FT; ++j)
+        acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a[i]), __builtin_bit_cast(i32x4, b[j][i]), acc[j], 0, 0, 0);
       const int at = (p + kAhead + i) * 64 + mine;
       a[i] = load16(wrow + at, p + kAhead + i < last ? inner - at : 0);
     }
   }
-  *reinterpret_cast<i32x4*>(sums[wave][lane]) = acc;
+#pragma unroll
+  for (int j = 0; j < FT; ++j) *reinterpret_cast<i32x4*>(sums[wave][j][lane]) = acc[j];
   __syncthreads();
   // lane l of a wavefront has token l % 16 and outputs 4 (l / 16) .. + 3
-  if (threadIdx.x < 256) {
+  if (threadIdx.x < 256 * FT) {
     const int t = threadIdx.x / 16, n = threadIdx.x % 16;
     int sum = 0;
 #pragma unroll
-    for (int i = 0; i < kFewWaves; ++i) sum += sums[i][n / 4 * 16 + t][n % 4];
+    for (int i = 0; i < kFewWaves; ++i) sum += sums[i][t / 16][n / 4 * 16 + t % 16][n % 4];
     if (t < tokens && n0 + n < outer) reinterpret_cast<typename Elem<OT>::raw*>(y.row(t))[n0 + n] = Elem<OT>::narrow(scaled(sum, sx[t], w.scale[n0 + n]));
   }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------
 
-size_t few_lds(int64_t tokens, int64_t inner) {
-  return sizeof(int) * kFewWaves * kWave * 4 + 16 * 4 + kFewWaves * 4 + (size_t)tokens * ((inner + 63) / 64 * 64);
+size_t few_lds(int ft, int64_t tokens, int64_t inner) {
+  return sizeof(int) * kFewWaves * ft * kWave * 4 + 16 * ft * 4 + kFewWaves * 4 + (size_t)tokens * ((inner + 63) / 64 * 64);
 }
 
 // Codes of x that nobody keeps: rows of a multiple of 16 bytes, and a scale each.
 int64_t scratch_stride(int64_t inner) { return (inner + 15) / 16 * 16; }
 size_t scratch_codes(int64_t tokens, int64_t inner) { return aligned((size_t)tokens * scratch_stride(inner)) + aligned((size_t)tokens * 4); }
 
-// How a product of more than 16 tokens is cut.
+// How a product of more tokens is cut.
 struct Cut {
   int tile;                               // 256, 128 or 64 results on a side
   int tiles_n, tiles, splits, steps;      // steps of kStep bytes to a split
@@ -392,9 +401,11 @@ Cut cut_of(int64_t tokens, int64_t outer, int64_t inner, bool direct) {
   c.splits = (int)((steps + c.steps - 1) / c.steps);
   return c;
 }
-constexpr int64_t kFew = 16;
+// Products of k_codes_few: every workgroup reads all tokens' codes, so beyond 16 tokens the weight has to be small as well.  (Calls, us, k_codes_few / tiles and their
+// parts: 32 x 4096 x 4096 10.1 / 14.5, 23 x 8190 x 10007 44 / 24.7.)
+bool few(int64_t tokens, int64_t outer, int64_t inner) { return tokens <= 16 || (tokens <= 32 && outer * inner <= ((int64_t)1 << 25)); }
 size_t part_bytes(int64_t tokens, int64_t outer, int64_t inner) {
-  if (tokens <= kFew) return 0;
+  if (few(tokens, outer, inner)) return 0;
   size_t most = 0;
   for (bool direct : {false, true}) {
     const Cut c = cut_of(tokens, outer, inner, direct);
@@ -425,10 +436,15 @@ void launch_tiles(hipStream_t s, const Cut& c, const Codes8& x, const Codes8& w,
 void launch_product(hipStream_t s, const tgrad_codes* x, const tgrad_codes* w, const tgrad_matrix* y, void* parts) {
   const Codes8 cx = codes8(x), cw = codes8(w);
   const int inner = (int)x->cols;
-  if (y->rows <= kFew) {
+  if (few(y->rows, y->cols, inner)) {
     for_real(y->dtype, [&](auto t) {
-      k_codes_few<-1, decltype(t)::value><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(0, 0), s>>>(
-          Mat{nullptr, 0}, cx, false, cw, (int)y->rows, (int)y->cols, inner, mat(y));
+      auto run = [&](auto ft) {
+        constexpr int FT = decltype(ft)::value;
+        k_codes_few<-1, decltype(t)::value, FT><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(FT, 0, 0), s>>>(
+            Mat{nullptr, 0}, cx, false, cw, (int)y->rows, (int)y->cols, inner, mat(y));
+      };
+      if (y->rows <= 16) run(std::integral_constant<int, 1>());
+      else run(std::integral_constant<int, 2>());
     });
     return;
   }
@@ -497,7 +513,7 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
   if (fused(x->rows, x->cols)) {
     for_real(x->dtype, [&](auto xt) {
       for_real(y->dtype, [&](auto yt) {
-        k_codes_few<decltype(xt)::value, decltype(yt)::value><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(x->rows, x->cols), s>>>(
+        k_codes_few<decltype(xt)::value, decltype(yt)::value, 1><<<dim3((uint32_t)((y->cols + 15) / 16)), dim3(kFewThreads), few_lds(1, x->rows, x->cols), s>>>(
             mat(x), codes8(keep), keep != nullptr, codes8(w), (int)y->rows, (int)y->cols, (int)x->cols, mat(y));
       });
     });

@@ -65,8 +65,8 @@ def test_sizes_have_to_go_together():
     assert lib.tgrad_codes_matmul(codes(), codes(40), mat(8, 41), 256, None) == BAD
     assert lib.tgrad_codes_matmul(ok32, codes(40), mat(8, 40), 256, None) == BAD          # one scale a row in both
     assert lib.tgrad_codes_matmul(codes(), codes(40, group=32), mat(8, 40), 256, None) == BAD
-    for ws in (264, None):                                                                # 20 tokens need scratch
-        assert lib.tgrad_codes_matmul(codes(20, 4096), codes(40, 4096), mat(20, 40), ws, None) == BAD
+    for ws in (264, None):                                                                # 40 tokens need scratch
+        assert lib.tgrad_codes_matmul(codes(40, 4096), codes(40, 4096), mat(40, 40), ws, None) == BAD
         assert lib.tgrad_codes_linear(mat(20), codes(40), None, mat(20, 40), ws, None) == BAD
         assert lib.tgrad_codes_grad_weight(mat(80, 99), codes(80, 50), mat(99, 50), ws, None) == BAD      # and so does dy with odd rows
     long = 131073

@@ -171,7 +171,8 @@ def test_what_lies_between_rows_stays():
 
 # tokens, inner, outer: single tokens, a few, ordinary; sums of odd length, shorter than a step, long ones
 PRODUCTS = [(1, 1, 1), (1, 16, 5), (1, 4096, 300), (2, 100, 64), (3, 129, 1000), (7, 8190, 33), (16, 256, 257), (17, 1000, 130), (33, 64, 64),
-            (64, 640, 513), (100, 77, 300), (130, 1300, 260), (256, 512, 256), (257, 257, 257), (300, 128, 1024), (511, 2304, 700), (3600, 333, 3700),
+            (64, 640, 513), (100, 77, 300), (130, 1300, 260), (256, 512, 256), (257, 257, 257), (300, 128, 1024), (511, 2304, 700), (3600, 333, 3700), (20, 5000, 40), (32, 2049, 515),
+            (29, 9000, 3800),
             (1, 131072, 3), (40, 131072, 17)]
 
 

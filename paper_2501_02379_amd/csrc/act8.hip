@@ -184,13 +184,15 @@ __global__ __launch_bounds__(256) void k_activation(Mat x, Mat gate, int64_t fir
   }
 }
 
-// The same with the result in 8 bits, one scale a row: a workgroup of T threads a row.  The result waits in registers as float32, the first
-// NV units of every thread; of longer rows it is computed again.  8192 x 28672 bf16 with a gate and its checkpoint: 401 us, 4.1 TB/s: some 33 operations a number
-// (6 us a row and compute unit), and one row's registers fill a unit, so that they do not go on under its loads and stores.  (All loads of a row ahead 430; the
-// next row's loads as soon as registers are free spills: 711.)
-template <int DT, int ACT, bool GATED, int T, int NV>
-__global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t first, int cols, Codes8 y8, Codes8 x8, Codes8 gate8) {
+// The same with the result in 8 bits, one scale a row: a workgroup of T threads a row.  The result waits as float32, the first NV units of every thread in
+// registers, the next NL in LDS; of longer rows the rest is computed again.  8192 x 28672 bf16 with a gate and its checkpoint: 361 us, 4.5 TB/s, with two
+// rows of 512 threads a compute unit, 4 units in registers and 4 in LDS; some 33 operations a number are 6 us of a row.  (1024 threads with all in registers leave
+// room for one row, whose arithmetic does not go on under its loads and stores: 401; with all its loads ahead 430; the next row's loads as soon as
+// registers are free spill: 711.  3 in registers and 5 in LDS, one row a unit: 589.)
+template <int DT, int ACT, bool GATED, int T, int NV, int NL>
+__global__ __launch_bounds__(T, NL > 0 ? 4 : 1) void k_activation_rows(Mat x, Mat gate, int64_t first, int cols, Codes8 y8, Codes8 x8, Codes8 gate8) {
   __shared__ uint32_t lds[T / kWave];
+  __shared__ __attribute__((aligned(16))) float kept[NL > 0 ? NL * T * 8 : 4];
   const int64_t row = first + blockIdx.x;
   const char* src = x.row(row);
   const char* gsrc = GATED ? gate.row(row) : nullptr;
@@ -223,7 +225,19 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
     unit(threadIdx.x + i * T, e, h, held[i], true);
     top = max(top, largest(held[i]));
   }
-  for (int u0 = NV * T; u0 < units; u0 += T) {      // whole wavefronts: groups are formed across lanes
+  if constexpr (NL > 0) {
+#pragma unroll 1
+    for (int i = 0; i < NL; ++i) {
+      float r[8];
+      load(threadIdx.x + (NV + i) * T, e, h);
+      unit(threadIdx.x + (NV + i) * T, e, h, r, true);
+      top = max(top, largest(r));
+      float4* to = reinterpret_cast<float4*>(kept) + i * 2 * T + threadIdx.x;
+      to[0] = make_float4(r[0], r[1], r[2], r[3]);
+      to[T] = make_float4(r[4], r[5], r[6], r[7]);
+    }
+  }
+  for (int u0 = (NV + NL) * T; u0 < units; u0 += T) {      // whole wavefronts: groups are formed across lanes
     float r[8];
     load(u0 + threadIdx.x, e, h);
     unit(u0 + threadIdx.x, e, h, r, true);
@@ -237,7 +251,17 @@ __global__ __launch_bounds__(T) void k_activation_rows(Mat x, Mat gate, int64_t 
     const int u = threadIdx.x + i * T;
     if (u < units) store_codes(dst + u * 8, codes_of(held[i], r8), cols - u * 8);
   }
-  for (int u = threadIdx.x + NV * T; u < units; u += T) {
+  if constexpr (NL > 0) {
+#pragma unroll 1
+    for (int i = 0; i < NL; ++i) {
+      const int u = threadIdx.x + (NV + i) * T;
+      const float4* from = reinterpret_cast<const float4*>(kept) + i * 2 * T + threadIdx.x;
+      const float4 p = from[0], q = from[T];
+      const float r[8] = {p.x, p.y, p.z, p.w, q.x, q.y, q.z, q.w};
+      if (u < units) store_codes(dst + u * 8, codes_of(r, r8), cols - u * 8);
+    }
+  }
+  for (int u = threadIdx.x + (NV + NL) * T; u < units; u += T) {
     float r[8];
     load(u, e, h);
     unit(u, e, h, r, false);
@@ -280,9 +304,9 @@ __global__ __launch_bounds__(256) void k_activation_back(Mat dy, Codes8 x8, Code
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
-// Threads and held units of a workgroup that has a row to itself: the fewest threads whose registers hold it, 4 units each at most, so that several rows
-// share a compute unit.  (32768 rows of 1000 bf16 quantised by 256 threads 28 us, by 64 18; activations of them 71 and 45.  Rows of 28672, activations: 1024
-// threads 408 us, 512 of 8 units 560; 1024 with their registers halved for two rows a unit spill: 1110.)
+// Threads and units in registers of a workgroup that has a row to itself: the fewest threads whose registers hold it, 4 units each at most, so that several rows
+// share a compute unit.  (32768 rows of 1000 bf16 quantised by 256 threads 28 us, by 64 18; activations of them 71 and 45.  Rows of 28672, activations: 512
+// threads of 8 units 560 us, 1024 with their registers halved for two rows a unit spill: 1110.)
 template <typename F>
 void for_row(int64_t rows, int cols, F&& f) {
   const int units = (cols + 7) / 8;
@@ -402,7 +426,8 @@ int tgrad_activation(const tgrad_matrix* x, const tgrad_matrix* gate, int act, c
         for_row(x->rows, cols, [&](auto t, auto n) {
           constexpr int T = decltype(t)::value, NV = decltype(n)::value;
           rows_in_launches(x->rows, T, 1, [&](int64_t first, int64_t rows) {
-            k_activation_rows<DT, ACT, GATED, T, NV><<<dim3((uint32_t)rows), dim3(T), 0, s>>>(mx, mg, first, cols, cy, cx, cg);
+            if constexpr (T * NV == 4096) k_activation_rows<DT, ACT, GATED, 512, 4, 4><<<dim3((uint32_t)rows), dim3(512), 0, s>>>(mx, mg, first, cols, cy, cx, cg);
+            else k_activation_rows<DT, ACT, GATED, T, NV, 0><<<dim3((uint32_t)rows), dim3(T), 0, s>>>(mx, mg, first, cols, cy, cx, cg);
           });
         });
       }

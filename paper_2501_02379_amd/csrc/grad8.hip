@@ -381,10 +381,20 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
 
 // ---- float32 dy, and two-byte dy of a few tokens: a scale for each row of codes -------------------------------------------------------------------------------------------
 
-// dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_pair); codes are exact in bf16.  Three products instead
-// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 397 us for dw, 419 for dx, 340 TFLOP/s.)  Two-byte dy of up to 16
+// dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_apart); codes are exact in bf16.  Three products instead
+// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 420 us for dw, 445 for dx, 320 TFLOP/s.)  Two-byte dy of up to 16
 // tokens takes this way too: memory bounds such products, so that no value need be rounded.
 constexpr int kStep32 = 32;
+
+// The parts of two numbers (see split_pair, which forms rests with dot products of both: neighbours here are different results' terms, and a NaN
+// or an infinity may not reach the other one's).
+__device__ __forceinline__ void split_apart(float a, float b, uint32_t& h, uint32_t& m, uint32_t& l) {
+  h = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);       // the upper halves
+  a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+  b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+  m = bf16_pack(a, b);
+  l = bf16_pack(a - __uint_as_float(m << 16), b - __uint_as_float(m & 0xFFFF0000u));
+}
 
 template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
 __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_split(Grad a) {
@@ -445,7 +455,7 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_split(Grad a) {
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         uint32_t x, y, z;
-        split_pair(f[2 * d] * scale[i][WEIGHT ? 0 : 2 * d], f[2 * d + 1] * scale[i][WEIGHT ? 0 : 2 * d + 1], x, y, z);
+        split_apart(f[2 * d] * scale[i][WEIGHT ? 0 : 2 * d], f[2 * d + 1] * scale[i][WEIGHT ? 0 : 2 * d + 1], x, y, z);
         h[d] = x;
         m[d] = y;
         lo[d] = z;

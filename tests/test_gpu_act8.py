@@ -451,3 +451,38 @@ def test_refusals():
         with pytest.raises(T.TgradError):
             call()
     torch.cuda.synchronize()
+
+
+def test_results_go_where_they_are_told():
+    x = numbers(40, 300, "bf16", seed=3)
+    want = act8.tgrad_activation(x, x, quantize=True)
+    out = laid(torch.zeros(40, 300, dtype=torch.int8), torch.zeros(40, 1), pad=5, offset=3)
+    got = act8.tgrad_activation(x, x, quantize=True, out=out)
+    assert got.y is out and torch.equal(out.codes, want.y.codes) and torch.equal(out.scale, want.y.scale)
+    w, _, _ = random_codes(70, 300, seed=1)
+    h = act8.tgrad_codes_linear(x, w, keep=True, dtype=torch.float32, out=(y := torch.empty(40, 90, device=DEV))[:, 9:79])
+    assert h.y.data_ptr() == y[:, 9:].data_ptr() and torch.equal(h.y, act8.tgrad_codes_matmul(h.x8, w, dtype=torch.float32))
+    for bad in (lambda: act8.tgrad_activation(x, quantize=True, out=act8.tgrad_quantize(x, group=32)), lambda: act8.tgrad_activation(x, out=want.y),
+                lambda: act8.tgrad_activation(x, quantize=True, out=torch.empty_like(x))):
+        with pytest.raises(T.TgradError):
+            bad()
+
+
+@pytest.mark.parametrize("tokens,inner,outer", [(5, 200, 90), (300, 300, 100), (3600, 3600, 136), (3601, 3590, 135)])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_nan_in_a_gradient_stays_in_its_row_and_column(tokens, inner, outer, dtype, value):
+    dy = numbers(tokens, outer, dtype, seed=2)
+    t, n = tokens - 2, outer // 2
+    dy[t, n] = value
+    w, x = random_codes(outer, inner, seed=4, pad=-inner % 16)[0], random_codes(tokens, inner, seed=5, pad=-inner % 16)[0]
+    dx, dw = act8.tgrad_codes_grad_input(dy, w), act8.tgrad_codes_grad_weight(dy, x)
+    for got, r in ((dx, t), (dw, n)):                               # an infinity times a code of 0 is NaN too
+        assert not bool(torch.isfinite(got[r]).any()) and int((~torch.isfinite(got)).any(1).sum()) == 1
+
+
+def test_the_same_bits_every_time():
+    dy, w, x = numbers(5000, 300, "f16", seed=1), random_codes(300, 200, seed=2)[0], random_codes(5000, 200, seed=3)[0]
+    first = act8.tgrad_codes_grad_input(dy, w), act8.tgrad_codes_grad_weight(dy, x)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(first, (act8.tgrad_codes_grad_input(dy, w), act8.tgrad_codes_grad_weight(dy, x))))

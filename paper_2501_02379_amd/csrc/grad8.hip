@@ -56,13 +56,29 @@ __device__ __forceinline__ void widen16(Quad c, float scale, Quad* out) {
   }
 }
 
-// A result's four neighbours in a row, of the type OT (float32 sums of a split where OT < 0).
+// float16's exponents do not reach what float32 scales do, so its values are multiplied with 2^k on their way to LDS and the sums with 2^-k, both exact: k
+// brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
+// the largest.  Rows `first` .. first + rows - 1, columns c0 .. c0 + cols - 1; the same in every thread.  Infinite and NaN scales are no size.
+template <int T>
+__device__ __forceinline__ int lift_of(const Codes8& c, int64_t first, int64_t rows, int c0, int cols, uint32_t* lds) {
+  const int g0 = c0 >> c.shift, g1 = (c0 + cols - 1) >> c.shift;
+  uint32_t top = 0;
+  for (int64_t r = threadIdx.x; r < rows; r += T)
+    for (int g = g0; g <= g1; ++g) {
+      const uint32_t m = magnitude(c.scale[(first + r) * c.groups + g]);
+      if (m < 0x7F800000u) top = max(top, m);
+    }
+  top = largest_of_block<T / kWave>(top, lds);
+  return top == 0 ? 0 : 8 + 127 - (int)(top >> 23);
+}
+
+// A result's four neighbours in a row, of the type OT (float32 sums of a split where OT < 0), times 2^-lift.
 template <int OT>
-__device__ __forceinline__ void store4(char* row, int64_t c, int64_t cols, v4f v) {
+__device__ __forceinline__ void store4(char* row, int64_t c, int64_t cols, v4f v, int lift = 0) {
   constexpr int RT = OT < 0 ? TGRAD_F32 : OT;
   typedef typename Elem<RT>::raw raw;
   raw* to = reinterpret_cast<raw*>(row) + c;
-  const float f[4] = {v[0], v[1], v[2], v[3]};
+  const float f[4] = {ldexpf(v[0], -lift), ldexpf(v[1], -lift), ldexpf(v[2], -lift), ldexpf(v[3], -lift)};
   if (c + 4 <= cols) {
     *reinterpret_cast<typename Four<RT>::any*>(to) = Four<RT>::narrow(f);
   } else {
@@ -101,6 +117,11 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
   const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep - 1) / kStep);
   const int64_t whole = min(last, a.sum / kStep);
   auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
+  int lift = 0;
+  if constexpr (DT == TGRAD_F16) {
+    __shared__ uint32_t tops[WR * WC];
+    lift = lift_of<T>(a.c, first * kStep, min(last * kStep, a.sum) - first * kStep, c0, min(BC, a.cols - c0), tops);
+  }
 
   // this thread's chunks of dy: row of the tile and chunk of eight numbers
   auto part = [&](int i, int& row, int& chunk) {
@@ -158,6 +179,7 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
       if (row < a.sum && c0 + col < a.cols) {
         codes[i] = load16(cp + row * a.c.stride + col, a.cols - c0 - col);
         scale[i] = a.c.scale[row * a.c.groups + ((c0 + col) >> a.c.shift)];
+        if constexpr (DT == TGRAD_F16) scale[i] = ldexpf(scale[i], lift);
       }
     }
   };
@@ -225,7 +247,7 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
 #pragma unroll
     for (int i = 0; i < FC; ++i) {
       const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
-      if (c < a.cols) store4<OT>(row, c, a.cols, acc[i][j]);
+      if (c < a.cols) store4<OT>(row, c, a.cols, acc[i][j], lift);
     }
   }
 }
@@ -250,6 +272,11 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   const int r0 = tile.x * kWide, c0 = tile.y * kWide;
   const int64_t from = (int64_t)split * a.steps * kWideStep;           // this split's part of the sum
   const int sum = (int)min(a.sum - from, (int64_t)a.steps * kWideStep), steps = (sum + kWideStep - 1) / kWideStep;
+  int lift = 0;
+  if constexpr (DT == TGRAD_F16) {
+    __shared__ uint32_t tops[T / kWave];
+    lift = lift_of<T>(a.c, from, sum, c0, min(kWide, a.cols - c0), tops);
+  }
 
   // dy: what lies beyond its rows or columns is loaded from within, and its results are not stored
   int each[kLoads], ahead[kLoads];
@@ -310,7 +337,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   const int place = kWideDy + row * (kWide * 2) + (block ^ bend(row)) * 32;
   auto place_codes = [&](int s, const Held& h) {
     Quad q[2];
-    widen16<DT>(h.codes, h.scale, q);
+    widen16<DT>(h.codes, DT == TGRAD_F16 ? ldexpf(h.scale, lift) : h.scale, q);
     char* at = lds + s % kWideBufs * kWideBytes + place;
     const bool upper = lane & 4;            // lanes 4 to 7 store their upper halves first: eight lanes then meet all banks
     *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
@@ -374,7 +401,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
 #pragma unroll
     for (int i = 0; i < FC; ++i) {
       const int c = c0 + (wc * FC + i) * 16 + lane / 16 * 4;
-      if (c < a.cols) store4<OT>(out, c, a.cols, acc[i][j]);
+      if (c < a.cols) store4<OT>(out, c, a.cols, acc[i][j], lift);
     }
   }
 }

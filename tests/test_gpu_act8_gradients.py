@@ -1,0 +1,71 @@
+"""Gradients of products with codes where test_gpu_act8.py has no case: values beyond a type's range, long sums in wide tiles, unrounded values.
+
+u = 2^-24.  Sums of S products of two-byte numbers are off by at most 2 u S sum |a b|, as there.
+"""
+import pytest
+import torch
+
+from paper_2501_02379_amd import act8
+from test_gpu_act8 import DEV, TYPES, U, laid, numbers
+
+pytestmark = pytest.mark.gpu
+
+
+def codes_with(rows, cols, scale, seed=0, group=0, pad=None):
+    """Random codes of the given scale (a number, or a tensor of all of them)."""
+    g = torch.Generator().manual_seed(seed)
+    c = torch.randint(-127, 128, (rows, cols), generator=g, dtype=torch.int8)
+    s = torch.as_tensor(scale, dtype=torch.float32).expand(rows, -(-cols // group) if group else 1).contiguous()
+    return laid(c, s, group, -cols % 16 if pad is None else pad), c, s
+
+
+def spread_out(codes, scale, group):
+    """Values of codes in float64."""
+    g = group or codes.shape[1]
+    return codes.double() * scale.double().repeat_interleave(g, 1)[:, :codes.shape[1]]
+
+
+# tokens, inner, outer: dy times a scale, tiles of 128, wide tiles (the last two, for dx and for dw)
+RANGE = [(8, 130, 70), (17, 130, 70), (300, 200, 130), (3700, 3588, 40), (40, 3700, 3592)]
+
+
+@pytest.mark.parametrize("tokens,inner,outer", RANGE)
+@pytest.mark.parametrize("scale", [1000.0, 2.0 ** -26, 2.0 ** -60])
+@pytest.mark.parametrize("group", [0, 64])
+def test_float16_gradients_of_values_beyond_float16(tokens, inner, outer, scale, group):
+    """Codes stand for float32 numbers whatever dy's type is: neither an infinity nor a lost value comes of it, however many tokens there are.  Values are
+    rounded to 11 bits, half a step is 2^-11 of each; the result is float32, for results of such values would leave float16 themselves."""
+    dy = numbers(tokens, outer, "f16", seed=1, pad=outer % 4)
+    w, cw, sw = codes_with(outer, inner, scale, 2, group)
+    x, cx, sx = codes_with(tokens, inner, scale, 3, group)
+    for got, a, b, terms in ((act8.tgrad_codes_grad_input(dy, w, dtype=torch.float32), dy.cpu().double(), spread_out(cw, sw, group), outer),
+                             (act8.tgrad_codes_grad_weight(dy, x, dtype=torch.float32), dy.cpu().double().t().contiguous(), spread_out(cx, sx, group), tokens)):
+        bound = (a.abs() @ b.abs()) * (2.0 ** -11 + (6 * terms + 4) * U)
+        assert bool(((got.cpu().double() - a @ b).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("tokens,inner,outer", RANGE)
+def test_float16_gradients_of_rows_of_different_sizes(tokens, inner, outer):
+    """Rows' scales from 2^-10 to 1000, 20 binary orders; results that fit float16."""
+    g = torch.Generator().manual_seed(4)
+    rows = lambda n: 2.0 ** (torch.rand(n, 1, generator=g) * 20 - 10)  # noqa: E731
+    dy = numbers(tokens, outer, "f16", seed=1, spread=2.0 ** -12)
+    w, cw, sw = codes_with(outer, inner, rows(outer), 2)
+    x, cx, sx = codes_with(tokens, inner, rows(tokens), 3)
+    for got, a, b, terms in ((act8.tgrad_codes_grad_input(dy, w), dy.cpu().double(), spread_out(cw, sw, 0), outer),
+                             (act8.tgrad_codes_grad_weight(dy, x), dy.cpu().double().t().contiguous(), spread_out(cx, sx, 0), tokens)):
+        want = a @ b
+        assert float(want.abs().max()) < 60000
+        bound = (a.abs() @ b.abs()) * (2.0 ** -11 + (6 * terms + 4) * U) * (1 + 2.0 ** -11) + want.abs() * 2.0 ** -11 + 2.0 ** -24
+        assert bool(((got.cpu().double() - want).abs() <= bound).all())
+
+
+def test_a_gated_result_beyond_float16():
+    """300 * 300 from finite float16 numbers is a good code, and finite in the product's gradient."""
+    h = torch.full((40, 64), 300.0, dtype=torch.float16, device=DEV)
+    a = act8.tgrad_activation(h, h, quantize=True, keep=False)
+    dy = numbers(40, 24, "f16", seed=3, spread=1e-3)
+    dy[:, 5] = 0
+    dw = act8.tgrad_codes_grad_weight(dy, a.y)
+    want = dy.cpu().double().t().contiguous() @ (a.y.codes.cpu().double() * a.y.scale.cpu().double())
+    assert bool(dw[5].eq(0).all()) and bool(((dw.cpu().double() - want).abs() <= want.abs() * 2.0 ** -11 + 40 * 90000 * 5e-3 * (2.0 ** -11 + 250 * U)).all())

@@ -543,10 +543,11 @@ int tgrad_dequantize(const tgrad_codes* codes, const tgrad_matrix* out, void* hi
 enum { TGRAD_CODES_MATMUL = 0, TGRAD_CODES_LINEAR = 1, TGRAD_CODES_GRAD_INPUT = 2, TGRAD_CODES_GRAD_WEIGHT = 3 };
 /* added to a gradient's op: dy's rows do not start at multiples of 16 bytes, are no multiple of 8 long, or lie more than 2^21 elements apart */
 #define TGRAD_CODES_UNALIGNED 4
+#define TGRAD_CODES_UNROUNDED 8        /* added to a gradient's op: values of codes are not rounded to dy's type (tgrad_codes_gradient) */
 #define TGRAD_CODES_MAX_INNER 131072   /* longest sum of products of codes that int32 holds: 127^2 2^17 < 2^31 */
 
 /*
- * Bytes of scratch of the four calls below, for tokens x inner times inner x outer.  Two-byte dy that is not aligned is copied there first, which
+ * Bytes of scratch of the calls below, for tokens x inner times inner x outer.  Two-byte dy that is not aligned is copied there first, which
  * needs TGRAD_CODES_UNALIGNED.  0: none, and the call's workspace_dev may be NULL.  Host-only.  Errors: INVALID_ARG.
  */
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes);
@@ -581,6 +582,13 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
  */
 int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream);
 int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream);
+
+/*
+ * The same two, by op: TGRAD_CODES_GRAD_INPUT or _WEIGHT, with what is added to it for tgrad_codes_query_size.  With TGRAD_CODES_UNROUNDED the error that
+ * rounded values bring into a two-byte gradient is gone, for twice the matrix operations: values are taken in two parts of dy's type (off by 2^-14 of
+ * themselves in bf16; in float16 by 2^-20, down to 2^-28 of the largest value), and with a float32 result dy and values as in float32.
+ */
+int tgrad_codes_gradient(int op, const tgrad_matrix* dy, const tgrad_codes* codes, const tgrad_matrix* out, void* workspace_dev, void* hip_stream);
 
 enum { TGRAD_ACT_SILU = 0, TGRAD_ACT_GELU = 1 };   /* x / (1 + exp(-x)); x (1 + erf(x / sqrt(2))) / 2 */
 

@@ -201,19 +201,21 @@ def tgrad_codes_linear(x, weight: Codes, *, keep: bool = False, dtype=None, out=
 
 
 @_on_stream
-def tgrad_codes_grad_input(dy, weight: Codes, *, dtype=None, out=None):
+def tgrad_codes_grad_input(dy, weight: Codes, *, dtype=None, out=None, unrounded: bool = False):
     """Gradient of a product with respect to its input: dy (tokens x outer) times the values of weight (outer x inner).  `dtype`: of the
-    result, dy's or float32."""
-    return _gradient("tgrad_codes_grad_input", T.TGRAD_CODES_GRAD_INPUT, dy, weight, dtype, out)
+    result, dy's or float32.  unrounded: values of codes are not rounded to a two-byte dy's type first, which takes twice as long and leaves the
+    result's own rounding as its error."""
+    return _gradient(T.TGRAD_CODES_GRAD_INPUT, dy, weight, dtype, out, unrounded)
 
 
 @_on_stream
-def tgrad_codes_grad_weight(dy, x: Codes, *, dtype=None, out=None):
-    """Gradient of a product with respect to its weight: dy (tokens x outer) transposed, times the values of x (tokens x inner)."""
-    return _gradient("tgrad_codes_grad_weight", T.TGRAD_CODES_GRAD_WEIGHT, dy, x, dtype, out)
+def tgrad_codes_grad_weight(dy, x: Codes, *, dtype=None, out=None, unrounded: bool = False):
+    """Gradient of a product with respect to its weight: dy (tokens x outer) transposed, times the values of x (tokens x inner).  `dtype`, `unrounded`:
+    as above."""
+    return _gradient(T.TGRAD_CODES_GRAD_WEIGHT, dy, x, dtype, out, unrounded)
 
 
-def _gradient(name, op, dy, codes, dtype, out):
+def _gradient(op, dy, codes, dtype, out, unrounded):
     d = describe(dy, "dy")
     dev = dy.device
     dtype = dtype or dy.dtype
@@ -228,8 +230,10 @@ def _gradient(name, op, dy, codes, dtype, out):
     out, e = _result(out, "out", dy, rows, c.cols, dtype)
     if (d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8 or d.row_stride > 1 << 21:
         op += T.TGRAD_CODES_UNALIGNED
+    if unrounded:
+        op += T.TGRAD_CODES_UNROUNDED
     ws, at = scratch(_scratch_bytes(op, tokens, c.cols, outer), dev)
-    call(dev, getattr(T.load(), name), name, C.byref(d), C.byref(c), C.byref(e), at, stream_of(dev))
+    call(dev, T.load().tgrad_codes_gradient, "tgrad_codes_gradient", op, C.byref(d), C.byref(c), C.byref(e), at, stream_of(dev))
     return out
 
 

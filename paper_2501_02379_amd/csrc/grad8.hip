@@ -56,6 +56,30 @@ __device__ __forceinline__ void widen16(Quad c, float scale, Quad* out) {
   }
 }
 
+// One of the two parts of unrounded values: the upper one, rounded towards zero, or what that leaves, rounded.  The upper part is that of the value less 2^-9
+// (float16: 2^-12) of itself, so that both parts have the value's sign and neither is 0: an infinity in dy stays the infinity that it is.  Together they
+// are off by 2^-8 (2^-7 + 2^-9) of the value at most, float16 2^-11 (2^-10 + 2^-12).
+template <int DT, bool REST>
+__device__ __forceinline__ void widen16_part(Quad c, float scale, Quad* out) {
+  const float less = scale * (DT == TGRAD_F16 ? 1.f - 0x1p-12f : 1.f - 0x1p-9f);
+#pragma unroll
+  for (int h = 0; h < 8; ++h) {
+    const uint32_t pair = c[h / 2] >> (h % 2 * 16);
+    const float x = (float)(int8_t)pair, y = (float)(int8_t)(pair >> 8);
+    const float a = in_float32(x * less), b = in_float32(y * less);
+    uint32_t v;
+    if constexpr (DT == TGRAD_F16) {
+      const auto u = __builtin_amdgcn_cvt_pkrtz(a, b);
+      const _Float16 r[2] = {(_Float16)in_float32(fmaf(x, scale, -(float)u[0])), (_Float16)in_float32(fmaf(y, scale, -(float)u[1]))};
+      v = REST ? __builtin_bit_cast(uint32_t, r) : __builtin_bit_cast(uint32_t, u);
+    } else {
+      const float r = fmaf(x, scale, -__uint_as_float(__float_as_uint(a) & 0xFFFF0000u)), q = fmaf(y, scale, -__uint_as_float(__float_as_uint(b) & 0xFFFF0000u));
+      v = REST ? bf16_pack(r, q) : __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+    out[h / 4][h % 4] = v;
+  }
+}
+
 // float16's exponents do not reach what float32 scales do, so its values are multiplied with 2^k on their way to LDS and the sums with 2^-k, both exact: k
 // brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
 // the largest.  Rows `first` .. first + rows - 1, columns c0 .. c0 + cols - 1; the same in every thread.  Infinite and NaN scales are no size.
@@ -104,7 +128,9 @@ constexpr int kStep = 64;                 // of the sum in LDS at a time
 
 // WR x WC wavefronts, each FR x FC results of 16 x 16; two steps in LDS, one barrier a step.  WEIGHT: dy lies across the sum, else along it (rows of
 // 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end; codes go through registers, a step ahead.
-template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT>
+// PARTS = 2: values unrounded.  A step is then taken in two turns, with its values' upper parts and with what they leave (both beside each other in LDS would leave
+// room for one workgroup a compute unit).
+template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT, int PARTS>
 __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
   constexpr int T = WR * WC * 64, BR = WR * FR * 16, BC = WC * FC * 16;
   constexpr int kDy = BR * kStep * 2, kBytes = kDy + BC * kStep * 2;
@@ -115,8 +141,9 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
   const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
   const int r0 = tile.x * BR, c0 = tile.y * BC;
   const int64_t first = (int64_t)split * a.steps, last = min(first + a.steps, (a.sum + kStep - 1) / kStep);
-  const int64_t whole = min(last, a.sum / kStep);
-  auto place_of = [&](int64_t s) { return lds + (int)((s - first) & 1) * kBytes; };
+  // turns: PARTS of them a step; `whole` of them on steps that lie within the sum
+  const int64_t turns = (last - first) * PARTS, whole = max((min(last, a.sum / kStep) - first) * PARTS, (int64_t)0);
+  auto place_of = [&](int64_t q) { return lds + (int)(q & 1) * kBytes; };
   int lift = 0;
   if constexpr (DT == TGRAD_F16) {
     __shared__ uint32_t tops[WR * WC];
@@ -144,9 +171,10 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
     each[i] = WEIGHT ? row * (int)a.dy.stride + min(chunk * 8, a.dy_rows - r0 - 8) * 2 : min(row, a.rows - 1 - r0) * (int)a.dy.stride + chunk * 16;
   }
   const char* dy0 = WEIGHT ? a.dy.data + (int64_t)r0 * 2 : a.dy.row(r0);
-  auto fill = [&](int64_t s) {
+  auto fill = [&](int64_t q) {
+    const int64_t s = first + q / PARTS;
     const Ref g = ref(dy0 + (WEIGHT ? s * kStep * a.dy.stride : s * kStep * 2));
-    char* l = place_of(s) + wave * kWave * 16;
+    char* l = place_of(q) + wave * kWave * 16;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, each[i]);
   };
@@ -160,8 +188,8 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
       else held[i] = load8<DT>(a.dy.row(min(r0 + row, a.rows - 1)) + (s * kStep + chunk * 8) * 2, a.sum - s * kStep - chunk * 8);
     }
   };
-  auto place = [&](int64_t s) {
-    char* l = place_of(s) + threadIdx.x * 16;
+  auto place = [&](int64_t q) {
+    char* l = place_of(q) + threadIdx.x * 16;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) *reinterpret_cast<Quad*>(l + i * T * 16) = held[i];
   };
@@ -183,24 +211,26 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
       }
     }
   };
-  auto place_codes = [&](int64_t s) {
-    char* l = place_of(s) + kDy;
+  auto place_codes = [&](int64_t q) {
+    char* l = place_of(q) + kDy;
 #pragma unroll
     for (int i = 0; i < kCodes; ++i) {
       const int id = i * T + (int)threadIdx.x, row = id / (BC / 16), block = id % (BC / 16);
-      Quad q[2];
-      widen16<DT>(codes[i], scale[i], q);
+      Quad v[2];
+      if constexpr (PARTS == 1) widen16<DT>(codes[i], scale[i], v);
+      else if (q & 1) widen16_part<DT, true>(codes[i], scale[i], v);
+      else widen16_part<DT, false>(codes[i], scale[i], v);
       char* at = l + row * (BC * 2) + (block ^ bend(row)) * 32;
       const bool upper = lane & 4;          // lanes 4 to 7 store their upper halves first: eight lanes then meet all banks
-      *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
-      *reinterpret_cast<Quad*>(at + (upper ? 0 : 16)) = upper ? q[0] : q[1];
+      *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? v[1] : v[0];
+      *reinterpret_cast<Quad*>(at + (upper ? 0 : 16)) = upper ? v[0] : v[1];
     }
   };
 
   v4f acc[FC][FR] = {};
   const int wr = wave % WR, wc = wave / WR;
-  auto multiply = [&](int64_t s) {
-    const char* l = place_of(s);
+  auto multiply = [&](int64_t q) {
+    const char* l = place_of(q);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       Quad c[FC], d[FR];
@@ -218,25 +248,32 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
     }
   };
 
+  // the codes of a step's second turn are there from its first one
+  auto next_codes = [&](int64_t q) {
+    if (q < turns && q % PARTS == 0) read_codes(first + q / PARTS);
+  };
   read_codes(first);
-  if (first < whole) fill(first);
-  place_codes(first);
-  if (first + 1 < last) read_codes(first + 1);
-  for (int64_t s = first; s < whole; ++s) {
+  if (whole > 0) fill(0);
+  place_codes(0);
+  next_codes(1);
+  for (int64_t q = 0; q < whole; ++q) {
     barrier_but<0>();
-    if (s + 1 < last) {
-      if (s + 1 < whole) fill(s + 1);
-      place_codes(s + 1);
-      if (s + 2 < last) read_codes(s + 2);
+    if (q + 1 < turns) {
+      if (q + 1 < whole) fill(q + 1);
+      place_codes(q + 1);
+      next_codes(q + 2);
     }
-    multiply(s);
+    multiply(q);
   }
-  if (whole < last) {                       // the sum's end, less than a step
-    read(whole);
+  if (whole < turns) {                      // the sum's end, less than a step
+    read(first + whole / PARTS);
     __syncthreads();
-    place(whole);
-    __syncthreads();
-    multiply(whole);
+    for (int64_t q = whole; q < turns; ++q) {
+      if (q > whole) place_codes(q);        // into the place of turn q - 2, which everyone is done with
+      place(q);
+      __syncthreads();
+      multiply(q);
+    }
   }
 
 #pragma unroll
@@ -262,7 +299,9 @@ constexpr int kWide = 256, kWideStep = 32, kWideBufs = 4, kWideDy = kWide * kWid
 // 8192^3 bf16: dw 925 us, dx 985 (1190 and 1115 TFLOP/s; with loads to LDS that the compiler waits for 1130 and 1143).  The matrix instructions alone reach 1650
 // to 2030 on random numbers.
 // RAGGED: the codes' last row ends within a chunk (its branch costs the others 12 percent).
-template <int DT, int OT, bool WEIGHT, bool RAGGED>
+// PARTS = 2: values unrounded.  32 of the sum are two steps here, one with the values' upper parts and one with what they leave; dy is fetched again, from the caches.
+// 8192^3 bf16: dw 1870 us, dx 1860, 590 TFLOP/s of 1180.  (Both parts in one step, dy read once, need 70 to 100 registers more than there are.)
+template <int DT, int OT, bool WEIGHT, bool RAGGED, int PARTS>
 __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   constexpr int T = 512, FR = 8, FC = 4, kLoads = kWideDy / 16 / T;
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -271,7 +310,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   const int2 tile = tile_of(blockIdx.x % a.tiles, a.tiles, a.tiles_c);
   const int r0 = tile.x * kWide, c0 = tile.y * kWide;
   const int64_t from = (int64_t)split * a.steps * kWideStep;           // this split's part of the sum
-  const int sum = (int)min(a.sum - from, (int64_t)a.steps * kWideStep), steps = (sum + kWideStep - 1) / kWideStep;
+  const int sum = (int)min(a.sum - from, (int64_t)a.steps * kWideStep), steps = (sum + kWideStep - 1) / kWideStep * PARTS;
   int lift = 0;
   if constexpr (DT == TGRAD_F16) {
     __shared__ uint32_t tops[T / kWave];
@@ -296,15 +335,15 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   const char* dy0 = WEIGHT ? a.dy.row(from) + (int64_t)r0 * 2 : a.dy.row(r0) + from * 2;
   const int across_bytes = min(a.dy_rows - r0, kWide) * 2;
   auto fill = [&](int s) {
-    const int left = min(sum - s * kWideStep, kWideStep);
+    const int at = s / PARTS * kWideStep, left = min(sum - at, kWideStep);
     char* l = lds + s % kWideBufs * kWideBytes + wave * kWave * 16;
     if constexpr (WEIGHT) {
       const int bytes = (left - 1) * (int)a.dy.stride + across_bytes;
-      const Ref g = ref(dy0 + (int64_t)s * kWideStep * a.dy.stride, left > 0 ? bytes : 0);
+      const Ref g = ref(dy0 + at * a.dy.stride, left > 0 ? bytes : 0);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, each[i]);
     } else {
-      const Ref g = ref(dy0 + (int64_t)s * kWideStep * 2);
+      const Ref g = ref(dy0 + (int64_t)at * 2);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) to_lds_uncounted(g, l + i * T * 16, ahead[i] < left ? each[i] : 0x7FFFFFFC);
     }
@@ -321,11 +360,11 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   const int8_t* codes0 = a.c.codes + from * a.c.stride + c0;
   const float* scale0 = a.c.scale + from * a.c.groups;
   auto read_codes = [&](int s, Held& h) {
-    const int left = min(sum - s * kWideStep, kWideStep);
-    const bool end = from + s * kWideStep + left >= a.sum;             // this step has the last row, or nothing
+    const int row0 = s / PARTS * kWideStep, left = min(sum - row0, kWideStep);
+    const bool end = from + row0 + left >= a.sum;                      // this step has the last row, or nothing
     const int bytes = left * (int)a.c.stride - (end ? (int)a.c.stride - (a.cols - c0) : 0);
-    const int8_t* at = codes0 + (int64_t)s * kWideStep * a.c.stride;
-    const Ref g = ref(scale0 + (int64_t)s * kWideStep * a.c.groups, max(left, 0) * (int)a.c.groups * 4);
+    const int8_t* at = codes0 + row0 * a.c.stride;
+    const Ref g = ref(scale0 + row0 * a.c.groups, max(left, 0) * (int)a.c.groups * 4);
     h.codes = __builtin_bit_cast(Quad, __builtin_amdgcn_raw_buffer_load_b128(ref(at, left > 0 ? bytes : 0), code_at, 0, 0));
     h.scale = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(g, scale_at, 0, 0));
     if (RAGGED && end && left > 0) {        // buffers end at whole dwords: the last row's end byte by byte.  All loads are then waited for
@@ -335,9 +374,11 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     }
   };
   const int place = kWideDy + row * (kWide * 2) + (block ^ bend(row)) * 32;
-  auto place_codes = [&](int s, const Held& h) {
+  auto place_codes = [&](int s, auto rest, const Held& h) {
     Quad q[2];
-    widen16<DT>(h.codes, DT == TGRAD_F16 ? ldexpf(h.scale, lift) : h.scale, q);
+    const float scale = DT == TGRAD_F16 ? ldexpf(h.scale, lift) : h.scale;
+    if constexpr (PARTS == 1) widen16<DT>(h.codes, scale, q);
+    else widen16_part<DT, decltype(rest)::value>(h.codes, scale, q);
     char* at = lds + s % kWideBufs * kWideBytes + place;
     const bool upper = lane & 4;            // lanes 4 to 7 store their upper halves first: eight lanes then meet all banks
     *reinterpret_cast<Quad*>(at + (upper ? 16 : 0)) = upper ? q[1] : q[0];
@@ -347,7 +388,9 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   v4f acc[FC][FR] = {};
   const int wc = wave % 4, wr = wave / 4;
   const bool late = wave >= 4;
-  auto step = [&](int s, Held& h) {
+  const std::false_type even;
+  const std::true_type odd;
+  auto step = [&](int s, auto parity, Held& h) {
     Quad c[FC], d[FR];
     const char* l = lds + s % kWideBufs * kWideBytes;
 #pragma unroll
@@ -360,7 +403,7 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
     // dy of s + 1 has to be there; behind it came codes of s + 2, dy of s + 2, codes of s + 3
     turn_but<kLoads + 4>();
     __builtin_amdgcn_s_setprio(1);
-    place_codes(s + 2, h);
+    place_codes(s + 2, parity, h);
     fill(s + 3);                            // behind the sum's end both read zeros
     read_codes(s + 4, h);
 #pragma unroll
@@ -381,15 +424,15 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   fill(0);
   fill(1);
   fill(2);
-  place_codes(0, h0);
-  place_codes(1, h1);
+  place_codes(0, even, h0);
+  place_codes(1, odd, h1);
   read_codes(2, h0);
   read_codes(3, h1);
   turn_but<0>();
   if (late) turn();
   for (int s = 0; s < steps; s += 2) {
-    step(s, h0);
-    step(s + 1, h1);                        // with an odd number of steps the last one adds zeros
+    step(s, even, h0);
+    step(s + 1, odd, h1);                   // with an odd number of steps the last one adds zeros
   }
   if (!late) turn();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -556,9 +599,9 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_split(Grad a) {
   }
 }
 
-// ---- float32 dy, a scale for groups of columns: 64 x 64 results a workgroup, 4 x 4 a thread, float32 ---------------------------------------
+// ---- float32 dy or float32 results of unrounded values, a scale for groups of columns: 64 x 64 results a workgroup, 4 x 4 a thread, float32 -------
 
-template <bool WEIGHT>
+template <int DT, bool WEIGHT>
 __global__ __launch_bounds__(256) void k_grad_groups(Grad a) {
   __shared__ float as[16][65], bs[16][65];
   const int r0 = blockIdx.x / a.tiles_c * 64, c0 = blockIdx.x % a.tiles_c * 64;
@@ -572,7 +615,7 @@ __global__ __launch_bounds__(256) void k_grad_groups(Grad a) {
       const int s = WEIGHT ? e / 64 : e % 16, r = WEIGHT ? e % 64 : e / 16, v = e / 64, k = e % 64;
       float x = 0.f, y = 0.f;
       if (s0 + s < a.sum && r0 + r < a.rows)
-        x = WEIGHT ? reinterpret_cast<const float*>(a.dy.row(s0 + s))[r0 + r] : reinterpret_cast<const float*>(a.dy.row(r0 + r))[s0 + s];
+        x = Elem<DT>::widen(reinterpret_cast<const typename Elem<DT>::raw*>(a.dy.row(WEIGHT ? s0 + s : r0 + r))[WEIGHT ? r0 + r : s0 + s]);
       if (s0 + v < a.sum && c0 + k < a.cols)
         y = (float)a.c.codes[(s0 + v) * a.c.stride + c0 + k] * a.c.scale[(s0 + v) * a.c.groups + ((c0 + k) >> a.c.shift)];
       as[s][r] = x;
@@ -654,11 +697,11 @@ void launch_cut(hipStream_t s, Kern k, int threads, size_t lds, const Cut& c, co
   k<<<dim3((uint32_t)(c.tiles * c.splits)), dim3(threads), lds, s>>>(g);
 }
 
-template <int DT, int OT, bool WEIGHT>
+template <int DT, int OT, bool WEIGHT, int PARTS>
 void launch_tiles(hipStream_t s, const Cut& c, const Grad& g) {
-  if (c.tile == kWide && g.cols % 16) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, true>, 512, kWideBufs * kWideBytes, c, g);
-  else if (c.tile == kWide) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, false>, 512, kWideBufs * kWideBytes, c, g);
-  else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT>, 256, 2 * (128 + 128) * kStep * 2, c, g);
+  if (c.tile == kWide && g.cols % 16) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, true, PARTS>, 512, kWideBufs * kWideBytes, c, g);
+  else if (c.tile == kWide) launch_cut(s, k_grad_wide<DT, OT, WEIGHT, false, PARTS>, 512, kWideBufs * kWideBytes, c, g);
+  else launch_cut(s, k_grad_tiles<2, 2, 4, 4, DT, OT, WEIGHT, PARTS>, 256, 2 * (128 + 128) * kStep * 2, c, g);
 }
 
 void launch_add(hipStream_t s, const float* part, int splits, const tgrad_matrix* out) {
@@ -675,18 +718,26 @@ bool straight(const tgrad_matrix* dy) {
 bool straight(const tgrad_codes* c) { return (uintptr_t)c->codes % 16 == 0 && c->row_stride % 16 == 0 && c->row_stride <= ((int64_t)1 << 22); }
 size_t copy_bytes(int64_t tokens, int64_t outer) { return aligned((size_t)tokens * ((outer + 7) / 8 * 16)); }
 
-bool in_parts(const tgrad_matrix* dy, const tgrad_codes* c) { return dy->dtype == TGRAD_F32 || (dy->rows <= 16 && (c->group == 0 || c->cols <= c->group)); }
+bool one_scale(const tgrad_codes* c) { return c->group == 0 || c->cols <= c->group; }
+// float32 sums of numbers with 24 bits: float32 dy, and float32 results of unrounded values.
+bool full(const tgrad_matrix* dy, const tgrad_matrix* out, bool unrounded) { return dy->dtype == TGRAD_F32 || (unrounded && out->dtype == TGRAD_F32); }
+// dy in parts, or element by element: no tile reads dy's rows as they are, and none is copied.
+bool by_element(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, bool unrounded) {
+  return full(dy, out, unrounded) || (dy->rows <= 16 && one_scale(c));
+}
 
 template <bool WEIGHT>
-void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* scratch) {
+void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, bool unrounded, void* scratch) {
   Grad g{mat(dy), codes8(c), mat(out), WEIGHT ? dy->rows : dy->cols, (int)out->rows, (int)out->cols, 0, 0, 0, (int)out->rows};
-  if (dy->dtype == TGRAD_F32 && g.c.groups > 1) {
+  if (full(dy, out, unrounded) && !one_scale(c)) {
     g.tiles_c = (g.cols + 63) / 64;
-    k_grad_groups<WEIGHT><<<dim3((uint32_t)((g.rows + 63) / 64 * (int64_t)g.tiles_c)), dim3(256), 0, s>>>(g);
+    for_real(dy->dtype, [&](auto t) {
+      k_grad_groups<decltype(t)::value, WEIGHT><<<dim3((uint32_t)((g.rows + 63) / 64 * (int64_t)g.tiles_c)), dim3(256), 0, s>>>(g);
+    });
     return;
   }
   char* parts = static_cast<char*>(scratch);
-  const bool split = in_parts(dy, c);
+  const bool split = by_element(dy, c, out, unrounded);
   if (!split && !straight(dy) && dy->rows > 0) {
     const int64_t per = (dy->cols + 7) / 8;
     rows_in_launches(dy->rows, 256, (per + 255) / 256, [&](int64_t first, int64_t rows) {
@@ -709,7 +760,12 @@ void launch_gradient(hipStream_t s, const tgrad_matrix* dy, const tgrad_codes* c
     auto run = [&](auto o) {
       constexpr int OT = decltype(o)::value;
       if (split) launch_cut(s, k_grad_split<2, 2, 4, 4, DT, OT, WEIGHT>, 256, 2 * (3 * 128 + 128) * kStep32 * 2, cut, g);
-      else if constexpr (DT != TGRAD_F32) launch_tiles<DT, OT, WEIGHT>(s, cut, g);
+      else if constexpr (DT != TGRAD_F32) {
+        if constexpr (OT != TGRAD_F32) {
+          if (unrounded) return launch_tiles<DT, OT, WEIGHT, 2>(s, cut, g);
+        }
+        launch_tiles<DT, OT, WEIGHT, 1>(s, cut, g);
+      }
     };
     if (cut.splits > 1) run(std::integral_constant<int, -1>());
     else if (out->dtype == DT) run(t);
@@ -742,16 +798,16 @@ namespace {
 bool reachable(const tgrad_matrix* dy) { return dy->rows <= ((int64_t)1 << 30) && (dy->dtype == TGRAD_F32 || dy->cols <= ((int64_t)1 << 21)); }
 
 template <bool WEIGHT>
-int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
+int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* out, bool unrounded, void* workspace_dev, void* hip_stream) {
   if (!good(dy) || !good(c) || !good(out)) return TGRAD_ERR_INVALID_ARG;
   if (out->dtype != dy->dtype && out->dtype != TGRAD_F32) return TGRAD_ERR_INVALID_ARG;
   if (c->rows != (WEIGHT ? dy->rows : dy->cols) || !same_size(out, WEIGHT ? dy->cols : dy->rows, c->cols)) return TGRAD_ERR_INVALID_ARG;
   if (too_many(out) || !reachable(dy)) return TGRAD_ERR_UNSUPPORTED;
-  const bool copy = !in_parts(dy, c) && !straight(dy);
+  const bool copy = !by_element(dy, c, out, unrounded) && !straight(dy);
   if (!scratch_ok(workspace_dev, gradient_scratch(WEIGHT, copy, dy->rows, c->cols, dy->cols))) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
   if (out->rows == 0) return TGRAD_OK;
-  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, workspace_dev);
+  launch_gradient<WEIGHT>(static_cast<hipStream_t>(hip_stream), dy, c, out, unrounded, workspace_dev);
   return launched();
 }
 
@@ -760,11 +816,19 @@ int gradient(const tgrad_matrix* dy, const tgrad_codes* c, const tgrad_matrix* o
 extern "C" {
 
 int tgrad_codes_grad_input(const tgrad_matrix* dy, const tgrad_codes* w, const tgrad_matrix* dx, void* workspace_dev, void* hip_stream) {
-  return gradient<false>(dy, w, dx, workspace_dev, hip_stream);
+  return gradient<false>(dy, w, dx, false, workspace_dev, hip_stream);
 }
 
 int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const tgrad_matrix* dw, void* workspace_dev, void* hip_stream) {
-  return gradient<true>(dy, x, dw, workspace_dev, hip_stream);
+  return gradient<true>(dy, x, dw, false, workspace_dev, hip_stream);
+}
+
+int tgrad_codes_gradient(int op, const tgrad_matrix* dy, const tgrad_codes* codes, const tgrad_matrix* out, void* workspace_dev, void* hip_stream) {
+  const bool unrounded = op & TGRAD_CODES_UNROUNDED;
+  op &= ~(TGRAD_CODES_UNROUNDED | TGRAD_CODES_UNALIGNED);
+  if (op == TGRAD_CODES_GRAD_INPUT) return gradient<false>(dy, codes, out, unrounded, workspace_dev, hip_stream);
+  if (op == TGRAD_CODES_GRAD_WEIGHT) return gradient<true>(dy, codes, out, unrounded, workspace_dev, hip_stream);
+  return TGRAD_ERR_INVALID_ARG;
 }
 
 }  // extern "C"

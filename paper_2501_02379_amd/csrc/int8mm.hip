@@ -479,9 +479,9 @@ size_t linear_scratch(int64_t tokens, int64_t outer, int64_t inner) {
 extern "C" {
 
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes) {
-  const bool copy = op & TGRAD_CODES_UNALIGNED;
-  if (copy) op -= TGRAD_CODES_UNALIGNED;
-  if (!workspace_bytes || op < (copy ? TGRAD_CODES_GRAD_INPUT : TGRAD_CODES_MATMUL) || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
+  const bool copy = op & TGRAD_CODES_UNALIGNED, gradient = op >= TGRAD_CODES_UNALIGNED;
+  if (op > 0) op &= ~(TGRAD_CODES_UNALIGNED | TGRAD_CODES_UNROUNDED);
+  if (!workspace_bytes || op < (gradient ? TGRAD_CODES_GRAD_INPUT : TGRAD_CODES_MATMUL) || op > TGRAD_CODES_GRAD_WEIGHT) return TGRAD_ERR_INVALID_ARG;
   if (!extents_ok(tokens, inner, inner) || !extents_ok(outer, inner, inner)) return TGRAD_ERR_INVALID_ARG;
   *workspace_bytes = op == TGRAD_CODES_MATMUL ? product_scratch(tokens, outer, inner)
                    : op == TGRAD_CODES_LINEAR ? linear_scratch(tokens, outer, inner)

@@ -21,7 +21,7 @@ TGRAD_SELECT_RANDOM = 1
 TGRAD_ORDER_US_LR, TGRAD_ORDER_LR_US, TGRAD_ORDER_SUM = 0, 1, 2
 
 TGRAD_CODES_MATMUL, TGRAD_CODES_LINEAR, TGRAD_CODES_GRAD_INPUT, TGRAD_CODES_GRAD_WEIGHT = 0, 1, 2, 3
-TGRAD_CODES_UNALIGNED = 4
+TGRAD_CODES_UNALIGNED, TGRAD_CODES_UNROUNDED = 4, 8
 TGRAD_ACT_SILU, TGRAD_ACT_GELU = 0, 1
 
 TGRAD_OK = 0
@@ -48,7 +48,7 @@ EXPORTS = (
     "tgrad_token_logprobs", "tgrad_token_logprobs_backward", "tgrad_loss_query_size", "tgrad_policy_loss",
     "tgrad_preference_loss",
     "tgrad_quantize", "tgrad_dequantize", "tgrad_codes_query_size", "tgrad_codes_matmul", "tgrad_codes_linear", "tgrad_codes_grad_input",
-    "tgrad_codes_grad_weight", "tgrad_activation", "tgrad_activation_backward", "tgrad_block_norm", "tgrad_block_norm_query_size",
+    "tgrad_codes_grad_weight", "tgrad_codes_gradient", "tgrad_activation", "tgrad_activation_backward", "tgrad_block_norm", "tgrad_block_norm_query_size",
     "tgrad_block_norm_backward",
 )
 
@@ -204,6 +204,7 @@ def load():
     lib.tgrad_codes_linear.argtypes = [mat, cod, cod, mat, vp, vp]
     lib.tgrad_codes_grad_input.argtypes = [mat, cod, mat, vp, vp]
     lib.tgrad_codes_grad_weight.argtypes = [mat, cod, mat, vp, vp]
+    lib.tgrad_codes_gradient.argtypes = [i32, mat, cod, mat, vp, vp]
     lib.tgrad_activation.argtypes = [mat, mat, i32, mat, cod, cod, cod, vp]
     lib.tgrad_activation_backward.argtypes = [mat, cod, cod, i32, mat, mat, vp]
     lib.tgrad_block_norm.argtypes = [blk, mat, mat, mat, mat, cod, vp, vp]

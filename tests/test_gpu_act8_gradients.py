@@ -69,3 +69,70 @@ def test_a_gated_result_beyond_float16():
     dw = act8.tgrad_codes_grad_weight(dy, a.y)
     want = dy.cpu().double().t().contiguous() @ (a.y.codes.cpu().double() * a.y.scale.cpu().double())
     assert bool(dw[5].eq(0).all()) and bool(((dw.cpu().double() - want).abs() <= want.abs() * 2.0 ** -11 + 40 * 90000 * 5e-3 * (2.0 ** -11 + 250 * U)).all())
+
+
+# ---- unrounded values -----------------------------------------------------------------------------------------------------------
+
+# what the two parts of a value leave of it
+PARTS = {"bf16": 2.0 ** -8 * (2.0 ** -7 + 2.0 ** -9), "f16": 2.0 ** -11 * (2.0 ** -10 + 2.0 ** -12)}
+# tokens, inner, outer: single tokens, around 16, sums that end within a step, wide tiles (dx, dw), wide tiles with the sum in splits (dw, dx)
+UNROUNDED = [(1, 40, 30), (5, 64, 33), (17, 100, 70), (64, 128, 256), (100, 513, 66), (257, 255, 129), (5000, 64, 32), (3700, 3588, 40), (300, 3700, 3592), (40003, 500, 768), (2040, 2030, 4100)]
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "f32"), ("f16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("tokens,inner,outer", UNROUNDED)
+def test_unrounded_gradients(tokens, inner, outer, dtype, out):
+    """A value is off by PARTS of itself, or with a float32 result by u; sums and the result's rounding come on top."""
+    t, u, tiny = TYPES[out]
+    dy = numbers(tokens, outer, dtype, seed=1, pad=outer % 4, offset=outer % 3)
+    for group, pad in ((0, None), (0, 3), (32, None)) if tokens < 20000 else ((0, None),):
+        scales = lambda n: torch.rand(n, -(-inner // group) if group else 1, generator=torch.Generator().manual_seed(9)) * 0.02 + 0.001  # noqa: E731
+        w, cw, sw = codes_with(outer, inner, scales(outer), 2, group, pad)
+        x, cx, sx = codes_with(tokens, inner, scales(tokens), 3, group, pad)
+        for call, c, a, b, terms in ((act8.tgrad_codes_grad_input, w, dy.cpu().double(), spread_out(cw, sw, group), outer),
+                                     (act8.tgrad_codes_grad_weight, x, dy.cpu().double().t().contiguous(), spread_out(cx, sx, group), tokens)):
+            got = call(dy, c, dtype=t, unrounded=True)
+            want, size = a @ b, a.abs() @ b.abs()
+            value = PARTS[dtype] if out == dtype != "f32" else U
+            off = (got.cpu().double() - want).abs()
+            assert got.dtype is t and bool((off <= size * (value + (6 * terms + 4) * U) * (1 + u) + want.abs() * u + tiny).all())
+            if want.numel() > 2000:
+                # That bound is wide where sums are long.  Terms of random signs: what their values are off by is PARTS of the result in the 2-norm, 1/40 of
+                # the result's own rounding (some 0.4 u of it), and what float32 sums are off by, in any order, grows as the root of the terms.
+                own = float((want.to(t).double() - want).norm())
+                assert float(off.norm()) <= 1.02 * own + (2 * terms ** 0.5 + 4) * U * float(want.norm())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens,inner,outer", [(17, 130, 70), (300, 200, 130), (3700, 3588, 40)])
+def test_an_infinity_in_a_gradient_stays_one(tokens, inner, outer, dtype):
+    """Infinite where the other factor is a number but 0, with its sign; NaN where that is 0."""
+    dy = numbers(tokens, outer, dtype, seed=2)
+    t, n = tokens - 2, outer // 2
+    dy[t, n] = float("-inf")
+    w, cw, _ = codes_with(outer, inner, 0.01, 4)
+    x, cx, _ = codes_with(tokens, inner, 0.01, 5)
+    for unrounded in (False, True):
+        dx, dw = (f(dy, c, unrounded=unrounded).cpu() for f, c in ((act8.tgrad_codes_grad_input, w), (act8.tgrad_codes_grad_weight, x)))
+        for row, codes in ((dx[t], cw[n]), (dw[n], cx[t])):
+            assert torch.equal(row.isnan(), codes == 0) and torch.equal(row == float("-inf"), codes > 0) and torch.equal(row == float("inf"), codes < 0)
+
+
+def test_unrounded_gradients_captured_and_on_another_stream():
+    dy, w, x = numbers(700, 300, "bf16", seed=1), codes_with(300, 200, 0.01, 2)[0], codes_with(700, 200, 0.01, 3)[0]
+    both = lambda **kw: (act8.tgrad_codes_grad_input(dy, w, unrounded=True, **kw), act8.tgrad_codes_grad_weight(dy, x, unrounded=True, **kw))  # noqa: E731
+    want = both()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = both(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for _ in range(3):
+        dy.mul_(1.5)
+        graph.replay()
+        want = both()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -251,8 +251,9 @@ def _own(s):
     if s["op"] == "linear":
         return [act8.tgrad_codes_linear(s["x"], act8.Codes(s["w"], s["w_scale"], 0)).y]
     if s["op"] == "gradients":
-        dx = act8.tgrad_codes_grad_input(s["dy"], act8.Codes(s["w"], s["w_scale"], 0))
-        return [dx, act8.tgrad_codes_grad_weight(s["dy"], act8.Codes(s["x8"], s["x_scale"], 0))]
+        # the plain form's values are float32, and are not rounded to dy's type either
+        dx = act8.tgrad_codes_grad_input(s["dy"], act8.Codes(s["w"], s["w_scale"], 0), unrounded=True)
+        return [dx, act8.tgrad_codes_grad_weight(s["dy"], act8.Codes(s["x8"], s["x_scale"], 0), unrounded=True)]
     if s["op"] == "activation":
         a = act8.tgrad_activation(s["x"], s["gate"], act=s["act"], group=s["group"], quantize=s["quantize"])
         y = act8.tgrad_dequantize(a.y, s["x"].dtype) if s["quantize"] else a.y

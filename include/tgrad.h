@@ -575,7 +575,7 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
  *   dx[t, k] = sum_n dy[t, n] w[n, k]     dw[n, k] = sum_t dy[t, n] x[t, k]
  * w and x are the values of codes, in groups of any size.  bf16 and float16: values are rounded to as many bits as dy's type has, whatever its
  * exponents reach (float16: 11 bits down to 2^-28 of the largest value, fewer below), products are exact and added up in float32.  float32, and up to 16 tokens of codes with a scale a row: dy times that scale is
- * rounded to float32 and split into three bf16 parts, which keep 24 bits (below 2^-110 the last ones are lost; an infinity becomes NaN), codes are exact.
+ * rounded to float32 and split into three bf16 parts, which keep 24 bits (below 2^-110 the last ones are lost), codes are exact.
  *  dx, dw  dy's type, or TGRAD_F32; rounded once.  The order of the sums depends on sizes and alignment alone.
  *  workspace_dev  as above.
  * Errors: INVALID_ARG, UNSUPPORTED (2^33 results, more than 2^30 tokens, two-byte rows of more than 2^21), HIP.

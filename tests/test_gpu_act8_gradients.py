@@ -136,3 +136,21 @@ def test_unrounded_gradients_captured_and_on_another_stream():
         want = both()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype,out,tokens", [("f32", "f32", 5), ("f32", "f32", 300), ("bf16", "bf16", 5), ("f16", "f16", 16), ("bf16", "f32", 300), ("f16", "f32", 300)])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf")])
+@pytest.mark.parametrize("inner,outer", [(130, 70), (200, 131)])
+def test_an_infinity_stays_one_where_dy_is_split(tokens, inner, outer, dtype, out, value):
+    dy = numbers(tokens, outer, dtype, seed=2)
+    t, n = tokens - 2, outer // 2
+    dy[t, n] = value
+    w, cw, _ = codes_with(outer, inner, 0.01, 4)
+    x, cx, _ = codes_with(tokens, inner, 0.01, 5)
+    dx, dw = (f(dy, c, unrounded=True, dtype=TYPES[out][0]).cpu() for f, c in ((act8.tgrad_codes_grad_input, w), (act8.tgrad_codes_grad_weight, x)))
+    for row, codes in ((dx[t], cw[n]), (dw[n], cx[t])):
+        assert torch.equal(row.isnan(), codes == 0) and torch.equal(row == value, codes > 0) and torch.equal(row == -value, codes < 0)
+    nan = torch.tensor([0x7F800001], dtype=torch.int32, device=DEV).view(torch.float32)              # a NaN whose upper half is infinity's
+    if dtype == "f32":
+        dy[t, n] = nan
+        assert bool(act8.tgrad_codes_grad_input(dy, w)[t].isnan().all()) and bool(act8.tgrad_codes_grad_weight(dy, x)[n].isnan().all())

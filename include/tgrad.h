@@ -548,7 +548,8 @@ enum { TGRAD_CODES_MATMUL = 0, TGRAD_CODES_LINEAR = 1, TGRAD_CODES_GRAD_INPUT = 
 
 /*
  * Bytes of scratch of the calls below, for tokens x inner times inner x outer.  Two-byte dy that is not aligned is copied there first, which
- * needs TGRAD_CODES_UNALIGNED.  0: none, and the call's workspace_dev may be NULL.  Host-only.  Errors: INVALID_ARG.
+ * needs TGRAD_CODES_UNALIGNED; but for up to 16 tokens of codes with a scale a row and for unrounded values with a float32 result, which copy none,
+ * as float32 dy does not.  0: none, and the call's workspace_dev may be NULL.  Host-only.  Errors: INVALID_ARG.
  */
 int tgrad_codes_query_size(int op, int64_t tokens, int64_t inner, int64_t outer, size_t* workspace_bytes);
 

@@ -228,8 +228,9 @@ def _gradient(op, dy, codes, dtype, out, unrounded):
         c = describe_codes(codes, "x", dy, rows=d.rows)
         tokens, outer, rows = d.rows, d.cols, d.cols
     out, e = _result(out, "out", dy, rows, c.cols, dtype)
-    if (d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8 or d.row_stride > 1 << 21:
-        op += T.TGRAD_CODES_UNALIGNED
+    if dy.dtype is not torch.float32 and not (unrounded and dtype is torch.float32) and not (d.rows <= 16 and (not c.group or c.cols <= c.group)) and \
+            ((d.data or 0) % 16 or d.row_stride % 8 or d.cols % 8 or d.row_stride > 1 << 21):
+        op += T.TGRAD_CODES_UNALIGNED                      # where the library copies dy
     if unrounded:
         op += T.TGRAD_CODES_UNROUNDED
     ws, at = scratch(_scratch_bytes(op, tokens, c.cols, outer), dev)

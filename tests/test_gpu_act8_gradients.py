@@ -2,10 +2,12 @@
 
 u = 2^-24.  Sums of S products of two-byte numbers are off by at most 2 u S sum |a b|, as there.
 """
+import ctypes as C
+
 import pytest
 import torch
 
-from paper_2501_02379_amd import act8
+from paper_2501_02379_amd import act8, tgrad as T
 from test_gpu_act8 import DEV, TYPES, U, laid, numbers
 
 pytestmark = pytest.mark.gpu
@@ -154,3 +156,22 @@ def test_an_infinity_stays_one_where_dy_is_split(tokens, inner, outer, dtype, ou
     if dtype == "f32":
         dy[t, n] = nan
         assert bool(act8.tgrad_codes_grad_input(dy, w)[t].isnan().all()) and bool(act8.tgrad_codes_grad_weight(dy, x)[n].isnan().all())
+
+
+@pytest.mark.parametrize("tokens,dtype,out,unrounded,group,copied", [
+    (300, "f32", "f32", False, 0, False), (300, "f32", "f32", False, 32, False), (16, "bf16", "bf16", False, 0, False), (16, "bf16", "bf16", False, 32, True),
+    (17, "bf16", "bf16", False, 0, True), (300, "f16", "f16", True, 0, True), (300, "f16", "f32", False, 0, True), (300, "f16", "f32", True, 0, False),
+    (300, "f16", "f32", True, 32, False)])
+def test_scratch_for_a_copy_only_where_there_is_one(tokens, dtype, out, unrounded, group, copied, monkeypatch):
+    """dy in odd rows is copied into aligned ones where its type has two bytes and tiles read it as it is; other calls ask for no such memory."""
+    outer, inner = 131, 64
+    dy = numbers(tokens, outer, dtype, seed=2)
+    w, x = codes_with(outer, inner, 0.01, 4, group)[0], codes_with(tokens, inner, 0.01, 5, group)[0]
+    asked = []
+    given = act8.scratch
+    monkeypatch.setattr(act8, "scratch", lambda n, device: (asked.append(n), given(n, device))[1])
+    for op, call, c in ((T.TGRAD_CODES_GRAD_INPUT, act8.tgrad_codes_grad_input, w), (T.TGRAD_CODES_GRAD_WEIGHT, act8.tgrad_codes_grad_weight, x)):
+        n = C.c_size_t(0)
+        assert T.load().tgrad_codes_query_size(op + (T.TGRAD_CODES_UNALIGNED if copied else 0), tokens, inner, outer, C.byref(n)) == T.TGRAD_OK
+        call(dy, c, dtype=TYPES[out][0], unrounded=unrounded)
+        assert asked.pop() == n.value

@@ -566,7 +566,8 @@ int tgrad_codes_matmul(const tgrad_codes* x, const tgrad_codes* w, const tgrad_m
 
 /*
  * tgrad_quantize of x into `keep` (group 0), then tgrad_codes_matmul of it, with the same results; for a few tokens in one launch.
- *  keep   receives the codes of x, for the backward pass.  NULL: not kept.
+ *  keep   receives the codes of x, for the backward pass.  NULL: not kept, and they lie in scratch.
+ *  workspace_dev  as above; with `keep` the size for TGRAD_CODES_MATMUL is enough.
  */
 int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_codes* keep, const tgrad_matrix* y,
                       void* workspace_dev, void* hip_stream);

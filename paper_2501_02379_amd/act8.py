@@ -195,7 +195,7 @@ def tgrad_codes_linear(x, weight: Codes, *, keep: bool = False, dtype=None, out=
         refuse("dtype: float32, bfloat16 or float16")
     y, e = _result(out, "out", x, d.rows, w.rows, dtype)
     x8, c = new_codes(d.rows, d.cols, 0, dev) if keep else (None, None)
-    ws, at = scratch(_scratch_bytes(T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows), dev)
+    ws, at = scratch(_scratch_bytes(T.TGRAD_CODES_MATMUL if keep else T.TGRAD_CODES_LINEAR, d.rows, d.cols, w.rows), dev)
     call(dev, T.load().tgrad_codes_linear, "tgrad_codes_linear", C.byref(d), C.byref(w), _ref(c), C.byref(e), at, stream_of(dev))
     return Linear(y, x8)
 

@@ -506,7 +506,7 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
   if (x->cols != w->cols || !same_size(y, x->rows, w->rows)) return TGRAD_ERR_INVALID_ARG;
   if (keep && (!good(keep) || keep->group || !same_size(keep, x->rows, x->cols))) return TGRAD_ERR_INVALID_ARG;
   if (too_many(y) || x->cols > TGRAD_CODES_MAX_INNER) return TGRAD_ERR_UNSUPPORTED;
-  if (!scratch_ok(workspace_dev, linear_scratch(y->rows, y->cols, x->cols))) return TGRAD_ERR_INVALID_ARG;
+  if (!scratch_ok(workspace_dev, keep ? product_scratch(y->rows, y->cols, x->cols) : linear_scratch(y->rows, y->cols, x->cols))) return TGRAD_ERR_INVALID_ARG;
   if (pending()) return TGRAD_ERR_HIP;
   if (y->rows == 0) return TGRAD_OK;
   const hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -519,8 +519,11 @@ int tgrad_codes_linear(const tgrad_matrix* x, const tgrad_codes* w, const tgrad_
     });
     return launched();
   }
-  char* own_codes = static_cast<char*>(workspace_dev) + part_bytes(y->rows, y->cols, x->cols);
-  tgrad_codes own{own_codes, reinterpret_cast<float*>(own_codes + aligned((size_t)x->rows * scratch_stride(x->cols))), x->rows, x->cols, scratch_stride(x->cols), 0};
+  tgrad_codes own = {};
+  if (!keep) {
+    char* at = static_cast<char*>(workspace_dev) + part_bytes(y->rows, y->cols, x->cols);
+    own = tgrad_codes{at, reinterpret_cast<float*>(at + aligned((size_t)x->rows * scratch_stride(x->cols))), x->rows, x->cols, scratch_stride(x->cols), 0};
+  }
   const tgrad_codes* c = keep ? keep : &own;
   launch_quantize(s, x, c);
   launch_product(s, c, w, y, workspace_dev);

@@ -175,3 +175,16 @@ def test_scratch_for_a_copy_only_where_there_is_one(tokens, dtype, out, unrounde
         assert T.load().tgrad_codes_query_size(op + (T.TGRAD_CODES_UNALIGNED if copied else 0), tokens, inner, outer, C.byref(n)) == T.TGRAD_OK
         call(dy, c, dtype=TYPES[out][0], unrounded=unrounded)
         assert asked.pop() == n.value
+
+
+@pytest.mark.parametrize("tokens,inner,outer", [(3, 200, 90), (8, 4096, 64), (40, 4096, 40), (700, 300, 200)])
+def test_no_scratch_for_codes_that_are_kept(tokens, inner, outer, monkeypatch):
+    x, w = numbers(tokens, inner, "bf16", seed=1), codes_with(outer, inner, 0.01, 2)[0]
+    want = act8.tgrad_codes_linear(x, w).y
+    asked = []
+    given = act8.scratch
+    monkeypatch.setattr(act8, "scratch", lambda n, device: (asked.append(n), given(n, device))[1])
+    n = C.c_size_t(0)
+    assert T.load().tgrad_codes_query_size(T.TGRAD_CODES_MATMUL, tokens, inner, outer, C.byref(n)) == T.TGRAD_OK
+    y, x8 = act8.tgrad_codes_linear(x, w, keep=True)
+    assert asked == [n.value] and torch.equal(y, want) and torch.equal(act8.tgrad_codes_matmul(x8, w), want)

@@ -8,9 +8,17 @@ using namespace tgrad;
 
 namespace {
 
-// Activations and their derivatives.
-template <int ACT> struct Act;
-template <> struct Act<TGRAD_ACT_SILU> {
+// Activations and their derivatives.  FULL, for float32: exponentials whose argument's rounding is made good, so that errors do not grow with it (exp2's
+// argument of -30 is off by 2^-20, which is 10 u of the result); two-byte results and codes round that away.  (Float32 8192^2, us, with it and without: result
+// 101 and 99, backward pass with gate 170 and 167, gelu 176 and 171; as codes it would be 197 and 137, gelu 357 and 159.)
+__device__ __forceinline__ float exp2_of(float t, float rest) {          // 2^(t + rest), a small rest; t <= 0
+  t = in_float32(t);                                                     // the rest is that of t as it was rounded
+  const float n = rintf(t), e = __builtin_amdgcn_exp2f(t - n);
+  return ldexpf(fmaf(e, rest * 0.69314718f, e), (int)n);
+}
+
+template <int ACT, bool FULL> struct Act;
+template <> struct Act<TGRAD_ACT_SILU, false> {
   static __device__ __forceinline__ float value(float v) { return v * __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
   static __device__ __forceinline__ void both(float v, float& y, float& slope) {
     const float p = __builtin_amdgcn_rcpf(1.f + __expf(-v));
@@ -18,13 +26,41 @@ template <> struct Act<TGRAD_ACT_SILU> {
     slope = p * (1.f + v * (1.f - p));
   }
 };
+// From q = exp(-|v|) <= 1: 1 / (1 + q) and q / (1 + q) are p and 1 - p, or the other way round, each with all its digits.
+template <> struct Act<TGRAD_ACT_SILU, true> {
+  static __device__ __forceinline__ void parts(float v, float& p, float& other) {
+    constexpr float kLog2e = 1.44269502f, kLow = 1.92596303e-08f;
+    const float z = fminf(fabsf(v), 1000.f), t = z * -kLog2e;
+    const float q = exp2_of(t, fmaf(z, -kLow, fmaf(z, -kLog2e, -t)));
+    const float r = __builtin_amdgcn_rcpf(1.f + q), s = q * r;
+    p = v < 0.f ? s : r;
+    other = v < 0.f ? r : s;
+  }
+  static __device__ __forceinline__ float value(float v) {
+    float p, other;
+    parts(v, p, other);
+    return v * p;
+  }
+  static __device__ __forceinline__ void both(float v, float& y, float& slope) {
+    float p, other;
+    parts(v, p, other);
+    y = v * p;
+    slope = p * fmaf(v, other, 1.f);
+  }
+};
 // The normal distribution function from its tail, Phi(-z) = exp(-z^2 / 2) P(t) with t = 1 / (1 + c z), z = |v|: P(t) = exp(z^2 / 2) Phi(-z) is smooth on 0..1,
 // and a polynomial fitted to it by least squares in 64 bits, weighted by 1 / P, is off by 1e-07 of it.  Tails keep their digits that way, which
 // (1 + erf) / 2 loses below -2.  (With erfc of the device library: 519 us where silu takes 409.)
-template <> struct Act<TGRAD_ACT_GELU> {
+template <bool FULL> struct Act<TGRAD_ACT_GELU, FULL> {
   static __device__ __forceinline__ void tail(float v, float& bell, float& q) {
     const float z = fabsf(v);
-    bell = __builtin_amdgcn_exp2f(v * v * -0.72134752f);
+    if constexpr (FULL) {
+      constexpr float kHalf = 0.721347511f, kLow = 9.62981517e-09f;      // log2(e) / 2
+      const float w = fminf(z, 64.f), s = w * w, a = s * -kHalf;
+      bell = exp2_of(a, fmaf(s, -kLow, fmaf(s, -kHalf, -a)) - fmaf(w, w, -s) * kHalf);
+    } else {
+      bell = __builtin_amdgcn_exp2f(v * v * -0.72134752f);
+    }
     const float t = __builtin_amdgcn_rcpf(fmaf(0.40f, z, 1.f));
     float p = 3.219981867e-02f;
     p = fmaf(p, t, -1.766817470e-01f);
@@ -147,11 +183,11 @@ __global__ __launch_bounds__(256) void k_dequantize(Codes8 c, int64_t first, int
 
 // ---- activation ---------------------------------------------------------------------------------------------------------------
 
-template <int DT, int ACT, bool GATED>
+template <int ACT, bool GATED, bool FULL>
 __device__ __forceinline__ void activate(const float* v, const float* g, float* y) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    y[i] = Act<ACT>::value(v[i]);
+    y[i] = Act<ACT, FULL>::value(v[i]);
     if constexpr (GATED) y[i] *= g[i];
   }
 }
@@ -173,7 +209,7 @@ __global__ __launch_bounds__(256) void k_activation(Mat x, Mat gate, int64_t fir
   e.get(v);
   h.get(g);
   if (p.in) {
-    activate<DT, ACT, GATED>(v, g, r);
+    activate<ACT, GATED, DT == TGRAD_F32>(v, g, r);
     Eight<DT> o;
     o.set(r);
     o.store(y.row(p.row) + at, cols - p.col);
@@ -212,7 +248,7 @@ __global__ __launch_bounds__(T, NL > 0 ? 4 : 1) void k_activation_rows(Mat x, Ma
     const Place p{row, u * 8, u < units};
     e.get(v);
     h.get(g);
-    activate<DT, ACT, GATED>(v, g, r);
+    activate<ACT, GATED, false>(v, g, r);
     if (keep && x8.codes) {
       keep_group(v, p, cols, x8);
       if constexpr (GATED) keep_group(g, p, cols, gate8);
@@ -287,7 +323,7 @@ __global__ __launch_bounds__(256) void k_activation_back(Mat dy, Codes8 x8, Code
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float y, slope;
-    Act<ACT>::both(v[i], y, slope);
+    Act<ACT, DT == TGRAD_F32>::both(v[i], y, slope);
     a[i] = d[i] * slope;
     if constexpr (GATED) {
       a[i] = d[i] * g[i] * slope;

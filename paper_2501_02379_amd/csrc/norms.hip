@@ -3,7 +3,7 @@
 //
 // With n the normed vector and r its factor 1 / sqrt(mean((v - m)^2) + eps), a gradient u with respect to n goes on as
 // r (u - n mean(u n) [- mean(u)]).  Forward two reads and two writes a number, backward four and two, for 14 and 26 operations: memory bounds both, so a
-// row is read once and kept in registers through its sums.
+// row is read once and kept in registers through its sums.  (Backward up to 8192 columns: see k_block_norm_sums.)
 #include "block8.h"
 
 using namespace tgrad;
@@ -410,7 +410,9 @@ __global__ __launch_bounds__(T) void k_block_norm_back(Desc d, Back a) {
   }
 }
 
-// The sums of a row that is longer than kHeldCols, read twice (the second time from L2: 320 KB a row at most, one row a compute unit): a workgroup a row.
+// The sums of a row that is longer than kHeldCols, a workgroup a row.  dh and x_out are read twice here and once more by k_block_norm_back, dx_out, block and
+// gate once here and once there.  A row has 10 bytes a column, 20 in float32: 32 rows of a die are 2.6 to 21 MB, so that L2 (4 MB a die) holds
+// the shortest of them between the readings and the memory-side cache the others.
 template <int XT, int BT, bool BLOCK>
 __global__ __launch_bounds__(1024) void k_block_norm_sums(Desc d, Back a, int64_t first) {
   constexpr int T = 1024;
@@ -519,10 +521,10 @@ void launch_chunk_sums(hipStream_t s, const SumJobs& jobs, int cols) {
     k_chunk_sums<<<dim3((cols + 15) / 16, (uint32_t)std::min<int64_t>(all - at, 32768)), dim3(1024), 0, s>>>(jobs, at, cols);
 }
 
-// Threads and units of a row, all of them held in registers: up to 512 threads, so that a compute unit has three rows and more in turn (16384 x 8192 bf16: 299 us
-// with 1024 threads a row, 229 with 512; 8192 x 16384: 246 and 222).
+// Threads and units of a row, all of them held in registers: 512 threads up to 16384 columns, so that a compute unit has three rows and more in turn (16384 x
+// 8192 bf16: 299 us with 1024 threads a row, 229 with 512; 8192 x 16384: 246 and 222); 1024 beyond, whose registers are needed.
 template <typename F>
-void for_width(int64_t rows, int cols, F&& f) {
+void for_width(int cols, F&& f) {
   const int units = (cols + 7) / 8;
   typedef std::integral_constant<int, 64> t64;
   typedef std::integral_constant<int, 256> t256;
@@ -623,7 +625,7 @@ int tgrad_block_norm(const tgrad_block* desc, const tgrad_matrix* x, const tgrad
   const Codes8 c = codes8(h8);
   float4* st = reinterpret_cast<float4*>(stats);
   for_types(x->dtype, bt, [&](auto xt, auto yt) {
-    for_width(rows, (int)cols, [&](auto t, auto n) {
+    for_width((int)cols, [&](auto t, auto n) {
       constexpr int XT = decltype(xt)::value, BT = decltype(yt)::value, T = decltype(t)::value, NV = decltype(n)::value;
       rows_in_launches(rows, T, 1, [&](int64_t first, int64_t some) {
         if (block) k_block_norm<XT, BT, true, T, NV><<<dim3((uint32_t)some), dim3(T), 0, s>>>(d, first, mx, mb, mo, mh, c, st);

@@ -45,12 +45,6 @@ __device__ __forceinline__ void barrier_but() {
   asm volatile("" ::: "memory");
 }
 
-// A barrier behind which everyone's LDS stores are there; loads to registers stay on their way.
-__device__ __forceinline__ void barrier_lds() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 // The same for the wide tiles, whose two halves of a workgroup take turns: while four wavefronts, one on each SIMD, read operands, the other four
 // multiply.  Nothing moves across.
 template <int N>

@@ -188,3 +188,39 @@ def test_no_scratch_for_codes_that_are_kept(tokens, inner, outer, monkeypatch):
     assert T.load().tgrad_codes_query_size(T.TGRAD_CODES_MATMUL, tokens, inner, outer, C.byref(n)) == T.TGRAD_OK
     y, x8 = act8.tgrad_codes_linear(x, w, keep=True)
     assert asked == [n.value] and torch.equal(y, want) and torch.equal(act8.tgrad_codes_matmul(x8, w), want)
+
+
+@pytest.mark.parametrize("tokens,inner,outer", RANGE)
+@pytest.mark.parametrize("scale", [1000.0, 2.0 ** -26, 2.0 ** -130, 2.0 ** 100])
+def test_unrounded_float16_values_beyond_float16(tokens, inner, outer, scale):
+    """Results that leave float16 are infinite, or at its end; the others are right."""
+    dy = (numbers(tokens, outer, "f16", seed=1) * 2.0 ** -6).contiguous()
+    w, cw, sw = codes_with(outer, inner, scale, 2)
+    x, cx, sx = codes_with(tokens, inner, scale, 3)
+    for call, c, a, b, terms in ((act8.tgrad_codes_grad_input, w, dy.cpu().double(), spread_out(cw, sw, 0), outer),
+                                 (act8.tgrad_codes_grad_weight, x, dy.cpu().double().t().contiguous(), spread_out(cx, sx, 0), tokens)):
+        want, size = a @ b, a.abs() @ b.abs()
+        for out in ("f16", "f32"):
+            t, u, tiny = TYPES[out]
+            got = call(dy, c, dtype=t, unrounded=True).cpu().double()
+            fits = want.abs() < 65000 if out == "f16" else torch.ones_like(want, dtype=torch.bool)
+            value = PARTS["f16"] if out == "f16" else U
+            # float32's own 2^-110 below which dy's last parts are lost, times codes: 2^-103 a term
+            lost = terms * 2.0 ** -103 if out == "f32" or tokens <= 16 else 0.0
+            off = (got - want).abs()
+            assert bool((off <= size * (value + (6 * terms + 4) * U) * (1 + u) + want.abs() * u + tiny + lost)[fits].all())
+            assert bool((got[~fits].isinf() | (got[~fits].abs() > 60000)).all())
+
+
+def test_scales_that_are_no_sizes():
+    """A row of codes with a NaN or an infinite scale spoils what it goes into, and float16's power of two is taken from the others."""
+    dy = numbers(64, 48, "f16", seed=1)
+    w, cw, sw = codes_with(48, 32, 2.0 ** -30, 2)
+    for bad in (float("nan"), float("inf")):
+        w.scale[7] = bad
+        for unrounded in (False, True):
+            assert not bool(torch.isfinite(act8.tgrad_codes_grad_input(dy, w, unrounded=unrounded)).any())
+            x, cx, sx = codes_with(64, 32, 2.0 ** -30, 3)
+            x.scale[5] = bad
+            d = act8.tgrad_codes_grad_weight(dy, x, dtype=torch.float32, unrounded=unrounded)
+            assert not bool(torch.isfinite(d).any())

@@ -81,7 +81,7 @@ __device__ __forceinline__ void widen16_part(Quad c, float scale, Quad* out) {
 }
 
 // float16's exponents do not reach what float32 scales do, so its values are multiplied with 2^k on their way to LDS and the sums with 2^-k, both exact: k
-// brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
+// (8192^3: 3 percent, the tile's scales read ahead of it) brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
 // the largest.  Rows `first` .. first + rows - 1, columns c0 .. c0 + cols - 1; the same in every thread.  Infinite and NaN scales are no size.
 template <int T>
 __device__ __forceinline__ int lift_of(const Codes8& c, int64_t first, int64_t rows, int c0, int cols, uint32_t* lds) {
@@ -128,6 +128,7 @@ constexpr int kStep = 64;                 // of the sum in LDS at a time
 
 // WR x WC wavefronts, each FR x FC results of 16 x 16; two steps in LDS, one barrier a step.  WEIGHT: dy lies across the sum, else along it (rows of
 // 128 bytes, chunk c of row r at chunk c ^ (r % 8)).  dy goes straight to LDS, but for the sum's end; codes go through registers, a step ahead.
+// (8192^3 bf16, codes in rows that the wide tiles do not take: 1390 us; unrounded 2840 and 2890.)
 // PARTS = 2: values unrounded.  A step is then taken in two turns, with its values' upper parts and with what they leave (both beside each other in LDS would leave
 // room for one workgroup a compute unit).
 template <int WR, int WC, int FR, int FC, int DT, int OT, bool WEIGHT, int PARTS>
@@ -296,11 +297,11 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_tiles(Grad a) {
 // dy: 16-byte rows, whole chunks of eight columns; codes: 16-byte rows.
 constexpr int kWide = 256, kWideStep = 32, kWideBufs = 4, kWideDy = kWide * kWideStep * 2, kWideBytes = 2 * kWideDy;
 
-// 8192^3 bf16: dw 925 us, dx 985 (1190 and 1115 TFLOP/s; with loads to LDS that the compiler waits for 1130 and 1143).  The matrix instructions alone reach 1650
+// 8192^3 bf16: dw 950 to 980 us, dx 965 to 1000 (1160 and 1140 TFLOP/s at best; with loads to LDS that the compiler waits for 1130 and 1143 us).  The matrix instructions alone reach 1650
 // to 2030 on random numbers.
 // RAGGED: the codes' last row ends within a chunk (its branch costs the others 12 percent).
 // PARTS = 2: values unrounded.  32 of the sum are two steps here, one with the values' upper parts and one with what they leave; dy is fetched again, from the caches.
-// 8192^3 bf16: dw 1870 us, dx 1860, 590 TFLOP/s of 1180.  (Both parts in one step, dy read once, need 70 to 100 registers more than there are.)
+// 8192^3 bf16: dw and dx 1860 to 1910 us, 1180 TFLOP/s of both parts' products.  (Both parts in one step, dy read once, need 70 to 100 registers more than there are.)
 template <int DT, int OT, bool WEIGHT, bool RAGGED, int PARTS>
 __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
   constexpr int T = 512, FR = 8, FC = 4, kLoads = kWideDy / 16 / T;
@@ -452,8 +453,8 @@ __global__ __launch_bounds__(512) void k_grad_wide(Grad a) {
 // ---- float32 dy, and two-byte dy of a few tokens: a scale for each row of codes -------------------------------------------------------------------------------------------
 
 // dy times a row's scale, rounded to float32, lies in LDS as three bf16 parts of 8 bits (split_apart); codes are exact in bf16.  Three products instead
-// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 420 us for dw, 445 for dx, 320 TFLOP/s.)  Two-byte dy of up to 16
-// tokens takes this way too: memory bounds such products, so that no value need be rounded.
+// of one, each 16 times as fast as the float32 matrix instructions'.  (4096^3: 420 us for dw, 425 for dx, 325 TFLOP/s.)  Two-byte dy of up to 16
+// tokens takes this way too: memory bounds such products, so that no value need be rounded; and float32 results of unrounded values.
 constexpr int kStep32 = 32;
 
 // The parts of eight numbers (see split_pair, which forms rests with dot products of both: neighbours here are different results' terms, and a NaN
@@ -608,6 +609,7 @@ __global__ __launch_bounds__(WR * WC * 64, 2) void k_grad_split(Grad a) {
 
 // ---- float32 dy or float32 results of unrounded values, a scale for groups of columns: 64 x 64 results a workgroup, 4 x 4 a thread, float32 -------
 
+// 4096^3: 2400 us, 57 TFLOP/s: two reads of LDS feed four products a thread.  Such codes are the activations' checkpoints, whose values go into no product.
 template <int DT, bool WEIGHT>
 __global__ __launch_bounds__(256) void k_grad_groups(Grad a) {
   __shared__ float as[16][65], bs[16][65];

@@ -35,7 +35,7 @@ __device__ __forceinline__ void store_scaled(char* row, int n, int outer, i32x4 
 // at chunk c ^ (r % 8), so that eight rows' loads of one chunk meet eight banks; `BUFS` steps are there or on their way.  One
 // barrier a step: it says that everyone's part of this step has arrived and that everyone is done with the step before, whose place is filled
 // next.  OT < 0: sums go to `part`, [split][tokens][outer], and are added up by k_add_parts.
-// STAGED: rows that do not start at multiples of 16 bytes go through registers.
+// STAGED: rows that do not start at multiples of 16 bytes go through registers (4096^3: 140 us instead of 69, 8192^3: 861 instead of 428).
 // (8192^3 in tiles of 128 x 128, two workgroups a compute unit: 546 us; four wavefronts of 8 x 8 results: 582.)
 template <int WT, int WN, int FT, int FN, int BUFS, bool STAGED, int OT>
 __global__ __launch_bounds__(WT * WN * 64, 2) void k_codes_tiles(Codes8 x, Codes8 w, int tokens, int outer, int inner, Mat y, int* part, int tiles_n, int tiles,
@@ -158,7 +158,8 @@ __global__ __launch_bounds__(WT * WN * 64, 2) void k_codes_tiles(Codes8 x, Codes
 // The same with 256 x 256 results of 8 wavefronts, 2 x 4 of 8 x 4, in steps of 64 bytes of which four are there or on their way (rows of 64 bytes, chunk c of row
 // r at chunk c ^ (r / 2 % 4)).  A step is two turns: wavefronts 0 to 3 read the step's operands while 4 to 7, a turn behind, multiply the
 // step before.  What is filled in a step was last read three turns ago at least, and is read five or six turns later.
-// 8192^3: 415 to 450 us, 2500 TOP/s, where k_codes_tiles of this size takes 460 to 510 (wavefronts 4 x 2 of 4 x 8: 488).  The card's power is the limit: the matrix
+// 8192^3: 428 us in calls behind one another (2570 TOP/s), 450 behind the launch that quantises, 476 from idle; k_codes_tiles of this size takes 460 to 510
+// (wavefronts 4 x 2 of 4 x 8: 488).  The card's power is the limit: the matrix
 // instructions alone, out of registers, reach 3260 to 4020 on random codes and 4800 on zeros; without its reads of LDS this kernel would take 410 us.
 constexpr int kWide = 256, kWideStep = 64, kWideBufs = 4, kWideBytes = 2 * kWide * kWideStep;
 

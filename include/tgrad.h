@@ -589,6 +589,7 @@ int tgrad_codes_grad_weight(const tgrad_matrix* dy, const tgrad_codes* x, const 
  * The same two, by op: TGRAD_CODES_GRAD_INPUT or _WEIGHT, with what is added to it for tgrad_codes_query_size.  With TGRAD_CODES_UNROUNDED the error that
  * rounded values bring into a two-byte gradient is gone, for twice the matrix operations: values are taken in two parts of dy's type (off by 2^-14 of
  * themselves in bf16; in float16 by 2^-20, down to 2^-28 of the largest value), and with a float32 result dy and values as in float32.
+ * Errors: as above; INVALID_ARG for another op.
  */
 int tgrad_codes_gradient(int op, const tgrad_matrix* dy, const tgrad_codes* codes, const tgrad_matrix* out, void* workspace_dev, void* hip_stream);
 

@@ -57,8 +57,8 @@ __device__ __forceinline__ void widen16(Quad c, float scale, Quad* out) {
 }
 
 // One of the two parts of unrounded values: the upper one, rounded towards zero, or what that leaves, rounded.  The upper part is that of the value less 2^-9
-// (float16: 2^-12) of itself, so that both parts have the value's sign and neither is 0: an infinity in dy stays the infinity that it is.  Together they
-// are off by 2^-8 (2^-7 + 2^-9) of the value at most, float16 2^-11 (2^-10 + 2^-12).
+// (float16: 2^-12) of itself, so that both parts have the value's sign and, but for float16's smallest, neither is 0: an infinity in dy stays the infinity that
+// it is.  Together they are off by 2^-8 (2^-7 + 2^-9) of the value at most, float16 2^-11 (2^-10 + 2^-12).
 template <int DT, bool REST>
 __device__ __forceinline__ void widen16_part(Quad c, float scale, Quad* out) {
   const float less = scale * (DT == TGRAD_F16 ? 1.f - 0x1p-12f : 1.f - 0x1p-9f);
@@ -81,8 +81,9 @@ __device__ __forceinline__ void widen16_part(Quad c, float scale, Quad* out) {
 }
 
 // float16's exponents do not reach what float32 scales do, so its values are multiplied with 2^k on their way to LDS and the sums with 2^-k, both exact: k
-// (8192^3: 3 percent, the tile's scales read ahead of it) brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
-// the largest.  Rows `first` .. first + rows - 1, columns c0 .. c0 + cols - 1; the same in every thread.  Infinite and NaN scales are no size.
+// brings the largest of the scales that a tile reads to 2^8..2^9, 127 times it to 65024 at most, below float16's end.  Values keep 11 bits down to 2^-28 of
+// the largest.  Rows `first` .. first + rows - 1, columns c0 .. c0 + cols - 1; the same in every thread.  Infinite and NaN scales are no size.  (8192^3: 3
+// percent, for the tile's scales are read ahead of its loop.)
 template <int T>
 __device__ __forceinline__ int lift_of(const Codes8& c, int64_t first, int64_t rows, int c0, int cols, uint32_t* lds) {
   const int g0 = c0 >> c.shift, g1 = (c0 + cols - 1) >> c.shift;
